@@ -292,6 +292,118 @@ int dlcx_select_rank_from(const int32_t *rprime_dev, int n_matrices, int32_t *rp
                           int32_t *rprime_inout_host, int32_t *r_next_out_host,
                           int32_t *H_next_out_host, void *stream);
 
+/* ---- the inner step: what runs between two outer steps (InnerOpt of Alg. 2, AdamW in Appendix A.3) ----
+ *
+ * K workers that share theta_g in one GPU's memory, or requests that are answered with it, differ by
+ * low-rank adapters: y = theta_g x + s_a P_a Q_a^T x for a row of adapter a.  The projection itself is
+ * a plain product of the caller's; the calls below do what stands beside it, and the update of the
+ * adapters (or of any other tensors) between two outer steps.  The factors of an adapter have the
+ * layout of every factor here, so dlcx_decompress folds a trained adapter into an error buffer. */
+
+#define DLCX_MAX_ADAPTERS 1024
+#define DLCX_MAX_TENSORS (1 << 20)
+
+typedef struct {
+    int64_t m, n;    /* the projection's outputs and inputs, 1 .. 2^24 each                            */
+    int32_t r;       /* columns of a stored factor, 1 .. DLCX_MAX_RANK                                 */
+    int32_t count;   /* adapters, 1 .. DLCX_MAX_ADAPTERS                                               */
+    int32_t dtype;   /* DLCX_F32 or DLCX_BF16: of x, y, dy, dx and of the factors                      */
+} dlcx_adapter_desc;
+
+/* Rows grouped by adapter: which rows each adapter has, in order, and how they are cut into tiles.
+ * ids: `rows` device ints, the adapter of each row; a value outside [0, count) is no adapter.  One
+ * route serves every projection and both directions of a batch; dlcx_adapter_forward and
+ * _backward make their own in the workspace where they get none.  rows 0 .. 2^24. */
+size_t dlcx_adapter_route_bytes(int64_t rows, int32_t count);
+int dlcx_adapter_route(int64_t rows, const int32_t *ids, int32_t count, void *route, void *stream);
+
+/* Device scratch of either call below for this descriptor and up to `rows` rows.  0 on a bad
+ * descriptor.  Host only. */
+size_t dlcx_adapter_workspace_bytes(const dlcx_adapter_desc *desc, int64_t rows);
+
+/* For every row t with adapter a:
+ *   h[t][c] = sum_i x[t][i] Q_a[c][i] ;  y_out[t][j] = y_in[t][j] + scale[a] sum_c h[t][c] P_a[c][j]
+ * and for a row without one h[t] = 0, y_out[t] = y_in[t].  x is rows x n, y rows x m, row-major with
+ * row strides ldx, ldy_in, ldy_out in elements (no smaller than the row); q is count x r x n, p is
+ * count x r x m, h_out rows x r fp32 (backward reads it).  y_in may be y_out, or NULL for zeros.
+ * scale (count floats) NULL: 1.  ranks (count ints) NULL: r; only the first ranks[a] columns of adapter a
+ * are read, columns of h from there on are 0.  route NULL: formed here.  x, y and the factors may have any
+ * alignment and stride that their type has; 16-byte aligned rows are faster.  bf16: products on
+ * the bf16 matrix cores with fp32 sums, h rounded to bf16 as their operand (not in h_out), y rounded
+ * once; fp32: fp32 matrix cores.  y_out, h_out and the workspace overlap nothing else. */
+int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
+                         const int32_t *ids, const void *q, const void *p, const float *scale,
+                         const int32_t *ranks, const void *route, const void *y_in, int64_t ldy_in,
+                         void *y_out, int64_t ldy_out, float *h_out, void *workspace, void *stream);
+
+/* Its gradient, from dy (rows x m, stride lddy), x and h of the forward call:
+ *   g[t][c] = scale[a] sum_j dy[t][j] P_a[c][j] ;  dx_out[t][i] = dx_in[t][i] + sum_c g[t][c] Q_a[c][i]
+ *   dq_out[a][c][i] = sum over the rows t of adapter a of g[t][c] x[t][i]
+ *   dp_out[a][c][j] = scale[a] times the sum over the same rows of h[t][c] dy[t][j]
+ * dx_in (what the projection itself gives) may be dx_out, or NULL for zeros; dq_out (count x r x n) and
+ * dp_out (count x r x m) are fp32 and overwritten, with zeros from column ranks[a] on and for adapters
+ * without rows.  The order of a sum hangs on rows, count, sizes and the rows' ids alone.  bf16: as above;
+ * the sums over rows take g and h in three bf16 pieces (error 2^-24 per product). */
+int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
+                          const void *dy, int64_t lddy, const int32_t *ids, const void *q,
+                          const void *p, const float *scale, const int32_t *ranks, const void *route,
+                          const float *h, const void *dx_in, int64_t lddx_in, void *dx_out,
+                          int64_t lddx_out, float *dq_out, float *dp_out, void *workspace,
+                          void *stream);
+
+/* One tensor of an optimizer step: `numel` consecutive elements.  param (DLCX_F32 or DLCX_BF16), grad
+ * (either type), the moments m and v: fp32 (state_bits 32), or codes of 8 bits (state_bits 8) with a
+ * fp32 scale for every 128 elements (the last group may be shorter) in m_scale and v_scale:
+ *   m       = c |c| m_scale, c = -127 .. 127 (int8),    m_scale = largest |m| of the group / 127^2
+ *   sqrt(v) = c^2 v_scale,   c = 0 .. 255 (uint8),      v_scale = largest sqrt(v) of the group / 255^2
+ * (squares of the codes: steps that shrink with the value, 0.8 % of the largest one near it and a 1/127^2
+ * or 1/255^2 of it near zero; c of v is at least 1 where v > 0, so that a small v never turns into a
+ * zero denominator).  copy (bf16, fp32 parameters only) or NULL receives the updated
+ * parameter rounded.  All but the scales are 16-byte aligned.  For dlcx_grad_norm alone, param NULL
+ * and the rest ignored. */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void *copy;
+    int64_t numel;
+    float lr_scale, weight_decay; /* the step's learning rate is lr * lr_scale                        */
+    int32_t param_dtype, grad_dtype, state_bits;
+    int32_t reserved; /* 0 */
+} dlcx_tensor;
+
+/* The tensors of a step, laid out on the device once: `memory` (dlcx_tensor_table_bytes(count) bytes,
+ * 256-byte aligned) receives what the kernels look up, *table_out_host what the calls below take.  The
+ * tensors' own addresses are kept, nothing of their contents.  Two calls on one table that overlap in
+ * time are the caller's to order. */
+typedef struct {
+    void *memory;
+    int64_t blocks;
+    int32_t count, steps; /* steps: every tensor has what dlcx_adamw needs */
+} dlcx_table;
+size_t dlcx_tensor_table_bytes(int32_t count);
+int dlcx_tensor_table(const dlcx_tensor *tensors_host, int32_t count, void *memory,
+                      dlcx_table *table_out_host, void *stream);
+
+/* *norm_out (device) = grad_scale * sqrt(sum of g^2 over all gradients of the table); squares and sums in
+ * fp64, one rounding, no atomics on the sum: the same bits from run to run. */
+int dlcx_grad_norm(const dlcx_table *table_host, double grad_scale, float *norm_out, void *stream);
+
+/* One AdamW step (decoupled weight decay) on every tensor of the table, the step'th (from 1):
+ *   g  = grad_scale * grad, times max_norm / norm where norm > max_norm
+ *   m <- beta1 m + (1 - beta1) g ;  v <- beta2 v + (1 - beta2) g^2
+ *   p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32, from the moments before they are rounded to 8 bits.  norm: a device float (this
+ * gradient's, or a whole model's of which the table is a part), or NULL for no clipping.  A norm that is not
+ * finite leaves parameters, moments and copies as they are. */
+int dlcx_adamw(const dlcx_table *table_host, double lr, double beta1, double beta2, double eps,
+               int64_t step, double grad_scale, const float *norm, double max_norm, void *stream);
+
+/* What 8-bit moments stand for, as DLCX_F32 or DLCX_BF16 (rounded): second == 0 for m, 1 for v. */
+int dlcx_state_decode(int second, const void *codes, const float *scales, int64_t numel, void *out,
+                      int out_dtype, void *stream);
+
 /* ---- helpers: the steps the entry points above are made of ---------------------------- */
 
 /* Size of one worker's payload for one factor: what Alg. 1 hands to the AllReduce of Alg. 2 is

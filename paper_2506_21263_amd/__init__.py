@@ -18,6 +18,8 @@ PHASE_P, PHASE_Q = 0, 1
 F32, BF16 = 0, 1
 MMA_FMA, MMA_F32, MMA_BF16, MMA_F16 = 0, 1, 2, 3
 MAX_RANK, MAX_WORKERS = 256, 16
+MAX_ADAPTERS, MAX_TENSORS = 1024, 1 << 20
+STATE_GROUP = 128  # elements of an 8-bit moment that share a scale
 
 
 class DlcxError(RuntimeError):
@@ -34,6 +36,29 @@ class Desc(C.Structure):
 
 def desc(m, n, r, qbits, group, mma=MMA_FMA):
     return Desc(m, n, r, qbits, group, mma)
+
+
+class AdapterDesc(C.Structure):
+    _fields_ = [("m", C.c_int64), ("n", C.c_int64), ("r", C.c_int32), ("count", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+def adapter_desc(m, n, r, count, dtype=BF16):
+    return AdapterDesc(m, n, r, count, dtype)
+
+
+class Tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("copy", C.c_void_p),
+                ("numel", C.c_int64), ("lr_scale", C.c_float), ("weight_decay", C.c_float),
+                ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class Table(C.Structure):
+    """The caller's handle of a table of tensors; `held` keeps what it points to alive."""
+    _fields_ = [("memory", C.c_void_p), ("blocks", C.c_int64), ("count", C.c_int32),
+                ("steps", C.c_int32)]
 
 
 _lib = None
@@ -84,6 +109,19 @@ SYMBOLS = {
     "dlcx_dequant_average": (_int, [_int, _vp, _vp, _i64, _int, _int, _vp, _vp]),
     "dlcx_orthonormalize": (_int, [_i64, _i32, _vp, _vp, _vp]),
     "dlcx_effective_rank": (_int, [_i64, _i32, _vp, C.c_double, _vp, _vp, _vp]),
+    "dlcx_adapter_route_bytes": (C.c_size_t, [_i64, _i32]),
+    "dlcx_adapter_route": (_int, [_i64, _vp, _i32, _vp, _vp]),
+    "dlcx_adapter_workspace_bytes": (C.c_size_t, [_vp, _i64]),
+    "dlcx_adapter_forward": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64,
+                                    _vp, _i64, _vp, _vp, _vp]),
+    "dlcx_adapter_backward": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp,
+                                     _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp]),
+    "dlcx_tensor_table_bytes": (C.c_size_t, [_i32]),
+    "dlcx_tensor_table": (_int, [_vp, _i32, _vp, _vp, _vp]),
+    "dlcx_grad_norm": (_int, [_vp, C.c_double, _vp, _vp]),
+    "dlcx_adamw": (_int, [_vp, C.c_double, C.c_double, C.c_double, C.c_double, _i64, C.c_double,
+                          _vp, C.c_double, _vp]),
+    "dlcx_state_decode": (_int, [_int, _vp, _vp, _i64, _vp, _int, _vp]),
     "dlcx_profile_enable": (_int, [_int]),
     "dlcx_profile_kernels": (_int, []),
     "dlcx_profile_name": (C.c_char_p, [_int]),
@@ -395,6 +433,144 @@ def dlcx_orthonormalize(L, r, p_inout, workspace, stream=None):
 def dlcx_effective_rank(L, r, q_bar, tau, rprime_out_dev, workspace, stream=None):
     _check(lib().dlcx_effective_rank(L, r, _ptr(q_bar), tau, _ptr(rprime_out_dev),
                                      _ptr(workspace), _stream(stream)), "dlcx_effective_rank")
+
+
+_CODE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _typed(t, dtype, numel, what):
+    """Address of a contiguous device tensor of that type with at least `numel` elements, or None."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == dtype and t.numel() >= numel and t.is_contiguous()):
+        raise ValueError("%s: a contiguous device tensor of %d elements of %s is wanted" % (what, numel, dtype))
+    return t.data_ptr()
+
+
+def _rows(t, rows, cols, dtype, what):
+    """Address and row stride of a rows x cols device matrix whose rows are contiguous."""
+    if t is None:
+        return None, cols
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols):
+        raise ValueError("%s: a %d x %d device matrix of %s is wanted" % (what, rows, cols, dtype))
+    step, inner = t.stride()
+    if (inner != 1 and cols > 1) or (step < cols and rows > 1):
+        raise ValueError("%s: the elements of a row have to be consecutive, and rows apart" % what)
+    return t.data_ptr(), (step if rows > 1 else cols)
+
+
+def dlcx_adapter_route_bytes(rows, count):
+    return lib().dlcx_adapter_route_bytes(rows, count)
+
+
+def dlcx_adapter_route(ids, count, route, stream=None):
+    """ids: int32 device tensor, one adapter (or a value outside [0, count)) per row."""
+    rows = ids.numel()
+    _typed(route, torch.uint8, dlcx_adapter_route_bytes(rows, count), "route")
+    _check(lib().dlcx_adapter_route(rows, _typed(ids, torch.int32, rows, "ids"), count, _ptr(route),
+                                    _stream(stream)), "dlcx_adapter_route")
+
+
+def dlcx_adapter_workspace_bytes(d, rows):
+    return lib().dlcx_adapter_workspace_bytes(C.byref(d), rows)
+
+
+def _adapter_common(d, rows, ids, q, p, scale, ranks, route, workspace):
+    dt = torch.bfloat16 if d.dtype == BF16 else torch.float32
+    return (dt, _typed(ids, torch.int32, rows, "ids"), _typed(q, dt, d.count * d.r * d.n, "q"),
+            _typed(p, dt, d.count * d.r * d.m, "p"), _typed(scale, torch.float32, d.count, "scale"),
+            _typed(ranks, torch.int32, d.count, "ranks"),
+            None if route is None else _typed(route, torch.uint8, dlcx_adapter_route_bytes(rows, d.count), "route"),
+            _typed(workspace, torch.uint8, dlcx_adapter_workspace_bytes(d, rows), "workspace"))
+
+
+def dlcx_adapter_forward(d, x, ids, q, p, y_in, y_out, h_out, workspace, scale=None, ranks=None,
+                         route=None, stream=None):
+    """x (rows x n), y_in (rows x m, None: zeros) and y_out may be views with a row stride."""
+    rows = x.shape[0]
+    dt, ids, q, p, scale, ranks, route, ws = _adapter_common(d, rows, ids, q, p, scale, ranks, route, workspace)
+    x, ldx = _rows(x, rows, d.n, dt, "x")
+    y_in, ldi = _rows(y_in, rows, d.m, dt, "y_in")
+    y_out, ldo = _rows(y_out, rows, d.m, dt, "y_out")
+    _check(lib().dlcx_adapter_forward(C.byref(d), rows, x, ldx, ids, q, p, scale, ranks, route, y_in, ldi,
+                                      y_out, ldo, _typed(h_out, torch.float32, rows * d.r, "h_out"), ws,
+                                      _stream(stream)), "dlcx_adapter_forward")
+
+
+def dlcx_adapter_backward(d, x, dy, ids, q, p, h, dx_in, dx_out, dq_out, dp_out, workspace,
+                          scale=None, ranks=None, route=None, stream=None):
+    """x, dy, dx_in (None: zeros) and dx_out may be views with a row stride; h is the forward call's."""
+    rows = x.shape[0]
+    dt, ids, q, p, scale, ranks, route, ws = _adapter_common(d, rows, ids, q, p, scale, ranks, route, workspace)
+    x, ldx = _rows(x, rows, d.n, dt, "x")
+    dy, lddy = _rows(dy, rows, d.m, dt, "dy")
+    dx_in, ldi = _rows(dx_in, rows, d.n, dt, "dx_in")
+    dx_out, ldo = _rows(dx_out, rows, d.n, dt, "dx_out")
+    _check(lib().dlcx_adapter_backward(C.byref(d), rows, x, ldx, dy, lddy, ids, q, p, scale, ranks, route,
+                                       _typed(h, torch.float32, rows * d.r, "h"), dx_in, ldi, dx_out, ldo,
+                                       _typed(dq_out, torch.float32, d.count * d.r * d.n, "dq_out"),
+                                       _typed(dp_out, torch.float32, d.count * d.r * d.m, "dp_out"), ws,
+                                       _stream(stream)), "dlcx_adapter_backward")
+
+
+def tensor(grad, param=None, m=None, v=None, m_scale=None, v_scale=None, copy=None, weight_decay=0.0,
+           lr_scale=1.0):
+    """One tensor of a step (contiguous device tensors of equal lengths).  Moments: float32, or int8
+    and uint8 codes with a float32 scale per STATE_GROUP elements.  Returns the structure and what it
+    points to."""
+    numel = grad.numel()
+    t = Tensor(grad=_typed(grad, grad.dtype, numel, "grad"), numel=numel, lr_scale=lr_scale,
+               weight_decay=weight_decay, grad_dtype=_CODE[grad.dtype], state_bits=32)
+    if param is not None:
+        eight = m.dtype != torch.float32
+        if param.numel() != numel:
+            raise ValueError("param and grad have different lengths")
+        t.param, t.param_dtype = _typed(param, param.dtype, numel, "param"), _CODE[param.dtype]
+        t.m = _typed(m, torch.int8 if eight else torch.float32, numel, "m")
+        t.v = _typed(v, torch.uint8 if eight else torch.float32, numel, "v")
+        t.copy = _typed(copy, torch.bfloat16, numel, "copy")
+        if eight:
+            groups = -(-numel // STATE_GROUP)
+            t.state_bits = 8
+            t.m_scale = _typed(m_scale, torch.float32, groups, "m_scale")
+            t.v_scale = _typed(v_scale, torch.float32, groups, "v_scale")
+    return t, (grad, param, m, v, m_scale, v_scale, copy)
+
+
+def dlcx_tensor_table_bytes(count):
+    return lib().dlcx_tensor_table_bytes(count)
+
+
+def dlcx_tensor_table(tensors, memory, stream=None):
+    """tensors: what `tensor` returned, one after the other.  The handle keeps them and `memory`."""
+    table = Table()
+    arr = (Tensor * max(len(tensors), 1))(*[t for t, _ in tensors])
+    _typed(memory, torch.uint8, dlcx_tensor_table_bytes(len(tensors)), "memory")
+    _check(lib().dlcx_tensor_table(arr, len(tensors), _ptr(memory), C.addressof(table), _stream(stream)),
+           "dlcx_tensor_table")
+    table.held = (memory, [held for _, held in tensors])
+    return table
+
+
+def dlcx_grad_norm(table, norm_out, grad_scale=1.0, stream=None):
+    _check(lib().dlcx_grad_norm(C.addressof(table), grad_scale, _typed(norm_out, torch.float32, 1, "norm_out"),
+                                _stream(stream)), "dlcx_grad_norm")
+
+
+def dlcx_adamw(table, lr, beta1, beta2, eps, step, norm=None, max_norm=0.0, grad_scale=1.0, stream=None):
+    _check(lib().dlcx_adamw(C.addressof(table), lr, beta1, beta2, eps, step, grad_scale,
+                            _typed(norm, torch.float32, 1, "norm"), max_norm, _stream(stream)), "dlcx_adamw")
+
+
+def dlcx_state_decode(codes, scales, out, stream=None):
+    """int8 codes are a first moment's, uint8 codes a second one's; out: float32 or bfloat16."""
+    if codes.dtype not in (torch.int8, torch.uint8) or out.dtype not in _CODE:
+        raise ValueError("int8 or uint8 codes, float32 or bfloat16 values")
+    n = codes.numel()
+    _check(lib().dlcx_state_decode(int(codes.dtype == torch.uint8), _typed(codes, codes.dtype, n, "codes"),
+                                   _typed(scales, torch.float32, -(-n // STATE_GROUP), "scales"), n,
+                                   _typed(out, out.dtype, n, "out"), _CODE[out.dtype], _stream(stream)),
+           "dlcx_state_decode")
 
 
 def dlcx_profile_enable(on):

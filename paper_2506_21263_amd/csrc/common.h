@@ -33,7 +33,9 @@ enum KernelId {
     KID_DELTA_EF = 0, KID_NESTEROV, KID_QUANTIZE, KID_DEQUANT_AVG, KID_PACK, KID_PROJECT_P,
     KID_PROJECT_Q, KID_SUM_SLABS, KID_RECONSTRUCT, KID_GRAM, KID_CHOL, KID_APPLY_W, KID_EFF_RANK,
     KID_ROUND, KID_QUANT_ROUND, KID_REQUANT, KID_EF_UPDATE,
-    KID_MFMA_PEAK, KID_TRAFFIC_PROBE, KID_COUNT
+    KID_MFMA_PEAK, KID_TRAFFIC_PROBE, KID_TENSOR_TABLE, KID_GRAD_NORM, KID_ADAMW,
+    KID_STATE_DECODE, KID_ADAPTER_ROUTE, KID_ADAPTER_DOWN, KID_ADAPTER_UP, KID_ADAPTER_ROWS,
+    KID_ADAPTER_GRAD, KID_ADAPTER_SUM, KID_COUNT
 };
 struct Timed {
     Timed(int kid, hipStream_t st);
@@ -127,6 +129,21 @@ int launch_ef_update(int K, const PtrPack<float *> &ef, const float *d, int64_t 
 int launch_mfma_peak(int workgroups, int iters, int operands, float *out, hipStream_t st);
 int launch_traffic_probe(int K, const PtrPack<float *> &ef, const PtrPack<const void *> &tl,
                          bool tl_bf16, float *theta, float *vel, int64_t numel, hipStream_t st);
+
+// ---- tensors of an inner optimizer step (k_adamw.hip) ----------------------------------
+int launch_tensor_table(const dlcx_tensor *tensors_host, int count, void *memory, dlcx_table *table,
+                        hipStream_t st);
+int launch_grad_norm(const dlcx_table &table, double grad_scale, float *norm_out, hipStream_t st);
+struct AdamwStep {
+    float beta1, one_minus_beta1, beta2, one_minus_beta2, eps;
+    float inv_sqrt_bc2;  // 1 / sqrt(1 - beta2^step)
+    double lr, lr_bc1;   // lr / (1 - beta1^step)
+    float grad_scale, max_norm;
+    const float *norm;
+};
+int launch_adamw(const dlcx_table &table, const AdamwStep &step, hipStream_t st);
+int launch_state_decode(int second, const void *codes, const float *scales, int64_t numel, void *out,
+                        int out_dtype, hipStream_t st);
 
 // ---- rank-r products ------------------------------------------------------------------
 // P_k = delta_k * Q_in   (delta m x n, q_in r x n, out r x m)

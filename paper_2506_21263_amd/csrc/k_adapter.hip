@@ -1,0 +1,940 @@
+// Low-rank adapters of many requests (or of K workers) beside a shared projection, and their
+// gradient.  With the rows of one adapter gathered, every product is one of three:
+//
+//   down  h[t][c] = sum_i x[t][i] F[c][i]           (x, Q) -> h      (dy, P) -> g
+//   up    y[t][j] = y_in[t][j] + sum_c h[t][c] F[c][j]   (h, P) -> y      (g, Q) -> dx
+//   grad  D[c][j] = sum_t u[t][c] z[t][j]           (h, dy) -> dP    (g, x) -> dQ
+//
+// A row is 2 to 60 KB and meets r <= 256 columns, so all three are bound by the stream of rows as long
+// as the matrix cores are fed from the registers the stream arrives in.
+#include "common.h"
+
+namespace dlcx {
+
+// ---- rows grouped by adapter ----------------------------------------------------------------------
+// Tables of tiles of one adapter's rows, in five sizes: a launch takes the one that fills the GPU.
+constexpr int kSizes = 5;
+__host__ __device__ constexpr int tile_rows(int size) { return 16 << (2 * size); }  // 16 .. 4096
+constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
+
+struct RouteView {
+    int32_t *ntiles;        // kSizes
+    int32_t *order;         // rows, an adapter's ones in their own order, adapter after adapter, then the rest
+    int4 *tiles[kSizes];    // adapter (-1: none), first place in `order`, rows, slab (-1: only tile)
+    int2 *spans[kSizes];    // per adapter: first slab (-1: one tile or none), tiles
+};
+static size_t route_view(int64_t rows, int count, char *base, RouteView *v) {
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char *p = base + at;
+        at += a256x(bytes);
+        return p;
+    };
+    RouteView w;
+    w.ntiles = (int32_t *)take(kSizes * sizeof(int32_t));
+    w.order = (int32_t *)take((size_t)rows * sizeof(int32_t));
+    for (int s = 0; s < kSizes; ++s) {
+        w.tiles[s] = (int4 *)take((size_t)(rows / tile_rows(s) + count + 1) * sizeof(int4));
+        w.spans[s] = (int2 *)take((size_t)count * sizeof(int2));
+    }
+    if (v) *v = w;
+    return at;
+}
+static inline int64_t max_tiles(int64_t rows, int count, int size) {
+    return rows / tile_rows(size) + (rows < count + 1 ? rows : count + 1);
+}
+
+// Exclusive prefix sum over the workgroup's threads; *total: the sum of all.
+__device__ __forceinline__ int scan_workgroup(int x, int *lds, int *total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    int y = x;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(y, d, 64);
+        if (lane >= d) y += up;
+    }
+    if (lane == 63) lds[wave] = y;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kRouteWaves; ++w) {
+        const int s = lds[w];
+        before += w < wave ? s : 0;
+        all += s;
+    }
+    __syncthreads();
+    *total = all;
+    return before + y - x;
+}
+
+// One workgroup sorts the rows by counting: every wavefront counts its own share, the counts become the
+// places where it writes, and the lanes of equal adapters find their order by ballots of the index's
+// bits, so the order within an adapter is that of the rows.
+__global__ __launch_bounds__(kRouteThreads) void adapter_route_kernel(int rows,
+                                                                      const int32_t *__restrict__ ids,
+                                                                      int count, RouteView v) {
+    extern __shared__ int lds[];
+    int *cursor = lds;                                // kRouteWaves x (count + 1)
+    int *first = cursor + kRouteWaves * (count + 1);  // count + 2: first place of each adapter
+    int *tile0 = first + count + 2;                   // count + 2: first tile of each adapter
+    int *slab0 = tile0 + count + 2;                   // count + 1
+    __shared__ int part[kRouteWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, buckets = count + 1;
+    const uint64_t below = (1ull << lane) - 1;
+    for (int i = threadIdx.x; i < kRouteWaves * buckets; i += kRouteThreads) cursor[i] = 0;
+    __syncthreads();
+    const int share = (rows + kRouteThreads - 1) / kRouteThreads * 64;
+    const int lo = min(rows, wave * share), hi = min(rows, lo + share);
+    int bits = 0;
+    while ((1 << bits) < buckets) ++bits;
+    int *mine = cursor + wave * buckets;
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int base = lo; base < hi; base += 8 * 64) {
+            int id[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int t = base + u * 64 + lane;
+                id[u] = t < hi ? ids[t] : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int t = base + u * 64 + lane;
+                const int b = id[u] >= 0 && id[u] < count ? id[u] : count;
+                uint64_t same = __ballot(t < hi);
+                if (same == 0) break;
+                for (int k = 0; k < bits; ++k) {
+                    const uint64_t one = __ballot((b >> k) & 1);
+                    same &= (b >> k) & 1 ? one : ~one;
+                }
+                if (t < hi) {
+                    const int rank = __popcll(same & below);
+                    if (pass == 1) v.order[mine[b] + rank] = t;
+                    wave_sync();
+                    if (rank == 0) mine[b] += __popcll(same);
+                }
+                wave_sync();
+            }
+        }
+        __syncthreads();
+        if (pass == 1) break;
+        int carry = 0;
+        for (int base = 0; base < buckets; base += kRouteThreads) {
+            const int b = base + (int)threadIdx.x;
+            int n = 0, total;
+            if (b < buckets)
+                for (int w = 0; w < kRouteWaves; ++w) n += cursor[w * buckets + b];
+            int at = carry + scan_workgroup(n, part, &total);
+            if (b < buckets) {
+                first[b] = at;
+                for (int w = 0; w < kRouteWaves; ++w) {
+                    const int c = cursor[w * buckets + b];
+                    cursor[w * buckets + b] = at;
+                    at += c;
+                }
+            }
+            carry += total;
+        }
+        if (threadIdx.x == 0) first[buckets] = rows;
+        __syncthreads();
+    }
+    for (int s = 0; s < kSizes; ++s) {
+        const int size = tile_rows(s);
+        int tiles = 0, slabs = 0;
+        for (int base = 0; base < buckets; base += kRouteThreads) {
+            const int b = base + (int)threadIdx.x;
+            const int n = b < buckets ? (first[b + 1] - first[b] + size - 1) / size : 0;
+            const int apart = n > 1 && b < count ? n : 0;
+            int all, more;
+            const int t0 = tiles + scan_workgroup(n, part, &all);
+            const int s0 = slabs + scan_workgroup(apart, part, &more);
+            if (b < buckets) {
+                tile0[b] = t0;
+                slab0[b] = apart ? s0 : -1;
+            }
+            if (b < count) v.spans[s][b] = make_int2(apart ? s0 : -1, n);
+            tiles += all;
+            slabs += more;
+        }
+        if (threadIdx.x == 0) {
+            tile0[buckets] = tiles;
+            v.ntiles[s] = tiles;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < tiles; i += kRouteThreads) {
+            int b = 0;  // the last one that begins at or before tile i (one without tiles begins with the next)
+            for (int len = buckets; len > 1;) {
+                const int half = len / 2;
+                if (tile0[b + half] <= i) b += half, len -= half;
+                else len = half;
+            }
+            const int k = i - tile0[b], at = first[b] + k * size;
+            v.tiles[s][i] = make_int4(b < count ? b : -1, at, min(size, first[b + 1] - at),
+                                      slab0[b] < 0 ? -1 : slab0[b] + k);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- operands -------------------------------------------------------------------------------------
+// A block of 16 x 32 (or 32 x 16) of an operand: lane l holds row (column) l % 16 and the 8 reduction
+// indices from 8 (l / 16) on.  bf16: one product of 16 x 16 x 32; fp32: eight of 16 x 16 x 4, the j-th with the
+// j-th index of every lane, which is a reordering of the same sum.  Element v of the result is
+// row 4 (l / 16) + v, column l % 16.
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 ab_bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 ab_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float ab_f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t ab_u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const ab_f32x2 x = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, ab_bf16x2));
+}
+__device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+struct Bf16 {
+    static constexpr int code = DLCX_BF16;
+    static constexpr int lane = 8;  // elements of 16 bytes
+    typedef uint16_t elem;
+    struct Frag {
+        ab_u32x4 w;
+    };
+    static __device__ __forceinline__ Frag zero() { return {ab_u32x4{0u, 0u, 0u, 0u}}; }
+    static __device__ __forceinline__ f32x4_t mma(const Frag &a, const Frag &b, f32x4_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ab_bf16x8, a.w),
+                                                       __builtin_bit_cast(ab_bf16x8, b.w), c, 0, 0, 0);
+    }
+    // elements k .. k + 7 of a row of `len`
+    template <bool VEC>
+    static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
+        Frag f = zero();
+        if constexpr (VEC) {
+            if (k < len) f.w = *reinterpret_cast<const ab_u32x4 *>(row + k);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < len) f.w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+        }
+        return f;
+    }
+    static __device__ __forceinline__ Frag pack(const float (&x)[8]) {
+        return {ab_u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}};
+    }
+    // x as a sum of three bf16 numbers, to 2^-24
+    static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[3]) {
+        float rest[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+        for (int h = 0; h < 3; ++h) {
+            f[h] = pack(rest);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                rest[2 * i] -= low_bf16(f[h].w[i]);
+                rest[2 * i + 1] -= high_bf16(f[h].w[i]);
+            }
+        }
+    }
+    static constexpr int pieces = 3;
+};
+struct F32 {
+    static constexpr int code = DLCX_F32;
+    static constexpr int lane = 4;
+    typedef float elem;
+    struct Frag {
+        float x[8];
+    };
+    static __device__ __forceinline__ Frag zero() {
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.x[i] = 0.f;
+        return f;
+    }
+    static __device__ __forceinline__ f32x4_t mma(const Frag &a, const Frag &b, f32x4_t c) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[j], b.x[j], c, 0, 0, 0);
+        return c;
+    }
+    template <bool VEC>
+    static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
+        Frag f = zero();
+        if constexpr (VEC) {
+            if (k < len) {
+                const f32x4_t a = *reinterpret_cast<const f32x4_t *>(row + k);
+                const f32x4_t b = *reinterpret_cast<const f32x4_t *>(row + k + 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f.x[i] = a[i], f.x[4 + i] = b[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < len) f.x[i] = row[k + i];
+        }
+        return f;
+    }
+    static __device__ __forceinline__ Frag pack(const float (&x)[8]) {
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.x[i] = x[i];
+        return f;
+    }
+    static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[1]) { f[0] = pack(x); }
+    static constexpr int pieces = 1;
+};
+
+// 16 bytes of a row from element j on; elements from `len` on are zero.
+template <typename T, bool VEC>
+__device__ __forceinline__ ab_u32x4 load16(const typename T::elem *row, int j, int len) {
+    ab_u32x4 w = {0u, 0u, 0u, 0u};
+    if constexpr (VEC) {
+        if (j < len) w = *reinterpret_cast<const ab_u32x4 *>(row + j);
+    } else {
+#pragma unroll
+        for (int i = 0; i < T::lane; ++i)
+            if (j + i < len) {
+                if constexpr (T::lane == 8)
+                    w[i / 2] |= (uint32_t)row[j + i] << (16 * (i & 1));
+                else
+                    w[i] = __float_as_uint(row[j + i]);
+            }
+    }
+    return w;
+}
+
+// Eight rows of 16 bytes each, turned: fragment s holds element s of the eight rows.  Where the rows are
+// 8 (l / 16) + 0 .. 7 of a block and lane l has the elements from lane * g(l % 16) on, that is an
+// operand block of the columns lane * g(0 .. 15) + s without a word moved between lanes.
+__device__ __forceinline__ void turn(const ab_u32x4 (&row)[8], Bf16::Frag (&f)[8]) {
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+            f[s].w[p] = __builtin_amdgcn_perm(row[2 * p + 1][s / 2], row[2 * p][s / 2],
+                                              s & 1 ? 0x07060302u : 0x05040100u);
+}
+__device__ __forceinline__ void turn(const ab_u32x4 (&row)[8], F32::Frag (&f)[4]) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[s].x[j] = __uint_as_float(row[j][s]);
+}
+
+__device__ __forceinline__ int adapter_rank(int adapter, const int32_t *ranks, int r) {
+    return adapter < 0 ? 0 : ranks ? max(0, min(ranks[adapter], r)) : r;
+}
+
+// ---- down -------------------------------------------------------------------------------------------
+struct DownArgs {
+    const void *x;       // rows x len
+    int64_t ldx;
+    const void *f;       // count x r x len
+    const float *scale;  // what the result is multiplied with, or nullptr
+    const int32_t *ranks;
+    float *out;          // rows x r; splits of the reduction `stride` floats apart
+    int64_t stride;
+    int len, r, split_len;
+};
+
+// A workgroup has RT x 16 rows of one adapter, CT x 16 columns and a share of the reduction, which its
+// eight wavefronts divide again, 64 elements each in turn: every element of the factor is
+// read once per workgroup, and no wavefront waits for another before the end.
+constexpr int kDownWaves = 8;
+template <typename T, int RT, int CT, bool VEC>
+__global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a, const int32_t *ntiles,
+                                                                       const int4 *__restrict__ tiles,
+                                                                       const int32_t *__restrict__ order) {
+    __shared__ f32x4_t sums[kDownWaves / 2][RT * CT][64];
+    if ((int)blockIdx.x >= *ntiles) return;
+    const int4 tile = tiles[blockIdx.x];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
+    const int c0 = blockIdx.y * CT * 16;
+    const int rank = adapter_rank(tile.x, a.ranks, a.r);
+    float *out = a.out + blockIdx.z * a.stride;
+    if (c0 >= rank) {  // nothing but zeros here
+        for (int i = threadIdx.x; i < tile.z * CT * 16; i += kDownWaves * 64) {
+            const int c = c0 + i % (CT * 16);
+            if (c < a.r) out[(int64_t)order[tile.y + i / (CT * 16)] * a.r + c] = 0.f;
+        }
+        return;
+    }
+    const typename T::elem *xrow[RT], *frow[CT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)  // rows and columns beyond the last are the last again: not stored
+        xrow[i] = (const typename T::elem *)a.x +
+                  (int64_t)order[tile.y + min(i * 16 + row16, tile.z - 1)] * a.ldx;
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+        frow[i] = (const typename T::elem *)a.f +
+                  ((int64_t)tile.x * a.r + min(c0 + i * 16 + row16, rank - 1)) * a.len;
+    f32x4_t acc[RT][CT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[i][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int lo = blockIdx.z * a.split_len, hi = min(a.len, lo + a.split_len);
+    for (int k0 = lo + wave * 64; k0 < hi; k0 += kDownWaves * 64) {
+        typename T::Frag x[2][RT], f[2][CT];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = k0 + u * 32 + quad * 8;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) x[u][i] = T::template load8<VEC>(xrow[i], k, hi);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) f[u][c] = T::template load8<VEC>(frow[c], k, hi);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) acc[i][c] = T::mma(x[u][i], f[u][c], acc[i][c]);
+    }
+#pragma unroll
+    for (int half = kDownWaves / 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) sums[wave - half][i * CT + c][lane] = acc[i][c];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) acc[i][c] += sums[wave][i * CT + c][lane];
+        __syncthreads();
+    }
+    if (wave != 0) return;
+    const float scale = a.scale ? a.scale[tile.x] : 1.f;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int t = i * 16 + quad * 4 + v;
+            if (t >= tile.z) continue;
+            float *row = out + (int64_t)order[tile.y + t] * a.r;
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const int col = c0 + c * 16 + row16;
+                if (col < a.r) row[col] = col < rank ? scale * acc[i][c][v] : 0.f;
+            }
+        }
+}
+
+// ---- up ---------------------------------------------------------------------------------------------
+struct UpArgs {
+    const float *h;      // splits x rows x r, `stride` floats apart
+    int64_t stride;
+    float *h_out;        // their sum goes here (nullptr: it is there)
+    const void *f;       // count x r x len
+    const float *scale;
+    const int32_t *ranks;
+    const void *y_in;    // or nullptr
+    void *y_out;         // rows x len
+    int64_t ldi, ldo;
+    int len, r, splits, copy;  // copy: rows without adapter are to be written too
+};
+
+// A workgroup has 256 bytes of columns and up to `size` rows of one adapter.  It turns the factor's
+// columns into operand blocks in LDS once; then each wavefront takes 16 rows at a time: lane l has row
+// l % 16, and of its columns four times 16 bytes, which four lanes make 64 in a row.
+constexpr int kUpWaves = 4;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, const int32_t *ntiles,
+                                                                   const int4 *__restrict__ tiles,
+                                                                   const int32_t *__restrict__ order) {
+    extern __shared__ __attribute__((aligned(16))) char up_lds[];
+    typedef typename T::Frag Frag;
+    typedef typename T::elem elem;
+    Frag *blocks = reinterpret_cast<Frag *>(up_lds);  // [step][tile of columns][lane]
+    if ((int)blockIdx.y >= *ntiles) return;
+    const int4 tile = tiles[blockIdx.y];
+    if (tile.x < 0 && !a.copy) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
+    const int j0 = blockIdx.x * 16 * T::lane;
+    const int rank = adapter_rank(tile.x, a.ranks, a.r);
+    const int steps = (rank + 31) / 32;
+    const float scale = tile.x >= 0 && a.scale ? a.scale[tile.x] : 1.f;
+    for (int s = wave; s < steps; s += kUpWaves) {
+        const elem *f = (const elem *)a.f + ((int64_t)tile.x * a.r + s * 32 + quad * 8) * a.len;
+        const int j = j0 + T::lane * (4 * (row16 & 3) + row16 / 4);
+        ab_u32x4 rows[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            rows[i] = s * 32 + quad * 8 + i < rank ? load16<T, VEC>(f + (int64_t)i * a.len, j, a.len)
+                                                   : ab_u32x4{0u, 0u, 0u, 0u};
+        Frag turned[T::lane];
+        turn(rows, turned);
+#pragma unroll
+        for (int t = 0; t < T::lane; ++t) blocks[(s * T::lane + t) * 64 + lane] = turned[t];
+    }
+    __syncthreads();
+    for (int t0 = wave * 16; t0 < tile.z; t0 += kUpWaves * 16) {
+        const bool valid = t0 + row16 < tile.z;
+        const int64_t t = order[tile.y + min(t0 + row16, tile.z - 1)];
+        const elem *in = (const elem *)a.y_in + t * a.ldi;
+        ab_u32x4 y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            y[i] = a.y_in && valid ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len)
+                                   : ab_u32x4{0u, 0u, 0u, 0u};
+        f32x4_t acc[T::lane];
+#pragma unroll
+        for (int c = 0; c < T::lane; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < steps; ++s) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = s * 32 + quad * 8 + i;
+                x[i] = 0.f;
+                if (c < a.r) {
+                    for (int k = 0; k < a.splits; ++k) x[i] += a.h[k * a.stride + t * a.r + c];
+                    if (a.h_out && blockIdx.x == 0 && valid) a.h_out[t * a.r + c] = x[i];
+                }
+                x[i] *= scale;
+            }
+            const Frag h = T::pack(x);
+#pragma unroll
+            for (int c = 0; c < T::lane; ++c) acc[c] = T::mma(blocks[(s * T::lane + c) * 64 + lane], h, acc[c]);
+        }
+        if (a.h_out && blockIdx.x == 0 && valid)  // columns beyond the rank's last step
+            for (int c = steps * 32 + quad; c < a.r; c += 4) a.h_out[t * a.r + c] = 0.f;
+        if (!valid) continue;
+        elem *out = (elem *)a.y_out + t * a.ldo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + T::lane * (4 * i + quad);
+            ab_u32x4 w;
+            if constexpr (T::lane == 8) {
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+                    w[p] = pack2(low_bf16(y[i][p]) + acc[2 * p][i], high_bf16(y[i][p]) + acc[2 * p + 1][i]);
+            } else {
+#pragma unroll
+                for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(y[i][p]) + acc[p][i]);
+            }
+            if constexpr (VEC) {
+                if (j < a.len) *reinterpret_cast<ab_u32x4 *>(out + j) = w;
+            } else {
+#pragma unroll
+                for (int p = 0; p < T::lane; ++p)
+                    if (j + p < a.len) {
+                        if constexpr (T::lane == 8)
+                            out[j + p] = (uint16_t)(w[p / 2] >> (16 * (p & 1)));
+                        else
+                            out[j + p] = __uint_as_float(w[p]);
+                    }
+            }
+        }
+    }
+}
+
+// ---- grad -------------------------------------------------------------------------------------------
+struct GradProduct {
+    const float *u;      // rows x r
+    const float *scale;
+    const void *z;       // rows x len
+    int64_t ldz;
+    float *out;          // count x r x len
+    float *slabs;        // slab x r x len
+    int len, vec;
+};
+struct GradArgs {
+    GradProduct prod[2];
+    const int32_t *ranks;
+    int r, blocks0;  // column blocks of the first product
+};
+
+// A workgroup has 256 bytes of columns, CT x 16 columns of the factor and up to `size` rows of one adapter, 32
+// at a time to each of its wavefronts in turn.
+constexpr int kGradWaves = 4;
+template <typename T, int CT, bool VEC>
+__device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int rank, const int4 &tile,
+                                                  const int32_t *__restrict__ order, int c0, int j0,
+                                                  f32x4_t (*sums)[CT * T::lane][64]) {
+    typedef typename T::elem elem;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
+    f32x4_t acc[CT][T::lane];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int s = 0; s < T::lane; ++s) acc[c][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t0 = wave * 32; t0 < tile.z; t0 += kGradWaves * 32) {
+        int64_t t[8];
+        ab_u32x4 z[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int at = t0 + quad * 8 + i;
+            t[i] = at < tile.z ? order[tile.y + at] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            z[i] = t[i] >= 0 ? load16<T, VEC>((const elem *)p.z + t[i] * p.ldz, j0 + T::lane * row16, p.len)
+                             : ab_u32x4{0u, 0u, 0u, 0u};
+        typename T::Frag u[CT][T::pieces];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            const int col = c0 + c * 16 + row16;
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = t[i] >= 0 && col < rank ? p.u[t[i] * r + col] : 0.f;
+            T::split(x, u[c]);
+        }
+        typename T::Frag turned[T::lane];
+        turn(z, turned);
+#pragma unroll
+        for (int s = 0; s < T::lane; ++s)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int h = 0; h < T::pieces; ++h) acc[c][s] = T::mma(u[c][h], turned[s], acc[c][s]);
+    }
+#pragma unroll
+    for (int half = kGradWaves / 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int s = 0; s < T::lane; ++s) sums[wave - half][c * T::lane + s][lane] = acc[c][s];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int s = 0; s < T::lane; ++s) acc[c][s] += sums[wave][c * T::lane + s][lane];
+        __syncthreads();
+    }
+    if (wave != 0) return;
+    const float scale = p.scale ? p.scale[tile.x] : 1.f;
+    float *out = tile.w < 0 ? p.out + (int64_t)tile.x * r * p.len : p.slabs + (int64_t)tile.w * r * p.len;
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int col = c0 + c * 16 + quad * 4 + v;
+            if (col >= r) continue;
+            float *row = out + (int64_t)col * p.len;
+            const int j = j0 + T::lane * row16;
+#pragma unroll
+            for (int s = 0; s < T::lane; s += 4) {
+                const f32x4_t w = {scale * acc[c][s][v], scale * acc[c][s + 1][v], scale * acc[c][s + 2][v],
+                                   scale * acc[c][s + 3][v]};
+                if constexpr (VEC) {
+                    if (j + s < p.len) *reinterpret_cast<f32x4_t *>(row + j + s) = w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (j + s + i < p.len) row[j + s + i] = w[i];
+                }
+            }
+        }
+}
+template <typename T, int CT>
+__global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradArgs a, const int32_t *ntiles,
+                                                                          const int4 *__restrict__ tiles,
+                                                                          const int32_t *__restrict__ order) {
+    __shared__ f32x4_t sums[kGradWaves / 2][CT * T::lane][64];
+    if ((int)blockIdx.y >= *ntiles) return;
+    const int4 tile = tiles[blockIdx.y];
+    if (tile.x < 0) return;
+    const int rank = adapter_rank(tile.x, a.ranks, a.r);
+    const int second = (int)blockIdx.x >= a.blocks0;
+    const GradProduct &p = a.prod[second];
+    const int j0 = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 16 * T::lane, c0 = blockIdx.z * CT * 16;
+    if (p.vec)
+        adapter_grad_rows<T, CT, true>(p, a.r, rank, tile, order, c0, j0, sums);
+    else
+        adapter_grad_rows<T, CT, false>(p, a.r, rank, tile, order, c0, j0, sums);
+}
+
+// Gradients of adapters with several tiles, as the sum of their slabs in the rows' order, and zeros for
+// adapters without rows.
+__global__ __launch_bounds__(256) void adapter_sum_kernel(GradArgs a, const int2 *__restrict__ spans) {
+    const int2 span = spans[blockIdx.y];
+    if (span.y == 1) return;
+    const GradProduct &p = a.prod[blockIdx.z];
+    const int64_t size = (int64_t)a.r * p.len;
+    const int64_t step = (int64_t)gridDim.x * 256;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < size; e += step) {
+        double sum = 0.0;
+        for (int k = 0; k < span.y; ++k) sum += p.slabs[(span.x + k) * size + e];
+        p.out[blockIdx.y * size + e] = (float)sum;
+    }
+}
+
+// ---- launches -----------------------------------------------------------------------------------------
+static int launch_route(int64_t rows, const int32_t *ids, int count, const RouteView &v, hipStream_t st) {
+    const size_t lds = sizeof(int) * ((size_t)kRouteWaves * (count + 1) + 3 * (count + 2));
+    static size_t granted = 0;
+    int rc = grant_dynamic_lds((const void *)adapter_route_kernel, lds, &granted, "adapter_route lds");
+    if (rc != DLCX_OK) return rc;
+    Timed timed(KID_ADAPTER_ROUTE, st);
+    adapter_route_kernel<<<1, kRouteThreads, lds, st>>>((int)rows, ids, count, v);
+    return check_launch("adapter_route");
+}
+
+static inline bool rows_aligned(const void *p, int64_t ld, int es) { return aligned16(p) && ld * es % 16 == 0; }
+
+struct DownPlan {
+    int size, splits, split_len;
+};
+// Tiles of 64 rows where they fill the GPU, else of 16; what is missing to a workgroup for every
+// compute unit comes from splitting the reduction, no shorter than 512 elements.
+static DownPlan plan_down(int64_t rows, int count, int64_t len, int r) {
+    DownPlan p;
+    const int64_t cols = ceil_div(r, r > 32 ? 64 : 32);
+    p.size = rows * cols >= 64 * 256 ? 1 : 0;
+    const int64_t groups = ceil_div(rows, tile_rows(p.size)) * cols;
+    int64_t splits = ceil_div(256, groups);
+    const int64_t most = ceil_div(len, 512);
+    splits = splits < most ? splits : most;
+    splits = splits < 16 ? splits : 16;
+    p.split_len = (int)(ceil_div(ceil_div(len, splits), 64) * 64);
+    p.splits = (int)ceil_div(len, p.split_len);
+    return p;
+}
+
+template <typename T, int RT, int CT>
+static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const RouteView &v, int size, hipStream_t st) {
+    if (vec)
+        adapter_down_kernel<T, RT, CT, true><<<grid, kDownWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+    else
+        adapter_down_kernel<T, RT, CT, false><<<grid, kDownWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+}
+template <typename T>
+static int launch_down(const DownArgs &a, const DownPlan &plan, int64_t rows, int count, const RouteView &v,
+                       hipStream_t st) {
+    const int es = sizeof(typename T::elem);
+    const bool vec = rows_aligned(a.x, a.ldx, es) && aligned16(a.f) && a.len % 8 == 0;
+    const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
+    const dim3 grid((unsigned)max_tiles(rows, count, plan.size), (unsigned)ceil_div(a.r, ct * 16), (unsigned)plan.splits);
+    Timed timed(KID_ADAPTER_DOWN, st);
+    if (plan.size == 1) {
+        if (ct == 4) down_kernel<T, 4, 4>(a, vec, grid, v, 1, st);
+        else if (ct == 2) down_kernel<T, 4, 2>(a, vec, grid, v, 1, st);
+        else down_kernel<T, 4, 1>(a, vec, grid, v, 1, st);
+    } else {
+        if (ct == 4) down_kernel<T, 1, 4>(a, vec, grid, v, 0, st);
+        else if (ct == 2) down_kernel<T, 1, 2>(a, vec, grid, v, 0, st);
+        else down_kernel<T, 1, 1>(a, vec, grid, v, 0, st);
+    }
+    return check_launch("adapter_down");
+}
+
+template <typename T>
+static int launch_up(const UpArgs &a, int64_t rows, int count, const RouteView &v, hipStream_t st) {
+    const int es = sizeof(typename T::elem);
+    const bool vec = aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.ldo, es) &&
+                     (!a.y_in || rows_aligned(a.y_in, a.ldi, es));
+    const int64_t cols = ceil_div(a.len, 16 * T::lane);
+    int size = 3;
+    while (size > 1 && ceil_div(rows, tile_rows(size)) * cols < 1024) --size;
+    const size_t lds = (size_t)ceil_div(a.r, 32) * T::lane * 64 * sizeof(typename T::Frag);
+    static size_t granted[2] = {0, 0};
+    const void *kernel = vec ? (const void *)adapter_up_kernel<T, true> : (const void *)adapter_up_kernel<T, false>;
+    const int rc = grant_dynamic_lds(kernel, lds, &granted[vec], "adapter_up lds");
+    if (rc != DLCX_OK) return rc;
+    const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, count, size));
+    Timed timed(KID_ADAPTER_UP, st);
+    if (vec)
+        adapter_up_kernel<T, true><<<grid, kUpWaves * 64, lds, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+    else
+        adapter_up_kernel<T, false><<<grid, kUpWaves * 64, lds, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+    return check_launch("adapter_up");
+}
+
+constexpr int kGradGroups = 512;
+static int grad_size(int64_t rows, int64_t m, int64_t n, int lane) {
+    const int64_t cols = ceil_div(m, 16 * lane) + ceil_div(n, 16 * lane);
+    int size = 4;
+    while (size > 1 && ceil_div(rows, tile_rows(size)) * cols < kGradGroups) --size;
+    return size;
+}
+template <typename T>
+static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, const RouteView &v, hipStream_t st) {
+    const int64_t cols = a.blocks0 + ceil_div(a.prod[1].len, 16 * T::lane);
+    if (rows > 0) {
+        const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
+        const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, count, size), (unsigned)ceil_div(a.r, ct * 16));
+        Timed timed(KID_ADAPTER_GRAD, st);
+        if (ct == 4)
+            adapter_grad_kernel<T, 4><<<grid, kGradWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+        else if (ct == 2)
+            adapter_grad_kernel<T, 2><<<grid, kGradWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+        else
+            adapter_grad_kernel<T, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+        const int rc = check_launch("adapter_grad");
+        if (rc != DLCX_OK) return rc;
+    }
+    const int64_t most = (int64_t)a.r * (a.prod[0].len > a.prod[1].len ? a.prod[0].len : a.prod[1].len);
+    const int64_t gx = ceil_div(most, 1024);
+    Timed timed(KID_ADAPTER_SUM, st);
+    adapter_sum_kernel<<<dim3((unsigned)(gx < 256 ? gx : 256), (unsigned)count, 2), 256, 0, st>>>(a, v.spans[size]);
+    return check_launch("adapter_sum");
+}
+
+// ---- workspace: [own route][split sums of h or g][g][slabs of dP][slabs of dQ] ----------------------
+// Room for `rows` rows has room for fewer, though those are split further.  Sums: splits of tiles of 16
+// are at most 256 / (rows / 16) + 1, and at most 16.  Slabs: at most two for every full tile (of
+// adapters with more than one); tiles below the largest size are taken only where four times larger
+// ones make less than kGradGroups workgroups, so there are less than 4 kGradGroups / cols of them.
+struct AdapterSpace {
+    RouteView route;
+    float *split, *g, *slab_p, *slab_q;
+};
+static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base, AdapterSpace *s) {
+    AdapterSpace w;
+    size_t at = route_view(rows, d->count, (char *)base, &w.route);
+    auto take = [&](size_t bytes) {
+        char *p = (char *)base + at;
+        at += a256x(bytes);
+        return (float *)p;
+    };
+    const int lane = d->dtype == DLCX_BF16 ? Bf16::lane : F32::lane;
+    const int64_t cols = ceil_div(d->m, 16 * lane) + ceil_div(d->n, 16 * lane);
+    const size_t row = (size_t)d->r * sizeof(float);
+    w.split = take(row * (size_t)(16 * rows < rows + 4096 ? 16 * rows : rows + 4096));
+    w.g = take(row * (size_t)rows);
+    const int64_t small = 2 * (rows / tile_rows(1)), mid = ceil_div(kGradGroups * 8, cols);
+    const int64_t large = 2 * (rows / tile_rows(4));
+    const int64_t slabs = small < mid ? small : mid > large ? mid : large;
+    w.slab_p = take(row * (size_t)(slabs * d->m));
+    w.slab_q = take(row * (size_t)(slabs * d->n));
+    if (s) *s = w;
+    return at;
+}
+
+// h = x F^T (into `h`), then y_out = y_in + h G: the forward pass, and the first half of the gradient.
+template <typename T>
+static int down_and_up(const DownArgs &down, const UpArgs &up, int64_t rows, int count, float *split, float *h,
+                       const RouteView &v, hipStream_t st) {
+    const DownPlan plan = plan_down(rows, count, down.len, down.r);
+    DownArgs d = down;
+    d.split_len = plan.split_len;
+    d.stride = rows * d.r;
+    d.out = plan.splits > 1 ? split : h;
+    int rc = launch_down<T>(d, plan, rows, count, v, st);
+    if (rc != DLCX_OK) return rc;
+    UpArgs u = up;
+    u.h = d.out;
+    u.stride = d.stride;
+    u.splits = plan.splits;
+    u.h_out = plan.splits > 1 ? h : nullptr;
+    // (a row without adapter stays as it is where it is updated in place, unless its sums are still to be written)
+    u.copy = u.y_in != u.y_out || plan.splits > 1;
+    return launch_up<T>(u, rows, count, v, st);
+}
+
+}  // namespace dlcx
+
+using namespace dlcx;
+
+// ---- entry points -------------------------------------------------------------------------------------
+extern "C" {
+
+static int check_adapter(const dlcx_adapter_desc *d, int64_t rows) {
+    if (!d || rows < 0 || rows > (1 << 24)) return DLCX_EINVAL;
+    if (d->m < 1 || d->n < 1 || d->m > (1 << 24) || d->n > (1 << 24)) return DLCX_EINVAL;
+    if (d->r < 1 || d->r > DLCX_MAX_RANK || d->count < 1 || d->count > DLCX_MAX_ADAPTERS) return DLCX_EINVAL;
+    if (d->dtype != DLCX_F32 && d->dtype != DLCX_BF16) return DLCX_EINVAL;
+    return DLCX_OK;
+}
+static bool misaligned(const void *p, unsigned to) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+size_t dlcx_adapter_route_bytes(int64_t rows, int32_t count) {
+    if (rows < 0 || rows > (1 << 24) || count < 1 || count > DLCX_MAX_ADAPTERS) return 0;
+    return route_view(rows, count, nullptr, nullptr);
+}
+
+int dlcx_adapter_route(int64_t rows, const int32_t *ids, int32_t count, void *route, void *stream) {
+    if (rows < 0 || rows > (1 << 24) || count < 1 || count > DLCX_MAX_ADAPTERS) return DLCX_EINVAL;
+    if (!route || misaligned(route, 256) || (rows > 0 && (!ids || misaligned(ids, 4)))) return DLCX_EINVAL;
+    RouteView v;
+    route_view(rows, count, (char *)route, &v);
+    return launch_route(rows, ids, count, v, as_stream(stream));
+}
+
+size_t dlcx_adapter_workspace_bytes(const dlcx_adapter_desc *desc, int64_t rows) {
+    if (check_adapter(desc, rows) != DLCX_OK) return 0;
+    return adapter_space(desc, rows, nullptr, nullptr);
+}
+
+int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
+                         const int32_t *ids, const void *q, const void *p, const float *scale,
+                         const int32_t *ranks, const void *route, const void *y_in, int64_t ldy_in,
+                         void *y_out, int64_t ldy_out, float *h_out, void *workspace, void *stream) {
+    int rc = check_adapter(desc, rows);
+    if (rc != DLCX_OK) return rc;
+    if (rows == 0) return DLCX_OK;
+    const unsigned es = desc->dtype == DLCX_BF16 ? 2 : 4;
+    if (!x || !ids || !q || !p || !y_out || !h_out || !workspace) return DLCX_EINVAL;
+    if (misaligned(x, es) || misaligned(q, es) || misaligned(p, es) || misaligned(y_in, es) || misaligned(y_out, es))
+        return DLCX_EINVAL;
+    if (misaligned(ids, 4) || misaligned(scale, 4) || misaligned(ranks, 4) || misaligned(h_out, 4)) return DLCX_EINVAL;
+    if (misaligned(workspace, 256) || misaligned(route, 256)) return DLCX_EINVAL;
+    if (ldx < desc->n || ldy_out < desc->m || (y_in && ldy_in < desc->m)) return DLCX_EINVAL;
+    if (y_in == y_out && ldy_in != ldy_out) return DLCX_EINVAL;
+    hipStream_t st = as_stream(stream);
+    AdapterSpace s;
+    adapter_space(desc, rows, workspace, &s);
+    if (route)
+        route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
+    else if ((rc = launch_route(rows, ids, desc->count, s.route, st)) != DLCX_OK)
+        return rc;
+    DownArgs down = {x, ldx, q, nullptr, ranks, nullptr, 0, (int)desc->n, desc->r, 0};
+    UpArgs up = {nullptr, 0, nullptr, p, scale, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 1, 0};
+    return desc->dtype == DLCX_BF16
+               ? down_and_up<Bf16>(down, up, rows, desc->count, s.split, h_out, s.route, st)
+               : down_and_up<F32>(down, up, rows, desc->count, s.split, h_out, s.route, st);
+}
+
+int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
+                          const void *dy, int64_t lddy, const int32_t *ids, const void *q,
+                          const void *p, const float *scale, const int32_t *ranks, const void *route,
+                          const float *h, const void *dx_in, int64_t lddx_in, void *dx_out,
+                          int64_t lddx_out, float *dq_out, float *dp_out, void *workspace,
+                          void *stream) {
+    int rc = check_adapter(desc, rows);
+    if (rc != DLCX_OK) return rc;
+    const unsigned es = desc->dtype == DLCX_BF16 ? 2 : 4;
+    if (!q || !p || !dq_out || !dp_out || !workspace) return DLCX_EINVAL;
+    if (rows > 0 && (!x || !dy || !ids || !h || !dx_out)) return DLCX_EINVAL;
+    if (misaligned(x, es) || misaligned(dy, es) || misaligned(q, es) || misaligned(p, es) || misaligned(dx_in, es) ||
+        misaligned(dx_out, es))
+        return DLCX_EINVAL;
+    if (misaligned(ids, 4) || misaligned(scale, 4) || misaligned(ranks, 4) || misaligned(h, 4) ||
+        misaligned(dq_out, 4) || misaligned(dp_out, 4))
+        return DLCX_EINVAL;
+    if (misaligned(workspace, 256) || misaligned(route, 256)) return DLCX_EINVAL;
+    if (rows > 0 && (ldx < desc->n || lddy < desc->m || lddx_out < desc->n || (dx_in && lddx_in < desc->n)))
+        return DLCX_EINVAL;
+    if (rows > 0 && dx_in == dx_out && lddx_in != lddx_out) return DLCX_EINVAL;
+    hipStream_t st = as_stream(stream);
+    AdapterSpace s;
+    adapter_space(desc, rows, workspace, &s);
+    if (route)
+        route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
+    else if ((rc = launch_route(rows, ids, desc->count, s.route, st)) != DLCX_OK)
+        return rc;
+    if (rows > 0) {
+        DownArgs down = {dy, lddy, p, scale, ranks, nullptr, 0, (int)desc->m, desc->r, 0};
+        UpArgs up = {nullptr, 0, nullptr, q, nullptr, ranks, dx_in, dx_out, lddx_in, lddx_out, (int)desc->n,
+                     desc->r, 1, 0};
+        rc = desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, up, rows, desc->count, s.split, s.g, s.route, st)
+                                      : down_and_up<F32>(down, up, rows, desc->count, s.split, s.g, s.route, st);
+        if (rc != DLCX_OK) return rc;
+    }
+    const int lane = desc->dtype == DLCX_BF16 ? Bf16::lane : F32::lane;
+    GradArgs a;
+    a.prod[0] = {h, scale, dy, lddy, dp_out, s.slab_p, (int)desc->m, 0};
+    a.prod[1] = {s.g, nullptr, x, ldx, dq_out, s.slab_q, (int)desc->n, 0};
+    for (GradProduct &g : a.prod)
+        g.vec = rows_aligned(g.z, g.ldz, (int)es) && g.len % lane == 0 && aligned16(g.out);
+    a.ranks = ranks;
+    a.r = desc->r;
+    a.blocks0 = (int)ceil_div(desc->m, 16 * lane);
+    const int size = grad_size(rows, desc->m, desc->n, lane);
+    return desc->dtype == DLCX_BF16 ? launch_grad<Bf16>(a, rows, desc->count, size, s.route, st)
+                                    : launch_grad<F32>(a, rows, desc->count, size, s.route, st);
+}
+
+}  // extern "C"
