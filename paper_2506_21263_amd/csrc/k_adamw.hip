@@ -159,7 +159,7 @@ __device__ __forceinline__ void store_codes(void *base, int64_t e, int left, ad_
 // of the root, 1 / c of the value, so values down to 1e-4 of a group's largest m (2.5e-10 of its largest v)
 // keep a code of their own, which a linear code of 8 bits has for values down to 4e-3 only.
 __device__ __forceinline__ float decode_m(uint32_t w, int i, float scale) {
-    const float c = (float)((int32_t)(w << (24 - 8 * i)) >> 24);
+    const float c = (float)(((w ^ 0x80808080u) >> (8 * i)) & 0xFFu) - 128.f;
     return c * fabsf(c) * scale;
 }
 __device__ __forceinline__ float decode_v(uint32_t w, int i, float scale) {
@@ -182,12 +182,16 @@ __device__ __forceinline__ float group_scale(float amax, float top, float *inv) 
     *inv = none ? 0.f : top * top / amax;
     return none ? 0.f : amax * (1.f / (top * top));
 }
-// The code of x >= 0 is the integer next to sqrt(x / scale), both rounded correctly.  Four in five wavefronts
-// have it from a product and the hardware's root, which together are off by less than 7e-5 codes; one that
-// lies within 1e-4 of the middle between two codes is decided by the definition (exact_code).
+// The code of x >= 0 is the integer next to sqrt(x / scale), both operations rounded correctly, where x of a
+// second moment is a correctly rounded root itself.  With IEEE quotients and roots throughout the step
+// was bound by arithmetic (4.2 TB/s of 8192 x 28672 bf16 tensors); so a code is taken from a product and the
+// hardware's roots (1 unit in the last place), together off by less than 8e-5 codes, and where one of a
+// thread's lies within 1e-4 of the middle between two codes, all of them are decided by the definition.
 __device__ __forceinline__ float near_root(float x, float inv) { return __builtin_amdgcn_sqrtf(x * inv); }
-__device__ __forceinline__ bool undecided(float root, float code) { return fabsf(root - code) > 0.4999f; }
+__device__ __forceinline__ float from_middle(float root) { return fabsf(__builtin_amdgcn_fractf(root) - 0.5f); }
 __device__ __forceinline__ float exact_code(float x, float scale) { return rintf(sqrtf(x / scale)); }
+// Below this a group's largest v may have company whose hardware root is flushed to zero and whose code is not 1.
+constexpr float kTinyV = 0x1p-89f;
 
 // a x + b y with every operation rounded: what the codes of the moments hang on is then the same wherever
 // the formula is evaluated.
@@ -228,45 +232,47 @@ __device__ __forceinline__ void adamw_elements(const dlcx_tensor &t, const Adamw
         const float gi = g[i] * gs;
         m[i] = weighted_sum(m[i], s.beta1, gi, s.one_minus_beta1);
         v[i] = weighted_sum(v[i], s.beta2, gi * gi, s.one_minus_beta2);
-        root[i] = sqrtf(v[i]);
-        p[i] = p[i] * decay - rate * (m[i] / (root[i] * s.inv_sqrt_bc2 + s.eps));
+        if constexpr (BITS == 32) {
+            p[i] = p[i] * decay - rate * (m[i] / (sqrtf(v[i]) * s.inv_sqrt_bc2 + s.eps));
+        } else {
+            // (a v that the hardware's root would flush counts as the smallest one that it does not)
+            root[i] = __builtin_amdgcn_sqrtf(fmaxf(v[i], 0x1p-126f));
+            p[i] = p[i] * decay - rate * (m[i] * __builtin_amdgcn_rcpf(root[i] * s.inv_sqrt_bc2 + s.eps));
+        }
     }
     if constexpr (BITS == 8) {
         uint32_t am = 0, av = 0;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             am = max(am, __float_as_uint(m[i]) & 0x7FFFFFFFu);
-            av = max(av, __float_as_uint(root[i]) & 0x7FFFFFFFu);
+            av = max(av, __float_as_uint(v[i]) & 0x7FFFFFFFu);
         }
         float m_inv, v_inv;
+        const float v_max = __uint_as_float(row_max(av));
         m_scale = group_scale(__uint_as_float(row_max(am)), kTopM, &m_inv);
-        v_scale = group_scale(__uint_as_float(row_max(av)), kTopV, &v_inv);
-        mc = vc = ad_u32x2{0u, 0u};
-        float cm[kVec], cv[kVec];
-        bool open = false;
+        v_scale = group_scale(sqrtf(v_max), kTopV, &v_inv);
+        float cm[kVec], cv[kVec], closest = v_max < kTinyV ? 0.f : 1.f;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const float rm = near_root(fabsf(m[i]), m_inv), rv = near_root(root[i], v_inv);
-            cm[i] = rintf(rm);
-            cv[i] = rintf(rv);
-            open = open || undecided(rm, cm[i]) || undecided(rv, cv[i]);
+            cm[i] = near_root(fabsf(m[i]), m_inv);
+            cv[i] = near_root(root[i], v_inv);
+            closest = fminf(closest, fminf(from_middle(cm[i]), from_middle(cv[i])));
         }
-        if (open) {
+        if (closest < 1e-4f) {
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                if (m_scale > 0.f) cm[i] = exact_code(fabsf(m[i]), m_scale);
-                if (v_scale > 0.f) cv[i] = exact_code(root[i], v_scale);
+                cm[i] = m_scale > 0.f ? exact_code(fabsf(m[i]), m_scale) : 0.f;
+                cv[i] = v_scale > 0.f ? exact_code(sqrtf(v[i]), v_scale) : 0.f;
             }
         }
+        mc = vc = ad_u32x2{0u, 0u};
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            int c = (int)fminf(cm[i], kTopM);
-            c = m[i] < 0.f ? -c : c;
-            mc[i / 4] |= ((uint32_t)c & 0xFFu) << (8 * (i & 3));
-            c = (int)fminf(cv[i], kTopV);
-            c = v[i] > 0.f ? max(c, 1) : c;
-            vc[i / 4] |= (uint32_t)c << (8 * (i & 3));
+            const float c = copysignf(fminf(cm[i], kTopM), m[i]) + 128.f;
+            mc[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(rintf(c), i & 3, mc[i / 4]);
+            vc[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(rintf(v[i] > 0.f ? fmaxf(cv[i], 1.f) : 0.f), i & 3, vc[i / 4]);
         }
+        mc ^= 0x80808080u;
         if (left > 0) {
             store_codes(t.m, e, left, mc);
             store_codes(t.v, e, left, vc);
