@@ -12,164 +12,135 @@
 namespace dlcx {
 
 // ---- rows grouped by adapter ----------------------------------------------------------------------
-// Tables of tiles of one adapter's rows, in five sizes: a launch takes the one that fills the GPU.
-constexpr int kSizes = 5;
-__host__ __device__ constexpr int tile_rows(int size) { return 16 << (2 * size); }  // 16 .. 4096
+// Bucket a < count holds the rows of adapter a, bucket `count` the rows without one.  A launch cuts every
+// bucket into tiles of as many rows as fill the GPU; a workgroup finds its tile in the buckets' places.
 constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
 
-struct RouteView {
-    int32_t *ntiles;        // kSizes
-    int32_t *order;         // rows, an adapter's ones in their own order, adapter after adapter, then the rest
-    int4 *tiles[kSizes];    // adapter (-1: none), first place in `order`, rows, slab (-1: only tile)
-    int2 *spans[kSizes];    // per adapter: first slab (-1: one tile or none), tiles
+struct Route {
+    int32_t *first;  // count + 2: first place of each bucket in `order`, then the number of rows
+    int32_t *order;  // rows: bucket after bucket, in a bucket in the rows' own order
+    int count;
 };
-static size_t route_view(int64_t rows, int count, char *base, RouteView *v) {
-    size_t at = 0;
-    auto take = [&](size_t bytes) {
-        char *p = base + at;
-        at += a256x(bytes);
-        return p;
-    };
-    RouteView w;
-    w.ntiles = (int32_t *)take(kSizes * sizeof(int32_t));
-    w.order = (int32_t *)take((size_t)rows * sizeof(int32_t));
-    for (int s = 0; s < kSizes; ++s) {
-        w.tiles[s] = (int4 *)take((size_t)(rows / tile_rows(s) + count + 1) * sizeof(int4));
-        w.spans[s] = (int2 *)take((size_t)count * sizeof(int2));
-    }
-    if (v) *v = w;
-    return at;
+static size_t route_view(int64_t rows, int count, char *base, Route *v) {
+    const size_t heads = a256x((size_t)(count + 2) * sizeof(int32_t));
+    if (v) *v = {(int32_t *)base, (int32_t *)(base + heads), count};
+    return heads + a256x((size_t)rows * sizeof(int32_t));
 }
 static inline int64_t max_tiles(int64_t rows, int count, int size) {
-    return rows / tile_rows(size) + (rows < count + 1 ? rows : count + 1);
+    return rows / size + (rows < count + 1 ? rows : count + 1);
 }
 
-// Exclusive prefix sum over the workgroup's threads; *total: the sum of all.
-__device__ __forceinline__ int scan_workgroup(int x, int *lds, int *total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    int y = x;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int up = __shfl_up(y, d, 64);
-        if (lane >= d) y += up;
+// Inclusive prefix sum over a wavefront's lanes.
+__device__ __forceinline__ int scan_wave(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+    return x;
+}
+
+struct Tile {
+    int adapter;  // -1: rows without one; -2: there is no such tile
+    int at, rows; // places in `order`
+    int slab;     // number among the tiles of adapters that have several, -1: the only one
+};
+// Tile `index` of the buckets' tiles of `size` rows; 64 buckets at a time, the same in every wavefront.
+__device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
+    const int lane = threadIdx.x & 63;
+    int tiles = 0, slabs = 0;
+    for (int base = 0; base <= r.count; base += 64) {
+        const int b = base + lane;
+        const int at = b <= r.count ? r.first[b] : 0, end = b <= r.count ? r.first[b + 1] : 0;
+        const int n = (end - at + size - 1) / size, several = n > 1 && b < r.count ? n : 0;
+        const int upto = tiles + scan_wave(n), slabs_upto = slabs + scan_wave(several);
+        const uint64_t after = __ballot(upto > index);
+        if (after) {
+            const int l = __ffsll((unsigned long long)after) - 1;
+            const int k = index - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+            const int from = __builtin_amdgcn_readlane(at, l) + k * size;
+            const int several_l = __builtin_amdgcn_readlane(several, l);
+            Tile t;
+            t.adapter = base + l < r.count ? base + l : -1;
+            t.at = from;
+            t.rows = min(size, __builtin_amdgcn_readlane(end, l) - from);
+            t.slab = several_l ? __builtin_amdgcn_readlane(slabs_upto, l) - several_l + k : -1;
+            return t;
+        }
+        tiles = __builtin_amdgcn_readlane(upto, 63);
+        slabs = __builtin_amdgcn_readlane(slabs_upto, 63);
     }
-    if (lane == 63) lds[wave] = y;
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < kRouteWaves; ++w) {
-        const int s = lds[w];
-        before += w < wave ? s : 0;
-        all += s;
-    }
-    __syncthreads();
-    *total = all;
-    return before + y - x;
+    return {-2, 0, 0, -1};
 }
 
 // One workgroup sorts the rows by counting: every wavefront counts its own share, the counts become the
 // places where it writes, and the lanes of equal adapters find their order by ballots of the index's
 // bits, so the order within an adapter is that of the rows.
 __global__ __launch_bounds__(kRouteThreads) void adapter_route_kernel(int rows,
-                                                                      const int32_t *__restrict__ ids,
-                                                                      int count, RouteView v) {
-    extern __shared__ int lds[];
-    int *cursor = lds;                                // kRouteWaves x (count + 1)
-    int *first = cursor + kRouteWaves * (count + 1);  // count + 2: first place of each adapter
-    int *tile0 = first + count + 2;                   // count + 2: first tile of each adapter
-    int *slab0 = tile0 + count + 2;                   // count + 1
-    __shared__ int part[kRouteWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, buckets = count + 1;
-    const uint64_t below = (1ull << lane) - 1;
+                                                                      const int32_t *__restrict__ ids, Route r) {
+    extern __shared__ int cursor[];  // kRouteWaves x buckets
+    __shared__ int sums[kRouteWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, buckets = r.count + 1;
     for (int i = threadIdx.x; i < kRouteWaves * buckets; i += kRouteThreads) cursor[i] = 0;
-    __syncthreads();
     const int share = (rows + kRouteThreads - 1) / kRouteThreads * 64;
     const int lo = min(rows, wave * share), hi = min(rows, lo + share);
-    int bits = 0;
-    while ((1 << bits) < buckets) ++bits;
+    const int bits = 32 - __clz(buckets - 1);
     int *mine = cursor + wave * buckets;
+    int id[16];  // up to 16384 rows they are read once for both passes
+    __syncthreads();
     for (int pass = 0; pass < 2; ++pass) {
-        for (int base = lo; base < hi; base += 8 * 64) {
-            int id[8];
+        for (int base = lo; base < hi; base += 16 * 64) {
+            if (pass == 0 || share > 16 * 64)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int t = base + u * 64 + lane;
-                id[u] = t < hi ? ids[t] : -1;
-            }
+                for (int u = 0; u < 16; ++u) {
+                    const int t = base + u * 64 + lane;
+                    id[u] = t < hi ? ids[t] : -1;
+                }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < 16; ++u) {
                 const int t = base + u * 64 + lane;
-                const int b = id[u] >= 0 && id[u] < count ? id[u] : count;
+                const int b = id[u] >= 0 && id[u] < r.count ? id[u] : r.count;
                 uint64_t same = __ballot(t < hi);
                 if (same == 0) break;
                 for (int k = 0; k < bits; ++k) {
                     const uint64_t one = __ballot((b >> k) & 1);
                     same &= (b >> k) & 1 ? one : ~one;
                 }
-                if (t < hi) {
-                    const int rank = __popcll(same & below);
-                    if (pass == 1) v.order[mine[b] + rank] = t;
-                    wave_sync();
-                    if (rank == 0) mine[b] += __popcll(same);
-                }
+                const int rank = __popcll(same & ((1ull << lane) - 1));
+                if (t < hi && pass == 1) r.order[mine[b] + rank] = t;
+                wave_sync();
+                if (t < hi && rank == 0) mine[b] += __popcll(same);
                 wave_sync();
             }
         }
         __syncthreads();
-        if (pass == 1) break;
-        int carry = 0;
+        if (pass == 1) return;
+        int before = 0;
         for (int base = 0; base < buckets; base += kRouteThreads) {
             const int b = base + (int)threadIdx.x;
-            int n = 0, total;
+            int n = 0;
             if (b < buckets)
                 for (int w = 0; w < kRouteWaves; ++w) n += cursor[w * buckets + b];
-            int at = carry + scan_workgroup(n, part, &total);
+            const int upto = scan_wave(n);
+            if (lane == 63) sums[wave] = upto;
+            __syncthreads();
+            int at = before + upto - n;
+            for (int w = 0; w < kRouteWaves; ++w) {
+                at += w < wave ? sums[w] : 0;
+                before += sums[w];
+            }
             if (b < buckets) {
-                first[b] = at;
+                r.first[b] = at;
                 for (int w = 0; w < kRouteWaves; ++w) {
                     const int c = cursor[w * buckets + b];
                     cursor[w * buckets + b] = at;
                     at += c;
                 }
             }
-            carry += total;
+            __syncthreads();
         }
-        if (threadIdx.x == 0) first[buckets] = rows;
-        __syncthreads();
-    }
-    for (int s = 0; s < kSizes; ++s) {
-        const int size = tile_rows(s);
-        int tiles = 0, slabs = 0;
-        for (int base = 0; base < buckets; base += kRouteThreads) {
-            const int b = base + (int)threadIdx.x;
-            const int n = b < buckets ? (first[b + 1] - first[b] + size - 1) / size : 0;
-            const int apart = n > 1 && b < count ? n : 0;
-            int all, more;
-            const int t0 = tiles + scan_workgroup(n, part, &all);
-            const int s0 = slabs + scan_workgroup(apart, part, &more);
-            if (b < buckets) {
-                tile0[b] = t0;
-                slab0[b] = apart ? s0 : -1;
-            }
-            if (b < count) v.spans[s][b] = make_int2(apart ? s0 : -1, n);
-            tiles += all;
-            slabs += more;
-        }
-        if (threadIdx.x == 0) {
-            tile0[buckets] = tiles;
-            v.ntiles[s] = tiles;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < tiles; i += kRouteThreads) {
-            int b = 0;  // the last one that begins at or before tile i (one without tiles begins with the next)
-            for (int len = buckets; len > 1;) {
-                const int half = len / 2;
-                if (tile0[b + half] <= i) b += half, len -= half;
-                else len = half;
-            }
-            const int k = i - tile0[b], at = first[b] + k * size;
-            v.tiles[s][i] = make_int4(b < count ? b : -1, at, min(size, first[b + 1] - at),
-                                      slab0[b] < 0 ? -1 : slab0[b] + k);
-        }
-        __syncthreads();
+        if (threadIdx.x == 0) r.first[buckets] = rows;
     }
 }
 
@@ -339,20 +310,19 @@ struct DownArgs {
 // read once per workgroup, and no wavefront waits for another before the end.
 constexpr int kDownWaves = 8;
 template <typename T, int RT, int CT, bool VEC>
-__global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a, const int32_t *ntiles,
-                                                                       const int4 *__restrict__ tiles,
-                                                                       const int32_t *__restrict__ order) {
+__global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a, Route route) {
     __shared__ f32x4_t sums[kDownWaves / 2][RT * CT][64];
-    if ((int)blockIdx.x >= *ntiles) return;
-    const int4 tile = tiles[blockIdx.x];
+    const Tile tile = find_tile(route, RT * 16, blockIdx.x);
+    if (tile.adapter < -1) return;
+    const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
     const int c0 = blockIdx.y * CT * 16;
-    const int rank = adapter_rank(tile.x, a.ranks, a.r);
+    const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     float *out = a.out + blockIdx.z * a.stride;
     if (c0 >= rank) {  // nothing but zeros here
-        for (int i = threadIdx.x; i < tile.z * CT * 16; i += kDownWaves * 64) {
+        for (int i = threadIdx.x; i < tile.rows * CT * 16; i += kDownWaves * 64) {
             const int c = c0 + i % (CT * 16);
-            if (c < a.r) out[(int64_t)order[tile.y + i / (CT * 16)] * a.r + c] = 0.f;
+            if (c < a.r) out[(int64_t)order[i / (CT * 16)] * a.r + c] = 0.f;
         }
         return;
     }
@@ -360,11 +330,11 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
 #pragma unroll
     for (int i = 0; i < RT; ++i)  // rows and columns beyond the last are the last again: not stored
         xrow[i] = (const typename T::elem *)a.x +
-                  (int64_t)order[tile.y + min(i * 16 + row16, tile.z - 1)] * a.ldx;
+                  (int64_t)order[min(i * 16 + row16, tile.rows - 1)] * a.ldx;
 #pragma unroll
     for (int i = 0; i < CT; ++i)
         frow[i] = (const typename T::elem *)a.f +
-                  ((int64_t)tile.x * a.r + min(c0 + i * 16 + row16, rank - 1)) * a.len;
+                  ((int64_t)tile.adapter * a.r + min(c0 + i * 16 + row16, rank - 1)) * a.len;
     f32x4_t acc[RT][CT];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -404,14 +374,14 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
         __syncthreads();
     }
     if (wave != 0) return;
-    const float scale = a.scale ? a.scale[tile.x] : 1.f;
+    const float scale = a.scale ? a.scale[tile.adapter] : 1.f;
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int t = i * 16 + quad * 4 + v;
-            if (t >= tile.z) continue;
-            float *row = out + (int64_t)order[tile.y + t] * a.r;
+            if (t >= tile.rows) continue;
+            float *row = out + (int64_t)order[t] * a.r;
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 const int col = c0 + c * 16 + row16;
@@ -439,23 +409,21 @@ struct UpArgs {
 // l % 16, and of its columns four times 16 bytes, which four lanes make 64 in a row.
 constexpr int kUpWaves = 4;
 template <typename T, bool VEC>
-__global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, const int32_t *ntiles,
-                                                                   const int4 *__restrict__ tiles,
-                                                                   const int32_t *__restrict__ order) {
+__global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Route route, int size) {
     extern __shared__ __attribute__((aligned(16))) char up_lds[];
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
     Frag *blocks = reinterpret_cast<Frag *>(up_lds);  // [step][tile of columns][lane]
-    if ((int)blockIdx.y >= *ntiles) return;
-    const int4 tile = tiles[blockIdx.y];
-    if (tile.x < 0 && !a.copy) return;
+    const Tile tile = find_tile(route, size, blockIdx.y);
+    if (tile.adapter < (a.copy ? -1 : 0)) return;
+    const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
     const int j0 = blockIdx.x * 16 * T::lane;
-    const int rank = adapter_rank(tile.x, a.ranks, a.r);
+    const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int steps = (rank + 31) / 32;
-    const float scale = tile.x >= 0 && a.scale ? a.scale[tile.x] : 1.f;
+    const float scale = tile.adapter >= 0 && a.scale ? a.scale[tile.adapter] : 1.f;
     for (int s = wave; s < steps; s += kUpWaves) {
-        const elem *f = (const elem *)a.f + ((int64_t)tile.x * a.r + s * 32 + quad * 8) * a.len;
+        const elem *f = (const elem *)a.f + ((int64_t)tile.adapter * a.r + s * 32 + quad * 8) * a.len;
         const int j = j0 + T::lane * (4 * (row16 & 3) + row16 / 4);
         ab_u32x4 rows[8];
 #pragma unroll
@@ -468,9 +436,9 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, con
         for (int t = 0; t < T::lane; ++t) blocks[(s * T::lane + t) * 64 + lane] = turned[t];
     }
     __syncthreads();
-    for (int t0 = wave * 16; t0 < tile.z; t0 += kUpWaves * 16) {
-        const bool valid = t0 + row16 < tile.z;
-        const int64_t t = order[tile.y + min(t0 + row16, tile.z - 1)];
+    for (int t0 = wave * 16; t0 < tile.rows; t0 += kUpWaves * 16) {
+        const bool valid = t0 + row16 < tile.rows;
+        const int64_t t = order[min(t0 + row16, tile.rows - 1)];
         const elem *in = (const elem *)a.y_in + t * a.ldi;
         ab_u32x4 y[4];
 #pragma unroll
@@ -548,7 +516,7 @@ struct GradArgs {
 // at a time to each of its wavefronts in turn.
 constexpr int kGradWaves = 4;
 template <typename T, int CT, bool VEC>
-__device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int rank, const int4 &tile,
+__device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int rank, const Tile &tile,
                                                   const int32_t *__restrict__ order, int c0, int j0,
                                                   f32x4_t (*sums)[CT * T::lane][64]) {
     typedef typename T::elem elem;
@@ -558,13 +526,13 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int s = 0; s < T::lane; ++s) acc[c][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int t0 = wave * 32; t0 < tile.z; t0 += kGradWaves * 32) {
+    for (int t0 = wave * 32; t0 < tile.rows; t0 += kGradWaves * 32) {
         int64_t t[8];
         ab_u32x4 z[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int at = t0 + quad * 8 + i;
-            t[i] = at < tile.z ? order[tile.y + at] : -1;
+            t[i] = at < tile.rows ? order[at] : -1;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -604,8 +572,8 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
         __syncthreads();
     }
     if (wave != 0) return;
-    const float scale = p.scale ? p.scale[tile.x] : 1.f;
-    float *out = tile.w < 0 ? p.out + (int64_t)tile.x * r * p.len : p.slabs + (int64_t)tile.w * r * p.len;
+    const float scale = p.scale ? p.scale[tile.adapter] : 1.f;
+    float *out = tile.slab < 0 ? p.out + (int64_t)tile.adapter * r * p.len : p.slabs + (int64_t)tile.slab * r * p.len;
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -629,14 +597,12 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
         }
 }
 template <typename T, int CT>
-__global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradArgs a, const int32_t *ntiles,
-                                                                          const int4 *__restrict__ tiles,
-                                                                          const int32_t *__restrict__ order) {
+__global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradArgs a, Route route, int size) {
     __shared__ f32x4_t sums[kGradWaves / 2][CT * T::lane][64];
-    if ((int)blockIdx.y >= *ntiles) return;
-    const int4 tile = tiles[blockIdx.y];
-    if (tile.x < 0) return;
-    const int rank = adapter_rank(tile.x, a.ranks, a.r);
+    const Tile tile = find_tile(route, size, blockIdx.y);
+    if (tile.adapter < 0) return;
+    const int32_t *__restrict__ order = route.order + tile.at;
+    const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int second = (int)blockIdx.x >= a.blocks0;
     const GradProduct &p = a.prod[second];
     const int j0 = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 16 * T::lane, c0 = blockIdx.z * CT * 16;
@@ -648,27 +614,34 @@ __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradAr
 
 // Gradients of adapters with several tiles, as the sum of their slabs in the rows' order, and zeros for
 // adapters without rows.
-__global__ __launch_bounds__(256) void adapter_sum_kernel(GradArgs a, const int2 *__restrict__ spans) {
-    const int2 span = spans[blockIdx.y];
-    if (span.y == 1) return;
+__global__ __launch_bounds__(256) void adapter_sum_kernel(GradArgs a, Route route, int size) {
+    int tiles = 0, slab = 0;
+    for (int b = threadIdx.x & 63; b <= (int)blockIdx.y; b += 64) {
+        const int n = (route.first[b + 1] - route.first[b] + size - 1) / size;
+        if (b == (int)blockIdx.y) tiles = n;
+        else slab += n > 1 ? n : 0;
+    }
+    tiles = __builtin_amdgcn_readlane(scan_wave(tiles), 63);
+    slab = __builtin_amdgcn_readlane(scan_wave(slab), 63);
+    if (tiles == 1) return;
     const GradProduct &p = a.prod[blockIdx.z];
-    const int64_t size = (int64_t)a.r * p.len;
+    const int64_t elems = (int64_t)a.r * p.len;
     const int64_t step = (int64_t)gridDim.x * 256;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < size; e += step) {
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < elems; e += step) {
         double sum = 0.0;
-        for (int k = 0; k < span.y; ++k) sum += p.slabs[(span.x + k) * size + e];
-        p.out[blockIdx.y * size + e] = (float)sum;
+        for (int k = 0; k < tiles; ++k) sum += p.slabs[(slab + k) * elems + e];
+        p.out[blockIdx.y * elems + e] = (float)sum;
     }
 }
 
 // ---- launches -----------------------------------------------------------------------------------------
-static int launch_route(int64_t rows, const int32_t *ids, int count, const RouteView &v, hipStream_t st) {
-    const size_t lds = sizeof(int) * ((size_t)kRouteWaves * (count + 1) + 3 * (count + 2));
+static int launch_route(int64_t rows, const int32_t *ids, const Route &r, hipStream_t st) {
+    const size_t lds = sizeof(int) * (size_t)kRouteWaves * (r.count + 1);
     static size_t granted = 0;
     int rc = grant_dynamic_lds((const void *)adapter_route_kernel, lds, &granted, "adapter_route lds");
     if (rc != DLCX_OK) return rc;
     Timed timed(KID_ADAPTER_ROUTE, st);
-    adapter_route_kernel<<<1, kRouteThreads, lds, st>>>((int)rows, ids, count, v);
+    adapter_route_kernel<<<1, kRouteThreads, lds, st>>>((int)rows, ids, r);
     return check_launch("adapter_route");
 }
 
@@ -682,8 +655,8 @@ struct DownPlan {
 static DownPlan plan_down(int64_t rows, int count, int64_t len, int r) {
     DownPlan p;
     const int64_t cols = ceil_div(r, r > 32 ? 64 : 32);
-    p.size = rows * cols >= 64 * 256 ? 1 : 0;
-    const int64_t groups = ceil_div(rows, tile_rows(p.size)) * cols;
+    p.size = rows * cols >= 64 * 256 ? 64 : 16;
+    const int64_t groups = ceil_div(rows, p.size) * cols;
     int64_t splits = ceil_div(256, groups);
     const int64_t most = ceil_div(len, 512);
     splits = splits < most ? splits : most;
@@ -694,40 +667,40 @@ static DownPlan plan_down(int64_t rows, int count, int64_t len, int r) {
 }
 
 template <typename T, int RT, int CT>
-static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const RouteView &v, int size, hipStream_t st) {
+static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const Route &v, hipStream_t st) {
     if (vec)
-        adapter_down_kernel<T, RT, CT, true><<<grid, kDownWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+        adapter_down_kernel<T, RT, CT, true><<<grid, kDownWaves * 64, 0, st>>>(a, v);
     else
-        adapter_down_kernel<T, RT, CT, false><<<grid, kDownWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+        adapter_down_kernel<T, RT, CT, false><<<grid, kDownWaves * 64, 0, st>>>(a, v);
 }
 template <typename T>
-static int launch_down(const DownArgs &a, const DownPlan &plan, int64_t rows, int count, const RouteView &v,
+static int launch_down(const DownArgs &a, const DownPlan &plan, int64_t rows, int count, const Route &v,
                        hipStream_t st) {
     const int es = sizeof(typename T::elem);
     const bool vec = rows_aligned(a.x, a.ldx, es) && aligned16(a.f) && a.len % 8 == 0;
     const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
     const dim3 grid((unsigned)max_tiles(rows, count, plan.size), (unsigned)ceil_div(a.r, ct * 16), (unsigned)plan.splits);
     Timed timed(KID_ADAPTER_DOWN, st);
-    if (plan.size == 1) {
-        if (ct == 4) down_kernel<T, 4, 4>(a, vec, grid, v, 1, st);
-        else if (ct == 2) down_kernel<T, 4, 2>(a, vec, grid, v, 1, st);
-        else down_kernel<T, 4, 1>(a, vec, grid, v, 1, st);
+    if (plan.size == 64) {
+        if (ct == 4) down_kernel<T, 4, 4>(a, vec, grid, v, st);
+        else if (ct == 2) down_kernel<T, 4, 2>(a, vec, grid, v, st);
+        else down_kernel<T, 4, 1>(a, vec, grid, v, st);
     } else {
-        if (ct == 4) down_kernel<T, 1, 4>(a, vec, grid, v, 0, st);
-        else if (ct == 2) down_kernel<T, 1, 2>(a, vec, grid, v, 0, st);
-        else down_kernel<T, 1, 1>(a, vec, grid, v, 0, st);
+        if (ct == 4) down_kernel<T, 1, 4>(a, vec, grid, v, st);
+        else if (ct == 2) down_kernel<T, 1, 2>(a, vec, grid, v, st);
+        else down_kernel<T, 1, 1>(a, vec, grid, v, st);
     }
     return check_launch("adapter_down");
 }
 
 template <typename T>
-static int launch_up(const UpArgs &a, int64_t rows, int count, const RouteView &v, hipStream_t st) {
+static int launch_up(const UpArgs &a, int64_t rows, int count, const Route &v, hipStream_t st) {
     const int es = sizeof(typename T::elem);
     const bool vec = aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.ldo, es) &&
                      (!a.y_in || rows_aligned(a.y_in, a.ldi, es));
     const int64_t cols = ceil_div(a.len, 16 * T::lane);
-    int size = 3;
-    while (size > 1 && ceil_div(rows, tile_rows(size)) * cols < 1024) --size;
+    int size = 1024;
+    while (size > 64 && ceil_div(rows, size) * cols < 1024) size /= 2;
     const size_t lds = (size_t)ceil_div(a.r, 32) * T::lane * 64 * sizeof(typename T::Frag);
     static size_t granted[2] = {0, 0};
     const void *kernel = vec ? (const void *)adapter_up_kernel<T, true> : (const void *)adapter_up_kernel<T, false>;
@@ -736,49 +709,50 @@ static int launch_up(const UpArgs &a, int64_t rows, int count, const RouteView &
     const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, count, size));
     Timed timed(KID_ADAPTER_UP, st);
     if (vec)
-        adapter_up_kernel<T, true><<<grid, kUpWaves * 64, lds, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+        adapter_up_kernel<T, true><<<grid, kUpWaves * 64, lds, st>>>(a, v, size);
     else
-        adapter_up_kernel<T, false><<<grid, kUpWaves * 64, lds, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+        adapter_up_kernel<T, false><<<grid, kUpWaves * 64, lds, st>>>(a, v, size);
     return check_launch("adapter_up");
 }
 
 constexpr int kGradGroups = 512;
 static int grad_size(int64_t rows, int64_t m, int64_t n, int lane) {
     const int64_t cols = ceil_div(m, 16 * lane) + ceil_div(n, 16 * lane);
-    int size = 4;
-    while (size > 1 && ceil_div(rows, tile_rows(size)) * cols < kGradGroups) --size;
+    int size = 4096;
+    while (size > 64 && ceil_div(rows, size) * cols < kGradGroups) size /= 2;
     return size;
 }
 template <typename T>
-static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, const RouteView &v, hipStream_t st) {
+static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, const Route &v, hipStream_t st) {
     const int64_t cols = a.blocks0 + ceil_div(a.prod[1].len, 16 * T::lane);
     if (rows > 0) {
         const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
         const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, count, size), (unsigned)ceil_div(a.r, ct * 16));
         Timed timed(KID_ADAPTER_GRAD, st);
         if (ct == 4)
-            adapter_grad_kernel<T, 4><<<grid, kGradWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+            adapter_grad_kernel<T, 4><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
         else if (ct == 2)
-            adapter_grad_kernel<T, 2><<<grid, kGradWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+            adapter_grad_kernel<T, 2><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
         else
-            adapter_grad_kernel<T, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v.ntiles + size, v.tiles[size], v.order);
+            adapter_grad_kernel<T, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
         const int rc = check_launch("adapter_grad");
         if (rc != DLCX_OK) return rc;
     }
     const int64_t most = (int64_t)a.r * (a.prod[0].len > a.prod[1].len ? a.prod[0].len : a.prod[1].len);
     const int64_t gx = ceil_div(most, 1024);
     Timed timed(KID_ADAPTER_SUM, st);
-    adapter_sum_kernel<<<dim3((unsigned)(gx < 256 ? gx : 256), (unsigned)count, 2), 256, 0, st>>>(a, v.spans[size]);
+    adapter_sum_kernel<<<dim3((unsigned)(gx < 256 ? gx : 256), (unsigned)count, 2), 256, 0, st>>>(a, v,
+                                                                                                      size);
     return check_launch("adapter_sum");
 }
 
 // ---- workspace: [own route][split sums of h or g][g][slabs of dP][slabs of dQ] ----------------------
 // Room for `rows` rows has room for fewer, though those are split further.  Sums: splits of tiles of 16
 // are at most 256 / (rows / 16) + 1, and at most 16.  Slabs: at most two for every full tile (of
-// adapters with more than one); tiles below the largest size are taken only where four times larger
-// ones make less than kGradGroups workgroups, so there are less than 4 kGradGroups / cols of them.
+// adapters with more than one); tiles below the largest size are taken only where twice as large
+// ones make less than kGradGroups workgroups, so there are less than 2 kGradGroups / cols of them.
 struct AdapterSpace {
-    RouteView route;
+    Route route;
     float *split, *g, *slab_p, *slab_q;
 };
 static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base, AdapterSpace *s) {
@@ -794,8 +768,7 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
     const size_t row = (size_t)d->r * sizeof(float);
     w.split = take(row * (size_t)(16 * rows < rows + 4096 ? 16 * rows : rows + 4096));
     w.g = take(row * (size_t)rows);
-    const int64_t small = 2 * (rows / tile_rows(1)), mid = ceil_div(kGradGroups * 8, cols);
-    const int64_t large = 2 * (rows / tile_rows(4));
+    const int64_t small = 2 * (rows / 64), mid = ceil_div(kGradGroups * 4, cols), large = 2 * (rows / 4096);
     const int64_t slabs = small < mid ? small : mid > large ? mid : large;
     w.slab_p = take(row * (size_t)(slabs * d->m));
     w.slab_q = take(row * (size_t)(slabs * d->n));
@@ -806,7 +779,7 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
 // h = x F^T (into `h`), then y_out = y_in + h G: the forward pass, and the first half of the gradient.
 template <typename T>
 static int down_and_up(const DownArgs &down, const UpArgs &up, int64_t rows, int count, float *split, float *h,
-                       const RouteView &v, hipStream_t st) {
+                       const Route &v, hipStream_t st) {
     const DownPlan plan = plan_down(rows, count, down.len, down.r);
     DownArgs d = down;
     d.split_len = plan.split_len;
@@ -848,9 +821,9 @@ size_t dlcx_adapter_route_bytes(int64_t rows, int32_t count) {
 int dlcx_adapter_route(int64_t rows, const int32_t *ids, int32_t count, void *route, void *stream) {
     if (rows < 0 || rows > (1 << 24) || count < 1 || count > DLCX_MAX_ADAPTERS) return DLCX_EINVAL;
     if (!route || misaligned(route, 256) || (rows > 0 && (!ids || misaligned(ids, 4)))) return DLCX_EINVAL;
-    RouteView v;
+    Route v;
     route_view(rows, count, (char *)route, &v);
-    return launch_route(rows, ids, count, v, as_stream(stream));
+    return launch_route(rows, ids, v, as_stream(stream));
 }
 
 size_t dlcx_adapter_workspace_bytes(const dlcx_adapter_desc *desc, int64_t rows) {
@@ -878,7 +851,7 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
     adapter_space(desc, rows, workspace, &s);
     if (route)
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
-    else if ((rc = launch_route(rows, ids, desc->count, s.route, st)) != DLCX_OK)
+    else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     DownArgs down = {x, ldx, q, nullptr, ranks, nullptr, 0, (int)desc->n, desc->r, 0};
     UpArgs up = {nullptr, 0, nullptr, p, scale, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 1, 0};
@@ -913,7 +886,7 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     adapter_space(desc, rows, workspace, &s);
     if (route)
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
-    else if ((rc = launch_route(rows, ids, desc->count, s.route, st)) != DLCX_OK)
+    else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     if (rows > 0) {
         DownArgs down = {dy, lddy, p, scale, ranks, nullptr, 0, (int)desc->m, desc->r, 0};
