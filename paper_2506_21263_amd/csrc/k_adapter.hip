@@ -45,16 +45,18 @@ struct Tile {
     int adapter;  // -1: rows without one; -2: there is no such tile
     int at, rows; // places in `order`
     int slab;     // number among the tiles of adapters that have several, -1: the only one
+    int block;    // number of its first 32 rows, when all buckets are cut into blocks of 32
 };
 // Tile `index` of the buckets' tiles of `size` rows; 64 buckets at a time, the same in every wavefront.
 __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
     const int lane = threadIdx.x & 63;
-    int tiles = 0, slabs = 0;
+    int tiles = 0, slabs = 0, blocks = 0;
     for (int base = 0; base <= r.count; base += 64) {
         const int b = base + lane;
         const int at = b <= r.count ? r.first[b] : 0, end = b <= r.count ? r.first[b + 1] : 0;
         const int n = (end - at + size - 1) / size, several = n > 1 && b < r.count ? n : 0;
         const int upto = tiles + scan_wave(n), slabs_upto = slabs + scan_wave(several);
+        const int n32 = (end - at + 31) / 32, blocks_upto = blocks + scan_wave(n32);
         const uint64_t after = __ballot(upto > index);
         if (after) {
             const int l = __ffsll((unsigned long long)after) - 1;
@@ -66,12 +68,14 @@ __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
             t.at = from;
             t.rows = min(size, __builtin_amdgcn_readlane(end, l) - from);
             t.slab = several_l ? __builtin_amdgcn_readlane(slabs_upto, l) - several_l + k : -1;
+            t.block = __builtin_amdgcn_readlane(blocks_upto, l) - __builtin_amdgcn_readlane(n32, l) + k * (size / 32);
             return t;
         }
         tiles = __builtin_amdgcn_readlane(upto, 63);
         slabs = __builtin_amdgcn_readlane(slabs_upto, 63);
+        blocks = __builtin_amdgcn_readlane(blocks_upto, 63);
     }
-    return {-2, 0, 0, -1};
+    return {-2, 0, 0, -1, 0};
 }
 
 // One workgroup sorts the rows by counting: every wavefront counts its own share, the counts become the
@@ -190,6 +194,7 @@ struct Bf16 {
     static __device__ __forceinline__ Frag pack(const float (&x)[8]) {
         return {ab_u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}};
     }
+    static __device__ __forceinline__ elem round(float x) { return (uint16_t)pack2(x, x); }
     // x as a sum of three bf16 numbers, to 2^-24
     static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[3]) {
         float rest[8];
@@ -249,6 +254,7 @@ struct F32 {
         return f;
     }
     static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[1]) { f[0] = pack(x); }
+    static __device__ __forceinline__ elem round(float x) { return x; }
     static constexpr int pieces = 1;
 };
 
@@ -298,39 +304,56 @@ struct DownArgs {
     const void *x;       // rows x len
     int64_t ldx;
     const void *f;       // count x r x len
-    const float *scale;  // what the result is multiplied with, or nullptr
     const int32_t *ranks;
-    float *out;          // rows x r; splits of the reduction `stride` floats apart
+    float *out;          // rows x r, columns below the adapter's rank; splits of the reduction `stride` floats apart
     int64_t stride;
     int len, r, split_len;
 };
 
 // A workgroup has RT x 16 rows of one adapter, CT x 16 columns and a share of the reduction, which its
-// eight wavefronts divide again, 64 elements each in turn: every element of the factor is
-// read once per workgroup, and no wavefront waits for another before the end.
+// eight wavefronts divide again, 128 bytes each in turn: every element of the factor is read once per
+// workgroup, and no wavefront waits for another before the end.  The operands of a step are requested
+// before the products of the step before it.
 constexpr int kDownWaves = 8;
+template <typename T, int RT, int CT, bool VEC>
+struct DownStep {
+    static constexpr int U = T::lane / 4, elems = 32 * U;
+    typename T::Frag x[U][RT], f[U][CT];
+    __device__ __forceinline__ void load(const typename T::elem *const (&xrow)[RT],
+                                         const typename T::elem *const (&frow)[CT], int k0, int hi) {
+        const int quad = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u * 32 + quad * 8;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) x[u][i] = T::template load8<VEC>(xrow[i], k, hi);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) f[u][c] = T::template load8<VEC>(frow[c], k, hi);
+        }
+    }
+    __device__ __forceinline__ void add(f32x4_t (&acc)[RT][CT]) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) acc[i][c] = T::mma(x[u][i], f[u][c], acc[i][c]);
+    }
+};
 template <typename T, int RT, int CT, bool VEC>
 __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a, Route route) {
     __shared__ f32x4_t sums[kDownWaves / 2][RT * CT][64];
     const Tile tile = find_tile(route, RT * 16, blockIdx.x);
-    if (tile.adapter < -1) return;
+    if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
     const int c0 = blockIdx.y * CT * 16;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
-    float *out = a.out + blockIdx.z * a.stride;
-    if (c0 >= rank) {  // nothing but zeros here
-        for (int i = threadIdx.x; i < tile.rows * CT * 16; i += kDownWaves * 64) {
-            const int c = c0 + i % (CT * 16);
-            if (c < a.r) out[(int64_t)order[i / (CT * 16)] * a.r + c] = 0.f;
-        }
-        return;
-    }
+    if (c0 >= rank) return;
     const typename T::elem *xrow[RT], *frow[CT];
 #pragma unroll
     for (int i = 0; i < RT; ++i)  // rows and columns beyond the last are the last again: not stored
-        xrow[i] = (const typename T::elem *)a.x +
-                  (int64_t)order[min(i * 16 + row16, tile.rows - 1)] * a.ldx;
+        xrow[i] = (const typename T::elem *)a.x + (int64_t)order[min(i * 16 + row16, tile.rows - 1)] * a.ldx;
 #pragma unroll
     for (int i = 0; i < CT; ++i)
         frow[i] = (const typename T::elem *)a.f +
@@ -340,23 +363,20 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int c = 0; c < CT; ++c) acc[i][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    typedef DownStep<T, RT, CT, VEC> Step;
+    constexpr int stride = kDownWaves * Step::elems;
     const int lo = blockIdx.z * a.split_len, hi = min(a.len, lo + a.split_len);
-    for (int k0 = lo + wave * 64; k0 < hi; k0 += kDownWaves * 64) {
-        typename T::Frag x[2][RT], f[2][CT];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int k = k0 + u * 32 + quad * 8;
-#pragma unroll
-            for (int i = 0; i < RT; ++i) x[u][i] = T::template load8<VEC>(xrow[i], k, hi);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) f[u][c] = T::template load8<VEC>(frow[c], k, hi);
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) acc[i][c] = T::mma(x[u][i], f[u][c], acc[i][c]);
+    Step s0, s1;
+    int k = lo + wave * Step::elems;
+    s0.load(xrow, frow, k, hi);
+    while (k < hi) {
+        s1.load(xrow, frow, k + stride, hi);
+        s0.add(acc);
+        k += stride;
+        if (k >= hi) break;
+        s0.load(xrow, frow, k + stride, hi);
+        s1.add(acc);
+        k += stride;
     }
 #pragma unroll
     for (int half = kDownWaves / 2; half > 0; half /= 2) {
@@ -374,7 +394,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
         __syncthreads();
     }
     if (wave != 0) return;
-    const float scale = a.scale ? a.scale[tile.adapter] : 1.f;
+    float *out = a.out + blockIdx.z * a.stride;
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -385,30 +405,102 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 const int col = c0 + c * 16 + row16;
-                if (col < a.r) row[col] = col < rank ? scale * acc[i][c][v] : 0.f;
+                if (col < rank) row[col] = acc[i][c][v];
             }
         }
 }
 
+// ---- operands ---------------------------------------------------------------------------------------
+// What the other two products read of h (or g): the sum of its splits, in 32 bits as it is and as two
+// operands, so that they are formed once and not by every workgroup that has other columns.
+struct OperandJob {
+    const float *splits;  // rows x r each, `stride` floats apart
+    int64_t stride;
+    int n;
+    const float *scale_out, *scale_up;  // what `out` and `turned`, and what `up` are multiplied with; nullptr: 1
+    float *out;           // rows x r, or nullptr; zero from the adapter's rank on
+    void *up;             // rows x steps 32, or nullptr: for the product with the factor
+    void *turned;         // [block of 32 rows][16 columns][piece][lane], or nullptr: for the sums over rows
+};
+struct OperandArgs {
+    OperandJob job[2];
+    const int32_t *ranks;
+    int r, steps;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Route route) {
+    const Tile tile = find_tile(route, 32, blockIdx.x);
+    if (tile.adapter < -1) return;
+    const int32_t *__restrict__ order = route.order + tile.at;
+    const int rank = adapter_rank(tile.adapter, a.ranks, a.r), cols = a.steps * 32;
+    const OperandJob &j = a.job[blockIdx.y];
+    const float s_out = j.scale_out && tile.adapter >= 0 ? j.scale_out[tile.adapter] : 1.f;
+    const float s_up = j.scale_up && tile.adapter >= 0 ? j.scale_up[tile.adapter] : 1.f;
+    for (int e = threadIdx.x; e < 4 * cols; e += 256) {
+        const int c = e % cols, quad = e / cols;
+        int t[8];
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t[i] = quad * 8 + i < tile.rows ? order[quad * 8 + i] : -1;
+            x[i] = 0.f;
+        }
+        if (c < rank)
+            for (int k = 0; k < j.n; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (t[i] >= 0) x[i] += j.splits[k * j.stride + (int64_t)t[i] * a.r + c];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (t[i] < 0) continue;
+            if (j.up) ((typename T::elem *)j.up)[(int64_t)t[i] * cols + c] = T::round(x[i] * s_up);
+            x[i] *= s_out;
+            if (j.out && c < a.r) j.out[(int64_t)t[i] * a.r + c] = x[i];
+        }
+        if (j.turned) {
+            typename T::Frag f[T::pieces];
+            T::split(x, f);
+#pragma unroll
+            for (int h = 0; h < T::pieces; ++h)
+                ((typename T::Frag *)j.turned)[(((int64_t)tile.block * a.steps * 2 + c / 16) * T::pieces + h) * 64 +
+                                               quad * 16 + c % 16] = f[h];
+        }
+    }
+}
+
 // ---- up ---------------------------------------------------------------------------------------------
 struct UpArgs {
-    const float *h;      // splits x rows x r, `stride` floats apart
-    int64_t stride;
-    float *h_out;        // their sum goes here (nullptr: it is there)
+    const void *h;       // rows x steps 32, scaled
     const void *f;       // count x r x len
-    const float *scale;
     const int32_t *ranks;
     const void *y_in;    // or nullptr
     void *y_out;         // rows x len
     int64_t ldi, ldo;
-    int len, r, splits, copy;  // copy: rows without adapter are to be written too
+    int len, r, copy;    // copy: rows without adapter are to be written too
 };
 
 // A workgroup has 256 bytes of columns and up to `size` rows of one adapter.  It turns the factor's
 // columns into operand blocks in LDS once; then each wavefront takes 16 rows at a time: lane l has row
-// l % 16, and of its columns four times 16 bytes, which four lanes make 64 in a row.
+// l % 16, and of its columns four times 16 bytes, which four lanes make 64 in a row.  The rows of
+// the next round are requested before the products of this one.
 constexpr int kUpWaves = 4;
-template <typename T, bool VEC>
+template <typename T, int KT, bool VEC>
+struct UpRows {
+    ab_u32x4 y[4];
+    typename T::Frag h[KT];
+    __device__ __forceinline__ void load(const UpArgs &a, int64_t t, int j0, bool valid) {
+        const int quad = (threadIdx.x & 63) >> 4;
+        const typename T::elem *in = (const typename T::elem *)a.y_in + t * a.ldi;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            y[i] = a.y_in && valid ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len)
+                                   : ab_u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int s = 0; s < KT; ++s)
+            h[s] = T::template load8<true>((const typename T::elem *)a.h + t * (KT * 32), s * 32 + quad * 8, KT * 32);
+    }
+};
+template <typename T, int KT, bool VEC>
 __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Route route, int size) {
     extern __shared__ __attribute__((aligned(16))) char up_lds[];
     typedef typename T::Frag Frag;
@@ -420,8 +512,11 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
     const int j0 = blockIdx.x * 16 * T::lane;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
-    const int steps = (rank + 31) / 32;
-    const float scale = tile.adapter >= 0 && a.scale ? a.scale[tile.adapter] : 1.f;
+    const int steps = (rank + 31) / 32, last = tile.rows - 1;
+    int t0 = wave * 16;
+    int64_t t = order[min(t0 + row16, last)], t_next = order[min(t0 + kUpWaves * 16 + row16, last)];
+    UpRows<T, KT, VEC> now;
+    now.load(a, t, j0, t0 + row16 <= last);
     for (int s = wave; s < steps; s += kUpWaves) {
         const elem *f = (const elem *)a.f + ((int64_t)tile.adapter * a.r + s * 32 + quad * 8) * a.len;
         const int j = j0 + T::lane * (4 * (row16 & 3) + row16 / 4);
@@ -433,40 +528,23 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
         Frag turned[T::lane];
         turn(rows, turned);
 #pragma unroll
-        for (int t = 0; t < T::lane; ++t) blocks[(s * T::lane + t) * 64 + lane] = turned[t];
+        for (int c = 0; c < T::lane; ++c) blocks[(s * T::lane + c) * 64 + lane] = turned[c];
     }
     __syncthreads();
-    for (int t0 = wave * 16; t0 < tile.rows; t0 += kUpWaves * 16) {
-        const bool valid = t0 + row16 < tile.rows;
-        const int64_t t = order[min(t0 + row16, tile.rows - 1)];
-        const elem *in = (const elem *)a.y_in + t * a.ldi;
-        ab_u32x4 y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            y[i] = a.y_in && valid ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len)
-                                   : ab_u32x4{0u, 0u, 0u, 0u};
+    for (; t0 <= last; t0 += kUpWaves * 16) {
+        const bool valid = t0 + row16 <= last;
+        UpRows<T, KT, VEC> next;
+        next.load(a, t_next, j0, t0 + kUpWaves * 16 + row16 <= last);
+        const int64_t after = order[min(t0 + 2 * kUpWaves * 16 + row16, last)];
         f32x4_t acc[T::lane];
 #pragma unroll
         for (int c = 0; c < T::lane; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < steps; ++s) {
-            float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int c = s * 32 + quad * 8 + i;
-                x[i] = 0.f;
-                if (c < a.r) {
-                    for (int k = 0; k < a.splits; ++k) x[i] += a.h[k * a.stride + t * a.r + c];
-                    if (a.h_out && blockIdx.x == 0 && valid) a.h_out[t * a.r + c] = x[i];
-                }
-                x[i] *= scale;
-            }
-            const Frag h = T::pack(x);
+        for (int s = 0; s < KT; ++s)
+            if (s < steps)
 #pragma unroll
-            for (int c = 0; c < T::lane; ++c) acc[c] = T::mma(blocks[(s * T::lane + c) * 64 + lane], h, acc[c]);
-        }
-        if (a.h_out && blockIdx.x == 0 && valid)  // columns beyond the rank's last step
-            for (int c = steps * 32 + quad; c < a.r; c += 4) a.h_out[t * a.r + c] = 0.f;
-        if (!valid) continue;
+                for (int c = 0; c < T::lane; ++c)
+                    acc[c] = T::mma(blocks[(s * T::lane + c) * 64 + lane], now.h[s], acc[c]);
         elem *out = (elem *)a.y_out + t * a.ldo;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -475,17 +553,17 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
             if constexpr (T::lane == 8) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p)
-                    w[p] = pack2(low_bf16(y[i][p]) + acc[2 * p][i], high_bf16(y[i][p]) + acc[2 * p + 1][i]);
+                    w[p] = pack2(low_bf16(now.y[i][p]) + acc[2 * p][i], high_bf16(now.y[i][p]) + acc[2 * p + 1][i]);
             } else {
 #pragma unroll
-                for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(y[i][p]) + acc[p][i]);
+                for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(now.y[i][p]) + acc[p][i]);
             }
             if constexpr (VEC) {
-                if (j < a.len) *reinterpret_cast<ab_u32x4 *>(out + j) = w;
+                if (valid && j < a.len) *reinterpret_cast<ab_u32x4 *>(out + j) = w;
             } else {
 #pragma unroll
                 for (int p = 0; p < T::lane; ++p)
-                    if (j + p < a.len) {
+                    if (valid && j + p < a.len) {
                         if constexpr (T::lane == 8)
                             out[j + p] = (uint16_t)(w[p / 2] >> (16 * (p & 1)));
                         else
@@ -493,12 +571,15 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
                     }
             }
         }
+        now = next;
+        t = t_next;
+        t_next = after;
     }
 }
 
 // ---- grad -------------------------------------------------------------------------------------------
 struct GradProduct {
-    const float *u;      // rows x r
+    const void *u;       // turned operand
     const float *scale;
     const void *z;       // rows x len
     int64_t ldz;
@@ -509,52 +590,55 @@ struct GradProduct {
 struct GradArgs {
     GradProduct prod[2];
     const int32_t *ranks;
-    int r, blocks0;  // column blocks of the first product
+    int r, steps, blocks0;  // column blocks of the first product
 };
 
 // A workgroup has 256 bytes of columns, CT x 16 columns of the factor and up to `size` rows of one adapter, 32
-// at a time to each of its wavefronts in turn.
+// at a time to each of its wavefronts in turn; the next ones' are requested before this one's products.
 constexpr int kGradWaves = 4;
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p, const int32_t *__restrict__ order,
+                                          int t0, int rows, int j) {
+    const int quad = (threadIdx.x & 63) >> 4;
+    int t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = t0 + quad * 8 + i < rows ? order[t0 + quad * 8 + i] : -1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        z[i] = t[i] >= 0 ? load16<T, VEC>((const typename T::elem *)p.z + t[i] * p.ldz, j, p.len)
+                         : ab_u32x4{0u, 0u, 0u, 0u};
+}
 template <typename T, int CT, bool VEC>
-__device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int rank, const Tile &tile,
+__device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int steps, const Tile &tile,
                                                   const int32_t *__restrict__ order, int c0, int j0,
                                                   f32x4_t (*sums)[CT * T::lane][64]) {
-    typedef typename T::elem elem;
+    typedef typename T::Frag Frag;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
     f32x4_t acc[CT][T::lane];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int s = 0; s < T::lane; ++s) acc[c][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int j = j0 + T::lane * row16;
+    const Frag *u = (const Frag *)p.u + ((int64_t)tile.block * steps * 2 + c0 / 16) * T::pieces * 64 + lane;
+    const int64_t u_block = (int64_t)steps * 2 * T::pieces * 64;
+    ab_u32x4 z[8];
+    load_rows<T, VEC>(z, p, order, wave * 32, tile.rows, j);
     for (int t0 = wave * 32; t0 < tile.rows; t0 += kGradWaves * 32) {
-        int64_t t[8];
-        ab_u32x4 z[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at = t0 + quad * 8 + i;
-            t[i] = at < tile.rows ? order[at] : -1;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            z[i] = t[i] >= 0 ? load16<T, VEC>((const elem *)p.z + t[i] * p.ldz, j0 + T::lane * row16, p.len)
-                             : ab_u32x4{0u, 0u, 0u, 0u};
-        typename T::Frag u[CT][T::pieces];
+        Frag turned[T::lane];
+        turn(z, turned);
+        load_rows<T, VEC>(z, p, order, t0 + kGradWaves * 32, tile.rows, j);
+        const Frag *block = u + (t0 / 32) * u_block;
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-            const int col = c0 + c * 16 + row16;
-            float x[8];
+            if (c0 + c * 16 >= steps * 32) break;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = t[i] >= 0 && col < rank ? p.u[t[i] * r + col] : 0.f;
-            T::split(x, u[c]);
+            for (int h = 0; h < T::pieces; ++h) {
+                const Frag f = block[(c * T::pieces + h) * 64];
+#pragma unroll
+                for (int s = 0; s < T::lane; ++s) acc[c][s] = T::mma(f, turned[s], acc[c][s]);
+            }
         }
-        typename T::Frag turned[T::lane];
-        turn(z, turned);
-#pragma unroll
-        for (int s = 0; s < T::lane; ++s)
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int h = 0; h < T::pieces; ++h) acc[c][s] = T::mma(u[c][h], turned[s], acc[c][s]);
     }
 #pragma unroll
     for (int half = kGradWaves / 2; half > 0; half /= 2) {
@@ -581,7 +665,6 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
             const int col = c0 + c * 16 + quad * 4 + v;
             if (col >= r) continue;
             float *row = out + (int64_t)col * p.len;
-            const int j = j0 + T::lane * row16;
 #pragma unroll
             for (int s = 0; s < T::lane; s += 4) {
                 const f32x4_t w = {scale * acc[c][s][v], scale * acc[c][s + 1][v], scale * acc[c][s + 2][v],
@@ -602,14 +685,13 @@ __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradAr
     const Tile tile = find_tile(route, size, blockIdx.y);
     if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
-    const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int second = (int)blockIdx.x >= a.blocks0;
     const GradProduct &p = a.prod[second];
     const int j0 = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 16 * T::lane, c0 = blockIdx.z * CT * 16;
     if (p.vec)
-        adapter_grad_rows<T, CT, true>(p, a.r, rank, tile, order, c0, j0, sums);
+        adapter_grad_rows<T, CT, true>(p, a.r, a.steps, tile, order, c0, j0, sums);
     else
-        adapter_grad_rows<T, CT, false>(p, a.r, rank, tile, order, c0, j0, sums);
+        adapter_grad_rows<T, CT, false>(p, a.r, a.steps, tile, order, c0, j0, sums);
 }
 
 // Gradients of adapters with several tiles, as the sum of their slabs in the rows' order, and zeros for
@@ -646,6 +728,10 @@ static int launch_route(int64_t rows, const int32_t *ids, const Route &r, hipStr
 }
 
 static inline bool rows_aligned(const void *p, int64_t ld, int es) { return aligned16(p) && ld * es % 16 == 0; }
+
+// Steps of 32 columns of a factor that the up product is built for.
+static int up_steps(int r) { return r <= 32 ? 1 : r <= 64 ? 2 : r <= 128 ? 4 : 8; }
+constexpr int kUpRows = 256;
 
 struct DownPlan {
     int size, splits, split_len;
@@ -694,25 +780,37 @@ static int launch_down(const DownArgs &a, const DownPlan &plan, int64_t rows, in
 }
 
 template <typename T>
-static int launch_up(const UpArgs &a, int64_t rows, int count, const Route &v, hipStream_t st) {
+static int launch_operands(const OperandArgs &a, int jobs, int64_t rows, const Route &v, hipStream_t st) {
+    Timed timed(KID_ADAPTER_OPERAND, st);
+    adapter_operand_kernel<T><<<dim3((unsigned)max_tiles(rows, v.count, 32), (unsigned)jobs), 256, 0, st>>>(a, v);
+    return check_launch("adapter_operand");
+}
+
+template <typename T, int KT, bool VEC>
+static int up_kernel(const UpArgs &a, dim3 grid, const Route &v, int size, hipStream_t st) {
+    const size_t lds = (size_t)KT * T::lane * 64 * sizeof(typename T::Frag);
+    static size_t granted = 0;
+    const int rc = grant_dynamic_lds((const void *)adapter_up_kernel<T, KT, VEC>, lds, &granted, "adapter_up lds");
+    if (rc != DLCX_OK) return rc;
+    Timed timed(KID_ADAPTER_UP, st);
+    adapter_up_kernel<T, KT, VEC><<<grid, kUpWaves * 64, lds, st>>>(a, v, size);
+    return check_launch("adapter_up");
+}
+template <typename T>
+static int launch_up(const UpArgs &a, int64_t rows, const Route &v, hipStream_t st) {
     const int es = sizeof(typename T::elem);
     const bool vec = aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.ldo, es) &&
                      (!a.y_in || rows_aligned(a.y_in, a.ldi, es));
     const int64_t cols = ceil_div(a.len, 16 * T::lane);
-    int size = 1024;
+    int size = kUpRows;
     while (size > 64 && ceil_div(rows, size) * cols < 1024) size /= 2;
-    const size_t lds = (size_t)ceil_div(a.r, 32) * T::lane * 64 * sizeof(typename T::Frag);
-    static size_t granted[2] = {0, 0};
-    const void *kernel = vec ? (const void *)adapter_up_kernel<T, true> : (const void *)adapter_up_kernel<T, false>;
-    const int rc = grant_dynamic_lds(kernel, lds, &granted[vec], "adapter_up lds");
-    if (rc != DLCX_OK) return rc;
-    const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, count, size));
-    Timed timed(KID_ADAPTER_UP, st);
-    if (vec)
-        adapter_up_kernel<T, true><<<grid, kUpWaves * 64, lds, st>>>(a, v, size);
-    else
-        adapter_up_kernel<T, false><<<grid, kUpWaves * 64, lds, st>>>(a, v, size);
-    return check_launch("adapter_up");
+    const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, v.count, size));
+    switch (up_steps(a.r)) {
+    case 1: return vec ? up_kernel<T, 1, true>(a, grid, v, size, st) : up_kernel<T, 1, false>(a, grid, v, size, st);
+    case 2: return vec ? up_kernel<T, 2, true>(a, grid, v, size, st) : up_kernel<T, 2, false>(a, grid, v, size, st);
+    case 4: return vec ? up_kernel<T, 4, true>(a, grid, v, size, st) : up_kernel<T, 4, false>(a, grid, v, size, st);
+    default: return vec ? up_kernel<T, 8, true>(a, grid, v, size, st) : up_kernel<T, 8, false>(a, grid, v, size, st);
+    }
 }
 
 constexpr int kGradGroups = 512;
@@ -746,14 +844,15 @@ static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, con
     return check_launch("adapter_sum");
 }
 
-// ---- workspace: [own route][split sums of h or g][g][slabs of dP][slabs of dQ] ----------------------
+// ---- workspace: [own route][splits of h or g][operands][slabs of dP][slabs of dQ] ----------------
 // Room for `rows` rows has room for fewer, though those are split further.  Sums: splits of tiles of 16
 // are at most 256 / (rows / 16) + 1, and at most 16.  Slabs: at most two for every full tile (of
 // adapters with more than one); tiles below the largest size are taken only where twice as large
 // ones make less than kGradGroups workgroups, so there are less than 2 kGradGroups / cols of them.
 struct AdapterSpace {
     Route route;
-    float *split, *g, *slab_p, *slab_q;
+    float *split, *slab_p, *slab_q;
+    void *up, *turned_h, *turned_g;
 };
 static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base, AdapterSpace *s) {
     AdapterSpace w;
@@ -763,11 +862,16 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
         at += a256x(bytes);
         return (float *)p;
     };
-    const int lane = d->dtype == DLCX_BF16 ? Bf16::lane : F32::lane;
+    const bool low = d->dtype == DLCX_BF16;
+    const int lane = low ? Bf16::lane : F32::lane;
+    const size_t frag = low ? sizeof(Bf16::Frag) * Bf16::pieces : sizeof(F32::Frag) * F32::pieces;
     const int64_t cols = ceil_div(d->m, 16 * lane) + ceil_div(d->n, 16 * lane);
-    const size_t row = (size_t)d->r * sizeof(float);
+    const size_t row = (size_t)d->r * sizeof(float), steps = (size_t)up_steps(d->r);
     w.split = take(row * (size_t)(16 * rows < rows + 4096 ? 16 * rows : rows + 4096));
-    w.g = take(row * (size_t)rows);
+    w.up = take((size_t)rows * steps * 32 * (low ? 2 : 4));
+    const size_t turned = (size_t)max_tiles(rows, d->count, 32) * steps * 2 * 64 * frag;
+    w.turned_h = take(turned);
+    w.turned_g = take(turned);
     const int64_t small = 2 * (rows / 64), mid = ceil_div(kGradGroups * 4, cols), large = 2 * (rows / 4096);
     const int64_t slabs = small < mid ? small : mid > large ? mid : large;
     w.slab_p = take(row * (size_t)(slabs * d->m));
@@ -776,25 +880,29 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
     return at;
 }
 
-// h = x F^T (into `h`), then y_out = y_in + h G: the forward pass, and the first half of the gradient.
+// h = x F^T, then y_out = y_in + h G: the forward pass, and the first half of the gradient.  `job` says what
+// becomes of h; `other` of a second matrix of its form, or nullptr.
 template <typename T>
-static int down_and_up(const DownArgs &down, const UpArgs &up, int64_t rows, int count, float *split, float *h,
-                       const Route &v, hipStream_t st) {
-    const DownPlan plan = plan_down(rows, count, down.len, down.r);
+static int down_and_up(const DownArgs &down, OperandJob job, const OperandJob *other, const UpArgs &up, int64_t rows,
+                       const AdapterSpace &s, hipStream_t st) {
+    const DownPlan plan = plan_down(rows, s.route.count, down.len, down.r);
     DownArgs d = down;
     d.split_len = plan.split_len;
     d.stride = rows * d.r;
-    d.out = plan.splits > 1 ? split : h;
-    int rc = launch_down<T>(d, plan, rows, count, v, st);
+    d.out = s.split;
+    int rc = launch_down<T>(d, plan, rows, s.route.count, s.route, st);
+    if (rc != DLCX_OK) return rc;
+    job.splits = s.split;
+    job.stride = d.stride;
+    job.n = plan.splits;
+    job.up = s.up;
+    OperandArgs o = {{job, other ? *other : job}, d.ranks, d.r, up_steps(d.r)};
+    rc = launch_operands<T>(o, other ? 2 : 1, rows, s.route, st);
     if (rc != DLCX_OK) return rc;
     UpArgs u = up;
-    u.h = d.out;
-    u.stride = d.stride;
-    u.splits = plan.splits;
-    u.h_out = plan.splits > 1 ? h : nullptr;
-    // (a row without adapter stays as it is where it is updated in place, unless its sums are still to be written)
-    u.copy = u.y_in != u.y_out || plan.splits > 1;
-    return launch_up<T>(u, rows, count, v, st);
+    u.h = s.up;
+    u.copy = u.y_in != u.y_out;  // (a row without adapter stays as it is where it is updated in place)
+    return launch_up<T>(u, rows, s.route, st);
 }
 
 }  // namespace dlcx
@@ -853,11 +961,11 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
-    DownArgs down = {x, ldx, q, nullptr, ranks, nullptr, 0, (int)desc->n, desc->r, 0};
-    UpArgs up = {nullptr, 0, nullptr, p, scale, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 1, 0};
-    return desc->dtype == DLCX_BF16
-               ? down_and_up<Bf16>(down, up, rows, desc->count, s.split, h_out, s.route, st)
-               : down_and_up<F32>(down, up, rows, desc->count, s.split, h_out, s.route, st);
+    const DownArgs down = {x, ldx, q, ranks, nullptr, 0, (int)desc->n, desc->r, 0};
+    const OperandJob job = {nullptr, 0, 0, nullptr, scale, h_out, nullptr, nullptr};
+    const UpArgs up = {nullptr, p, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 0};
+    return desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, job, nullptr, up, rows, s, st)
+                                    : down_and_up<F32>(down, job, nullptr, up, rows, s, st);
 }
 
 int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
@@ -889,21 +997,23 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     if (rows > 0) {
-        DownArgs down = {dy, lddy, p, scale, ranks, nullptr, 0, (int)desc->m, desc->r, 0};
-        UpArgs up = {nullptr, 0, nullptr, q, nullptr, ranks, dx_in, dx_out, lddx_in, lddx_out, (int)desc->n,
-                     desc->r, 1, 0};
-        rc = desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, up, rows, desc->count, s.split, s.g, s.route, st)
-                                      : down_and_up<F32>(down, up, rows, desc->count, s.split, s.g, s.route, st);
+        const DownArgs down = {dy, lddy, p, ranks, nullptr, 0, (int)desc->m, desc->r, 0};
+        const OperandJob g = {nullptr, 0, 0, scale, scale, nullptr, nullptr, s.turned_g};
+        const OperandJob hj = {h, 0, 1, nullptr, nullptr, nullptr, nullptr, s.turned_h};
+        const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, lddx_in, lddx_out, (int)desc->n, desc->r, 0};
+        rc = desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, g, &hj, up, rows, s, st)
+                                      : down_and_up<F32>(down, g, &hj, up, rows, s, st);
         if (rc != DLCX_OK) return rc;
     }
     const int lane = desc->dtype == DLCX_BF16 ? Bf16::lane : F32::lane;
     GradArgs a;
-    a.prod[0] = {h, scale, dy, lddy, dp_out, s.slab_p, (int)desc->m, 0};
-    a.prod[1] = {s.g, nullptr, x, ldx, dq_out, s.slab_q, (int)desc->n, 0};
+    a.prod[0] = {s.turned_h, scale, dy, lddy, dp_out, s.slab_p, (int)desc->m, 0};
+    a.prod[1] = {s.turned_g, nullptr, x, ldx, dq_out, s.slab_q, (int)desc->n, 0};
     for (GradProduct &g : a.prod)
         g.vec = rows_aligned(g.z, g.ldz, (int)es) && g.len % lane == 0 && aligned16(g.out);
     a.ranks = ranks;
     a.r = desc->r;
+    a.steps = up_steps(desc->r);
     a.blocks0 = (int)ceil_div(desc->m, 16 * lane);
     const int size = grad_size(rows, desc->m, desc->n, lane);
     return desc->dtype == DLCX_BF16 ? launch_grad<Bf16>(a, rows, desc->count, size, s.route, st)
