@@ -178,16 +178,16 @@ struct Bf16 {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ab_bf16x8, a.w),
                                                        __builtin_bit_cast(ab_bf16x8, b.w), c, 0, 0, 0);
     }
-    // elements k .. k + 7 of a row of `len`
-    template <bool VEC>
+    // elements k .. k + 7 of a row of `len`; ALL: all of them are there
+    template <bool VEC, bool ALL = false>
     static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
         Frag f = zero();
         if constexpr (VEC) {
-            if (k < len) f.w = *reinterpret_cast<const ab_u32x4 *>(row + k);
+            if (ALL || k < len) f.w = *reinterpret_cast<const ab_u32x4 *>(row + k);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k + i < len) f.w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+                if (ALL || k + i < len) f.w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
         }
         return f;
     }
@@ -230,11 +230,11 @@ struct F32 {
         for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[j], b.x[j], c, 0, 0, 0);
         return c;
     }
-    template <bool VEC>
+    template <bool VEC, bool ALL = false>
     static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
         Frag f = zero();
         if constexpr (VEC) {
-            if (k < len) {
+            if (ALL || k < len) {
                 const f32x4_t a = *reinterpret_cast<const f32x4_t *>(row + k);
                 const f32x4_t b = *reinterpret_cast<const f32x4_t *>(row + k + 4);
 #pragma unroll
@@ -243,7 +243,7 @@ struct F32 {
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k + i < len) f.x[i] = row[k + i];
+                if (ALL || k + i < len) f.x[i] = row[k + i];
         }
         return f;
     }
@@ -258,12 +258,13 @@ struct F32 {
     static constexpr int pieces = 1;
 };
 
-// 16 bytes of a row from element j on; elements from `len` on are zero.
+// 16 bytes of a row from element j on.  Elements from `len` on belong to columns that nobody stores: they
+// are the row's last ones again where rows are read by 16 bytes, so that no lane waits at a branch.
 template <typename T, bool VEC>
 __device__ __forceinline__ ab_u32x4 load16(const typename T::elem *row, int j, int len) {
     ab_u32x4 w = {0u, 0u, 0u, 0u};
     if constexpr (VEC) {
-        if (j < len) w = *reinterpret_cast<const ab_u32x4 *>(row + j);
+        w = *reinterpret_cast<const ab_u32x4 *>(row + min(j, len - T::lane));
     } else {
 #pragma unroll
         for (int i = 0; i < T::lane; ++i)
@@ -319,6 +320,7 @@ template <typename T, int RT, int CT, bool VEC>
 struct DownStep {
     static constexpr int U = T::lane / 4, elems = 32 * U;
     typename T::Frag x[U][RT], f[U][CT];
+    template <bool ALL>
     __device__ __forceinline__ void load(const typename T::elem *const (&xrow)[RT],
                                          const typename T::elem *const (&frow)[CT], int k0, int hi) {
         const int quad = (threadIdx.x & 63) >> 4;
@@ -326,9 +328,9 @@ struct DownStep {
         for (int u = 0; u < U; ++u) {
             const int k = k0 + u * 32 + quad * 8;
 #pragma unroll
-            for (int i = 0; i < RT; ++i) x[u][i] = T::template load8<VEC>(xrow[i], k, hi);
+            for (int i = 0; i < RT; ++i) x[u][i] = T::template load8<VEC, ALL>(xrow[i], k, hi);
 #pragma unroll
-            for (int c = 0; c < CT; ++c) f[u][c] = T::template load8<VEC>(frow[c], k, hi);
+            for (int c = 0; c < CT; ++c) f[u][c] = T::template load8<VEC, ALL>(frow[c], k, hi);
         }
     }
     __device__ __forceinline__ void add(f32x4_t (&acc)[RT][CT]) const {
@@ -366,17 +368,26 @@ __global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs 
     typedef DownStep<T, RT, CT, VEC> Step;
     constexpr int stride = kDownWaves * Step::elems;
     const int lo = blockIdx.z * a.split_len, hi = min(a.len, lo + a.split_len);
-    Step s0, s1;
-    int k = lo + wave * Step::elems;
-    s0.load(xrow, frow, k, hi);
-    while (k < hi) {
-        s1.load(xrow, frow, k + stride, hi);
-        s0.add(acc);
-        k += stride;
-        if (k >= hi) break;
-        s0.load(xrow, frow, k + stride, hi);
-        s1.add(acc);
-        k += stride;
+    // `full` steps are inside the row with all their elements; the loads of one go out before the products of
+    // the one before it, the last one is loaded again instead of one beyond it
+    int k = lo + __builtin_amdgcn_readfirstlane(wave) * Step::elems;
+    const int full = hi - k >= Step::elems ? (hi - k - Step::elems) / stride + 1 : 0;
+    if (full > 0) {
+        Step s0, s1;
+        s0.template load<true>(xrow, frow, k, hi);
+        for (int i = 0; i < full; i += 2) {
+            const int k1 = k + min(i + 1, full - 1) * stride, k2 = k + min(i + 2, full - 1) * stride;
+            s1.template load<true>(xrow, frow, k1, hi);
+            s0.add(acc);
+            s0.template load<true>(xrow, frow, k2, hi);
+            if (i + 1 < full) s1.add(acc);
+        }
+        k += full * stride;
+    }
+    if (k < hi) {
+        Step rest;
+        rest.template load<false>(xrow, frow, k, hi);
+        rest.add(acc);
     }
 #pragma unroll
     for (int half = kDownWaves / 2; half > 0; half /= 2) {
@@ -445,11 +456,19 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
             t[i] = quad * 8 + i < tile.rows ? order[quad * 8 + i] : -1;
             x[i] = 0.f;
         }
-        if (c < rank)
-            for (int k = 0; k < j.n; ++k)
+        if (c < rank && t[0] >= 0)
+            for (int k = 0; k < j.n; k += 4) {
+                float part[4][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (t[i] >= 0) x[i] += j.splits[k * j.stride + (int64_t)t[i] * a.r + c];
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        part[u][i] = j.splits[min(k + u, j.n - 1) * j.stride + (int64_t)(t[i] < 0 ? t[0] : t[i]) * a.r + c];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] += k + u < j.n && t[i] >= 0 ? part[u][i] : 0.f;
+            }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (t[i] < 0) continue;
@@ -488,16 +507,16 @@ template <typename T, int KT, bool VEC>
 struct UpRows {
     ab_u32x4 y[4];
     typename T::Frag h[KT];
-    __device__ __forceinline__ void load(const UpArgs &a, int64_t t, int j0, bool valid) {
+    __device__ __forceinline__ void load(const UpArgs &a, int64_t t, int j0) {
         const int quad = (threadIdx.x & 63) >> 4;
         const typename T::elem *in = (const typename T::elem *)a.y_in + t * a.ldi;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            y[i] = a.y_in && valid ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len)
+            y[i] = a.y_in ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len)
                                    : ab_u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int s = 0; s < KT; ++s)
-            h[s] = T::template load8<true>((const typename T::elem *)a.h + t * (KT * 32), s * 32 + quad * 8, KT * 32);
+            h[s] = T::template load8<true, true>((const typename T::elem *)a.h + t * (KT * 32), s * 32 + quad * 8, KT * 32);
     }
 };
 template <typename T, int KT, bool VEC>
@@ -516,15 +535,15 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
     int t0 = wave * 16;
     int64_t t = order[min(t0 + row16, last)], t_next = order[min(t0 + kUpWaves * 16 + row16, last)];
     UpRows<T, KT, VEC> now;
-    now.load(a, t, j0, t0 + row16 <= last);
+    now.load(a, t, j0);
     for (int s = wave; s < steps; s += kUpWaves) {
-        const elem *f = (const elem *)a.f + ((int64_t)tile.adapter * a.r + s * 32 + quad * 8) * a.len;
+        // (columns from the rank on meet zeros in h: the last one again does for them)
+        const elem *f = (const elem *)a.f + (int64_t)tile.adapter * a.r * a.len;
         const int j = j0 + T::lane * (4 * (row16 & 3) + row16 / 4);
         ab_u32x4 rows[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            rows[i] = s * 32 + quad * 8 + i < rank ? load16<T, VEC>(f + (int64_t)i * a.len, j, a.len)
-                                                   : ab_u32x4{0u, 0u, 0u, 0u};
+            rows[i] = load16<T, VEC>(f + (int64_t)min(s * 32 + quad * 8 + i, rank - 1) * a.len, j, a.len);
         Frag turned[T::lane];
         turn(rows, turned);
 #pragma unroll
@@ -534,7 +553,7 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
     for (; t0 <= last; t0 += kUpWaves * 16) {
         const bool valid = t0 + row16 <= last;
         UpRows<T, KT, VEC> next;
-        next.load(a, t_next, j0, t0 + kUpWaves * 16 + row16 <= last);
+        next.load(a, t_next, j0);
         const int64_t after = order[min(t0 + 2 * kUpWaves * 16 + row16, last)];
         f32x4_t acc[T::lane];
 #pragma unroll
@@ -602,11 +621,10 @@ __device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p
     const int quad = (threadIdx.x & 63) >> 4;
     int t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = t0 + quad * 8 + i < rows ? order[t0 + quad * 8 + i] : -1;
+    for (int i = 0; i < 8; ++i) t[i] = order[min(t0 + quad * 8 + i, rows - 1)];  // (rows beyond meet zeros in u)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        z[i] = t[i] >= 0 ? load16<T, VEC>((const typename T::elem *)p.z + t[i] * p.ldz, j, p.len)
-                         : ab_u32x4{0u, 0u, 0u, 0u};
+        z[i] = load16<T, VEC>((const typename T::elem *)p.z + t[i] * p.ldz, j, p.len);
 }
 template <typename T, int CT, bool VEC>
 __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int steps, const Tile &tile,
