@@ -306,119 +306,79 @@ struct DownArgs {
     int64_t ldx;
     const void *f;       // count x r x len
     const int32_t *ranks;
-    float *out;          // rows x r, columns below the adapter's rank; splits of the reduction `stride` floats apart
+    float *out;          // rows x r, columns below the adapter's rank; shares of the reduction `stride` floats apart
     int64_t stride;
-    int len, r, split_len;
+    int len, r;
 };
 
-// A workgroup has RT x 16 rows of one adapter, CT x 16 columns and a share of the reduction, which its
-// eight wavefronts divide again, 128 bytes each in turn: every element of the factor is read once per
-// workgroup, and no wavefront waits for another before the end.  The operands of a step are requested
-// before the products of the step before it.
+// A workgroup has a share of the reduction (its eight wavefronts 256 to 512 bytes of it each), CT x 16 columns and
+// up to `size` rows of one adapter.  A wavefront keeps its part of the factor in registers and meets it with 16 rows
+// at a time; the eight sums are joined in LDS, in turn in two places, so that one barrier a round is enough.
+// With whole rows to a workgroup instead, the factor comes from L2 as often as there are tiles of
+// rows, by the same few channels at a time: 91 us for 16384 x 8192 at rank 64, 88 us for 4133 rows.
 constexpr int kDownWaves = 8;
-template <typename T, int RT, int CT, bool VEC>
-struct DownStep {
-    static constexpr int U = T::lane / 4, elems = 32 * U;
-    typename T::Frag x[U][RT], f[U][CT];
-    template <bool ALL>
-    __device__ __forceinline__ void load(const typename T::elem *const (&xrow)[RT],
-                                         const typename T::elem *const (&frow)[CT], int k0, int hi) {
-        const int quad = (threadIdx.x & 63) >> 4;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = k0 + u * 32 + quad * 8;
-#pragma unroll
-            for (int i = 0; i < RT; ++i) x[u][i] = T::template load8<VEC, ALL>(xrow[i], k, hi);
-#pragma unroll
-            for (int c = 0; c < CT; ++c) f[u][c] = T::template load8<VEC, ALL>(frow[c], k, hi);
-        }
-    }
-    __device__ __forceinline__ void add(f32x4_t (&acc)[RT][CT]) const {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) acc[i][c] = T::mma(x[u][i], f[u][c], acc[i][c]);
-    }
-};
-template <typename T, int RT, int CT, bool VEC>
-__global__ __launch_bounds__(kDownWaves * 64) void adapter_down_kernel(DownArgs a, Route route) {
-    __shared__ f32x4_t sums[kDownWaves / 2][RT * CT][64];
-    const Tile tile = find_tile(route, RT * 16, blockIdx.x);
+template <typename T>
+constexpr int down_steps(int ct) {  // of 32 elements, per wavefront
+    return (ct == 4 ? 4 : 8) * T::lane / 8;
+}
+template <typename T, int CT, bool VEC>
+__global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownArgs a, Route route, int size) {
+    constexpr int KS = down_steps<T>(CT);
+    typedef typename T::Frag Frag;
+    typedef typename T::elem elem;
+    __shared__ f32x4_t sums[2][kDownWaves][CT][64];
+    const Tile tile = find_tile(route, size, blockIdx.y);
     if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
-    const int c0 = blockIdx.y * CT * 16;
+    const int lane = threadIdx.x & 63, row16 = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int c0 = blockIdx.z * CT * 16, last = tile.rows - 1;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     if (c0 >= rank) return;
-    const typename T::elem *xrow[RT], *frow[CT];
+    const int k0 = (blockIdx.x * kDownWaves + wave) * KS * 32;
+    const bool whole = k0 + KS * 32 <= a.len;
+    auto load = [&](const elem *row, Frag (&f)[KS]) {
+        if (whole) {
 #pragma unroll
-    for (int i = 0; i < RT; ++i)  // rows and columns beyond the last are the last again: not stored
-        xrow[i] = (const typename T::elem *)a.x + (int64_t)order[min(i * 16 + row16, tile.rows - 1)] * a.ldx;
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, true>(row, k0 + s * 32 + quad * 8, a.len);
+        } else {
 #pragma unroll
-    for (int i = 0; i < CT; ++i)
-        frow[i] = (const typename T::elem *)a.f +
-                  ((int64_t)tile.adapter * a.r + min(c0 + i * 16 + row16, rank - 1)) * a.len;
-    f32x4_t acc[RT][CT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[i][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    typedef DownStep<T, RT, CT, VEC> Step;
-    constexpr int stride = kDownWaves * Step::elems;
-    const int lo = blockIdx.z * a.split_len, hi = min(a.len, lo + a.split_len);
-    // `full` steps are inside the row with all their elements; the loads of one go out before the products of
-    // the one before it, the last one is loaded again instead of one beyond it
-    int k = lo + __builtin_amdgcn_readfirstlane(wave) * Step::elems;
-    const int full = hi - k >= Step::elems ? (hi - k - Step::elems) / stride + 1 : 0;
-    if (full > 0) {
-        Step s0, s1;
-        s0.template load<true>(xrow, frow, k, hi);
-        for (int i = 0; i < full; i += 2) {
-            const int k1 = k + min(i + 1, full - 1) * stride, k2 = k + min(i + 2, full - 1) * stride;
-            s1.template load<true>(xrow, frow, k1, hi);
-            s0.add(acc);
-            s0.template load<true>(xrow, frow, k2, hi);
-            if (i + 1 < full) s1.add(acc);
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, false>(row, k0 + s * 32 + quad * 8, a.len);
         }
-        k += full * stride;
-    }
-    if (k < hi) {
-        Step rest;
-        rest.template load<false>(xrow, frow, k, hi);
-        rest.add(acc);
-    }
+    };
+    auto row_of = [&](int t0) { return (const elem *)a.x + (int64_t)order[min(t0 + row16, last)] * a.ldx; };
+    Frag f[CT][KS], now[KS], next[KS];
+    const elem *ahead = row_of(16);
+    load(row_of(0), now);
 #pragma unroll
-    for (int half = kDownWaves / 2; half > 0; half /= 2) {
-        if (wave >= half && wave < 2 * half)
+    for (int c = 0; c < CT; ++c)  // columns from the rank on are the last one again: not stored
+        load((const elem *)a.f + ((int64_t)tile.adapter * a.r + min(c0 + c * 16 + row16, rank - 1)) * a.len, f[c]);
+    float *out = a.out + blockIdx.x * a.stride;
+    for (int t0 = 0, turn = 0; t0 <= last; t0 += 16, turn ^= 1) {
+        load(ahead, next);
+        ahead = row_of(t0 + 32);
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+        for (int c = 0; c < CT; ++c) {
+            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < CT; ++c) sums[wave - half][i * CT + c][lane] = acc[i][c];
+            for (int s = 0; s < KS; ++s) acc = T::mma(now[s], f[c][s], acc);
+            sums[turn][wave][c][lane] = acc;
+        }
         __syncthreads();
-        if (wave < half)
+        if (wave < CT) {
+            f32x4_t acc = sums[turn][0][wave][lane];
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+            for (int w = 1; w < kDownWaves; ++w) acc += sums[turn][w][wave][lane];
+            const int col = c0 + wave * 16 + row16;
 #pragma unroll
-                for (int c = 0; c < CT; ++c) acc[i][c] += sums[wave][i * CT + c][lane];
-        __syncthreads();
-    }
-    if (wave != 0) return;
-    float *out = a.out + blockIdx.z * a.stride;
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int t = i * 16 + quad * 4 + v;
-            if (t >= tile.rows) continue;
-            float *row = out + (int64_t)order[t] * a.r;
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const int col = c0 + c * 16 + row16;
-                if (col < rank) row[col] = acc[i][c][v];
+            for (int v = 0; v < 4; ++v) {
+                const int t = t0 + quad * 4 + v;
+                if (t <= last && col < rank) out[(int64_t)order[t] * a.r + col] = acc[v];
             }
         }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) now[s] = next[s];
+    }
 }
 
 // ---- operands ---------------------------------------------------------------------------------------
@@ -749,51 +709,34 @@ static inline bool rows_aligned(const void *p, int64_t ld, int es) { return alig
 
 // Steps of 32 columns of a factor that the up product is built for.
 static int up_steps(int r) { return r <= 32 ? 1 : r <= 64 ? 2 : r <= 128 ? 4 : 8; }
-constexpr int kUpRows = 256;
+constexpr int kUpRows = 256, kDownRows = 256;  // most rows of a workgroup
 
-struct DownPlan {
-    int size, splits, split_len;
-};
-// Tiles of 64 rows where they fill the GPU, else of 16; what is missing to a workgroup for every
-// compute unit comes from splitting the reduction, no shorter than 512 elements.
-static DownPlan plan_down(int64_t rows, int count, int64_t len, int r) {
-    DownPlan p;
-    const int64_t cols = ceil_div(r, r > 32 ? 64 : 32);
-    p.size = rows * cols >= 64 * 256 ? 64 : 16;
-    const int64_t groups = ceil_div(rows, p.size) * cols;
-    int64_t splits = ceil_div(256, groups);
-    const int64_t most = ceil_div(len, 512);
-    splits = splits < most ? splits : most;
-    splits = splits < 16 ? splits : 16;
-    p.split_len = (int)(ceil_div(ceil_div(len, splits), 64) * 64);
-    p.splits = (int)ceil_div(len, p.split_len);
-    return p;
+static int down_tiles(int r) { return r > 32 ? 4 : r > 16 ? 2 : 1; }
+// Shares of a reduction over `len` elements.
+template <typename T>
+static int down_splits(int64_t len, int r) {
+    return (int)ceil_div(len, kDownWaves * 32 * down_steps<T>(down_tiles(r)));
 }
 
-template <typename T, int RT, int CT>
-static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const Route &v, hipStream_t st) {
+template <typename T, int CT>
+static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const Route &v, int size, hipStream_t st) {
     if (vec)
-        adapter_down_kernel<T, RT, CT, true><<<grid, kDownWaves * 64, 0, st>>>(a, v);
+        adapter_down_kernel<T, CT, true><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
     else
-        adapter_down_kernel<T, RT, CT, false><<<grid, kDownWaves * 64, 0, st>>>(a, v);
+        adapter_down_kernel<T, CT, false><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
 }
 template <typename T>
-static int launch_down(const DownArgs &a, const DownPlan &plan, int64_t rows, int count, const Route &v,
-                       hipStream_t st) {
-    const int es = sizeof(typename T::elem);
+static int launch_down(const DownArgs &a, int64_t rows, const Route &v, hipStream_t st) {
+    const int es = sizeof(typename T::elem), ct = down_tiles(a.r), splits = down_splits<T>(a.len, a.r);
     const bool vec = rows_aligned(a.x, a.ldx, es) && aligned16(a.f) && a.len % 8 == 0;
-    const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
-    const dim3 grid((unsigned)max_tiles(rows, count, plan.size), (unsigned)ceil_div(a.r, ct * 16), (unsigned)plan.splits);
+    const int64_t cols = ceil_div(a.r, ct * 16);
+    int size = kDownRows;
+    while (size > 16 && ceil_div(rows, size) * splits * cols < 768) size /= 2;
+    const dim3 grid((unsigned)splits, (unsigned)max_tiles(rows, v.count, size), (unsigned)cols);
     Timed timed(KID_ADAPTER_DOWN, st);
-    if (plan.size == 64) {
-        if (ct == 4) down_kernel<T, 4, 4>(a, vec, grid, v, st);
-        else if (ct == 2) down_kernel<T, 4, 2>(a, vec, grid, v, st);
-        else down_kernel<T, 4, 1>(a, vec, grid, v, st);
-    } else {
-        if (ct == 4) down_kernel<T, 1, 4>(a, vec, grid, v, st);
-        else if (ct == 2) down_kernel<T, 1, 2>(a, vec, grid, v, st);
-        else down_kernel<T, 1, 1>(a, vec, grid, v, st);
-    }
+    if (ct == 4) down_kernel<T, 4>(a, vec, grid, v, size, st);
+    else if (ct == 2) down_kernel<T, 2>(a, vec, grid, v, size, st);
+    else down_kernel<T, 1>(a, vec, grid, v, size, st);
     return check_launch("adapter_down");
 }
 
@@ -862,9 +805,8 @@ static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, con
     return check_launch("adapter_sum");
 }
 
-// ---- workspace: [own route][splits of h or g][operands][slabs of dP][slabs of dQ] ----------------
-// Room for `rows` rows has room for fewer, though those are split further.  Sums: splits of tiles of 16
-// are at most 256 / (rows / 16) + 1, and at most 16.  Slabs: at most two for every full tile (of
+// ---- workspace: [own route][shares of h or g][operands][slabs of dP][slabs of dQ] ----------------
+// Room for `rows` rows has room for fewer, though their gradients have smaller tiles.  Slabs: at most two for every full tile (of
 // adapters with more than one); tiles below the largest size are taken only where twice as large
 // ones make less than kGradGroups workgroups, so there are less than 2 kGradGroups / cols of them.
 struct AdapterSpace {
@@ -885,7 +827,8 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
     const size_t frag = low ? sizeof(Bf16::Frag) * Bf16::pieces : sizeof(F32::Frag) * F32::pieces;
     const int64_t cols = ceil_div(d->m, 16 * lane) + ceil_div(d->n, 16 * lane);
     const size_t row = (size_t)d->r * sizeof(float), steps = (size_t)up_steps(d->r);
-    w.split = take(row * (size_t)(16 * rows < rows + 4096 ? 16 * rows : rows + 4096));
+    const int64_t longer = d->m > d->n ? d->m : d->n;
+    w.split = take(row * (size_t)(rows * (low ? down_splits<Bf16>(longer, d->r) : down_splits<F32>(longer, d->r))));
     w.up = take((size_t)rows * steps * 32 * (low ? 2 : 4));
     const size_t turned = (size_t)max_tiles(rows, d->count, 32) * steps * 2 * 64 * frag;
     w.turned_h = take(turned);
@@ -903,16 +846,14 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
 template <typename T>
 static int down_and_up(const DownArgs &down, OperandJob job, const OperandJob *other, const UpArgs &up, int64_t rows,
                        const AdapterSpace &s, hipStream_t st) {
-    const DownPlan plan = plan_down(rows, s.route.count, down.len, down.r);
     DownArgs d = down;
-    d.split_len = plan.split_len;
     d.stride = rows * d.r;
     d.out = s.split;
-    int rc = launch_down<T>(d, plan, rows, s.route.count, s.route, st);
+    int rc = launch_down<T>(d, rows, s.route, st);
     if (rc != DLCX_OK) return rc;
     job.splits = s.split;
     job.stride = d.stride;
-    job.n = plan.splits;
+    job.n = down_splits<T>(d.len, d.r);
     job.up = s.up;
     OperandArgs o = {{job, other ? *other : job}, d.ranks, d.r, up_steps(d.r)};
     rc = launch_operands<T>(o, other ? 2 : 1, rows, s.route, st);
@@ -979,7 +920,7 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
-    const DownArgs down = {x, ldx, q, ranks, nullptr, 0, (int)desc->n, desc->r, 0};
+    const DownArgs down = {x, ldx, q, ranks, nullptr, 0, (int)desc->n, desc->r};
     const OperandJob job = {nullptr, 0, 0, nullptr, scale, h_out, nullptr, nullptr};
     const UpArgs up = {nullptr, p, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 0};
     return desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, job, nullptr, up, rows, s, st)
@@ -1015,7 +956,7 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     if (rows > 0) {
-        const DownArgs down = {dy, lddy, p, ranks, nullptr, 0, (int)desc->m, desc->r, 0};
+        const DownArgs down = {dy, lddy, p, ranks, nullptr, 0, (int)desc->m, desc->r};
         const OperandJob g = {nullptr, 0, 0, scale, scale, nullptr, nullptr, s.turned_g};
         const OperandJob hj = {h, 0, 1, nullptr, nullptr, nullptr, nullptr, s.turned_h};
         const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, lddx_in, lddx_out, (int)desc->n, desc->r, 0};
