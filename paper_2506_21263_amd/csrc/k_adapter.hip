@@ -166,6 +166,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// Sixteen bytes at any address that their elements may have: the memory system takes them in one request.
+__device__ __forceinline__ ab_u32x4 load_any(const void *p) {
+    ab_u32x4 w;
+    __builtin_memcpy(&w, p, sizeof w);
+    return w;
+}
+
 struct Bf16 {
     static constexpr int code = DLCX_BF16;
     static constexpr int lane = 8;  // elements of 16 bytes
@@ -181,13 +188,15 @@ struct Bf16 {
     // elements k .. k + 7 of a row of `len`; ALL: all of them are there
     template <bool VEC, bool ALL = false>
     static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
+        if constexpr (ALL && VEC) return {*reinterpret_cast<const ab_u32x4 *>(row + k)};
+        if constexpr (ALL) return {load_any(row + k)};
         Frag f = zero();
         if constexpr (VEC) {
-            if (ALL || k < len) f.w = *reinterpret_cast<const ab_u32x4 *>(row + k);
+            if (k < len) f.w = *reinterpret_cast<const ab_u32x4 *>(row + k);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (ALL || k + i < len) f.w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
+                if (k + i < len) f.w[i / 2] |= (uint32_t)row[k + i] << (16 * (i & 1));
         }
         return f;
     }
@@ -233,17 +242,15 @@ struct F32 {
     template <bool VEC, bool ALL = false>
     static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
         Frag f = zero();
-        if constexpr (VEC) {
-            if (ALL || k < len) {
-                const f32x4_t a = *reinterpret_cast<const f32x4_t *>(row + k);
-                const f32x4_t b = *reinterpret_cast<const f32x4_t *>(row + k + 4);
+        if (ALL || (VEC && k < len)) {
+            const ab_u32x4 a = VEC ? *reinterpret_cast<const ab_u32x4 *>(row + k) : load_any(row + k);
+            const ab_u32x4 b = VEC ? *reinterpret_cast<const ab_u32x4 *>(row + k + 4) : load_any(row + k + 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f.x[i] = a[i], f.x[4 + i] = b[i];
-            }
-        } else {
+            for (int i = 0; i < 4; ++i) f.x[i] = __uint_as_float(a[i]), f.x[4 + i] = __uint_as_float(b[i]);
+        } else if (!VEC) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (ALL || k + i < len) f.x[i] = row[k + i];
+                if (k + i < len) f.x[i] = row[k + i];
         }
         return f;
     }
@@ -265,6 +272,8 @@ __device__ __forceinline__ ab_u32x4 load16(const typename T::elem *row, int j, i
     ab_u32x4 w = {0u, 0u, 0u, 0u};
     if constexpr (VEC) {
         w = *reinterpret_cast<const ab_u32x4 *>(row + min(j, len - T::lane));
+    } else if (j + T::lane <= len) {
+        w = load_any(row + j);
     } else {
 #pragma unroll
         for (int i = 0; i < T::lane; ++i)
@@ -308,7 +317,7 @@ struct DownArgs {
     const int32_t *ranks;
     float *out;          // rows x r, columns below the adapter's rank; shares of the reduction `stride` floats apart
     int64_t stride;
-    int len, r;
+    int len, r, shares;
 };
 
 // A workgroup has a share of the reduction (its eight wavefronts 256 to 512 bytes of it each), CT x 16 columns and
@@ -327,15 +336,16 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
     __shared__ f32x4_t sums[2][kDownWaves][CT][64];
-    const Tile tile = find_tile(route, size, blockIdx.y);
+    const int share = (int)(blockIdx.x % (uint32_t)a.shares);
+    const Tile tile = find_tile(route, size, (int)(blockIdx.x / (uint32_t)a.shares));
     if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, row16 = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int c0 = blockIdx.z * CT * 16, last = tile.rows - 1;
+    const int c0 = blockIdx.y * CT * 16, last = tile.rows - 1;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     if (c0 >= rank) return;
-    const int k0 = (blockIdx.x * kDownWaves + wave) * KS * 32;
+    const int k0 = (share * kDownWaves + wave) * KS * 32;
     const bool whole = k0 + KS * 32 <= a.len;
     auto load = [&](const elem *row, Frag (&f)[KS]) {
         if (whole) {
@@ -353,7 +363,7 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
 #pragma unroll
     for (int c = 0; c < CT; ++c)  // columns from the rank on are the last one again: not stored
         load((const elem *)a.f + ((int64_t)tile.adapter * a.r + min(c0 + c * 16 + row16, rank - 1)) * a.len, f[c]);
-    float *out = a.out + blockIdx.x * a.stride;
+    float *out = a.out + share * a.stride;
     for (int t0 = 0, turn = 0; t0 <= last; t0 += 16, turn ^= 1) {
         load(ahead, next);
         ahead = row_of(t0 + 32);
@@ -456,6 +466,7 @@ struct UpArgs {
     void *y_out;         // rows x len
     int64_t ldi, ldo;
     int len, r, copy;    // copy: rows without adapter are to be written too
+    int blocks;          // of columns
 };
 
 // A workgroup has 256 bytes of columns and up to `size` rows of one adapter.  It turns the factor's
@@ -485,11 +496,12 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
     Frag *blocks = reinterpret_cast<Frag *>(up_lds);  // [step][tile of columns][lane]
-    const Tile tile = find_tile(route, size, blockIdx.y);
+    const uint32_t block = blockIdx.x % (uint32_t)a.blocks;
+    const Tile tile = find_tile(route, size, (int)(blockIdx.x / (uint32_t)a.blocks));
     if (tile.adapter < (a.copy ? -1 : 0)) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
-    const int j0 = blockIdx.x * 16 * T::lane;
+    const int j0 = (int)block * 16 * T::lane;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int steps = (rank + 31) / 32, last = tile.rows - 1;
     int t0 = wave * 16;
@@ -539,6 +551,8 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
             }
             if constexpr (VEC) {
                 if (valid && j < a.len) *reinterpret_cast<ab_u32x4 *>(out + j) = w;
+            } else if (j + T::lane <= a.len) {
+                if (valid) __builtin_memcpy(out + j, &w, sizeof w);
             } else {
 #pragma unroll
                 for (int p = 0; p < T::lane; ++p)
@@ -575,16 +589,19 @@ struct GradArgs {
 // A workgroup has 256 bytes of columns, CT x 16 columns of the factor and up to `size` rows of one adapter, 32
 // at a time to each of its wavefronts in turn; the next ones' are requested before this one's products.
 constexpr int kGradWaves = 4;
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p, const int32_t *__restrict__ order,
-                                          int t0, int rows, int j) {
-    const int quad = (threadIdx.x & 63) >> 4;
+struct RowIndex {
     int t[8];
+    __device__ __forceinline__ void load(const int32_t *__restrict__ order, int t0, int rows) {
+        const int quad = (threadIdx.x & 63) >> 4;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = order[min(t0 + quad * 8 + i, rows - 1)];  // (rows beyond meet zeros in u)
+        for (int i = 0; i < 8; ++i) t[i] = order[min(t0 + quad * 8 + i, rows - 1)];  // (rows beyond meet zeros in u)
+    }
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p, const RowIndex &at, int j) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        z[i] = load16<T, VEC>((const typename T::elem *)p.z + t[i] * p.ldz, j, p.len);
+        z[i] = load16<T, VEC>((const typename T::elem *)p.z + at.t[i] * p.ldz, j, p.len);
 }
 template <typename T, int CT, bool VEC>
 __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int steps, const Tile &tile,
@@ -601,21 +618,35 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
     const Frag *u = (const Frag *)p.u + ((int64_t)tile.block * steps * 2 + c0 / 16) * T::pieces * 64 + lane;
     const int64_t u_block = (int64_t)steps * 2 * T::pieces * 64;
     ab_u32x4 z[8];
-    load_rows<T, VEC>(z, p, order, wave * 32, tile.rows, j);
+    RowIndex at;
+    at.load(order, wave * 32, tile.rows);
+    load_rows<T, VEC>(z, p, at, j);
+    at.load(order, wave * 32 + kGradWaves * 32, tile.rows);
+    Frag f[2][T::pieces];
+    auto load_u = [&](Frag (&to)[T::pieces], int t0, int c) {
+#pragma unroll
+        for (int h = 0; h < T::pieces; ++h) to[h] = u[(t0 / 32) * u_block + (c * T::pieces + h) * 64];
+    };
+    const int ct = min(CT, (steps * 32 - c0) / 16);  // columns that there are operands for
+    if (wave * 32 < tile.rows) load_u(f[0], wave * 32, 0);
     for (int t0 = wave * 32; t0 < tile.rows; t0 += kGradWaves * 32) {
+        const int t1 = t0 + kGradWaves * 32 < tile.rows ? t0 + kGradWaves * 32 : t0;
         Frag turned[T::lane];
         turn(z, turned);
-        load_rows<T, VEC>(z, p, order, t0 + kGradWaves * 32, tile.rows, j);
-        const Frag *block = u + (t0 / 32) * u_block;
+        load_rows<T, VEC>(z, p, at, j);
+        at.load(order, t0 + 2 * kGradWaves * 32, tile.rows);
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-            if (c0 + c * 16 >= steps * 32) break;
+            load_u(f[(c + 1) & 1], c + 1 < CT ? t0 : t1, c + 1 < CT ? min(c + 1, ct - 1) : 0);
+            if (c < ct)
 #pragma unroll
-            for (int h = 0; h < T::pieces; ++h) {
-                const Frag f = block[(c * T::pieces + h) * 64];
+                for (int h = 0; h < T::pieces; ++h)
 #pragma unroll
-                for (int s = 0; s < T::lane; ++s) acc[c][s] = T::mma(f, turned[s], acc[c][s]);
-            }
+                    for (int s = 0; s < T::lane; ++s) acc[c][s] = T::mma(f[c & 1][h], turned[s], acc[c][s]);
+        }
+        if constexpr (CT & 1) {
+#pragma unroll
+            for (int h = 0; h < T::pieces; ++h) f[0][h] = f[1][h];
         }
     }
 #pragma unroll
@@ -649,6 +680,8 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
                                    scale * acc[c][s + 3][v]};
                 if constexpr (VEC) {
                     if (j + s < p.len) *reinterpret_cast<f32x4_t *>(row + j + s) = w;
+                } else if (j + s + 4 <= p.len) {
+                    __builtin_memcpy(row + j + s, &w, sizeof w);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -726,13 +759,16 @@ static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const Route &v, 
         adapter_down_kernel<T, CT, false><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
 }
 template <typename T>
-static int launch_down(const DownArgs &a, int64_t rows, const Route &v, hipStream_t st) {
+static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st) {
     const int es = sizeof(typename T::elem), ct = down_tiles(a.r), splits = down_splits<T>(a.len, a.r);
     const bool vec = rows_aligned(a.x, a.ldx, es) && aligned16(a.f) && a.len % 8 == 0;
     const int64_t cols = ceil_div(a.r, ct * 16);
     int size = kDownRows;
     while (size > 16 && ceil_div(rows, size) * splits * cols < 768) size /= 2;
-    const dim3 grid((unsigned)splits, (unsigned)max_tiles(rows, v.count, size), (unsigned)cols);
+    const int64_t groups = splits * max_tiles(rows, v.count, size);
+    if (groups > 0x7FFFFFFF) return DLCX_EINVAL;
+    a.shares = splits;
+    const dim3 grid((unsigned)groups, (unsigned)cols);
     Timed timed(KID_ADAPTER_DOWN, st);
     if (ct == 4) down_kernel<T, 4>(a, vec, grid, v, size, st);
     else if (ct == 2) down_kernel<T, 2>(a, vec, grid, v, size, st);
@@ -748,7 +784,7 @@ static int launch_operands(const OperandArgs &a, int jobs, int64_t rows, const R
 }
 
 template <typename T, int KT, bool VEC>
-static int up_kernel(const UpArgs &a, dim3 grid, const Route &v, int size, hipStream_t st) {
+static int up_kernel(const UpArgs &a, unsigned grid, const Route &v, int size, hipStream_t st) {
     const size_t lds = (size_t)KT * T::lane * 64 * sizeof(typename T::Frag);
     static size_t granted = 0;
     const int rc = grant_dynamic_lds((const void *)adapter_up_kernel<T, KT, VEC>, lds, &granted, "adapter_up lds");
@@ -758,14 +794,17 @@ static int up_kernel(const UpArgs &a, dim3 grid, const Route &v, int size, hipSt
     return check_launch("adapter_up");
 }
 template <typename T>
-static int launch_up(const UpArgs &a, int64_t rows, const Route &v, hipStream_t st) {
+static int launch_up(UpArgs a, int64_t rows, const Route &v, hipStream_t st) {
     const int es = sizeof(typename T::elem);
     const bool vec = aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.ldo, es) &&
                      (!a.y_in || rows_aligned(a.y_in, a.ldi, es));
     const int64_t cols = ceil_div(a.len, 16 * T::lane);
     int size = kUpRows;
     while (size > 64 && ceil_div(rows, size) * cols < 1024) size /= 2;
-    const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, v.count, size));
+    const int64_t groups = cols * max_tiles(rows, v.count, size);
+    if (groups > 0x7FFFFFFF) return DLCX_EINVAL;
+    a.blocks = (int)cols;
+    const unsigned grid = (unsigned)groups;
     switch (up_steps(a.r)) {
     case 1: return vec ? up_kernel<T, 1, true>(a, grid, v, size, st) : up_kernel<T, 1, false>(a, grid, v, size, st);
     case 2: return vec ? up_kernel<T, 2, true>(a, grid, v, size, st) : up_kernel<T, 2, false>(a, grid, v, size, st);
@@ -920,9 +959,9 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
-    const DownArgs down = {x, ldx, q, ranks, nullptr, 0, (int)desc->n, desc->r};
+    const DownArgs down = {x, ldx, q, ranks, nullptr, 0, (int)desc->n, desc->r, 1};
     const OperandJob job = {nullptr, 0, 0, nullptr, scale, h_out, nullptr, nullptr};
-    const UpArgs up = {nullptr, p, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 0};
+    const UpArgs up = {nullptr, p, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 0, 1};
     return desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, job, nullptr, up, rows, s, st)
                                     : down_and_up<F32>(down, job, nullptr, up, rows, s, st);
 }
@@ -956,10 +995,10 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     if (rows > 0) {
-        const DownArgs down = {dy, lddy, p, ranks, nullptr, 0, (int)desc->m, desc->r};
+        const DownArgs down = {dy, lddy, p, ranks, nullptr, 0, (int)desc->m, desc->r, 1};
         const OperandJob g = {nullptr, 0, 0, scale, scale, nullptr, nullptr, s.turned_g};
         const OperandJob hj = {h, 0, 1, nullptr, nullptr, nullptr, nullptr, s.turned_h};
-        const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, lddx_in, lddx_out, (int)desc->n, desc->r, 0};
+        const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, lddx_in, lddx_out, (int)desc->n, desc->r, 0, 1};
         rc = desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, g, &hj, up, rows, s, st)
                                       : down_and_up<F32>(down, g, &hj, up, rows, s, st);
         if (rc != DLCX_OK) return rc;
