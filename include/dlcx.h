@@ -324,7 +324,7 @@ size_t dlcx_adapter_workspace_bytes(const dlcx_adapter_desc *desc, int64_t rows)
 /* For every row t with adapter a:
  *   h[t][c] = sum_i x[t][i] Q_a[c][i] ;  y_out[t][j] = y_in[t][j] + scale[a] sum_c h[t][c] P_a[c][j]
  * and for a row without one h[t] = 0, y_out[t] = y_in[t].  x is rows x n, y rows x m, row-major with
- * row strides ldx, ldy_in, ldy_out in elements (no smaller than the row); q is count x r x n, p is
+ * row strides ldx, ldy_in, ldy_out in elements (from the row's length to 2^29); q is count x r x n, p is
  * count x r x m, h_out rows x r fp32 (backward reads it).  y_in may be y_out, or NULL for zeros.
  * scale (count floats) NULL: 1.  ranks (count ints) NULL: r; only the first ranks[a] columns of adapter a
  * are read, columns of h from there on are 0.  route NULL: formed here.  x, y and the factors may have any

@@ -310,12 +310,18 @@ __device__ __forceinline__ int adapter_rank(int adapter, const int32_t *ranks, i
 }
 
 // ---- down -------------------------------------------------------------------------------------------
+// Row t of a matrix whose rows are `pitch` bytes apart: one multiply-add.
+template <typename E>
+__device__ __forceinline__ const E *row_at(const void *base, uint32_t t, uint32_t pitch) {
+    return (const E *)((const char *)base + (uint64_t)t * pitch);
+}
+
 struct DownArgs {
     const void *x;       // rows x len
-    int64_t ldx;
+    uint32_t pitch;
     const void *f;       // count x r x len
     const int32_t *ranks;
-    float *out;          // rows x r, columns below the adapter's rank; shares of the reduction `stride` floats apart
+    float *out;          // places x r, columns below the adapter's rank; shares of the reduction `stride` floats apart
     int64_t stride;
     int len, r, shares;
 };
@@ -356,38 +362,53 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
             for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, false>(row, k0 + s * 32 + quad * 8, a.len);
         }
     };
-    auto row_of = [&](int t0) { return (const elem *)a.x + (int64_t)order[min(t0 + row16, last)] * a.ldx; };
-    Frag f[CT][KS], now[KS], next[KS];
-    const elem *ahead = row_of(16);
-    load(row_of(0), now);
-#pragma unroll
-    for (int c = 0; c < CT; ++c)  // columns from the rank on are the last one again: not stored
-        load((const elem *)a.f + ((int64_t)tile.adapter * a.r + min(c0 + c * 16 + row16, rank - 1)) * a.len, f[c]);
-    float *out = a.out + share * a.stride;
-    for (int t0 = 0, turn = 0; t0 <= last; t0 += 16, turn ^= 1) {
-        load(ahead, next);
-        ahead = row_of(t0 + 32);
+    auto index_of = [&](int t0) { return order[min(t0 + row16, last)]; };
+    auto load_row = [&](int t, Frag (&x)[KS]) { load(row_at<elem>(a.x, t, a.pitch), x); };
+    Frag f[CT][KS];
+    auto products = [&](const Frag (&x)[KS], int turn) {
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < KS; ++s) acc = T::mma(now[s], f[c][s], acc);
+            for (int s = 0; s < KS; ++s) acc = T::mma(x[s], f[c][s], acc);
             sums[turn][wave][c][lane] = acc;
         }
+    };
+    float *out = a.out + share * a.stride + (int64_t)tile.at * a.r;
+    auto join = [&](int t0, int turn) {
         __syncthreads();
-        if (wave < CT) {
-            f32x4_t acc = sums[turn][0][wave][lane];
+        if (wave >= CT) return;
+        f32x4_t acc = sums[turn][0][wave][lane];
 #pragma unroll
-            for (int w = 1; w < kDownWaves; ++w) acc += sums[turn][w][wave][lane];
-            const int col = c0 + wave * 16 + row16;
+        for (int w = 1; w < kDownWaves; ++w) acc += sums[turn][w][wave][lane];
+        const int col = c0 + wave * 16 + row16;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int t = t0 + quad * 4 + v;
-                if (t <= last && col < rank) out[(int64_t)order[t] * a.r + col] = acc[v];
-            }
+        for (int v = 0; v < 4; ++v) {
+            const int t = t0 + quad * 4 + v;
+            if (t <= last && col < rank) out[(int64_t)t * a.r + col] = acc[v];
         }
+    };
+    // Two sets of rows are on their way at any time.  Requests come back in order: the row numbers of a later
+    // set go out before the rows of an earlier one, and the sums are stored by place, which needs none.
+    Frag x0[KS], x1[KS];
+    load_row(index_of(0), x0);
+    load_row(index_of(16), x1);
+    int n0 = index_of(32), n1 = index_of(48);
 #pragma unroll
-        for (int s = 0; s < KS; ++s) now[s] = next[s];
+    for (int c = 0; c < CT; ++c)  // columns from the rank on are the last one again: not stored
+        load((const elem *)a.f + ((int64_t)tile.adapter * a.r + min(c0 + c * 16 + row16, rank - 1)) * a.len, f[c]);
+    for (int t0 = 0; t0 <= last; t0 += 32) {
+        products(x0, 0);
+        const int m0 = n0;
+        n0 = index_of(t0 + 64);
+        load_row(m0, x0);
+        join(t0, 0);
+        if (t0 + 16 > last) break;
+        products(x1, 1);
+        const int m1 = n1;
+        n1 = index_of(t0 + 80);
+        load_row(m1, x1);
+        join(t0 + 16, 1);
     }
 }
 
@@ -395,12 +416,12 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
 // What the other two products read of h (or g): the sum of its splits, in 32 bits as it is and as two
 // operands, so that they are formed once and not by every workgroup that has other columns.
 struct OperandJob {
-    const float *splits;  // rows x r each, `stride` floats apart
+    const float *splits;  // r columns each, `stride` floats apart
     int64_t stride;
-    int n;
+    int n, placed;        // placed: their rows are in the order of the places
     const float *scale_out, *scale_up;  // what `out` and `turned`, and what `up` are multiplied with; nullptr: 1
     float *out;           // rows x r, or nullptr; zero from the adapter's rank on
-    void *up;             // rows x steps 32, or nullptr: for the product with the factor
+    void *up;             // places x steps 32, or nullptr: for the product with the factor
     void *turned;         // [block of 32 rows][16 columns][piece][lane], or nullptr: for the sums over rows
 };
 struct OperandArgs {
@@ -426,6 +447,7 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
             t[i] = quad * 8 + i < tile.rows ? order[quad * 8 + i] : -1;
             x[i] = 0.f;
         }
+        const int place = tile.at + quad * 8;
         if (c < rank && t[0] >= 0)
             for (int k = 0; k < j.n; k += 4) {
                 float part[4][8];
@@ -433,7 +455,8 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        part[u][i] = j.splits[min(k + u, j.n - 1) * j.stride + (int64_t)(t[i] < 0 ? t[0] : t[i]) * a.r + c];
+                        part[u][i] = j.splits[min(k + u, j.n - 1) * j.stride +
+                                              (int64_t)(t[i] < 0 ? 0 : j.placed ? place + i : t[i]) * a.r + c];
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -442,7 +465,7 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (t[i] < 0) continue;
-            if (j.up) ((typename T::elem *)j.up)[(int64_t)t[i] * cols + c] = T::round(x[i] * s_up);
+            if (j.up) ((typename T::elem *)j.up)[(int64_t)(place + i) * cols + c] = T::round(x[i] * s_up);
             x[i] *= s_out;
             if (j.out && c < a.r) j.out[(int64_t)t[i] * a.r + c] = x[i];
         }
@@ -459,12 +482,12 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
 
 // ---- up ---------------------------------------------------------------------------------------------
 struct UpArgs {
-    const void *h;       // rows x steps 32, scaled
+    const void *h;       // places x steps 32, scaled
     const void *f;       // count x r x len
     const int32_t *ranks;
     const void *y_in;    // or nullptr
     void *y_out;         // rows x len
-    int64_t ldi, ldo;
+    uint32_t pitch_in, pitch_out;
     int len, r, copy;    // copy: rows without adapter are to be written too
     int blocks;          // of columns
 };
@@ -478,16 +501,16 @@ template <typename T, int KT, bool VEC>
 struct UpRows {
     ab_u32x4 y[4];
     typename T::Frag h[KT];
-    __device__ __forceinline__ void load(const UpArgs &a, int64_t t, int j0) {
+    __device__ __forceinline__ void load(const UpArgs &a, int64_t place, int t, int j0) {
         const int quad = (threadIdx.x & 63) >> 4;
-        const typename T::elem *in = (const typename T::elem *)a.y_in + t * a.ldi;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            y[i] = a.y_in ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len)
-                                   : ab_u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int s = 0; s < KT; ++s)
-            h[s] = T::template load8<true, true>((const typename T::elem *)a.h + t * (KT * 32), s * 32 + quad * 8, KT * 32);
+            h[s] = T::template load8<true, true>((const typename T::elem *)a.h + place * (KT * 32), s * 32 + quad * 8,
+                                                 KT * 32);
+        const typename T::elem *in = row_at<typename T::elem>(a.y_in, t, a.pitch_in);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            y[i] = a.y_in ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len) : ab_u32x4{0u, 0u, 0u, 0u};
     }
 };
 template <typename T, int KT, bool VEC>
@@ -504,10 +527,15 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
     const int j0 = (int)block * 16 * T::lane;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int steps = (rank + 31) / 32, last = tile.rows - 1;
-    int t0 = wave * 16;
-    int64_t t = order[min(t0 + row16, last)], t_next = order[min(t0 + kUpWaves * 16 + row16, last)];
-    UpRows<T, KT, VEC> now;
-    now.load(a, t, j0);
+    constexpr int round = kUpWaves * 16;
+    // Two rounds are on their way at any time; the row numbers of a later one go out before an earlier one's rows.
+    auto index_of = [&](int t0) { return order[min(t0 + row16, last)]; };
+    UpRows<T, KT, VEC> r0, r1;
+    auto load = [&](UpRows<T, KT, VEC> &r, int t0, int t) { r.load(a, tile.at + min(t0 + row16, last), t, j0); };
+    int t0 = wave * 16, i0 = index_of(t0), i1 = index_of(t0 + round);
+    int n0 = index_of(t0 + 2 * round), n1 = index_of(t0 + 3 * round);
+    load(r0, t0, i0);
+    load(r1, t0 + round, i1);
     for (int s = wave; s < steps; s += kUpWaves) {
         // (columns from the rank on meet zeros in h: the last one again does for them)
         const elem *f = (const elem *)a.f + (int64_t)tile.adapter * a.r * a.len;
@@ -522,11 +550,8 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
         for (int c = 0; c < T::lane; ++c) blocks[(s * T::lane + c) * 64 + lane] = turned[c];
     }
     __syncthreads();
-    for (; t0 <= last; t0 += kUpWaves * 16) {
+    auto products = [&](const UpRows<T, KT, VEC> &r, int t0, int t) {
         const bool valid = t0 + row16 <= last;
-        UpRows<T, KT, VEC> next;
-        next.load(a, t_next, j0);
-        const int64_t after = order[min(t0 + 2 * kUpWaves * 16 + row16, last)];
         f32x4_t acc[T::lane];
 #pragma unroll
         for (int c = 0; c < T::lane; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -535,8 +560,8 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
             if (s < steps)
 #pragma unroll
                 for (int c = 0; c < T::lane; ++c)
-                    acc[c] = T::mma(blocks[(s * T::lane + c) * 64 + lane], now.h[s], acc[c]);
-        elem *out = (elem *)a.y_out + t * a.ldo;
+                    acc[c] = T::mma(blocks[(s * T::lane + c) * 64 + lane], r.h[s], acc[c]);
+        elem *out = const_cast<elem *>(row_at<elem>(a.y_out, t, a.pitch_out));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int j = j0 + T::lane * (4 * i + quad);
@@ -544,10 +569,10 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
             if constexpr (T::lane == 8) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p)
-                    w[p] = pack2(low_bf16(now.y[i][p]) + acc[2 * p][i], high_bf16(now.y[i][p]) + acc[2 * p + 1][i]);
+                    w[p] = pack2(low_bf16(r.y[i][p]) + acc[2 * p][i], high_bf16(r.y[i][p]) + acc[2 * p + 1][i]);
             } else {
 #pragma unroll
-                for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(now.y[i][p]) + acc[p][i]);
+                for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(r.y[i][p]) + acc[p][i]);
             }
             if constexpr (VEC) {
                 if (valid && j < a.len) *reinterpret_cast<ab_u32x4 *>(out + j) = w;
@@ -564,9 +589,17 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
                     }
             }
         }
-        now = next;
-        t = t_next;
-        t_next = after;
+    };
+    for (; t0 <= last; t0 += 2 * round) {
+        products(r0, t0, i0);
+        i0 = n0;
+        n0 = index_of(t0 + 4 * round);
+        load(r0, t0 + 2 * round, i0);
+        if (t0 + round > last) break;
+        products(r1, t0 + round, i1);
+        i1 = n1;
+        n1 = index_of(t0 + 5 * round);
+        load(r1, t0 + 3 * round, i1);
     }
 }
 
@@ -575,7 +608,7 @@ struct GradProduct {
     const void *u;       // turned operand
     const float *scale;
     const void *z;       // rows x len
-    int64_t ldz;
+    uint32_t pitch;
     float *out;          // count x r x len
     float *slabs;        // slab x r x len
     int len, vec;
@@ -601,7 +634,7 @@ template <typename T, bool VEC>
 __device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p, const RowIndex &at, int j) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        z[i] = load16<T, VEC>((const typename T::elem *)p.z + at.t[i] * p.ldz, j, p.len);
+        z[i] = load16<T, VEC>(row_at<typename T::elem>(p.z, at.t[i], p.pitch), j, p.len);
 }
 template <typename T, int CT, bool VEC>
 __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int steps, const Tile &tile,
@@ -690,7 +723,7 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
             }
         }
 }
-template <typename T, int CT>
+template <typename T, int CT, bool VEC>
 __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradArgs a, Route route, int size) {
     __shared__ f32x4_t sums[kGradWaves / 2][CT * T::lane][64];
     const Tile tile = find_tile(route, size, blockIdx.y);
@@ -699,10 +732,7 @@ __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradAr
     const int second = (int)blockIdx.x >= a.blocks0;
     const GradProduct &p = a.prod[second];
     const int j0 = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 16 * T::lane, c0 = blockIdx.z * CT * 16;
-    if (p.vec)
-        adapter_grad_rows<T, CT, true>(p, a.r, a.steps, tile, order, c0, j0, sums);
-    else
-        adapter_grad_rows<T, CT, false>(p, a.r, a.steps, tile, order, c0, j0, sums);
+    adapter_grad_rows<T, CT, VEC>(p, a.r, a.steps, tile, order, c0, j0, sums);
 }
 
 // Gradients of adapters with several tiles, as the sum of their slabs in the rows' order, and zeros for
@@ -738,7 +768,7 @@ static int launch_route(int64_t rows, const int32_t *ids, const Route &r, hipStr
     return check_launch("adapter_route");
 }
 
-static inline bool rows_aligned(const void *p, int64_t ld, int es) { return aligned16(p) && ld * es % 16 == 0; }
+static inline bool rows_aligned(const void *p, uint32_t pitch) { return aligned16(p) && pitch % 16 == 0; }
 
 // Steps of 32 columns of a factor that the up product is built for.
 static int up_steps(int r) { return r <= 32 ? 1 : r <= 64 ? 2 : r <= 128 ? 4 : 8; }
@@ -760,11 +790,11 @@ static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const Route &v, 
 }
 template <typename T>
 static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st) {
-    const int es = sizeof(typename T::elem), ct = down_tiles(a.r), splits = down_splits<T>(a.len, a.r);
-    const bool vec = rows_aligned(a.x, a.ldx, es) && aligned16(a.f) && a.len % 8 == 0;
+    const int ct = down_tiles(a.r), splits = down_splits<T>(a.len, a.r);
+    const bool vec = rows_aligned(a.x, a.pitch) && aligned16(a.f) && a.len % 8 == 0;
     const int64_t cols = ceil_div(a.r, ct * 16);
     int size = kDownRows;
-    while (size > 16 && ceil_div(rows, size) * splits * cols < 768) size /= 2;
+    while (size > 16 && ceil_div(rows, size) * splits * cols < 500) size /= 2;
     const int64_t groups = splits * max_tiles(rows, v.count, size);
     if (groups > 0x7FFFFFFF) return DLCX_EINVAL;
     a.shares = splits;
@@ -796,8 +826,8 @@ static int up_kernel(const UpArgs &a, unsigned grid, const Route &v, int size, h
 template <typename T>
 static int launch_up(UpArgs a, int64_t rows, const Route &v, hipStream_t st) {
     const int es = sizeof(typename T::elem);
-    const bool vec = aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.ldo, es) &&
-                     (!a.y_in || rows_aligned(a.y_in, a.ldi, es));
+    const bool vec = aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.pitch_out) &&
+                     (!a.y_in || rows_aligned(a.y_in, a.pitch_in));
     const int64_t cols = ceil_div(a.len, 16 * T::lane);
     int size = kUpRows;
     while (size > 64 && ceil_div(rows, size) * cols < 1024) size /= 2;
@@ -820,6 +850,13 @@ static int grad_size(int64_t rows, int64_t m, int64_t n, int lane) {
     while (size > 64 && ceil_div(rows, size) * cols < kGradGroups) size /= 2;
     return size;
 }
+template <typename T, int CT>
+static void grad_kernel(const GradArgs &a, bool vec, dim3 grid, const Route &v, int size, hipStream_t st) {
+    if (vec)
+        adapter_grad_kernel<T, CT, true><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+    else
+        adapter_grad_kernel<T, CT, false><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+}
 template <typename T>
 static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, const Route &v, hipStream_t st) {
     const int64_t cols = a.blocks0 + ceil_div(a.prod[1].len, 16 * T::lane);
@@ -827,12 +864,10 @@ static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, con
         const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
         const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, count, size), (unsigned)ceil_div(a.r, ct * 16));
         Timed timed(KID_ADAPTER_GRAD, st);
-        if (ct == 4)
-            adapter_grad_kernel<T, 4><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
-        else if (ct == 2)
-            adapter_grad_kernel<T, 2><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
-        else
-            adapter_grad_kernel<T, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+        const bool vec = a.prod[0].vec && a.prod[1].vec;
+        if (ct == 4) grad_kernel<T, 4>(a, vec, grid, v, size, st);
+        else if (ct == 2) grad_kernel<T, 2>(a, vec, grid, v, size, st);
+        else grad_kernel<T, 1>(a, vec, grid, v, size, st);
         const int rc = check_launch("adapter_grad");
         if (rc != DLCX_OK) return rc;
     }
@@ -917,6 +952,7 @@ static int check_adapter(const dlcx_adapter_desc *d, int64_t rows) {
     if (d->dtype != DLCX_F32 && d->dtype != DLCX_BF16) return DLCX_EINVAL;
     return DLCX_OK;
 }
+constexpr int64_t kMaxStride = 1 << 29;  // elements; 32 bits of bytes
 static bool misaligned(const void *p, unsigned to) { return ((uintptr_t)p & (to - 1)) != 0; }
 
 size_t dlcx_adapter_route_bytes(int64_t rows, int32_t count) {
@@ -951,17 +987,19 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
     if (misaligned(ids, 4) || misaligned(scale, 4) || misaligned(ranks, 4) || misaligned(h_out, 4)) return DLCX_EINVAL;
     if (misaligned(workspace, 256) || misaligned(route, 256)) return DLCX_EINVAL;
     if (ldx < desc->n || ldy_out < desc->m || (y_in && ldy_in < desc->m)) return DLCX_EINVAL;
+    if (ldx > kMaxStride || ldy_out > kMaxStride || (y_in && ldy_in > kMaxStride)) return DLCX_EINVAL;
     if (y_in == y_out && ldy_in != ldy_out) return DLCX_EINVAL;
     hipStream_t st = as_stream(stream);
+    auto pitch = [es](int64_t ld) { return (uint32_t)(ld * es); };
     AdapterSpace s;
     adapter_space(desc, rows, workspace, &s);
     if (route)
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
-    const DownArgs down = {x, ldx, q, ranks, nullptr, 0, (int)desc->n, desc->r, 1};
-    const OperandJob job = {nullptr, 0, 0, nullptr, scale, h_out, nullptr, nullptr};
-    const UpArgs up = {nullptr, p, ranks, y_in, y_out, ldy_in, ldy_out, (int)desc->m, desc->r, 0, 1};
+    const DownArgs down = {x, pitch(ldx), q, ranks, nullptr, 0, (int)desc->n, desc->r, 1};
+    const OperandJob job = {nullptr, 0, 0, 1, nullptr, scale, h_out, nullptr, nullptr};
+    const UpArgs up = {nullptr, p, ranks, y_in, y_out, pitch(ldy_in), pitch(ldy_out), (int)desc->m, desc->r, 0, 1};
     return desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, job, nullptr, up, rows, s, st)
                                     : down_and_up<F32>(down, job, nullptr, up, rows, s, st);
 }
@@ -986,8 +1024,11 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     if (misaligned(workspace, 256) || misaligned(route, 256)) return DLCX_EINVAL;
     if (rows > 0 && (ldx < desc->n || lddy < desc->m || lddx_out < desc->n || (dx_in && lddx_in < desc->n)))
         return DLCX_EINVAL;
+    if (rows > 0 && (ldx > kMaxStride || lddy > kMaxStride || lddx_out > kMaxStride || (dx_in && lddx_in > kMaxStride)))
+        return DLCX_EINVAL;
     if (rows > 0 && dx_in == dx_out && lddx_in != lddx_out) return DLCX_EINVAL;
     hipStream_t st = as_stream(stream);
+    auto pitch = [es](int64_t ld) { return (uint32_t)(ld * es); };
     AdapterSpace s;
     adapter_space(desc, rows, workspace, &s);
     if (route)
@@ -995,20 +1036,20 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     if (rows > 0) {
-        const DownArgs down = {dy, lddy, p, ranks, nullptr, 0, (int)desc->m, desc->r, 1};
-        const OperandJob g = {nullptr, 0, 0, scale, scale, nullptr, nullptr, s.turned_g};
-        const OperandJob hj = {h, 0, 1, nullptr, nullptr, nullptr, nullptr, s.turned_h};
-        const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, lddx_in, lddx_out, (int)desc->n, desc->r, 0, 1};
+        const DownArgs down = {dy, pitch(lddy), p, ranks, nullptr, 0, (int)desc->m, desc->r, 1};
+        const OperandJob g = {nullptr, 0, 0, 1, scale, scale, nullptr, nullptr, s.turned_g};
+        const OperandJob hj = {h, 0, 1, 0, nullptr, nullptr, nullptr, nullptr, s.turned_h};
+        const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, pitch(lddx_in), pitch(lddx_out), (int)desc->n, desc->r, 0, 1};
         rc = desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, g, &hj, up, rows, s, st)
                                       : down_and_up<F32>(down, g, &hj, up, rows, s, st);
         if (rc != DLCX_OK) return rc;
     }
     const int lane = desc->dtype == DLCX_BF16 ? Bf16::lane : F32::lane;
     GradArgs a;
-    a.prod[0] = {s.turned_h, scale, dy, lddy, dp_out, s.slab_p, (int)desc->m, 0};
-    a.prod[1] = {s.turned_g, nullptr, x, ldx, dq_out, s.slab_q, (int)desc->n, 0};
+    a.prod[0] = {s.turned_h, scale, dy, pitch(lddy), dp_out, s.slab_p, (int)desc->m, 0};
+    a.prod[1] = {s.turned_g, nullptr, x, pitch(ldx), dq_out, s.slab_q, (int)desc->n, 0};
     for (GradProduct &g : a.prod)
-        g.vec = rows_aligned(g.z, g.ldz, (int)es) && g.len % lane == 0 && aligned16(g.out);
+        g.vec = rows_aligned(g.z, g.pitch) && g.len % lane == 0 && aligned16(g.out);
     a.ranks = ranks;
     a.r = desc->r;
     a.steps = up_steps(desc->r);
