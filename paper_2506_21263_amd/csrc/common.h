@@ -35,7 +35,7 @@ enum KernelId {
     KID_ROUND, KID_QUANT_ROUND, KID_REQUANT, KID_EF_UPDATE,
     KID_MFMA_PEAK, KID_TRAFFIC_PROBE, KID_TENSOR_TABLE, KID_GRAD_NORM, KID_ADAMW,
     KID_STATE_DECODE, KID_ADAPTER_ROUTE, KID_ADAPTER_DOWN, KID_ADAPTER_OPERAND, KID_ADAPTER_UP,
-    KID_ADAPTER_GRAD, KID_ADAPTER_SUM, KID_COUNT
+    KID_ADAPTER_ROWS, KID_ADAPTER_GRAD, KID_ADAPTER_SUM, KID_COUNT
 };
 struct Timed {
     Timed(int kid, hipStream_t st);

@@ -163,7 +163,7 @@ static const char *const kKernelNames[KID_COUNT] = {
     "project_q", "sum_slabs", "reconstruct", "gram_partials", "chol_inverse", "apply_w",
     "effective_rank", "round_fused", "quant_round", "requantize", "ef_update",
     "mfma_peak", "traffic_probe", "tensor_table", "grad_norm", "adamw", "state_decode",
-    "adapter_route", "adapter_down", "adapter_operand", "adapter_up", "adapter_grad", "adapter_sum"};
+    "adapter_route", "adapter_down", "adapter_operand", "adapter_up", "adapter_rows", "adapter_grad", "adapter_sum"};
 
 int dlcx_profile_enable(int on) {
     std::lock_guard<std::mutex> lock(g_prof_mutex);

@@ -20,10 +20,11 @@ struct Route {
     int32_t *first;  // count + 2: first place of each bucket in `order`, then the number of rows
     int32_t *order;  // rows: bucket after bucket, in a bucket in the rows' own order
     int count;
+    const int32_t *ids;  // not nullptr: no buckets, every row is a tile, in the rows' own order
 };
 static size_t route_view(int64_t rows, int count, char *base, Route *v) {
     const size_t heads = a256x((size_t)(count + 2) * sizeof(int32_t));
-    if (v) *v = {(int32_t *)base, (int32_t *)(base + heads), count};
+    if (v) *v = {(int32_t *)base, (int32_t *)(base + heads), count, nullptr};
     return heads + a256x((size_t)rows * sizeof(int32_t));
 }
 static inline int64_t max_tiles(int64_t rows, int count, int size) {
@@ -50,6 +51,10 @@ struct Tile {
 // Tile `index` of the buckets' tiles of `size` rows; 64 buckets at a time, the same in every wavefront.
 __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
     const int lane = threadIdx.x & 63;
+    if (r.ids) {
+        const int id = r.ids[index];
+        return {id >= 0 && id < r.count ? id : -1, index, 1, -1, 0};
+    }
     int tiles = 0, slabs = 0, blocks = 0;
     for (int base = 0; base <= r.count; base += 64) {
         const int b = base + lane;
@@ -204,6 +209,10 @@ struct Bf16 {
         return {ab_u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}};
     }
     static __device__ __forceinline__ elem round(float x) { return (uint16_t)pack2(x, x); }
+    static __device__ __forceinline__ float value(elem x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ __forceinline__ float at(const Frag &f, int i) {
+        return i & 1 ? high_bf16(f.w[i / 2]) : low_bf16(f.w[i / 2]);
+    }
     // x as a sum of three bf16 numbers, to 2^-24
     static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[3]) {
         float rest[8];
@@ -262,6 +271,8 @@ struct F32 {
     }
     static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[1]) { f[0] = pack(x); }
     static __device__ __forceinline__ elem round(float x) { return x; }
+    static __device__ __forceinline__ float value(elem x) { return x; }
+    static __device__ __forceinline__ float at(const Frag &f, int i) { return f.x[i]; }
     static constexpr int pieces = 1;
 };
 
@@ -362,7 +373,7 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
             for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, false>(row, k0 + s * 32 + quad * 8, a.len);
         }
     };
-    auto index_of = [&](int t0) { return order[min(t0 + row16, last)]; };
+    auto index_of = [&](int t0) { return route.ids ? tile.at : order[min(t0 + row16, last)]; };
     auto load_row = [&](int t, Frag (&x)[KS]) { load(row_at<elem>(a.x, t, a.pitch), x); };
     Frag f[CT][KS];
     auto products = [&](const Frag (&x)[KS], int turn) {
@@ -392,7 +403,7 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
     // set go out before the rows of an earlier one, and the sums are stored by place, which needs none.
     Frag x0[KS], x1[KS];
     load_row(index_of(0), x0);
-    load_row(index_of(16), x1);
+    if (last >= 16) load_row(index_of(16), x1);
     int n0 = index_of(32), n1 = index_of(48);
 #pragma unroll
     for (int c = 0; c < CT; ++c)  // columns from the rank on are the last one again: not stored
@@ -401,13 +412,13 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
         products(x0, 0);
         const int m0 = n0;
         n0 = index_of(t0 + 64);
-        load_row(m0, x0);
+        if (t0 + 32 <= last) load_row(m0, x0);
         join(t0, 0);
         if (t0 + 16 > last) break;
         products(x1, 1);
         const int m1 = n1;
         n1 = index_of(t0 + 80);
-        load_row(m1, x1);
+        if (t0 + 48 <= last) load_row(m1, x1);
         join(t0 + 16, 1);
     }
 }
@@ -603,6 +614,72 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
     }
 }
 
+// ---- few rows -----------------------------------------------------------------------------------------
+// Where each row has an adapter of its own there is nothing to share: a workgroup has one row and 512 columns, its
+// wavefronts every fourth column of the factor, and h stays in 32 bits.  The shares of h are added by every
+// workgroup for itself.
+struct RowsArgs {
+    const float *splits;  // rows x r, `stride` floats apart
+    int64_t stride;
+    int n;
+    const int32_t *ids, *ranks;
+    const float *scale;
+    const void *f;        // count x r x len
+    const void *y_in;     // or nullptr
+    void *y_out;
+    float *h_out;
+    uint32_t pitch_in, pitch_out;
+    int len, r, count;
+};
+constexpr int kRowsCols = 512;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void adapter_rows_kernel(RowsArgs a) {
+    typedef typename T::elem elem;
+    __shared__ float h[DLCX_MAX_RANK], sums[4][kRowsCols];
+    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x / 64, id = a.ids[t];
+    const int adapter = id >= 0 && id < a.count ? id : -1;
+    const int rank = adapter_rank(adapter, a.ranks, a.r);
+    if ((int)threadIdx.x < a.r) {
+        const int c = threadIdx.x;
+        float x = 0.f;
+        if (c < rank)
+            for (int k = 0; k < a.n; k += 8) {
+                float part[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) part[u] = a.splits[min(k + u, a.n - 1) * a.stride + (int64_t)t * a.r + c];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x += k + u < a.n ? part[u] : 0.f;
+            }
+        if (blockIdx.x == 0) a.h_out[(int64_t)t * a.r + c] = x;
+        h[c] = x * (adapter >= 0 && a.scale ? a.scale[adapter] : 1.f);
+    }
+    __syncthreads();
+    const int j = blockIdx.x * kRowsCols + lane * 8;
+    const elem *f = (const elem *)a.f + (int64_t)max(adapter, 0) * a.r * a.len;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const bool whole = j + 8 <= a.len;
+#pragma unroll 4
+    for (int c = wave; c < rank; c += 4) {
+        const typename T::Frag w = whole ? T::template load8<VEC, true>(f + (int64_t)c * a.len, j, a.len)
+                                         : T::template load8<false, false>(f + (int64_t)c * a.len, j, a.len);
+        const float s = h[c];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += s * T::at(w, i);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[wave][lane * 8 + i] = acc[i];
+    __syncthreads();
+    const elem *in = row_at<elem>(a.y_in, t, a.pitch_in);
+    elem *out = const_cast<elem *>(row_at<elem>(a.y_out, t, a.pitch_out));
+#pragma unroll
+    for (int k = threadIdx.x; k < kRowsCols; k += 256) {
+        const int col = blockIdx.x * kRowsCols + k;
+        if (col >= a.len) break;
+        const float y = (sums[0][k] + sums[1][k]) + (sums[2][k] + sums[3][k]);
+        out[col] = T::round(y + (a.y_in ? T::value(in[col]) : 0.f));
+    }
+}
+
 // ---- grad -------------------------------------------------------------------------------------------
 struct GradProduct {
     const void *u;       // turned operand
@@ -795,7 +872,7 @@ static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st)
     const int64_t cols = ceil_div(a.r, ct * 16);
     int size = kDownRows;
     while (size > 16 && ceil_div(rows, size) * splits * cols < 500) size /= 2;
-    const int64_t groups = splits * max_tiles(rows, v.count, size);
+    const int64_t groups = splits * (v.ids ? rows : max_tiles(rows, v.count, size));
     if (groups > 0x7FFFFFFF) return DLCX_EINVAL;
     a.shares = splits;
     const dim3 grid((unsigned)groups, (unsigned)cols);
@@ -805,6 +882,12 @@ static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st)
     else down_kernel<T, 1>(a, vec, grid, v, size, st);
     return check_launch("adapter_down");
 }
+
+// A row to a workgroup reads the factors once a row, from L2 where rows share an adapter; tiles read them once for
+// 16 rows or more, but take two launches more and the sorting.  Measured at 8192 x 8192 (rows / tiles, us): rank 16
+// 64 rows 8.4 / 18.8, 256 rows 19.9 / 19.9, rank 64 64 rows 15.6 / 21.9, 128 rows 26 / 22.5, rank 256 16 rows
+// 20.8 / 28.6, 64 rows 47 / 39.
+static bool few_rows(int64_t rows, int r) { return rows * r <= 4096; }
 
 template <typename T>
 static int launch_operands(const OperandArgs &a, int jobs, int64_t rows, const Route &v, hipStream_t st) {
@@ -915,6 +998,25 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
     return at;
 }
 
+template <typename T>
+static int down_and_rows(const DownArgs &down, RowsArgs a, int64_t rows, const AdapterSpace &s, hipStream_t st) {
+    DownArgs d = down;
+    d.stride = rows * d.r;
+    d.out = s.split;
+    Route v = {nullptr, nullptr, a.count, a.ids};
+    const int rc = launch_down<T>(d, rows, v, st);
+    if (rc != DLCX_OK) return rc;
+    a.splits = s.split;
+    a.stride = d.stride;
+    a.n = down_splits<T>(d.len, d.r);
+    const bool vec = aligned16(a.f) && a.len % 8 == 0;
+    const dim3 grid((unsigned)ceil_div(a.len, kRowsCols), (unsigned)rows);
+    Timed timed(KID_ADAPTER_ROWS, st);
+    if (vec) adapter_rows_kernel<T, true><<<grid, 256, 0, st>>>(a);
+    else adapter_rows_kernel<T, false><<<grid, 256, 0, st>>>(a);
+    return check_launch("adapter_rows");
+}
+
 // h = x F^T, then y_out = y_in + h G: the forward pass, and the first half of the gradient.  `job` says what
 // becomes of h; `other` of a second matrix of its form, or nullptr.
 template <typename T>
@@ -993,11 +1095,17 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
     auto pitch = [es](int64_t ld) { return (uint32_t)(ld * es); };
     AdapterSpace s;
     adapter_space(desc, rows, workspace, &s);
+    const DownArgs down = {x, pitch(ldx), q, ranks, nullptr, 0, (int)desc->n, desc->r, 1};
+    if (few_rows(rows, desc->r)) {
+        const RowsArgs a = {nullptr, 0, 0, ids, ranks, scale, p, y_in, y_out, h_out, pitch(ldy_in), pitch(ldy_out),
+                            (int)desc->m, desc->r, desc->count};
+        return desc->dtype == DLCX_BF16 ? down_and_rows<Bf16>(down, a, rows, s, st)
+                                        : down_and_rows<F32>(down, a, rows, s, st);
+    }
     if (route)
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
-    const DownArgs down = {x, pitch(ldx), q, ranks, nullptr, 0, (int)desc->n, desc->r, 1};
     const OperandJob job = {nullptr, 0, 0, 1, nullptr, scale, h_out, nullptr, nullptr};
     const UpArgs up = {nullptr, p, ranks, y_in, y_out, pitch(ldy_in), pitch(ldy_out), (int)desc->m, desc->r, 0, 1};
     return desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, job, nullptr, up, rows, s, st)
