@@ -1,0 +1,214 @@
+"""Inner steps of K workers that share one weight matrix in HBM and differ by low-rank adapters.
+
+Only sequencing lives here, as in the stage driver: the shared projection is a plain product, what
+stands beside it and the optimizer are entry points of the HIP library.
+
+    forward   y  = x theta_g^T                                   plain product of the working copy
+              y += s_a P_a Q_a^T x  for the rows of worker a     dlcx_adapter_forward
+    backward  dx = dy theta_g,  dx += ...,  dP_a, dQ_a           plain product, dlcx_adapter_backward
+    update    norm of each worker's gradients, AdamW             dlcx_grad_norm, dlcx_adamw
+    outer     delta_a = e_a - s_a P_a Q_a^T                      dlcx_decompress
+              and on as in Alg. 2: the replicas theta_l,a = theta_g + s_a P_a Q_a^T are never formed
+
+`python -m paper_2506_21263_amd.inner` trains two workers beside a 512 x 512 matrix towards a synthetic
+teacher, outer step after outer step, and prints the losses.
+"""
+import argparse
+
+import torch
+
+from . import (BF16, F32, PHASE_P, PHASE_Q, STATE_GROUP, adapter_desc, desc, dlcx_adamw,
+               dlcx_adapter_backward, dlcx_adapter_forward, dlcx_adapter_route,
+               dlcx_adapter_route_bytes, dlcx_adapter_workspace_bytes, dlcx_compress_average,
+               dlcx_decompress, dlcx_grad_norm, dlcx_orthonormalize, dlcx_outer_nesterov,
+               dlcx_tensor_table, dlcx_tensor_table_bytes, dlcx_workspace_bytes, tensor)
+
+
+class Route:
+    """Which rows of a batch belong to which adapter; one route serves every projection of the batch."""
+
+    def __init__(self, ids, count, stream=None):
+        self.ids = ids
+        self.table = torch.empty(dlcx_adapter_route_bytes(ids.numel(), count), device=ids.device,
+                                 dtype=torch.uint8)
+        dlcx_adapter_route(ids, count, self.table, stream=stream)
+
+
+class AdamW:
+    """AdamW over a list of parameters with given gradient buffers: moments of 32 or 8 bits, clipping
+    by the gradients' own norm (max_norm > 0), bf16 copies of fp32 parameters where wanted.
+    decays[i] is the weight decay of parameter i."""
+
+    def __init__(self, params, grads, lr, betas=(0.9, 0.95), eps=1e-8, decays=None, copies=None,
+                 bits=32, max_norm=0.0):
+        self.lr, self.betas, self.eps, self.max_norm, self.t = lr, betas, eps, max_norm, 0
+        dev = params[0].device
+        self.norm = torch.zeros(1, device=dev)
+        self.moments = []
+        tensors = []
+        for i, p in enumerate(params):
+            if bits == 8:
+                groups = -(-p.numel() // STATE_GROUP)
+                state = dict(m=torch.zeros(p.shape, device=dev, dtype=torch.int8),
+                             v=torch.zeros(p.shape, device=dev, dtype=torch.uint8),
+                             m_scale=torch.zeros(groups, device=dev),
+                             v_scale=torch.zeros(groups, device=dev))
+            else:
+                state = dict(m=torch.zeros(p.shape, device=dev), v=torch.zeros(p.shape, device=dev))
+            self.moments.append(state)
+            tensors.append(tensor(grads[i], p, copy=copies[i] if copies else None,
+                                  weight_decay=decays[i] if decays else 0.0, **state))
+        memory = torch.empty(dlcx_tensor_table_bytes(len(tensors)), device=dev, dtype=torch.uint8)
+        self.table = dlcx_tensor_table(tensors, memory)
+
+    def reset(self):
+        """Moments and step count of a new run."""
+        self.t = 0
+        for state in self.moments:
+            for x in state.values():
+                x.zero_()
+
+    def step(self, stream=None):
+        self.t += 1
+        clip = self.max_norm > 0
+        if clip:
+            dlcx_grad_norm(self.table, self.norm, stream=stream)
+        dlcx_adamw(self.table, self.lr, self.betas[0], self.betas[1], self.eps, self.t,
+                   norm=self.norm if clip else None, max_norm=self.max_norm, stream=stream)
+
+
+class AdapterProjection:
+    """One projection y = x theta^T with an adapter per worker.  q0: count x r x n draws; P starts at zero,
+    so a new adapter changes nothing.  Masters are fp32; the products read copies in `dtype`."""
+
+    def __init__(self, theta_g, q0, scale, max_rows, dtype=torch.bfloat16):
+        self.m, self.n = theta_g.shape
+        self.count, self.r = q0.shape[:2]
+        dev = theta_g.device
+        low = dtype == torch.bfloat16
+        self.d = adapter_desc(self.m, self.n, self.r, self.count, BF16 if low else F32)
+        self.dtype, self.q0 = dtype, q0
+        self.base = theta_g.to(dtype)
+        self.q = q0.clone()
+        self.p = torch.zeros(self.count, self.r, self.m, device=dev)
+        self.q_copy = self.q.to(dtype) if low else self.q
+        self.p_copy = self.p.to(dtype) if low else self.p
+        self.dq, self.dp = torch.zeros_like(self.q), torch.zeros_like(self.p)
+        self.scale_value = scale
+        self.scale = torch.full((self.count,), scale, device=dev)
+        self.workspace = torch.empty(dlcx_adapter_workspace_bytes(self.d, max_rows), device=dev,
+                                     dtype=torch.uint8)
+
+    def parameters(self, a):
+        """Parameters, gradients and copies of adapter a."""
+        copies = [self.p_copy[a], self.q_copy[a]] if self.dtype == torch.bfloat16 else None
+        return [self.p[a], self.q[a]], [self.dp[a], self.dq[a]], copies
+
+    def forward(self, x, route):
+        y = x @ self.base.t()
+        h = torch.empty(x.shape[0], self.r, device=x.device)
+        dlcx_adapter_forward(self.d, x, route.ids, self.q_copy, self.p_copy, y, y, h, self.workspace,
+                             scale=self.scale, route=route.table)
+        return y, h
+
+    def backward(self, x, h, dy, route):
+        """dx; the gradients of the factors are left in dq and dp."""
+        dx = dy @ self.base
+        dlcx_adapter_backward(self.d, x, dy, route.ids, self.q_copy, self.p_copy, h, dx, dx, self.dq,
+                              self.dp, self.workspace, scale=self.scale, route=route.table)
+        return dx
+
+    def fold(self, ef, workspace, group, mma):
+        """ef[a] <- ef[a] - s P_a Q_a^T for every worker: with e_a in ef[a], its pseudo-gradient."""
+        d = desc(self.m, self.n, self.r, 8, group, mma)
+        for a in range(self.count):
+            dlcx_decompress(d, self.p[a] * self.scale_value, self.q[a], None, [ef[a]],
+                            workspace=workspace)
+
+    def restart(self, theta_g):
+        """The adapters of the next inner phase, beside the updated weights."""
+        self.base.copy_(theta_g)
+        self.q.copy_(self.q0)
+        self.p.zero_()
+        if self.dtype == torch.bfloat16:
+            self.q_copy.copy_(self.q)
+            self.p_copy.zero_()
+
+
+class AdapterOuterStep:
+    """The outer step of Alg. 2 for a projection whose workers trained adapters.  M: the matrix's outer
+    state (stage.MatrixState); delayed, as in the paper: what is applied at step t is the average of
+    step t - 1."""
+
+    def __init__(self, M, lr, mu):
+        self.M, self.lr, self.mu, self.t = M, lr, mu, 0
+        dev = M.theta_g.device
+        self.delta_hat = torch.empty_like(M.theta_g)
+        self.workspace = torch.empty(max(M.workspace_bytes, dlcx_workspace_bytes(M.desc(), 1)),
+                                     device=dev, dtype=torch.uint8)
+
+    def step(self, proj):
+        M, ws = self.M, self.workspace
+        self.t += 1
+        if self.t >= 2:
+            dlcx_decompress(M.desc(M.r_prev), M.p_hat, M.q_bar, self.delta_hat, M.ef, workspace=ws)
+        proj.fold(M.ef, ws, M.group, M.mma)
+        if self.t >= 2:
+            dlcx_outer_nesterov(M.theta_g, M.v, self.delta_hat, self.lr, self.mu)
+        d = M.desc()
+        basis = M.q_bar if self.t >= 2 else M.q_in
+        dlcx_compress_average(d, PHASE_P, M.ef, basis, M.codes_p, M.scales_p, M.p_hat, ws)
+        dlcx_orthonormalize(M.m, M.r, M.p_hat, ws)
+        dlcx_compress_average(d, PHASE_Q, M.ef, M.p_hat, M.codes_q, M.scales_q, M.q_bar, ws)
+        M.r_prev = M.r
+        proj.restart(M.theta_g)
+
+
+def train(m=512, n=512, workers=2, r=8, rows=256, inner=20, outer=8, bits=32, dtype=torch.bfloat16,
+          lr=2e-2, outer_lr=0.3, outer_mu=0.0, max_norm=1.0, seed=0, device="cuda", say=None):
+    """Workers train adapters of rank r towards a teacher that is a rank-r step away from the shared
+    weights; every `inner` steps an outer step.  Every phase goes nearly the whole way, so with the step of
+    delay an outer rate above 1/4 already overshoots a little.  Returns the losses at the phases' starts."""
+    from .stage import MatrixState
+    from . import MMA_F32
+    gen = torch.Generator(device=device).manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, generator=gen, device=device)  # noqa: E731
+    theta = 0.02 * normal(m, n)
+    teacher = theta + 0.1 * normal(m, r) @ normal(r, n) / n ** 0.5
+    M = MatrixState(theta, workers, normal(2 * r, n), 8, 64, MMA_F32)
+    proj = AdapterProjection(theta, normal(workers, r, n) / n ** 0.5, 1.0, workers * rows, dtype)
+    optimizers = []
+    for a in range(workers):
+        params, grads, copies = proj.parameters(a)
+        optimizers.append(AdamW(params, grads, lr, copies=copies, bits=bits, max_norm=max_norm))
+    step = AdapterOuterStep(M, outer_lr, outer_mu)
+    route = Route((torch.arange(workers * rows, device=device) // rows).to(torch.int32), workers)
+    losses = []
+    for t in range(outer):
+        for opt in optimizers:
+            opt.reset()
+        for k in range(inner):
+            x = normal(workers * rows, n).to(dtype)      # every worker's own batch
+            want = x.float() @ teacher.t()
+            y, h = proj.forward(x, route)
+            off = y.float() - want
+            loss = (off * off).sum(1).view(workers, rows).mean(1) / m
+            proj.backward(x, h, (off * (2.0 / (rows * m))).to(dtype), route)
+            for opt in optimizers:
+                opt.step()
+            if k == 0:
+                losses.append(loss.mean())
+        if say:
+            say("outer step %d: loss %.5f at the start, %s after %d inner steps" % (
+                t + 1, float(losses[-1]), " ".join("%.5f" % v for v in loss.tolist()), inner))
+        step.step(proj)
+    return [float(v) for v in losses]
+
+
+if __name__ == "__main__":
+    ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    ap.add_argument("--bits", type=int, default=32, choices=(8, 32), help="of the optimizer's moments")
+    ap.add_argument("--outer", type=int, default=8)
+    ap.add_argument("--inner", type=int, default=20)
+    a = ap.parse_args()
+    train(bits=a.bits, outer=a.outer, inner=a.inner, say=lambda s: print(s, flush=True))
