@@ -163,8 +163,8 @@ def _ptr_array(ts):
 
 
 def _stream(stream):
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # torch.cuda.current_stream().cuda_stream, without making the object (3 us)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

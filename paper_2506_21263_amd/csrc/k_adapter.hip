@@ -504,24 +504,24 @@ struct UpArgs {
 };
 
 // A workgroup has 256 bytes of columns and up to `size` rows of one adapter.  It turns the factor's
-// columns into operand blocks in LDS once; then each wavefront takes 16 rows at a time: lane l has row
-// l % 16, and of its columns four times 16 bytes, which four lanes make 64 in a row.  The rows of
-// the next round are requested before the products of this one.
+// columns into operand blocks in LDS once; then each wavefront takes 16 rows at a time: lane l has rows
+// 4 (l / 16) + 0 .. 3 and 16 bytes of each, so that 16 lanes make 256 in a row.  (With a row to
+// every lane of 16 an access is 64 pieces for the L1, not 16: 128 us for 16384 x 8192 at rank 64.)
 constexpr int kUpWaves = 4;
 template <typename T, int KT, bool VEC>
 struct UpRows {
     ab_u32x4 y[4];
     typename T::Frag h[KT];
-    __device__ __forceinline__ void load(const UpArgs &a, int64_t place, int t, int j0) {
+    __device__ __forceinline__ void load(const UpArgs &a, int64_t place, const int (&t)[4], int j) {
         const int quad = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int s = 0; s < KT; ++s)
             h[s] = T::template load8<true, true>((const typename T::elem *)a.h + place * (KT * 32), s * 32 + quad * 8,
                                                  KT * 32);
-        const typename T::elem *in = row_at<typename T::elem>(a.y_in, t, a.pitch_in);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            y[i] = a.y_in ? load16<T, VEC>(in, j0 + T::lane * (4 * i + quad), a.len) : ab_u32x4{0u, 0u, 0u, 0u};
+        for (int v = 0; v < 4; ++v)
+            y[v] = a.y_in ? load16<T, VEC>(row_at<typename T::elem>(a.y_in, t[v], a.pitch_in), j, a.len)
+                          : ab_u32x4{0u, 0u, 0u, 0u};
     }
 };
 template <typename T, int KT, bool VEC>
@@ -535,22 +535,27 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
     if (tile.adapter < (a.copy ? -1 : 0)) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
-    const int j0 = (int)block * 16 * T::lane;
+    const int j = ((int)block * 16 + row16) * T::lane;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int steps = (rank + 31) / 32, last = tile.rows - 1;
     constexpr int round = kUpWaves * 16;
     // Two rounds are on their way at any time; the row numbers of a later one go out before an earlier one's rows.
-    auto index_of = [&](int t0) { return order[min(t0 + row16, last)]; };
+    auto index_of = [&](int t0, int (&t)[4]) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) t[v] = order[min(t0 + quad * 4 + v, last)];
+    };
     UpRows<T, KT, VEC> r0, r1;
-    auto load = [&](UpRows<T, KT, VEC> &r, int t0, int t) { r.load(a, tile.at + min(t0 + row16, last), t, j0); };
-    int t0 = wave * 16, i0 = index_of(t0), i1 = index_of(t0 + round);
-    int n0 = index_of(t0 + 2 * round), n1 = index_of(t0 + 3 * round);
+    auto load = [&](UpRows<T, KT, VEC> &r, int t0, const int (&t)[4]) { r.load(a, tile.at + min(t0 + row16, last), t, j); };
+    int t0 = wave * 16, i0[4], i1[4], n0[4], n1[4];
+    index_of(t0, i0);
+    index_of(t0 + round, i1);
+    index_of(t0 + 2 * round, n0);
+    index_of(t0 + 3 * round, n1);
     load(r0, t0, i0);
     load(r1, t0 + round, i1);
     for (int s = wave; s < steps; s += kUpWaves) {
         // (columns from the rank on meet zeros in h: the last one again does for them)
         const elem *f = (const elem *)a.f + (int64_t)tile.adapter * a.r * a.len;
-        const int j = j0 + T::lane * (4 * (row16 & 3) + row16 / 4);
         ab_u32x4 rows[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -561,8 +566,7 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
         for (int c = 0; c < T::lane; ++c) blocks[(s * T::lane + c) * 64 + lane] = turned[c];
     }
     __syncthreads();
-    auto products = [&](const UpRows<T, KT, VEC> &r, int t0, int t) {
-        const bool valid = t0 + row16 <= last;
+    auto products = [&](const UpRows<T, KT, VEC> &r, int t0, const int (&t)[4]) {
         f32x4_t acc[T::lane];
 #pragma unroll
         for (int c = 0; c < T::lane; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -571,19 +575,19 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
             if (s < steps)
 #pragma unroll
                 for (int c = 0; c < T::lane; ++c)
-                    acc[c] = T::mma(blocks[(s * T::lane + c) * 64 + lane], r.h[s], acc[c]);
-        elem *out = const_cast<elem *>(row_at<elem>(a.y_out, t, a.pitch_out));
+                    acc[c] = T::mma(r.h[s], blocks[(s * T::lane + c) * 64 + lane], acc[c]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = j0 + T::lane * (4 * i + quad);
+        for (int v = 0; v < 4; ++v) {
+            const bool valid = t0 + quad * 4 + v <= last;
+            elem *out = const_cast<elem *>(row_at<elem>(a.y_out, t[v], a.pitch_out));
             ab_u32x4 w;
             if constexpr (T::lane == 8) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p)
-                    w[p] = pack2(low_bf16(r.y[i][p]) + acc[2 * p][i], high_bf16(r.y[i][p]) + acc[2 * p + 1][i]);
+                    w[p] = pack2(low_bf16(r.y[v][p]) + acc[2 * p][v], high_bf16(r.y[v][p]) + acc[2 * p + 1][v]);
             } else {
 #pragma unroll
-                for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(r.y[i][p]) + acc[p][i]);
+                for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(r.y[v][p]) + acc[p][v]);
             }
             if constexpr (VEC) {
                 if (valid && j < a.len) *reinterpret_cast<ab_u32x4 *>(out + j) = w;
@@ -601,15 +605,19 @@ __global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Rou
             }
         }
     };
+    auto copy = [](int (&to)[4], const int (&from)[4]) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) to[v] = from[v];
+    };
     for (; t0 <= last; t0 += 2 * round) {
         products(r0, t0, i0);
-        i0 = n0;
-        n0 = index_of(t0 + 4 * round);
+        copy(i0, n0);
+        index_of(t0 + 4 * round, n0);
         load(r0, t0 + 2 * round, i0);
         if (t0 + round > last) break;
         products(r1, t0 + round, i1);
-        i1 = n1;
-        n1 = index_of(t0 + 5 * round);
+        copy(i1, n1);
+        index_of(t0 + 5 * round, n1);
         load(r1, t0 + 3 * round, i1);
     }
 }
