@@ -525,7 +525,7 @@ struct UpRows {
     }
 };
 template <typename T, int KT, bool VEC>
-__global__ __launch_bounds__(kUpWaves * 64) void adapter_up_kernel(UpArgs a, Route route, int size) {
+__global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 ? 3 : 2) void adapter_up_kernel(UpArgs a, Route route, int size) {
     extern __shared__ __attribute__((aligned(16))) char up_lds[];
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
