@@ -15,6 +15,7 @@ namespace dlcx {
 // Bucket a < count holds the rows of adapter a, bucket `count` the rows without one.  A launch cuts every
 // bucket into tiles of as many rows as fill the GPU; a workgroup finds its tile in the buckets' places.
 constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
+constexpr int kRouteKept = 1024;  // rows of a wavefront whose buckets stay in LDS from one pass to the next
 
 struct Route {
     int32_t *first;  // count + 2: first place of each bucket in `order`, then the number of rows
@@ -85,10 +86,11 @@ __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
 
 // One workgroup sorts the rows by counting: every wavefront counts its own share, the counts become the
 // places where it writes, and the lanes of equal adapters find their order by ballots of the index's
-// bits, so the order within an adapter is that of the rows.
+// bits, so the order within an adapter is that of the rows.  It runs alone, so the loops are kept short: the code
+// of an unrolled one came from memory for longer than it ran (16384 rows 18 us, now 12).
 __global__ __launch_bounds__(kRouteThreads) void adapter_route_kernel(int rows,
                                                                       const int32_t *__restrict__ ids, Route r) {
-    extern __shared__ int cursor[];  // kRouteWaves x buckets
+    extern __shared__ int cursor[];  // kRouteWaves x buckets, then kRouteKept buckets of every wavefront's rows
     __shared__ int sums[kRouteWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, buckets = r.count + 1;
     for (int i = threadIdx.x; i < kRouteWaves * buckets; i += kRouteThreads) cursor[i] = 0;
@@ -96,22 +98,41 @@ __global__ __launch_bounds__(kRouteThreads) void adapter_route_kernel(int rows,
     const int lo = min(rows, wave * share), hi = min(rows, lo + share);
     const int bits = 32 - __clz(buckets - 1);
     int *mine = cursor + wave * buckets;
-    int id[16];  // up to 16384 rows they are read once for both passes
+    uint16_t *kept = reinterpret_cast<uint16_t *>(cursor + kRouteWaves * buckets) + wave * kRouteKept;
+    int run = -1, run_at = 0;  // a bucket whose count (or place) is ahead of the one in LDS
+    auto settle = [&](int pass) {
+        if (run >= 0 && lane == 0) mine[run] = pass == 0 ? mine[run] + run_at : run_at;
+        run = -1;
+        wave_sync();
+    };
     __syncthreads();
     for (int pass = 0; pass < 2; ++pass) {
-        for (int base = lo; base < hi; base += 16 * 64) {
-            if (pass == 0 || share > 16 * 64)
+        for (int base = lo; base < hi; base += kRouteKept) {
+            if (pass == 0 || share > kRouteKept) {
+                int id[kRouteKept / 64];
 #pragma unroll
-                for (int u = 0; u < 16; ++u) {
-                    const int t = base + u * 64 + lane;
-                    id[u] = t < hi ? ids[t] : -1;
-                }
+                for (int u = 0; u < kRouteKept / 64; ++u) id[u] = ids[min(base + u * 64 + lane, rows - 1)];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) {
-                const int t = base + u * 64 + lane;
-                const int b = id[u] >= 0 && id[u] < r.count ? id[u] : r.count;
+                for (int u = 0; u < kRouteKept / 64; ++u)
+                    kept[u * 64 + lane] = (uint16_t)(id[u] >= 0 && id[u] < r.count ? id[u] : r.count);
+                wave_sync();
+            }
+#pragma unroll 1
+            for (int t0 = base; t0 < min(hi, base + kRouteKept); t0 += 64) {
+                const int t = t0 + lane, b = kept[t - base], b0 = __builtin_amdgcn_readfirstlane(b);
                 uint64_t same = __ballot(t < hi);
-                if (same == 0) break;
+                if (__ballot(t < hi && b != b0) == 0) {  // rows of one bucket, as the rows before them or not
+                    if (b0 != run) {
+                        settle(pass);
+                        run = b0;
+                        run_at = pass == 0 ? 0 : mine[b0];
+                    }
+                    if (pass == 1 && t < hi) r.order[run_at + lane] = t;
+                    run_at += __popcll(same);
+                    continue;
+                }
+                settle(pass);
+#pragma unroll 1
                 for (int k = 0; k < bits; ++k) {
                     const uint64_t one = __ballot((b >> k) & 1);
                     same &= (b >> k) & 1 ? one : ~one;
@@ -123,6 +144,7 @@ __global__ __launch_bounds__(kRouteThreads) void adapter_route_kernel(int rows,
                 wave_sync();
             }
         }
+        settle(pass);
         __syncthreads();
         if (pass == 1) return;
         int before = 0;
@@ -844,7 +866,7 @@ __global__ __launch_bounds__(256) void adapter_sum_kernel(GradArgs a, Route rout
 
 // ---- launches -----------------------------------------------------------------------------------------
 static int launch_route(int64_t rows, const int32_t *ids, const Route &r, hipStream_t st) {
-    const size_t lds = sizeof(int) * (size_t)kRouteWaves * (r.count + 1);
+    const size_t lds = (size_t)kRouteWaves * ((r.count + 1) * sizeof(int) + kRouteKept * sizeof(uint16_t));
     static size_t granted = 0;
     int rc = grant_dynamic_lds((const void *)adapter_route_kernel, lds, &granted, "adapter_route lds");
     if (rc != DLCX_OK) return rc;
