@@ -471,8 +471,8 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
     const OperandJob &j = a.job[blockIdx.y];
     const float s_out = j.scale_out && tile.adapter >= 0 ? j.scale_out[tile.adapter] : 1.f;
     const float s_up = j.scale_up && tile.adapter >= 0 ? j.scale_up[tile.adapter] : 1.f;
-    for (int e = threadIdx.x; e < 4 * cols; e += 256) {
-        const int c = e % cols, quad = e / cols;
+    const int c = blockIdx.z * 64 + threadIdx.x % 64, quad = threadIdx.x / 64;
+    if (c < cols) {
         int t[8];
         float x[8];
 #pragma unroll
@@ -657,7 +657,7 @@ struct RowsArgs {
     const void *f;        // count x r x len
     const void *y_in;     // or nullptr
     void *y_out;
-    float *h_out;
+    float *h_out;         // or nullptr
     uint32_t pitch_in, pitch_out;
     int len, r, count;
 };
@@ -680,7 +680,7 @@ __global__ __launch_bounds__(256) void adapter_rows_kernel(RowsArgs a) {
 #pragma unroll
                 for (int u = 0; u < 8; ++u) x += k + u < a.n ? part[u] : 0.f;
             }
-        if (blockIdx.x == 0) a.h_out[(int64_t)t * a.r + c] = x;
+        if (a.h_out && blockIdx.x == 0) a.h_out[(int64_t)t * a.r + c] = x;
         h[c] = x * (adapter >= 0 && a.scale ? a.scale[adapter] : 1.f);
     }
     __syncthreads();
@@ -723,11 +723,13 @@ struct GradProduct {
 struct GradArgs {
     GradProduct prod[2];
     const int32_t *ranks;
-    int r, steps, blocks0;  // column blocks of the first product
+    int r, steps, blocks0, blocks;  // column blocks of the first product and of both
 };
 
-// A workgroup has 256 bytes of columns, CT x 16 columns of the factor and up to `size` rows of one adapter, 32
-// at a time to each of its wavefronts in turn; the next ones' are requested before this one's products.
+// A wavefront has 256 bytes of columns, CT x 16 columns of the factor and rows of one adapter, 32 at a time, the next
+// ones requested before the products of these.  In long tiles the workgroup's wavefronts take rows in
+// turn and join their sums in LDS; in tiles of up to kGradShort rows there is little to share (79 rows of 57
+// adapters, rank 45, fp32: 82 us that way) and each has columns of its own.
 constexpr int kGradWaves = 4;
 struct RowIndex {
     int t[8];
@@ -743,12 +745,13 @@ __device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p
     for (int i = 0; i < 8; ++i)
         z[i] = load16<T, VEC>(row_at<typename T::elem>(p.z, at.t[i], p.pitch), j, p.len);
 }
-template <typename T, int CT, bool VEC>
+template <typename T, int CT, bool VEC, int SPLIT>
 __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int steps, const Tile &tile,
                                                   const int32_t *__restrict__ order, int c0, int j0,
                                                   f32x4_t (*sums)[CT * T::lane][64]) {
     typedef typename T::Frag Frag;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
+    const int lane = threadIdx.x & 63, row16 = lane & 15, quad = lane >> 4;
+    const int wave = SPLIT == 1 ? 0 : threadIdx.x / 64;
     f32x4_t acc[CT][T::lane];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
@@ -761,7 +764,7 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
     RowIndex at;
     at.load(order, wave * 32, tile.rows);
     load_rows<T, VEC>(z, p, at, j);
-    at.load(order, wave * 32 + kGradWaves * 32, tile.rows);
+    at.load(order, wave * 32 + SPLIT * 32, tile.rows);
     Frag f[2][T::pieces];
     auto load_u = [&](Frag (&to)[T::pieces], int t0, int c) {
 #pragma unroll
@@ -769,12 +772,12 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
     };
     const int ct = min(CT, (steps * 32 - c0) / 16);  // columns that there are operands for
     if (wave * 32 < tile.rows) load_u(f[0], wave * 32, 0);
-    for (int t0 = wave * 32; t0 < tile.rows; t0 += kGradWaves * 32) {
-        const int t1 = t0 + kGradWaves * 32 < tile.rows ? t0 + kGradWaves * 32 : t0;
+    for (int t0 = wave * 32; t0 < tile.rows; t0 += SPLIT * 32) {
+        const int t1 = t0 + SPLIT * 32 < tile.rows ? t0 + SPLIT * 32 : t0;
         Frag turned[T::lane];
         turn(z, turned);
         load_rows<T, VEC>(z, p, at, j);
-        at.load(order, t0 + 2 * kGradWaves * 32, tile.rows);
+        at.load(order, t0 + 2 * SPLIT * 32, tile.rows);
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             load_u(f[(c + 1) & 1], c + 1 < CT ? t0 : t1, c + 1 < CT ? min(c + 1, ct - 1) : 0);
@@ -790,7 +793,7 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
         }
     }
 #pragma unroll
-    for (int half = kGradWaves / 2; half > 0; half /= 2) {
+    for (int half = SPLIT / 2; half > 0; half /= 2) {
         if (wave >= half && wave < 2 * half)
 #pragma unroll
             for (int c = 0; c < CT; ++c)
@@ -830,16 +833,21 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
             }
         }
 }
-template <typename T, int CT, bool VEC>
+// SPLIT wavefronts share the rows of a block of columns, or (1) each has a block of its own.
+template <typename T, int CT, bool VEC, int SPLIT>
 __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradArgs a, Route route, int size) {
-    __shared__ f32x4_t sums[kGradWaves / 2][CT * T::lane][64];
+    __shared__ f32x4_t sums[SPLIT == 1 ? 1 : SPLIT / 2][SPLIT == 1 ? 1 : CT * T::lane][64];
     const Tile tile = find_tile(route, size, blockIdx.y);
     if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
-    const int second = (int)blockIdx.x >= a.blocks0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int block = SPLIT == 1 ? (int)blockIdx.x * kGradWaves + wave : (int)blockIdx.x;
+    if (block >= a.blocks) return;
+    const int second = block >= a.blocks0;
     const GradProduct &p = a.prod[second];
-    const int j0 = ((int)blockIdx.x - (second ? a.blocks0 : 0)) * 16 * T::lane, c0 = blockIdx.z * CT * 16;
-    adapter_grad_rows<T, CT, VEC>(p, a.r, a.steps, tile, order, c0, j0, sums);
+    const int j0 = (block - (second ? a.blocks0 : 0)) * 16 * T::lane, c0 = blockIdx.z * CT * 16;
+    adapter_grad_rows<T, CT, VEC, SPLIT>(p, a.r, a.steps, tile, order, c0, j0,
+                                         reinterpret_cast<f32x4_t (*)[CT * T::lane][64]>(&sums));
 }
 
 // Gradients of adapters with several tiles, as the sum of their slabs in the rows' order, and zeros for
@@ -922,7 +930,8 @@ static bool few_rows(int64_t rows, int r) { return rows * r <= 4096; }
 template <typename T>
 static int launch_operands(const OperandArgs &a, int jobs, int64_t rows, const Route &v, hipStream_t st) {
     Timed timed(KID_ADAPTER_OPERAND, st);
-    adapter_operand_kernel<T><<<dim3((unsigned)max_tiles(rows, v.count, 32), (unsigned)jobs), 256, 0, st>>>(a, v);
+    adapter_operand_kernel<T><<<dim3((unsigned)max_tiles(rows, v.count, 32), (unsigned)jobs,
+                                              (unsigned)ceil_div(a.steps, 2)), 256, 0, st>>>(a, v);
     return check_launch("adapter_operand");
 }
 
@@ -963,19 +972,26 @@ static int grad_size(int64_t rows, int64_t m, int64_t n, int lane) {
     while (size > 64 && ceil_div(rows, size) * cols < kGradGroups) size /= 2;
     return size;
 }
+constexpr int kGradShort = 128;
 template <typename T, int CT>
 static void grad_kernel(const GradArgs &a, bool vec, dim3 grid, const Route &v, int size, hipStream_t st) {
-    if (vec)
-        adapter_grad_kernel<T, CT, true><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
-    else
-        adapter_grad_kernel<T, CT, false><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+    if (size <= kGradShort) {
+        grid.x = (grid.x + kGradWaves - 1) / kGradWaves;
+        if (vec)
+            adapter_grad_kernel<T, CT, true, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+        else
+            adapter_grad_kernel<T, CT, false, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+    } else if (vec) {
+        adapter_grad_kernel<T, CT, true, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+    } else {
+        adapter_grad_kernel<T, CT, false, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+    }
 }
 template <typename T>
 static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, const Route &v, hipStream_t st) {
-    const int64_t cols = a.blocks0 + ceil_div(a.prod[1].len, 16 * T::lane);
     if (rows > 0) {
         const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
-        const dim3 grid((unsigned)cols, (unsigned)max_tiles(rows, count, size), (unsigned)ceil_div(a.r, ct * 16));
+        const dim3 grid((unsigned)a.blocks, (unsigned)max_tiles(rows, count, size), (unsigned)ceil_div(a.r, ct * 16));
         Timed timed(KID_ADAPTER_GRAD, st);
         const bool vec = a.prod[0].vec && a.prod[1].vec;
         if (ct == 4) grad_kernel<T, 4>(a, vec, grid, v, size, st);
@@ -1028,17 +1044,27 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
     return at;
 }
 
+// `operands`: the two matrices that the sums over rows need are formed as well (of the first, what down leaves).
 template <typename T>
-static int down_and_rows(const DownArgs &down, RowsArgs a, int64_t rows, const AdapterSpace &s, hipStream_t st) {
+static int down_and_rows(const DownArgs &down, RowsArgs a, int64_t rows, OperandArgs *operands, const AdapterSpace &s,
+                         hipStream_t st) {
     DownArgs d = down;
     d.stride = rows * d.r;
     d.out = s.split;
-    Route v = {nullptr, nullptr, a.count, a.ids};
-    const int rc = launch_down<T>(d, rows, v, st);
+    const Route by_row = {nullptr, nullptr, a.count, a.ids};
+    int rc = launch_down<T>(d, rows, by_row, st);
     if (rc != DLCX_OK) return rc;
     a.splits = s.split;
     a.stride = d.stride;
     a.n = down_splits<T>(d.len, d.r);
+    if (operands) {
+        OperandJob &g = operands->job[0];
+        g.splits = a.splits;
+        g.stride = a.stride;
+        g.n = a.n;
+        rc = launch_operands<T>(*operands, 2, rows, s.route, st);
+        if (rc != DLCX_OK) return rc;
+    }
     const bool vec = aligned16(a.f) && a.len % 8 == 0;
     const dim3 grid((unsigned)ceil_div(a.len, kRowsCols), (unsigned)rows);
     Timed timed(KID_ADAPTER_ROWS, st);
@@ -1129,8 +1155,8 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
     if (few_rows(rows, desc->r)) {
         const RowsArgs a = {nullptr, 0, 0, ids, ranks, scale, p, y_in, y_out, h_out, pitch(ldy_in), pitch(ldy_out),
                             (int)desc->m, desc->r, desc->count};
-        return desc->dtype == DLCX_BF16 ? down_and_rows<Bf16>(down, a, rows, s, st)
-                                        : down_and_rows<F32>(down, a, rows, s, st);
+        return desc->dtype == DLCX_BF16 ? down_and_rows<Bf16>(down, a, rows, nullptr, s, st)
+                                        : down_and_rows<F32>(down, a, rows, nullptr, s, st);
     }
     if (route)
         route_view(rows, desc->count, (char *)const_cast<void *>(route), &s.route);
@@ -1174,12 +1200,20 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     if (rows > 0) {
+        const bool low = desc->dtype == DLCX_BF16, few = few_rows(rows, desc->r);
         const DownArgs down = {dy, pitch(lddy), p, ranks, nullptr, 0, (int)desc->m, desc->r, 1};
-        const OperandJob g = {nullptr, 0, 0, 1, scale, scale, nullptr, nullptr, s.turned_g};
+        const OperandJob g = {nullptr, 0, 0, few ? 0 : 1, scale, scale, nullptr, nullptr, s.turned_g};
         const OperandJob hj = {h, 0, 1, 0, nullptr, nullptr, nullptr, nullptr, s.turned_h};
-        const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, pitch(lddx_in), pitch(lddx_out), (int)desc->n, desc->r, 0, 1};
-        rc = desc->dtype == DLCX_BF16 ? down_and_up<Bf16>(down, g, &hj, up, rows, s, st)
-                                      : down_and_up<F32>(down, g, &hj, up, rows, s, st);
+        if (few) {
+            const RowsArgs a = {nullptr, 0, 0, ids, ranks, scale, q, dx_in, dx_out, nullptr, pitch(lddx_in),
+                                pitch(lddx_out), (int)desc->n, desc->r, desc->count};
+            OperandArgs o = {{g, hj}, ranks, desc->r, up_steps(desc->r)};
+            rc = low ? down_and_rows<Bf16>(down, a, rows, &o, s, st) : down_and_rows<F32>(down, a, rows, &o, s, st);
+        } else {
+            const UpArgs up = {nullptr, q, ranks, dx_in, dx_out, pitch(lddx_in), pitch(lddx_out), (int)desc->n,
+                               desc->r, 0, 1};
+            rc = low ? down_and_up<Bf16>(down, g, &hj, up, rows, s, st) : down_and_up<F32>(down, g, &hj, up, rows, s, st);
+        }
         if (rc != DLCX_OK) return rc;
     }
     const int lane = desc->dtype == DLCX_BF16 ? Bf16::lane : F32::lane;
@@ -1192,6 +1226,7 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     a.r = desc->r;
     a.steps = up_steps(desc->r);
     a.blocks0 = (int)ceil_div(desc->m, 16 * lane);
+    a.blocks = a.blocks0 + (int)ceil_div(desc->n, 16 * lane);
     const int size = grad_size(rows, desc->m, desc->n, lane);
     return desc->dtype == DLCX_BF16 ? launch_grad<Bf16>(a, rows, desc->count, size, s.route, st)
                                     : launch_grad<F32>(a, rows, desc->count, size, s.route, st);
