@@ -49,7 +49,9 @@ struct Tile {
     int slab;     // number among the tiles of adapters that have several, -1: the only one
     int block;    // number of its first 32 rows, when all buckets are cut into blocks of 32
 };
-// Tile `index` of the buckets' tiles of `size` rows; 64 buckets at a time, the same in every wavefront.
+// Tile `index` of the buckets' tiles of up to `size` rows; 64 buckets at a time, the same in every wavefront.
+// EVEN: a bucket's tiles have equal numbers of rows, in sixteens; else all but the last have `size`.
+template <bool EVEN>
 __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
     const int lane = threadIdx.x & 63;
     if (r.ids) {
@@ -67,12 +69,16 @@ __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
         if (after) {
             const int l = __ffsll((unsigned long long)after) - 1;
             const int k = index - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
-            const int from = __builtin_amdgcn_readlane(at, l) + k * size;
+            const int begin = __builtin_amdgcn_readlane(at, l), stop = __builtin_amdgcn_readlane(end, l);
+            const int each = EVEN ? ((stop - begin + 16 * __builtin_amdgcn_readlane(n, l) - 1) /
+                                     (16 * __builtin_amdgcn_readlane(n, l))) * 16 : size;
+            const int from = begin + k * each;
+            if (EVEN && from >= stop) return {-2, 0, 0, -1, 0};
             const int several_l = __builtin_amdgcn_readlane(several, l);
             Tile t;
             t.adapter = base + l < r.count ? base + l : -1;
             t.at = from;
-            t.rows = min(size, __builtin_amdgcn_readlane(end, l) - from);
+            t.rows = min(each, stop - from);
             t.slab = several_l ? __builtin_amdgcn_readlane(slabs_upto, l) - several_l + k : -1;
             t.block = __builtin_amdgcn_readlane(blocks_upto, l) - __builtin_amdgcn_readlane(n32, l) + k * (size / 32);
             return t;
@@ -376,7 +382,7 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
     typedef typename T::elem elem;
     __shared__ f32x4_t sums[2][kDownWaves][CT][64];
     const int share = (int)(blockIdx.x % (uint32_t)a.shares);
-    const Tile tile = find_tile(route, size, (int)(blockIdx.x / (uint32_t)a.shares));
+    const Tile tile = find_tile<true>(route, size, (int)(blockIdx.x / (uint32_t)a.shares));
     if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, row16 = lane & 15, quad = lane >> 4;
@@ -464,7 +470,7 @@ struct OperandArgs {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Route route) {
-    const Tile tile = find_tile(route, 32, blockIdx.x);
+    const Tile tile = find_tile<false>(route, 32, blockIdx.x);
     if (tile.adapter < -1) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r), cols = a.steps * 32;
@@ -553,7 +559,7 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
     typedef typename T::elem elem;
     Frag *blocks = reinterpret_cast<Frag *>(up_lds);  // [step][tile of columns][lane]
     const uint32_t block = blockIdx.x % (uint32_t)a.blocks;
-    const Tile tile = find_tile(route, size, (int)(blockIdx.x / (uint32_t)a.blocks));
+    const Tile tile = find_tile<true>(route, size, (int)(blockIdx.x / (uint32_t)a.blocks));
     if (tile.adapter < (a.copy ? -1 : 0)) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
@@ -837,7 +843,7 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
 template <typename T, int CT, bool VEC, int SPLIT>
 __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradArgs a, Route route, int size) {
     __shared__ f32x4_t sums[SPLIT == 1 ? 1 : SPLIT / 2][SPLIT == 1 ? 1 : CT * T::lane][64];
-    const Tile tile = find_tile(route, size, blockIdx.y);
+    const Tile tile = find_tile<false>(route, size, blockIdx.y);
     if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -908,8 +914,10 @@ static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st)
     const int ct = down_tiles(a.r), splits = down_splits<T>(a.len, a.r);
     const bool vec = rows_aligned(a.x, a.pitch) && aligned16(a.f) && a.len % 8 == 0;
     const int64_t cols = ceil_div(a.r, ct * 16);
-    int size = kDownRows;
-    while (size > 16 && ceil_div(rows, size) * splits * cols < 500) size /= 2;
+    // as few rows as two workgroups to a compute unit leave, half a tile more for every adapter
+    const int64_t most = ceil_div(512, splits * cols), spare = v.count < most ? v.count / 2 : most / 2;
+    int64_t fit = ceil_div(ceil_div(rows, most > spare ? most - spare : 1), 16) * 16;
+    const int size = (int)(fit < kDownRows ? fit : kDownRows);
     const int64_t groups = splits * (v.ids ? rows : max_tiles(rows, v.count, size));
     if (groups > 0x7FFFFFFF) return DLCX_EINVAL;
     a.shares = splits;
