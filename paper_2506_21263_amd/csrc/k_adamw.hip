@@ -369,8 +369,11 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(TableView tv, int c
 __global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double *__restrict__ partial, int n,
                                                                double scale, float *out) {
     __shared__ double lds[kThreads / 64];
-    double acc = 0.0;
-    for (int i = threadIdx.x; i < n; i += kThreads) acc += partial[i];
+    double x[kNormGroups / kThreads], acc = 0.0;
+#pragma unroll
+    for (int u = 0; u < kNormGroups / kThreads; ++u) x[u] = partial[min(u * kThreads + (int)threadIdx.x, n - 1)];
+#pragma unroll
+    for (int u = 0; u < kNormGroups / kThreads; ++u) acc += u * kThreads + (int)threadIdx.x < n ? x[u] : 0.0;
     acc = workgroup_sum(acc, lds);
     if (threadIdx.x == 0) *out = (float)(scale * sqrt(acc));
 }
