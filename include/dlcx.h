@@ -356,9 +356,9 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
  * fp32 scale for every 128 elements (the last group may be shorter) in m_scale and v_scale:
  *   m       = c |c| m_scale, c = -127 .. 127 (int8),    m_scale = largest |m| of the group / 127^2
  *   sqrt(v) = c^2 v_scale,   c = 0 .. 255 (uint8),      v_scale = largest sqrt(v) of the group / 255^2
- * (squares of the codes: steps that shrink with the value, 0.8 % of the largest one near it and a 1/127^2
- * or 1/255^2 of it near zero; c of v is at least 1 where v > 0, so that a small v never turns into a
- * zero denominator).  copy (bf16, fp32 parameters only) or NULL receives the updated
+ * (squares of the codes: steps that shrink with the value, from 2/127 or 2/255 of the largest one near it
+ * to 1/127^2 or 1/255^2 of it near zero; c of v is at least 1 where v > 0, so that a small v never turns
+ * into a zero denominator).  copy (bf16, fp32 parameters only) or NULL receives the updated
  * parameter rounded.  All but the scales are 16-byte aligned.  For dlcx_grad_norm alone, param NULL
  * and the rest ignored. */
 typedef struct {

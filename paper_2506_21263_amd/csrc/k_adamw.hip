@@ -4,6 +4,10 @@
 // All of them are streams over the tensors' elements, bound by HBM.  A launch covers every tensor
 // of a table: the elements are cut into blocks of kBlock, a tensor's last block may be shorter, and
 // table.start holds each tensor's first block, so a workgroup finds its tensor by searching there.
+//
+// Measured: AdamW with fp32 moments 5.0 TB/s (26.5 M fp32 elements in 140 tensors 160 us; 50 M with bf16
+// gradients 290 us), with 8-bit moments 4.8 TB/s (856 M bf16 elements 1.79 ms), where a copy of 2 GiB reaches
+// 4.9; the norm of 856 M bf16 gradients 252 us, 6.8 TB/s, of 26.5 M fp32 ones 24 + 3 us.
 #include <math.h>
 
 #include "common.h"
@@ -155,9 +159,9 @@ __device__ __forceinline__ void store_codes(void *base, int64_t e, int left, ad_
 }
 
 // ---- 8-bit moments ------------------------------------------------------------------------------
-// The square of the code times the scale: an error of at most half a code is a relative error of 1 / (2 c)
-// of the root, 1 / c of the value, so values down to 1e-4 of a group's largest m (2.5e-10 of its largest v)
-// keep a code of their own, which a linear code of 8 bits has for values down to 4e-3 only.
+// The square of the code times the scale: half a code off is a relative error of 1 / (2 c) of the root, 1 / c of
+// the value, so values down to 6e-5 of a group's largest m (2.5e-10 of its largest v) keep a code of their
+// own, where a linear code ends at 8e-3 (4e-3).
 __device__ __forceinline__ float decode_m(uint32_t w, int i, float scale) {
     const float c = (float)(((w ^ 0x80808080u) >> (8 * i)) & 0xFFu) - 128.f;
     return c * fabsf(c) * scale;
@@ -184,7 +188,7 @@ __device__ __forceinline__ float group_scale(float amax, float top, float *inv) 
 }
 // The code of x >= 0 is the integer next to sqrt(x / scale), both operations rounded correctly, where x of a
 // second moment is a correctly rounded root itself.  With IEEE quotients and roots throughout the step
-// was bound by arithmetic (4.2 TB/s of 8192 x 28672 bf16 tensors); so a code is taken from a product and the
+// was bound by arithmetic (4.2 TB/s, now 4.8); so a code is taken from a product and the
 // hardware's roots (1 unit in the last place), together off by less than 8e-5 codes, and where one of a
 // thread's lies within 1e-4 of the middle between two codes, all of them are decided by the definition.
 __device__ __forceinline__ float near_root(float x, float inv) { return __builtin_amdgcn_sqrtf(x * inv); }

@@ -369,7 +369,9 @@ struct DownArgs {
 // up to `size` rows of one adapter.  A wavefront keeps its part of the factor in registers and meets it with 16 rows
 // at a time; the eight sums are joined in LDS, in turn in two places, so that one barrier a round is enough.
 // With whole rows to a workgroup instead, the factor comes from L2 as often as there are tiles of
-// rows, by the same few channels at a time: 91 us for 16384 x 8192 at rank 64, 88 us for 4133 rows.
+// rows, by the same few channels at a time: 91 us for 16384 x 8192 bf16 at rank 64, 88 us for 4133 rows.
+// This form: 74 us (3.6 TB/s of rows, and 34 MB of shares) and 27 us.  The stream of rows alone, in this pattern,
+// takes 62 of the 74; the products and the join 6 each.
 constexpr int kDownWaves = 8;
 template <typename T>
 constexpr int down_steps(int ct) {  // of 32 elements, per wavefront
@@ -453,7 +455,8 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
 
 // ---- operands ---------------------------------------------------------------------------------------
 // What the other two products read of h (or g): the sum of its splits, in 32 bits as it is and as two
-// operands, so that they are formed once and not by every workgroup that has other columns.
+// operands, so that they are formed once and not by every workgroup that has other columns.  12 us for both of
+// 16384 rows at rank 64 (34 MB of shares, 4 of h, 15 of operands).
 struct OperandJob {
     const float *splits;  // r columns each, `stride` floats apart
     int64_t stride;
@@ -534,7 +537,8 @@ struct UpArgs {
 // A workgroup has 256 bytes of columns and up to `size` rows of one adapter.  It turns the factor's
 // columns into operand blocks in LDS once; then each wavefront takes 16 rows at a time: lane l has rows
 // 4 (l / 16) + 0 .. 3 and 16 bytes of each, so that 16 lanes make 256 in a row.  (With a row to
-// every lane of 16 an access is 64 pieces for the L1, not 16: 128 us for 16384 x 8192 at rank 64.)
+// every lane of 16 an access is 64 pieces for the L1, not 16: 128 us for 16384 x 8192 at rank 64.)  HBM
+// bounds it: 104 us, 5.2 TB/s, what copies of this pattern reach.
 constexpr int kUpWaves = 4;
 template <typename T, int KT, bool VEC>
 struct UpRows {
@@ -653,7 +657,7 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
 // ---- few rows -----------------------------------------------------------------------------------------
 // Where each row has an adapter of its own there is nothing to share: a workgroup has one row and 512 columns, its
 // wavefronts every fourth column of the factor, and h stays in 32 bits.  The shares of h are added by every
-// workgroup for itself.
+// workgroup for itself.  96 rows of 64 adapters beside 28672 columns at rank 16: 14 us for 88 MB of factors.
 struct RowsArgs {
     const float *splits;  // rows x r, `stride` floats apart
     int64_t stride;
@@ -735,7 +739,10 @@ struct GradArgs {
 // A wavefront has 256 bytes of columns, CT x 16 columns of the factor and rows of one adapter, 32 at a time, the next
 // ones requested before the products of these.  In long tiles the workgroup's wavefronts take rows in
 // turn and join their sums in LDS; in tiles of up to kGradShort rows there is little to share (79 rows of 57
-// adapters, rank 45, fp32: 82 us that way) and each has columns of its own.
+// adapters, rank 45, fp32: 82 us that way, 39 this) and each has columns of its own.
+// 16384 rows of 8192 + 8192 columns at rank 64: 145 us, 3.7 TB/s.  128 accumulators leave a wavefront registers for
+// one set of rows on its way, 64 KB a compute unit, which carries 4.1 TB/s; two thirds of the matrix products
+// (the second and third piece of h and g) cost 13 us of the 145.
 constexpr int kGradWaves = 4;
 struct RowIndex {
     int t[8];
