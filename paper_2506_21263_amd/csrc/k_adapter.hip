@@ -207,7 +207,6 @@ __device__ __forceinline__ ab_u32x4 load_any(const void *p) {
 }
 
 struct Bf16 {
-    static constexpr int code = DLCX_BF16;
     static constexpr int lane = 8;  // elements of 16 bytes
     typedef uint16_t elem;
     struct Frag {
@@ -237,6 +236,11 @@ struct Bf16 {
         return {ab_u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}};
     }
     static __device__ __forceinline__ elem round(float x) { return (uint16_t)pack2(x, x); }
+    static __device__ __forceinline__ void drop(Frag &f, int n) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f.w[i / 2] &= i < n ? (i & 1 ? 0x0000FFFFu : 0xFFFF0000u) : 0xFFFFFFFFu;
+    }
     static __device__ __forceinline__ float value(elem x) { return __uint_as_float((uint32_t)x << 16); }
     static __device__ __forceinline__ float at(const Frag &f, int i) {
         return i & 1 ? high_bf16(f.w[i / 2]) : low_bf16(f.w[i / 2]);
@@ -259,7 +263,6 @@ struct Bf16 {
     static constexpr int pieces = 3;
 };
 struct F32 {
-    static constexpr int code = DLCX_F32;
     static constexpr int lane = 4;
     typedef float elem;
     struct Frag {
@@ -299,31 +302,53 @@ struct F32 {
     }
     static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[1]) { f[0] = pack(x); }
     static __device__ __forceinline__ elem round(float x) { return x; }
+    // the first n elements are zero
+    static __device__ __forceinline__ void drop(Frag &f, int n) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.x[i] = i < n ? 0.f : f.x[i];
+    }
     static __device__ __forceinline__ float value(elem x) { return x; }
     static __device__ __forceinline__ float at(const Frag &f, int i) { return f.x[i]; }
     static constexpr int pieces = 1;
 };
 
-// 16 bytes of a row from element j on.  Elements from `len` on belong to columns that nobody stores: they
-// are the row's last ones again where rows are read by 16 bytes, so that no lane waits at a branch.
+// Where a lane's 16 bytes of a row begin that should begin at element j: at the row's last 16 where it ends before
+// j + lane, so that no lane waits at a branch.  What it has twice then, or beyond the row, it does not store.
+template <typename T>
+__device__ __forceinline__ int column_base(int j, int len) {
+    return len >= T::lane ? min(j, len - T::lane) : j;
+}
 template <typename T, bool VEC>
-__device__ __forceinline__ ab_u32x4 load16(const typename T::elem *row, int j, int len) {
+__device__ __forceinline__ ab_u32x4 load16(const typename T::elem *row, int base, int len) {
+    if constexpr (VEC) return *reinterpret_cast<const ab_u32x4 *>(row + base);
+    if (len >= T::lane) return load_any(row + base);
     ab_u32x4 w = {0u, 0u, 0u, 0u};
-    if constexpr (VEC) {
-        w = *reinterpret_cast<const ab_u32x4 *>(row + min(j, len - T::lane));
-    } else if (j + T::lane <= len) {
-        w = load_any(row + j);
-    } else {
 #pragma unroll
-        for (int i = 0; i < T::lane; ++i)
-            if (j + i < len) {
-                if constexpr (T::lane == 8)
-                    w[i / 2] |= (uint32_t)row[j + i] << (16 * (i & 1));
-                else
-                    w[i] = __float_as_uint(row[j + i]);
-            }
-    }
+    for (int i = 0; i < T::lane; ++i)
+        if (base + i < len) {
+            if constexpr (T::lane == 8)
+                w[i / 2] |= (uint32_t)row[base + i] << (16 * (i & 1));
+            else
+                w[i] = __float_as_uint(row[base + i]);
+        }
     return w;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store16(typename T::elem *row, const ab_u32x4 &w, int base, int j, int len) {
+    if (VEC || j + T::lane <= len) {
+        if (j >= len) return;
+        if constexpr (VEC) *reinterpret_cast<ab_u32x4 *>(row + base) = w;
+        else __builtin_memcpy(row + base, &w, sizeof w);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < T::lane; ++i)
+        if (base + i >= j && base + i < len) {
+            if constexpr (T::lane == 8)
+                row[base + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+            else
+                row[base + i] = __uint_as_float(w[i]);
+        }
 }
 
 // Eight rows of 16 bytes each, turned: fragment s holds element s of the eight rows.  Where the rows are
@@ -378,7 +403,7 @@ constexpr int down_steps(int ct) {  // of 32 elements, per wavefront
     return (ct == 4 ? 4 : 8) * T::lane / 8;
 }
 template <typename T, int CT, bool VEC>
-__global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownArgs a, Route route, int size) {
+__global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapter_down_kernel(DownArgs a, Route route, int size) {
     constexpr int KS = down_steps<T>(CT);
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
@@ -394,13 +419,19 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
     if (c0 >= rank) return;
     const int k0 = (share * kDownWaves + wave) * KS * 32;
     const bool whole = k0 + KS * 32 <= a.len;
+    // The lane's elements of step s.  Where a row that is not read by 16 aligned bytes ends before them, its last
+    // eight, of which the factor's are zero as far as another lane has them (shorter rows are read by element).
+    auto at = [&](int s) { return k0 + s * 32 + quad * 8; };
     auto load = [&](const elem *row, Frag (&f)[KS]) {
         if (whole) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, true>(row, k0 + s * 32 + quad * 8, a.len);
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, true>(row, at(s), a.len);
+        } else if (!VEC && a.len >= 8) {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, true>(row, min(at(s), a.len - 8), a.len);
         } else {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, false>(row, k0 + s * 32 + quad * 8, a.len);
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, false>(row, at(s), a.len);
         }
     };
     auto index_of = [&](int t0) { return route.ids ? tile.at : order[min(t0 + row16, last)]; };
@@ -438,6 +469,11 @@ __global__ __launch_bounds__(kDownWaves * 64, 2) void adapter_down_kernel(DownAr
 #pragma unroll
     for (int c = 0; c < CT; ++c)  // columns from the rank on are the last one again: not stored
         load((const elem *)a.f + ((int64_t)tile.adapter * a.r + min(c0 + c * 16 + row16, rank - 1)) * a.len, f[c]);
+    if (!VEC && !whole && a.len >= 8)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) T::drop(f[c][s], at(s) - min(at(s), a.len - 8));
     for (int t0 = 0; t0 <= last; t0 += 32) {
         products(x0, 0);
         const int m0 = n0;
@@ -567,7 +603,7 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
     if (tile.adapter < (a.copy ? -1 : 0)) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
-    const int j = ((int)block * 16 + row16) * T::lane;
+    const int j_row = ((int)block * 16 + row16) * T::lane, j = column_base<T>(j_row, a.len);
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int steps = (rank + 31) / 32, last = tile.rows - 1;
     constexpr int round = kUpWaves * 16;
@@ -621,20 +657,7 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
 #pragma unroll
                 for (int p = 0; p < 4; ++p) w[p] = __float_as_uint(__uint_as_float(r.y[v][p]) + acc[p][v]);
             }
-            if constexpr (VEC) {
-                if (valid && j < a.len) *reinterpret_cast<ab_u32x4 *>(out + j) = w;
-            } else if (j + T::lane <= a.len) {
-                if (valid) __builtin_memcpy(out + j, &w, sizeof w);
-            } else {
-#pragma unroll
-                for (int p = 0; p < T::lane; ++p)
-                    if (valid && j + p < a.len) {
-                        if constexpr (T::lane == 8)
-                            out[j + p] = (uint16_t)(w[p / 2] >> (16 * (p & 1)));
-                        else
-                            out[j + p] = __uint_as_float(w[p]);
-                    }
-            }
+            if (valid) store16<T, VEC>(out, w, j, j_row, a.len);
         }
     };
     auto copy = [](int (&to)[4], const int (&from)[4]) {
@@ -770,7 +793,7 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int s = 0; s < T::lane; ++s) acc[c][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const int j = j0 + T::lane * row16;
+    const int j_row = j0 + T::lane * row16, j = column_base<T>(j_row, p.len);
     const Frag *u = (const Frag *)p.u + ((int64_t)tile.block * steps * 2 + c0 / 16) * T::pieces * 64 + lane;
     const int64_t u_block = (int64_t)steps * 2 * T::pieces * 64;
     ab_u32x4 z[8];
@@ -834,14 +857,14 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
             for (int s = 0; s < T::lane; s += 4) {
                 const f32x4_t w = {scale * acc[c][s][v], scale * acc[c][s + 1][v], scale * acc[c][s + 2][v],
                                    scale * acc[c][s + 3][v]};
-                if constexpr (VEC) {
-                    if (j + s < p.len) *reinterpret_cast<f32x4_t *>(row + j + s) = w;
-                } else if (j + s + 4 <= p.len) {
-                    __builtin_memcpy(row + j + s, &w, sizeof w);
+                if (VEC || j_row + T::lane <= p.len) {
+                    if (j_row >= p.len) continue;
+                    if constexpr (VEC) *reinterpret_cast<f32x4_t *>(row + j + s) = w;
+                    else __builtin_memcpy(row + j + s, &w, sizeof w);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (j + s + i < p.len) row[j + s + i] = w[i];
+                        if (j + s + i >= j_row && j + s + i < p.len) row[j + s + i] = w[i];
                 }
             }
         }
