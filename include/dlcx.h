@@ -380,7 +380,7 @@ typedef struct {
 typedef struct {
     void *memory;
     int64_t blocks;
-    int32_t count, steps; /* steps: every tensor has what dlcx_adamw needs */
+    int32_t count, steps; /* steps: 0 where a tensor lacks what dlcx_adamw needs, or which kinds of moments there are */
 } dlcx_table;
 size_t dlcx_tensor_table_bytes(int32_t count);
 int dlcx_tensor_table(const dlcx_tensor *tensors_host, int32_t count, void *memory,

@@ -5,9 +5,9 @@
 // of a table: the elements are cut into blocks of kBlock, a tensor's last block may be shorter, and
 // table.start holds each tensor's first block, so a workgroup finds its tensor by searching there.
 //
-// Measured: AdamW with fp32 moments 5.0 TB/s (26.5 M fp32 elements in 140 tensors 160 us; 50 M with bf16
-// gradients 290 us), with 8-bit moments 4.8 TB/s (856 M bf16 elements 1.79 ms), where a copy of 2 GiB reaches
-// 4.9; the norm of 856 M bf16 gradients 252 us, 6.8 TB/s, of 26.5 M fp32 ones 24 + 3 us.
+// Measured: AdamW with fp32 moments 5.3 TB/s (26.5 M fp32 elements in 140 tensors 148 us; 50 M with bf16
+// gradients 264 us), with 8-bit moments 5.8 TB/s (856 M bf16 elements 1.47 ms), where a copy of 2 GiB reaches
+// 4.9; the norm of 856 M bf16 gradients 257 us, 6.7 TB/s, of 26.5 M fp32 ones 24 + 3 us.
 #include <math.h>
 
 #include "common.h"
@@ -21,6 +21,7 @@ constexpr int kBlock = 2 * kStep;             // elements of a block
 constexpr int kStateGroup = 128;              // elements that share a scale: 16 lanes
 constexpr int kNormGroups = 2048;             // most workgroups (and partial sums) of the norm
 constexpr int kTablePart = 32;                // tensors passed to one launch of the table's kernel
+constexpr int kComplete = 1, kHas32 = 2, kHas8 = 4;  // of a table's `steps`
 constexpr float kTopM = 127.f, kTopV = 255.f;
 
 // What `memory` of a table holds.
@@ -83,79 +84,123 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, ad_bf16x2));
 }
 
-// Eight elements from `e` on, of which `left` (1 .. 8; less or equal 0: none) are inside the tensor.
+// Where a thread's elements begin: `first`, the workgroup's, is the same in all lanes, so that an access takes its
+// address from scalar registers and one 32-bit offset.  A pointer read from the table is not known to be one
+// to global memory unless it is said.
+#define AD_GLOBAL __attribute__((address_space(1)))
+template <class T>
+__device__ __forceinline__ AD_GLOBAL T *elements(const void *base, int64_t first) {
+    AD_GLOBAL char *p = (AD_GLOBAL char *)base + first * (int64_t)sizeof(T);
+    return (AD_GLOBAL T *)(p + threadIdx.x * (kVec * (unsigned)sizeof(T)));
+}
+
+// A thread's elements as they lie in memory: all of them, or the `left` (less than 8; less or equal 0: none) that are
+// inside the tensor and zeros.  All loads of a step come before what is made of any of them, in one branch
+// each for whole and for part, so that none waits for another.
 template <int DT>
-__device__ __forceinline__ void load_floats(const void *base, int64_t e, int left, float (&x)[kVec]) {
-    if (left >= kVec) {
-        if constexpr (DT == DLCX_F32) {
-            const ad_f32x4 *p = reinterpret_cast<const ad_f32x4 *>((const float *)base + e);
-            const ad_f32x4 a = __builtin_nontemporal_load(p), b = __builtin_nontemporal_load(p + 1);
+struct Raw {
+    uint32_t w[DT == DLCX_F32 ? kVec : kVec / 2];
+};
+// STREAM: past the caches' order of use.  Against plain loads: 8-bit moments 1.47 (1.61) ms, a norm over
+// 1.7 GB 257 (303) us and over 106 MB 28 (25); but 32-bit moments, whose 12 or 14 bytes an element read and
+// written at the same places, 155 (148) and 278 (264) us, so those are plain.  Stores: all streamed, 1.47 (1.66) ms
+// and 278 (282) us.
+template <class T, bool STREAM>
+__device__ __forceinline__ T load_vector(AD_GLOBAL const T *p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    return *p;
+}
+template <int DT, bool STREAM = true>
+__device__ __forceinline__ Raw<DT> load_whole(const void *base, int64_t first) {
+    Raw<DT> x;
+    if constexpr (DT == DLCX_F32) {
+        AD_GLOBAL const ad_u32x4 *p = (AD_GLOBAL const ad_u32x4 *)elements<const float>(base, first);
+        const ad_u32x4 a = load_vector<ad_u32x4, STREAM>(p), b = load_vector<ad_u32x4, STREAM>(p + 1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-        } else {
-            const ad_u32x4 a = __builtin_nontemporal_load(
-                reinterpret_cast<const ad_u32x4 *>((const uint16_t *)base + e));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = __uint_as_float(a[i] << 16);
-                x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
-            }
-        }
+        for (int i = 0; i < 4; ++i) x.w[i] = a[i], x.w[4 + i] = b[i];
     } else {
+        AD_GLOBAL const ad_u32x4 *p = (AD_GLOBAL const ad_u32x4 *)elements<const uint16_t>(base, first);
+        const ad_u32x4 a = load_vector<ad_u32x4, STREAM>(p);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            x[i] = 0.f;
-            if (i < left)
-                x[i] = DT == DLCX_F32 ? ((const float *)base)[e + i]
-                                      : __uint_as_float((uint32_t)((const uint16_t *)base)[e + i] << 16);
-        }
+        for (int i = 0; i < 4; ++i) x.w[i] = a[i];
+    }
+    return x;
+}
+template <int DT>
+__device__ __forceinline__ Raw<DT> load_part(const void *base, int64_t first, int left) {
+    Raw<DT> x;
+    if constexpr (DT == DLCX_F32) {
+        AD_GLOBAL const uint32_t *p = elements<const uint32_t>(base, first);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x.w[i] = i < left ? p[i] : 0u;
+    } else {
+        AD_GLOBAL const uint16_t *p = elements<const uint16_t>(base, first);
+#pragma unroll
+        for (int i = 0; i < kVec; i += 2)
+            x.w[i / 2] = (i < left ? p[i] : 0u) | (i + 1 < left ? (uint32_t)p[i + 1] << 16 : 0u);
+    }
+    return x;
+}
+template <int DT>
+__device__ __forceinline__ void unpack(const Raw<DT> &r, float (&x)[kVec]) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        if constexpr (DT == DLCX_F32)
+            x[i] = __uint_as_float(r.w[i]);
+        else
+            x[i] = __uint_as_float(i & 1 ? r.w[i / 2] & 0xFFFF0000u : r.w[i / 2] << 16);
     }
 }
 template <int DT>
-__device__ __forceinline__ void store_floats(void *base, int64_t e, int left, const float (&x)[kVec]) {
+__device__ __forceinline__ void store_floats(void *base, int64_t first, int left, const float (&x)[kVec]) {
     uint32_t b[4];
     if constexpr (DT != DLCX_F32) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) b[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
     }
+    AD_GLOBAL float *f = elements<float>(base, first);
+    AD_GLOBAL uint16_t *h = elements<uint16_t>(base, first);
     if (left >= kVec) {
         if constexpr (DT == DLCX_F32) {
-            ad_f32x4 *p = reinterpret_cast<ad_f32x4 *>((float *)base + e);
+            AD_GLOBAL ad_f32x4 *p = (AD_GLOBAL ad_f32x4 *)f;
             const ad_f32x4 lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
             __builtin_nontemporal_store(lo, p);
             __builtin_nontemporal_store(hi, p + 1);
         } else {
             const ad_u32x4 w = {b[0], b[1], b[2], b[3]};
-            __builtin_nontemporal_store(w, reinterpret_cast<ad_u32x4 *>((uint16_t *)base + e));
+            __builtin_nontemporal_store(w, (AD_GLOBAL ad_u32x4 *)h);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
             if (i < left) {
                 if constexpr (DT == DLCX_F32)
-                    ((float *)base)[e + i] = x[i];
+                    f[i] = x[i];
                 else
-                    ((uint16_t *)base)[e + i] = (uint16_t)(b[i / 2] >> (16 * (i & 1)));
+                    h[i] = (uint16_t)(b[i / 2] >> (16 * (i & 1)));
             }
     }
 }
-__device__ __forceinline__ ad_u32x2 load_codes(const void *base, int64_t e, int left) {
-    if (left >= kVec)
-        return __builtin_nontemporal_load(reinterpret_cast<const ad_u32x2 *>((const uint8_t *)base + e));
+__device__ __forceinline__ ad_u32x2 load_whole_codes(const void *base, int64_t first) {
+    return __builtin_nontemporal_load((AD_GLOBAL const ad_u32x2 *)elements<const uint8_t>(base, first));
+}
+__device__ __forceinline__ ad_u32x2 load_part_codes(const void *base, int64_t first, int left) {
+    AD_GLOBAL const uint8_t *p = elements<const uint8_t>(base, first);
     ad_u32x2 w = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
-        if (i < left) w[i / 4] |= (uint32_t)((const uint8_t *)base)[e + i] << (8 * (i & 3));
+        if (i < left) w[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
     return w;
 }
-__device__ __forceinline__ void store_codes(void *base, int64_t e, int left, ad_u32x2 w) {
+__device__ __forceinline__ void store_codes(void *base, int64_t first, int left, ad_u32x2 w) {
+    AD_GLOBAL uint8_t *p = elements<uint8_t>(base, first);
     if (left >= kVec) {
-        __builtin_nontemporal_store(w, reinterpret_cast<ad_u32x2 *>((uint8_t *)base + e));
+        __builtin_nontemporal_store(w, (AD_GLOBAL ad_u32x2 *)p);
         return;
     }
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
-        if (i < left) ((uint8_t *)base)[e + i] = (uint8_t)(w[i / 4] >> (8 * (i & 3)));
+        if (i < left) p[i] = (uint8_t)(w[i / 4] >> (8 * (i & 3)));
 }
 
 // ---- 8-bit moments ------------------------------------------------------------------------------
@@ -163,7 +208,7 @@ __device__ __forceinline__ void store_codes(void *base, int64_t e, int left, ad_
 // the value, so values down to 6e-5 of a group's largest m (2.5e-10 of its largest v) keep a code of their
 // own, where a linear code ends at 8e-3 (4e-3).
 __device__ __forceinline__ float decode_m(uint32_t w, int i, float scale) {
-    const float c = (float)(((w ^ 0x80808080u) >> (8 * i)) & 0xFFu) - 128.f;
+    const float c = (float)(int8_t)(w >> (8 * i));
     return c * fabsf(c) * scale;
 }
 __device__ __forceinline__ float decode_v(uint32_t w, int i, float scale) {
@@ -183,17 +228,27 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
 // below 2^-100 gives scale 0 and codes 0, as the quantiser of the payloads does.
 __device__ __forceinline__ float group_scale(float amax, float top, float *inv) {
     const bool none = amax < 0x1p-100f;
-    *inv = none ? 0.f : top * top / amax;
-    return none ? 0.f : amax * (1.f / (top * top));
+    const float scale = none ? 0.f : amax * (1.f / (top * top));
+    *inv = none ? 0.f : __builtin_amdgcn_rcpf(scale);
+    return scale;
 }
 // The code of x >= 0 is the integer next to sqrt(x / scale), both operations rounded correctly, where x of a
-// second moment is a correctly rounded root itself.  With IEEE quotients and roots throughout the step
-// was bound by arithmetic (4.2 TB/s, now 4.8); so a code is taken from a product and the
-// hardware's roots (1 unit in the last place), together off by less than 8e-5 codes, and where one of a
-// thread's lies within 1e-4 of the middle between two codes, all of them are decided by the definition.
+// second moment is a correctly rounded root itself.  With IEEE quotients and roots throughout the step was bound
+// by its arithmetic (4.2 TB/s; it still takes 55 vector instructions an element, nine tenths of the time that
+// 5.8 TB/s leave).  So a code is taken from a product and the hardware's roots and reciprocals (1 unit in the
+// last place), together off by 1e-4 codes at most, and only where that lies within 1.25e-4 of the middle between
+// two codes is it decided by the definition: one code in 4000, hardly ever two of a thread's sixteen.
 __device__ __forceinline__ float near_root(float x, float inv) { return __builtin_amdgcn_sqrtf(x * inv); }
 __device__ __forceinline__ float from_middle(float root) { return fabsf(__builtin_amdgcn_fractf(root) - 0.5f); }
 __device__ __forceinline__ float exact_code(float x, float scale) { return rintf(sqrtf(x / scale)); }
+constexpr float kUndecided = 1.25e-4f;
+// (the conversion rounds to the nearest, to even codes from the middle)
+__device__ __forceinline__ void put_m(ad_u32x2 &w, int i, float root, float m) {
+    w[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(copysignf(fminf(root, kTopM), m) + 128.f, i & 3, w[i / 4]);
+}
+__device__ __forceinline__ void put_v(ad_u32x2 &w, int i, float root, float v) {
+    w[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(v > 0.f ? fmaxf(root, 1.f) : 0.f, i & 3, w[i / 4]);
+}
 // Below this a group's largest v may have company whose hardware root is flushed to zero and whose code is not 1.
 constexpr float kTinyV = 0x1p-89f;
 
@@ -207,22 +262,46 @@ __device__ __forceinline__ float weighted_sum(float x, float a, float y, float b
 
 template <int PDT, int GDT, int BITS>
 __device__ __forceinline__ void adamw_elements(const dlcx_tensor &t, const AdamwStep &s, float gs,
-                                               float decay, float rate, int64_t e, int left) {
+                                               float decay, float rate, int64_t first, int left) {
     float p[kVec], g[kVec], m[kVec], v[kVec];
     float m_scale = 0.f, v_scale = 0.f;
     ad_u32x2 mc = {0u, 0u}, vc = {0u, 0u};
-    const int64_t group = e / kStateGroup;
-    if (BITS == 8 && left > 0) {
-        mc = load_codes(t.m, e, left);
-        vc = load_codes(t.v, e, left);
-        m_scale = t.m_scale[group];
-        v_scale = t.v_scale[group];
+    const unsigned mine = threadIdx.x / (kStateGroup / kVec);
+    AD_GLOBAL float *const m_scales = (AD_GLOBAL float *)t.m_scale + first / kStateGroup;
+    AD_GLOBAL float *const v_scales = (AD_GLOBAL float *)t.v_scale + first / kStateGroup;
+    Raw<PDT> rp;
+    Raw<GDT> rg;
+    Raw<DLCX_F32> rm, rv;
+    if (left >= kVec) {
+        if constexpr (BITS == 8) {
+            mc = load_whole_codes(t.m, first);
+            vc = load_whole_codes(t.v, first);
+            m_scale = m_scales[mine];
+            v_scale = v_scales[mine];
+        } else {
+            rm = load_whole<DLCX_F32, BITS == 8>(t.m, first);
+            rv = load_whole<DLCX_F32, BITS == 8>(t.v, first);
+        }
+        rp = load_whole<PDT, BITS == 8>(t.param, first);
+        rg = load_whole<GDT, BITS == 8>(t.grad, first);
+    } else {
+        if constexpr (BITS == 8) {
+            mc = load_part_codes(t.m, first, left);
+            vc = load_part_codes(t.v, first, left);
+            m_scale = left > 0 ? m_scales[mine] : 0.f;
+            v_scale = left > 0 ? v_scales[mine] : 0.f;
+        } else {
+            rm = load_part<DLCX_F32>(t.m, first, left);
+            rv = load_part<DLCX_F32>(t.v, first, left);
+        }
+        rp = load_part<PDT>(t.param, first, left);
+        rg = load_part<GDT>(t.grad, first, left);
     }
-    load_floats<PDT>(t.param, e, left, p);
-    load_floats<GDT>(t.grad, e, left, g);
+    unpack(rp, p);
+    unpack(rg, g);
     if constexpr (BITS == 32) {
-        load_floats<DLCX_F32>(t.m, e, left, m);
-        load_floats<DLCX_F32>(t.v, e, left, v);
+        unpack(rm, m);
+        unpack(rv, v);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
@@ -240,7 +319,7 @@ __device__ __forceinline__ void adamw_elements(const dlcx_tensor &t, const Adamw
             p[i] = p[i] * decay - rate * (m[i] / (sqrtf(v[i]) * s.inv_sqrt_bc2 + s.eps));
         } else {
             // (a v that the hardware's root would flush counts as the smallest one that it does not)
-            root[i] = __builtin_amdgcn_sqrtf(fmaxf(v[i], 0x1p-126f));
+            root[i] = __builtin_amdgcn_sqrtf(__uint_as_float(max(__float_as_uint(v[i]), 0x00800000u)));
             p[i] = p[i] * decay - rate * (m[i] * __builtin_amdgcn_rcpf(root[i] * s.inv_sqrt_bc2 + s.eps));
         }
     }
@@ -249,50 +328,57 @@ __device__ __forceinline__ void adamw_elements(const dlcx_tensor &t, const Adamw
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             am = max(am, __float_as_uint(m[i]) & 0x7FFFFFFFu);
-            av = max(av, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+            av = max(av, __float_as_uint(v[i]));  // (v >= 0 or a NaN, whose sign makes it the larger)
         }
         float m_inv, v_inv;
         const float v_max = __uint_as_float(row_max(av));
         m_scale = group_scale(__uint_as_float(row_max(am)), kTopM, &m_inv);
         v_scale = group_scale(sqrtf(v_max), kTopV, &v_inv);
-        float cm[kVec], cv[kVec], closest = v_max < kTinyV ? 0.f : 1.f;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            cm[i] = near_root(fabsf(m[i]), m_inv);
-            cv[i] = near_root(root[i], v_inv);
-            closest = fminf(closest, fminf(from_middle(cm[i]), from_middle(cv[i])));
-        }
-        if (closest < 1e-4f) {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                cm[i] = m_scale > 0.f ? exact_code(fabsf(m[i]), m_scale) : 0.f;
-                cv[i] = v_scale > 0.f ? exact_code(sqrtf(v[i]), v_scale) : 0.f;
-            }
-        }
+        float m_closest = 1.f, v_closest = 1.f;
         mc = vc = ad_u32x2{0u, 0u};
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const float c = copysignf(fminf(cm[i], kTopM), m[i]) + 128.f;
-            mc[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(rintf(c), i & 3, mc[i / 4]);
-            vc[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(rintf(v[i] > 0.f ? fmaxf(cv[i], 1.f) : 0.f), i & 3, vc[i / 4]);
+            const float cm = near_root(fabsf(m[i]), m_inv), cv = near_root(root[i], v_inv);
+            m_closest = fminf(m_closest, from_middle(cm));
+            v_closest = fminf(v_closest, from_middle(cv));
+            put_m(mc, i, cm, m[i]);
+            put_v(vc, i, cv, v[i]);
+        }
+        if (m_closest < kUndecided) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (from_middle(near_root(fabsf(m[i]), m_inv)) < kUndecided)
+                    put_m(mc, i, m_scale > 0.f ? exact_code(fabsf(m[i]), m_scale) : 0.f, m[i]);
+        }
+        const bool tiny = v_max < kTinyV;
+        if (v_closest < kUndecided || tiny) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (from_middle(near_root(root[i], v_inv)) < kUndecided || tiny)
+                    put_v(vc, i, v_scale > 0.f ? exact_code(sqrtf(v[i]), v_scale) : 0.f, v[i]);
         }
         mc ^= 0x80808080u;
         if (left > 0) {
-            store_codes(t.m, e, left, mc);
-            store_codes(t.v, e, left, vc);
+            store_codes(t.m, first, left, mc);
+            store_codes(t.v, first, left, vc);
             if (threadIdx.x % (kStateGroup / kVec) == 0) {
-                t.m_scale[group] = m_scale;
-                t.v_scale[group] = v_scale;
+                m_scales[mine] = m_scale;
+                v_scales[mine] = v_scale;
             }
         }
     } else {
-        store_floats<DLCX_F32>(t.m, e, left, m);
-        store_floats<DLCX_F32>(t.v, e, left, v);
+        store_floats<DLCX_F32>(t.m, first, left, m);
+        store_floats<DLCX_F32>(t.v, first, left, v);
     }
-    store_floats<PDT>(t.param, e, left, p);
-    if (PDT == DLCX_F32 && t.copy != nullptr) store_floats<DLCX_BF16>(t.copy, e, left, p);
+    store_floats<PDT>(t.param, first, left, p);
+    if (PDT == DLCX_F32 && t.copy != nullptr) store_floats<DLCX_BF16>(t.copy, first, left, p);
 }
 
+// A workgroup has 1 / PARTS of a block: with 32-bit moments one step, 264 us for the 50 M elements against 274 with
+// two, one after the other; with 8-bit ones two, 1.47 ms against 1.54, since what every thread does before its
+// first element is worth the arithmetic of one.  A table with both kinds takes two launches.
+constexpr int kParts32 = 2, kParts8 = 1;
+template <int BITS, int PARTS>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(TableView tv, int count, int64_t blocks,
                                                          AdamwStep s) {
     float gs = s.grad_scale;
@@ -301,48 +387,53 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(TableView tv, int count
         if (!(fabsf(norm) < __builtin_inff())) return;
         if (norm > s.max_norm) gs *= s.max_norm / norm;
     }
-    const int64_t block = (int64_t)blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
+    const int64_t part = (int64_t)blockIdx.x + (int64_t)blockIdx.y * gridDim.x, block = part / PARTS;
     if (block >= blocks) return;
     const int which = find_tensor(tv.start, count, (int)block);
     const dlcx_tensor t = tv.tensor[which];
+    if ((t.state_bits == 8) != (BITS == 8)) return;
     const float decay = (float)(1.0 - s.lr * (double)t.lr_scale * (double)t.weight_decay);
     const float rate = (float)(s.lr_bc1 * (double)t.lr_scale);
-    const int64_t first = (block - tv.start[which]) * kBlock, numel = t.numel;
-    const int kind = t.param_dtype + 2 * t.grad_dtype + (t.state_bits == 8 ? 4 : 0);
-#define DLCX_ADAMW_KIND(P, G, B)                                                               \
-    for (int u = 0; u < kBlock / kStep; ++u) {                                                 \
-        const int64_t e = first + u * kStep + threadIdx.x * kVec;                              \
-        const int64_t rest = numel - e;                                                        \
-        adamw_elements<P, G, B>(t, s, gs, decay, rate, e, rest > kVec ? kVec : (int)rest);     \
-    }                                                                                          \
-    break
-    switch (kind) {
-    case 0: DLCX_ADAMW_KIND(DLCX_F32, DLCX_F32, 32);
-    case 1: DLCX_ADAMW_KIND(DLCX_BF16, DLCX_F32, 32);
-    case 2: DLCX_ADAMW_KIND(DLCX_F32, DLCX_BF16, 32);
-    case 3: DLCX_ADAMW_KIND(DLCX_BF16, DLCX_BF16, 32);
-    case 4: DLCX_ADAMW_KIND(DLCX_F32, DLCX_F32, 8);
-    case 5: DLCX_ADAMW_KIND(DLCX_BF16, DLCX_F32, 8);
-    case 6: DLCX_ADAMW_KIND(DLCX_F32, DLCX_BF16, 8);
-    default: DLCX_ADAMW_KIND(DLCX_BF16, DLCX_BF16, 8);
+    int64_t first = (block - tv.start[which]) * kBlock + (int)(part % PARTS) * (kBlock / PARTS);
+#pragma unroll 1
+    for (int u = 0; u < kBlock / kStep / PARTS; ++u, first += kStep) {
+        const int64_t rest = t.numel - first;
+        const int left = (rest > kStep ? kStep : (int)rest) - (int)threadIdx.x * kVec;
+        if (t.param_dtype == DLCX_F32) {
+            if (t.grad_dtype == DLCX_F32)
+                adamw_elements<DLCX_F32, DLCX_F32, BITS>(t, s, gs, decay, rate, first, left);
+            else
+                adamw_elements<DLCX_F32, DLCX_BF16, BITS>(t, s, gs, decay, rate, first, left);
+        } else {
+            if (t.grad_dtype == DLCX_F32)
+                adamw_elements<DLCX_BF16, DLCX_F32, BITS>(t, s, gs, decay, rate, first, left);
+            else
+                adamw_elements<DLCX_BF16, DLCX_BF16, BITS>(t, s, gs, decay, rate, first, left);
+        }
     }
-#undef DLCX_ADAMW_KIND
 }
 
 // ---- global norm --------------------------------------------------------------------------------
 // fp64 throughout: a square of fp32 has room there at any size, and the order of the sum no weight.
 template <int DT>
 __device__ __forceinline__ double sum_squares(const void *grad, int64_t first, int64_t numel, double acc) {
-    float x[kBlock / kStep][kVec];
+    constexpr int kSteps = kBlock / kStep;
+    Raw<DT> r[kSteps];
+    if (numel - first >= kBlock) {
 #pragma unroll
-    for (int u = 0; u < kBlock / kStep; ++u) {
-        const int64_t e = first + u * kStep + threadIdx.x * kVec, rest = numel - e;
-        load_floats<DT>(grad, e, rest > kVec ? kVec : (int)(rest < 0 ? 0 : rest), x[u]);
+        for (int u = 0; u < kSteps; ++u) r[u] = load_whole<DT>(grad, first + u * kStep);
+    } else {
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u)
+            r[u] = load_part<DT>(grad, first + u * kStep, (int)(numel - first) - u * kStep - (int)threadIdx.x * kVec);
     }
 #pragma unroll
-    for (int u = 0; u < kBlock / kStep; ++u)
+    for (int u = 0; u < kSteps; ++u) {
+        float x[kVec];
+        unpack(r[u], x);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) acc = fma((double)x[u][i], (double)x[u][i], acc);
+        for (int i = 0; i < kVec; ++i) acc = fma((double)x[i], (double)x[i], acc);
+    }
     return acc;
 }
 
@@ -385,16 +476,16 @@ __global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double *__r
 template <int SECOND, int DT>
 __global__ __launch_bounds__(kThreads) void state_decode_kernel(const void *codes, const float *scales,
                                                                 int64_t numel, void *out) {
-    const int64_t e = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * kVec, rest = numel - e;
-    if (rest <= 0) return;
-    const int left = rest > kVec ? kVec : (int)rest;
-    const ad_u32x2 w = load_codes(codes, e, left);
-    const float scale = scales[e / kStateGroup];
+    const int64_t first = (int64_t)blockIdx.x * kStep, rest = numel - first;
+    const int left = (rest > kStep ? kStep : (int)rest) - (int)threadIdx.x * kVec;
+    if (left <= 0) return;
+    const ad_u32x2 w = left >= kVec ? load_whole_codes(codes, first) : load_part_codes(codes, first, left);
+    const float scale = (scales + first / kStateGroup)[threadIdx.x / (kStateGroup / kVec)];
     float x[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
         x[i] = SECOND ? decode_v(w[i / 4], i & 3, scale) : decode_m(w[i / 4], i & 3, scale);
-    store_floats<DT>(out, e, left, x);
+    store_floats<DT>(out, first, left, x);
 }
 
 // ---- launches -----------------------------------------------------------------------------------
@@ -402,16 +493,19 @@ int launch_tensor_table(const dlcx_tensor *t, int count, void *memory, dlcx_tabl
                         hipStream_t st) {
     const TableView v = table_view(memory, count);
     int64_t blocks = 0;
-    int steps = 1;
+    int steps = kComplete;
+    bool complete = true;
     for (int i = 0; i < count; ++i) {
         blocks += ceil_div(t[i].numel, kBlock);
         if (blocks > 0x7FFFFFFF) return DLCX_EINVAL;
-        if (t[i].numel > 0 && t[i].param == nullptr) steps = 0;
+        if (t[i].numel == 0) continue;
+        if (t[i].param == nullptr) complete = false;
+        steps |= t[i].state_bits == 8 ? kHas8 : kHas32;
     }
     table->memory = memory;
     table->blocks = blocks;
     table->count = count;
-    table->steps = steps;
+    table->steps = complete ? steps : 0;
     TablePart part;
     int64_t at = 0;
     for (int i = 0; i < count; i += kTablePart) {
@@ -442,12 +536,17 @@ int launch_grad_norm(const dlcx_table &table, double grad_scale, float *norm_out
     return check_launch("grad_norm");
 }
 
+template <int BITS, int PARTS>
+static void launch_adamw_bits(const dlcx_table &table, const AdamwStep &step, hipStream_t st) {
+    const int64_t parts = table.blocks * PARTS, gx = parts < (1 << 20) ? parts : (1 << 20);
+    adamw_kernel<BITS, PARTS><<<dim3((unsigned)gx, (unsigned)ceil_div(parts, gx)), kThreads, 0, st>>>(
+        table_view(table.memory, table.count), table.count, table.blocks, step);
+}
 int launch_adamw(const dlcx_table &table, const AdamwStep &step, hipStream_t st) {
     if (table.blocks == 0) return DLCX_OK;
-    const int64_t gx = table.blocks < (1 << 20) ? table.blocks : (1 << 20);
     Timed timed(KID_ADAMW, st);
-    adamw_kernel<<<dim3((unsigned)gx, (unsigned)ceil_div(table.blocks, gx)), kThreads, 0, st>>>(
-        table_view(table.memory, table.count), table.count, table.blocks, step);
+    if (table.steps & kHas32) launch_adamw_bits<32, kParts32>(table, step, st);
+    if (table.steps & kHas8) launch_adamw_bits<8, kParts8>(table, step, st);
     return check_launch("adamw");
 }
 

@@ -5,6 +5,7 @@ rounding of 2^-8.  A code of 8 bits is at most half a code from the root it stan
 for the arithmetic that leads there (255 times a dozen roundings)."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -214,6 +215,30 @@ def test_moments_of_8_bits_at_their_edges():
     keep = torch.ones(n, dtype=torch.bool)
     keep[3 * G + 7] = False
     assert torch.isfinite(dev["param"].cpu()[keep]).all()
+
+
+@pytest.mark.parametrize("size", [1e-3, 1e-15, 1e-18, 1e12])
+def test_codes_are_those_of_the_formula_to_the_last(size):
+    """Every operation on the way to a code is one of fp32, rounded correctly: the codes of a step are those of
+    the formula, also where a root is next to the middle of two of them (among 2^20 some hundreds are).
+    (The roots here are numpy's: torch's on the CPU is not always the one next to the true root.)"""
+    def root(x):
+        return torch.from_numpy(np.sqrt(x.numpy()))
+
+    t = make(1 << 20, torch.bfloat16, torch.bfloat16, 8, 5, size=size)
+    dev = to_gpu([t])[0]
+    dlcx.dlcx_adamw(table_of([dev]), step=2, **HYPER)
+    g = t["grad"].float()
+    ms, vs = (t[k].repeat_interleave(G) for k in ("m_scale", "v_scale"))
+    m, v = t["m"].float(), t["v"].float()
+    m, v = m * m.abs() * ms, v * v * vs
+    m = m * HYPER["beta1"] + g * (1 - HYPER["beta1"])
+    v = v * v * HYPER["beta2"] + g * g * (1 - HYPER["beta2"])
+    for name, x, top, least in (("m", m, 127, 0), ("v", root(v), 255, 1)):
+        scale = x.abs().view(-1, G).amax(1) * (1.0 / top ** 2)
+        code = root(x.abs() / scale.repeat_interleave(G)).round().clamp(min=least) * x.sign()
+        assert torch.equal(dev[name + "_scale"].cpu(), scale), name
+        assert torch.equal(dev[name].cpu().float(), code), (name, (dev[name].cpu().float() != code).sum())
 
 
 @pytest.mark.parametrize("second", [False, True])
