@@ -743,6 +743,89 @@ __global__ __launch_bounds__(256) void adapter_rows_kernel(RowsArgs a) {
     }
 }
 
+// The same in one launch: every workgroup forms all of h for itself, its wavefronts the columns of h in turn (or,
+// where those are fewer, shares of n), before its own kRowCols columns of y.
+struct RowArgs {
+    const void *x, *q;
+    uint32_t pitch;
+    int n;
+};
+constexpr int kRowWaves = 16, kRowParts = 8, kRowCols = kRowWaves / kRowParts * 512;
+template <typename T, bool VEC>  // (not VEC and fewer than eight: those that there are)
+__device__ __forceinline__ typename T::Frag load_row8(const typename T::elem *row, int at, int len) {
+    if (!VEC && len < 8) return T::template load8<false, false>(row, at, len);
+    return T::template load8<VEC, true>(row, at, len);
+}
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kRowWaves * 64) void adapter_row_kernel(RowArgs d, RowsArgs a) {
+    typedef typename T::elem elem;
+    typedef typename T::Frag Frag;
+    __shared__ float part[DLCX_MAX_RANK], h[DLCX_MAX_RANK], sums[kRowParts][kRowCols];
+    const int t = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x / 64, id = a.ids[t];
+    const int adapter = id >= 0 && id < a.count ? id : -1;
+    const int rank = adapter_rank(adapter, a.ranks, a.r);
+    const elem *q = (const elem *)d.q + (int64_t)max(adapter, 0) * a.r * d.n;
+    const elem *p = (const elem *)a.f + (int64_t)max(adapter, 0) * a.r * a.len;
+    // what y needs is requested first: it does not depend on h
+    const int col = blockIdx.x * kRowCols + (int)threadIdx.x, c0 = wave % kRowParts;
+    // eight columns of y a lane; where fewer are left, the last eight, which others have too
+    const int j0 = blockIdx.x * kRowCols + wave / kRowParts * 512 + lane * 8, j = min(j0, max(a.len - 8, 0));
+    auto load_p = [&](int c) { return load_row8<T, VEC>(p + (int64_t)c * a.len, j, a.len); };
+    const float y_in = a.y_in && col < a.len ? T::value(row_at<elem>(a.y_in, t, a.pitch_in)[col]) : 0.f;
+    Frag w = rank > c0 ? load_p(c0) : T::zero();
+
+    const elem *x = row_at<elem>(d.x, t, d.pitch);
+    const int shares = rank > 0 && rank < kRowWaves ? kRowWaves / rank : 1;
+    const int share = (d.n + shares * 512 - 1) / (shares * 512) * 512;
+    for (int k = wave; k < rank * shares; k += kRowWaves) {
+        const int from = k % shares * share, to = min(from + share, d.n);
+        const elem *row = q + (int64_t)(k / shares) * d.n;
+        float acc = 0.f;
+#pragma unroll 4
+        for (int i = from + lane * 8; i < to; i += 512) {
+            const int at = VEC ? i : min(i, max(d.n - 8, 0));
+            Frag u = load_row8<T, VEC>(row, at, d.n), v = load_row8<T, VEC>(x, at, d.n);
+            if (!VEC && at < i) {
+                T::drop(u, i - at);
+                T::drop(v, i - at);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc = fmaf(T::at(u, e), T::at(v, e), acc);
+        }
+        for (int e = 32; e > 0; e >>= 1) acc += __shfl_xor(acc, e, 64);
+        if (lane == 0) part[k] = acc;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < a.r) {
+        const int c = threadIdx.x;
+        float sum = 0.f;
+        if (c < rank)
+            for (int k = 0; k < shares; ++k) sum += part[c * shares + k];
+        if (a.h_out && blockIdx.x == 0) a.h_out[(int64_t)t * a.r + c] = sum;
+        h[c] = sum * (adapter >= 0 && a.scale ? a.scale[adapter] : 1.f);
+    }
+    __syncthreads();
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int c = c0; c < rank; c += kRowParts) {
+        const Frag next = c + kRowParts < rank ? load_p(c + kRowParts) : T::zero();
+        const float s = h[c];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += s * T::at(w, i);
+        w = next;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = (VEC ? j0 : j) + i - (int)blockIdx.x * kRowCols;
+        if (VEC || at >= 0) sums[c0][at] = acc[i];
+    }
+    __syncthreads();
+    if (col >= a.len) return;
+    float y = 0.f;
+#pragma unroll
+    for (int k = 0; k < kRowParts; ++k) y += sums[k][threadIdx.x];
+    const_cast<elem *>(row_at<elem>(a.y_out, t, a.pitch_out))[col] = T::round(y + y_in);
+}
+
 // ---- grad -------------------------------------------------------------------------------------------
 struct GradProduct {
     const void *u;       // turned operand
@@ -964,6 +1047,16 @@ static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st)
 // 64 rows 8.4 / 18.8, 256 rows 19.9 / 19.9, rank 64 64 rows 15.6 / 21.9, 128 rows 26 / 22.5, rank 256 16 rows
 // 20.8 / 28.6, 64 rows 47 / 39.
 static bool few_rows(int64_t rows, int r) { return rows * r <= 4096; }
+// Few rows in one launch, where forming h in every workgroup costs less than a second launch: Q_a up to 300 KB, read by all
+// workgroups together up to 20 MB, and not more of them than the GPU holds at once.  us alone on the GPU and called from
+// the host, in two launches -> one: 1 row of 2048 + 2048 columns at rank 8: 6.6, 13 -> 4.6, 10; 128 rows of 64 adapters
+// of the same 7.7, 15 -> 5.5, 10; 8192 + 8192 at rank 16, 1 row 7.5, 13 -> 7.5, 9.  Beyond: 16 rows there (33 MB) 8.1, 13
+// -> 11.2, 11; rank 64 there (1 MB), 1 row 10.5, 14 -> 20, 20; 512 rows of the first (1024 workgroups) 10.3, 13 -> 15.1, 15.
+template <typename T>
+static bool one_launch(int64_t rows, int r, int64_t n, int64_t m) {
+    const int64_t bytes = r * n * (int64_t)sizeof(typename T::elem), groups = rows * ceil_div(m, kRowCols);
+    return bytes <= 300000 && groups <= 512 && groups * bytes <= 20000000;
+}
 
 template <typename T>
 static int launch_operands(const OperandArgs &a, int jobs, int64_t rows, const Route &v, hipStream_t st) {
@@ -1089,6 +1182,16 @@ static int down_and_rows(const DownArgs &down, RowsArgs a, int64_t rows, Operand
     DownArgs d = down;
     d.stride = rows * d.r;
     d.out = s.split;
+    if (!operands && one_launch<T>(rows, d.r, d.len, a.len)) {
+        const RowArgs x = {d.x, d.f, d.pitch, d.len};
+        const bool vec = aligned16(d.x) && aligned16(d.f) && aligned16(a.f) && d.pitch % 16 == 0 && d.len % 8 == 0 &&
+                         a.len % 8 == 0;
+        const dim3 grid((unsigned)ceil_div(a.len, kRowCols), (unsigned)rows);
+        Timed timed(KID_ADAPTER_ROWS, st);
+        if (vec) adapter_row_kernel<T, true><<<grid, kRowWaves * 64, 0, st>>>(x, a);
+        else adapter_row_kernel<T, false><<<grid, kRowWaves * 64, 0, st>>>(x, a);
+        return check_launch("adapter_rows");
+    }
     const Route by_row = {nullptr, nullptr, a.count, a.ids};
     int rc = launch_down<T>(d, rows, by_row, st);
     if (rc != DLCX_OK) return rc;

@@ -167,6 +167,22 @@ def test_adapters_and_their_gradient_against_64_bits(case, dtype):
     check(Case(dtype=dtype, **case))
 
 
+FEW = [(1, 2048, 2048, 8, 3), (1, 1, 1, 1, 1), (3, 5, 7, 2, 2), (2, 7, 1000, 5, 4), (2, 1025, 513, 17, 9), (40, 1023, 8, 100, 5),
+       (7, 1030, 2049, 33, 2), (1, 512, 4097, 16, 1), (9, 2047, 515, 256, 3),  # one launch
+       (5, 4096, 8192, 64, 4), (600, 333, 65, 6, 64), (20, 4101, 8191, 8, 7)]  # two (the last: in fp32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,m,n,r,count", FEW)
+@pytest.mark.parametrize("pad,shift", [(0, 0), (8, 0), (3, 1)])
+def test_few_rows_at_the_edges_of_their_forms(rows, m, n, r, count, dtype, pad, shift):
+    c = Case(rows, m, n, r, count, dtype, ranks=count > 2, seed=m, pad=pad, shift=shift)
+    want = c.oracle()
+    y, h = c.forward()
+    inside(h, want["h"], "h")
+    inside(y, want["y"], "y")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_routes_and_workspaces_serve_what_they_promise(dtype):
     c = Case(700, 264, 520, 24, 6, dtype, ranks=True)
