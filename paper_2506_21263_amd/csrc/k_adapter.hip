@@ -206,6 +206,18 @@ __device__ __forceinline__ ab_u32x4 load_any(const void *p) {
     return w;
 }
 
+// How rows are read and written: element by element where they begin anywhere, by 16 aligned bytes, or by these and past
+// the caches' order of use, for matrices of kStreamed bytes and more that pass by once.  A backward pass beside
+// 8192 + 8192 columns at rank 64, plain -> streamed, us: 16384 rows (268 MB a matrix) 339 -> 327 (down 73 -> 69, up 103 ->
+// 112, grad 146 -> 133: more of the rows of one product is in the cache for the next), 2000 rows (33 MB) 79 -> 77, 515
+// rows (8 MB) 56 -> 58; 4133 rows forward 76 -> 68.
+constexpr int kAnywhere = 0, kAligned = 1, kStream = 2;
+constexpr int64_t kStreamed = 24000000;
+template <bool STREAM>
+__device__ __forceinline__ ab_u32x4 load_vector(const void *p) {
+    const ab_u32x4 *v = reinterpret_cast<const ab_u32x4 *>(p);
+    return STREAM ? __builtin_nontemporal_load(v) : *v;
+}
 struct Bf16 {
     static constexpr int lane = 8;  // elements of 16 bytes
     typedef uint16_t elem;
@@ -218,9 +230,9 @@ struct Bf16 {
                                                        __builtin_bit_cast(ab_bf16x8, b.w), c, 0, 0, 0);
     }
     // elements k .. k + 7 of a row of `len`; ALL: all of them are there
-    template <bool VEC, bool ALL = false>
+    template <bool VEC, bool ALL = false, bool STREAM = false>
     static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
-        if constexpr (ALL && VEC) return {*reinterpret_cast<const ab_u32x4 *>(row + k)};
+        if constexpr (ALL && VEC) return {load_vector<STREAM>(row + k)};
         if constexpr (ALL) return {load_any(row + k)};
         Frag f = zero();
         if constexpr (VEC) {
@@ -279,12 +291,12 @@ struct F32 {
         for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[j], b.x[j], c, 0, 0, 0);
         return c;
     }
-    template <bool VEC, bool ALL = false>
+    template <bool VEC, bool ALL = false, bool STREAM = false>
     static __device__ __forceinline__ Frag load8(const elem *row, int k, int len) {
         Frag f = zero();
         if (ALL || (VEC && k < len)) {
-            const ab_u32x4 a = VEC ? *reinterpret_cast<const ab_u32x4 *>(row + k) : load_any(row + k);
-            const ab_u32x4 b = VEC ? *reinterpret_cast<const ab_u32x4 *>(row + k + 4) : load_any(row + k + 4);
+            const ab_u32x4 a = VEC ? load_vector<STREAM>(row + k) : load_any(row + k);
+            const ab_u32x4 b = VEC ? load_vector<STREAM>(row + k + 4) : load_any(row + k + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) f.x[i] = __uint_as_float(a[i]), f.x[4 + i] = __uint_as_float(b[i]);
         } else if (!VEC) {
@@ -318,9 +330,9 @@ template <typename T>
 __device__ __forceinline__ int column_base(int j, int len) {
     return len >= T::lane ? min(j, len - T::lane) : j;
 }
-template <typename T, bool VEC>
+template <typename T, int VEC>
 __device__ __forceinline__ ab_u32x4 load16(const typename T::elem *row, int base, int len) {
-    if constexpr (VEC) return *reinterpret_cast<const ab_u32x4 *>(row + base);
+    if constexpr (VEC) return load_vector<VEC == kStream>(row + base);
     if (len >= T::lane) return load_any(row + base);
     ab_u32x4 w = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -333,11 +345,12 @@ __device__ __forceinline__ ab_u32x4 load16(const typename T::elem *row, int base
         }
     return w;
 }
-template <typename T, bool VEC>
+template <typename T, int VEC>
 __device__ __forceinline__ void store16(typename T::elem *row, const ab_u32x4 &w, int base, int j, int len) {
     if (VEC || j + T::lane <= len) {
         if (j >= len) return;
-        if constexpr (VEC) *reinterpret_cast<ab_u32x4 *>(row + base) = w;
+        if constexpr (VEC == kStream) __builtin_nontemporal_store(w, reinterpret_cast<ab_u32x4 *>(row + base));
+        else if constexpr (VEC) *reinterpret_cast<ab_u32x4 *>(row + base) = w;
         else __builtin_memcpy(row + base, &w, sizeof w);
         return;
     }
@@ -395,14 +408,39 @@ struct DownArgs {
 // at a time; the eight sums are joined in LDS, in turn in two places, so that one barrier a round is enough.
 // With whole rows to a workgroup instead, the factor comes from L2 as often as there are tiles of
 // rows, by the same few channels at a time: 91 us for 16384 x 8192 bf16 at rank 64, 88 us for 4133 rows.
-// This form: 74 us (3.6 TB/s of rows, and 34 MB of shares) and 27 us.  The stream of rows alone, in this pattern,
-// takes 62 of the 74; the products and the join 6 each.
+// This form: 69 us (3.9 TB/s of rows, and 34 MB of shares) and 25 us.
+// In bf16 a load has 256 bytes of each of four rows, neighbouring lanes the same row; the four loads of sixteen rows
+// then change places within four lanes, into the layout of the matrix instructions.  With one row to each of 16
+// lanes instead (as fp32 rows are read): 79 and 31 us.
 constexpr int kDownWaves = 8;
 template <typename T>
 constexpr int down_steps(int ct) {  // of 32 elements, per wavefront
     return (ct == 4 ? 4 : 8) * T::lane / 8;
 }
-template <typename T, int CT, bool VEC>
+// Four vectors of 16 bytes in four neighbouring lanes change places: vector s of lane c is vector c of lane s after it.
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad_dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ void exchange(ab_u32x4 &a, ab_u32x4 &b, bool second, ab_u32x4 a_there, ab_u32x4 b_there) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = second ? b_there[i] : a[i];
+        b[i] = second ? b[i] : a_there[i];
+    }
+}
+template <int CTRL>
+__device__ __forceinline__ ab_u32x4 quad_dpp4(const ab_u32x4 &x) {
+    return ab_u32x4{quad_dpp<CTRL>(x[0]), quad_dpp<CTRL>(x[1]), quad_dpp<CTRL>(x[2]), quad_dpp<CTRL>(x[3])};
+}
+__device__ __forceinline__ void transpose_quads(Bf16::Frag (&f)[4]) {
+    const bool one = threadIdx.x & 1, two = threadIdx.x & 2;
+#pragma unroll
+    for (int s = 0; s < 4; s += 2) exchange(f[s].w, f[s + 1].w, one, quad_dpp4<0xB1>(f[s].w), quad_dpp4<0xB1>(f[s + 1].w));
+#pragma unroll
+    for (int s = 0; s < 2; ++s) exchange(f[s].w, f[s + 2].w, two, quad_dpp4<0x4E>(f[s].w), quad_dpp4<0x4E>(f[s + 2].w));
+}
+template <typename T, int CT, int VEC>
 __global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapter_down_kernel(DownArgs a, Route route, int size) {
     constexpr int KS = down_steps<T>(CT);
     typedef typename T::Frag Frag;
@@ -419,25 +457,51 @@ __global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapt
     if (c0 >= rank) return;
     const int k0 = (share * kDownWaves + wave) * KS * 32;
     const bool whole = k0 + KS * 32 <= a.len;
-    // The lane's elements of step s.  Where a row that is not read by 16 aligned bytes ends before them, its last
+    // The lane's elements of step s (with kQuads, after the exchange).  Where a row that is not read by 16 aligned bytes ends before them, its last
     // eight, of which the factor's are zero as far as another lane has them (shorter rows are read by element).
-    auto at = [&](int s) { return k0 + s * 32 + quad * 8; };
+    constexpr bool kQuads = VEC && T::lane == 8;
+    auto at = [&](int s) { return k0 + (kQuads ? s / 4 * 128 + quad * 32 + s % 4 * 8 : s * 32 + quad * 8); };
     auto load = [&](const elem *row, Frag (&f)[KS]) {
         if (whole) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, true>(row, at(s), a.len);
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC != 0, true>(row, at(s), a.len);
         } else if (!VEC && a.len >= 8) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, true>(row, min(at(s), a.len - 8), a.len);
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC != 0, true>(row, min(at(s), a.len - 8), a.len);
         } else {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC, false>(row, at(s), a.len);
+            for (int s = 0; s < KS; ++s) f[s] = T::template load8<VEC != 0, false>(row, at(s), a.len);
         }
     };
     auto index_of = [&](int t0) { return route.ids ? tile.at : order[min(t0 + row16, last)]; };
-    auto load_row = [&](int t, Frag (&x)[KS]) { load(row_at<elem>(a.x, t, a.pitch), x); };
+    auto load_row = [&](int t, Frag (&x)[KS]) {
+        if constexpr (kQuads) {
+            const int k = k0 + quad * 32 + (lane & 3) * 8;
+            const uint32_t n[4] = {quad_dpp<0x00>(t), quad_dpp<0x55>(t), quad_dpp<0xAA>(t), quad_dpp<0xFF>(t)};
+            if (whole) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    x[s] = T::template load8<true, true, VEC == kStream>(row_at<elem>(a.x, n[s % 4], a.pitch), k + s / 4 * 128, a.len);
+            } else {
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    x[s] = T::template load8<VEC != 0, false>(row_at<elem>(a.x, n[s % 4], a.pitch), k + s / 4 * 128, a.len);
+            }
+        } else {
+            load(row_at<elem>(a.x, t, a.pitch), x);
+        }
+    };
     Frag f[CT][KS];
-    auto products = [&](const Frag (&x)[KS], int turn) {
+    auto products = [&](Frag (&x)[KS], int turn) {
+        if constexpr (kQuads) {
+#pragma unroll
+            for (int s = 0; s < KS; s += 4) {
+                Frag y[4] = {x[s], x[s + 1], x[s + 2], x[s + 3]};
+                transpose_quads(y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[s + i] = y[i];
+            }
+        }
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
@@ -574,9 +638,9 @@ struct UpArgs {
 // columns into operand blocks in LDS once; then each wavefront takes 16 rows at a time: lane l has rows
 // 4 (l / 16) + 0 .. 3 and 16 bytes of each, so that 16 lanes make 256 in a row.  (With a row to
 // every lane of 16 an access is 64 pieces for the L1, not 16: 128 us for 16384 x 8192 at rank 64.)  HBM
-// bounds it: 104 us, 5.2 TB/s, what copies of this pattern reach.
+// bounds it: 104 us alone, 5.2 TB/s, what copies of this pattern reach (112 where it leaves grad its rows).
 constexpr int kUpWaves = 4;
-template <typename T, int KT, bool VEC>
+template <typename T, int KT, int VEC>
 struct UpRows {
     ab_u32x4 y[4];
     typename T::Frag h[KT];
@@ -592,7 +656,7 @@ struct UpRows {
                           : ab_u32x4{0u, 0u, 0u, 0u};
     }
 };
-template <typename T, int KT, bool VEC>
+template <typename T, int KT, int VEC>
 __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 ? 3 : 2) void adapter_up_kernel(UpArgs a, Route route, int size) {
     extern __shared__ __attribute__((aligned(16))) char up_lds[];
     typedef typename T::Frag Frag;
@@ -627,7 +691,7 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
         ab_u32x4 rows[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            rows[i] = load16<T, VEC>(f + (int64_t)min(s * 32 + quad * 8 + i, rank - 1) * a.len, j, a.len);
+            rows[i] = load16<T, VEC ? kAligned : kAnywhere>(f + (int64_t)min(s * 32 + quad * 8 + i, rank - 1) * a.len, j, a.len);
         Frag turned[T::lane];
         turn(rows, turned);
 #pragma unroll
@@ -846,7 +910,7 @@ struct GradArgs {
 // ones requested before the products of these.  In long tiles the workgroup's wavefronts take rows in
 // turn and join their sums in LDS; in tiles of up to kGradShort rows there is little to share (79 rows of 57
 // adapters, rank 45, fp32: 82 us that way, 39 this) and each has columns of its own.
-// 16384 rows of 8192 + 8192 columns at rank 64: 145 us, 3.7 TB/s.  128 accumulators leave a wavefront registers for
+// 16384 rows of 8192 + 8192 columns at rank 64: 133 us, 4.0 TB/s.  128 accumulators leave a wavefront registers for
 // one set of rows on its way, 64 KB a compute unit, which carries 4.1 TB/s; two thirds of the matrix products
 // (the second and third piece of h and g) cost 13 us of the 145.
 constexpr int kGradWaves = 4;
@@ -858,13 +922,13 @@ struct RowIndex {
         for (int i = 0; i < 8; ++i) t[i] = order[min(t0 + quad * 8 + i, rows - 1)];  // (rows beyond meet zeros in u)
     }
 };
-template <typename T, bool VEC>
+template <typename T, int VEC>
 __device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p, const RowIndex &at, int j) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         z[i] = load16<T, VEC>(row_at<typename T::elem>(p.z, at.t[i], p.pitch), j, p.len);
 }
-template <typename T, int CT, bool VEC, int SPLIT>
+template <typename T, int CT, int VEC, int SPLIT>
 __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int steps, const Tile &tile,
                                                   const int32_t *__restrict__ order, int c0, int j0,
                                                   f32x4_t (*sums)[CT * T::lane][64]) {
@@ -953,7 +1017,7 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
         }
 }
 // SPLIT wavefronts share the rows of a block of columns, or (1) each has a block of its own.
-template <typename T, int CT, bool VEC, int SPLIT>
+template <typename T, int CT, int VEC, int SPLIT>
 __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradArgs a, Route route, int size) {
     __shared__ f32x4_t sums[SPLIT == 1 ? 1 : SPLIT / 2][SPLIT == 1 ? 1 : CT * T::lane][64];
     const Tile tile = find_tile<false>(route, size, blockIdx.y);
@@ -1015,17 +1079,28 @@ static int down_splits(int64_t len, int r) {
     return (int)ceil_div(len, kDownWaves * 32 * down_steps<T>(down_tiles(r)));
 }
 
+template <typename T>
+static int access(bool aligned, int64_t rows, int64_t len) {
+    if (!aligned) return kAnywhere;
+    return rows * len * (int64_t)sizeof(typename T::elem) >= kStreamed ? kStream : kAligned;
+}
 template <typename T, int CT>
-static void down_kernel(const DownArgs &a, bool vec, dim3 grid, const Route &v, int size, hipStream_t st) {
-    if (vec)
-        adapter_down_kernel<T, CT, true><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
-    else
-        adapter_down_kernel<T, CT, false><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
+static void down_kernel(const DownArgs &a, int vec, dim3 grid, const Route &v, int size, hipStream_t st) {
+    if (vec == kAnywhere) {
+        adapter_down_kernel<T, CT, kAnywhere><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
+        return;
+    }
+    if constexpr (T::lane == 8)  // (fp32 rows: plain)
+        if (vec == kStream) {
+            adapter_down_kernel<T, CT, kStream><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
+            return;
+        }
+    adapter_down_kernel<T, CT, kAligned><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
 }
 template <typename T>
 static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st) {
     const int ct = down_tiles(a.r), splits = down_splits<T>(a.len, a.r);
-    const bool vec = rows_aligned(a.x, a.pitch) && aligned16(a.f) && a.len % 8 == 0;
+    const int vec = access<T>(rows_aligned(a.x, a.pitch) && aligned16(a.f) && a.len % 8 == 0, rows, a.len);
     const int64_t cols = ceil_div(a.r, ct * 16);
     // as few rows as two workgroups to a compute unit leave, half a tile more for every adapter
     const int64_t most = ceil_div(512, splits * cols), spare = v.count < most ? v.count / 2 : most / 2;
@@ -1066,7 +1141,7 @@ static int launch_operands(const OperandArgs &a, int jobs, int64_t rows, const R
     return check_launch("adapter_operand");
 }
 
-template <typename T, int KT, bool VEC>
+template <typename T, int KT, int VEC>
 static int up_kernel(const UpArgs &a, unsigned grid, const Route &v, int size, hipStream_t st) {
     const size_t lds = (size_t)KT * T::lane * 64 * sizeof(typename T::Frag);
     static size_t granted = 0;
@@ -1076,11 +1151,18 @@ static int up_kernel(const UpArgs &a, unsigned grid, const Route &v, int size, h
     adapter_up_kernel<T, KT, VEC><<<grid, kUpWaves * 64, lds, st>>>(a, v, size);
     return check_launch("adapter_up");
 }
+template <typename T, int KT>
+static int up_kernel(const UpArgs &a, int vec, unsigned grid, const Route &v, int size, hipStream_t st) {
+    return vec == kStream    ? up_kernel<T, KT, kStream>(a, grid, v, size, st)
+           : vec == kAligned ? up_kernel<T, KT, kAligned>(a, grid, v, size, st)
+                             : up_kernel<T, KT, kAnywhere>(a, grid, v, size, st);
+}
 template <typename T>
 static int launch_up(UpArgs a, int64_t rows, const Route &v, hipStream_t st) {
     const int es = sizeof(typename T::elem);
-    const bool vec = aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.pitch_out) &&
-                     (!a.y_in || rows_aligned(a.y_in, a.pitch_in));
+    const int vec = access<T>(aligned16(a.f) && (int64_t)a.len * es % 16 == 0 && rows_aligned(a.y_out, a.pitch_out) &&
+                                  (!a.y_in || rows_aligned(a.y_in, a.pitch_in)),
+                              rows, a.len);
     const int64_t cols = ceil_div(a.len, 16 * T::lane);
     int size = kUpRows;
     while (size > 64 && ceil_div(rows, size) * cols < 1024) size /= 2;
@@ -1089,10 +1171,10 @@ static int launch_up(UpArgs a, int64_t rows, const Route &v, hipStream_t st) {
     a.blocks = (int)cols;
     const unsigned grid = (unsigned)groups;
     switch (up_steps(a.r)) {
-    case 1: return vec ? up_kernel<T, 1, true>(a, grid, v, size, st) : up_kernel<T, 1, false>(a, grid, v, size, st);
-    case 2: return vec ? up_kernel<T, 2, true>(a, grid, v, size, st) : up_kernel<T, 2, false>(a, grid, v, size, st);
-    case 4: return vec ? up_kernel<T, 4, true>(a, grid, v, size, st) : up_kernel<T, 4, false>(a, grid, v, size, st);
-    default: return vec ? up_kernel<T, 8, true>(a, grid, v, size, st) : up_kernel<T, 8, false>(a, grid, v, size, st);
+    case 1: return up_kernel<T, 1>(a, vec, grid, v, size, st);
+    case 2: return up_kernel<T, 2>(a, vec, grid, v, size, st);
+    case 4: return up_kernel<T, 4>(a, vec, grid, v, size, st);
+    default: return up_kernel<T, 8>(a, vec, grid, v, size, st);
     }
 }
 
@@ -1105,17 +1187,19 @@ static int grad_size(int64_t rows, int64_t m, int64_t n, int lane) {
 }
 constexpr int kGradShort = 128;
 template <typename T, int CT>
-static void grad_kernel(const GradArgs &a, bool vec, dim3 grid, const Route &v, int size, hipStream_t st) {
-    if (size <= kGradShort) {
+static void grad_kernel(const GradArgs &a, int vec, dim3 grid, const Route &v, int size, hipStream_t st) {
+    if (size <= kGradShort) {  // (rows of kStreamed bytes in tiles as short as these are read plainly)
         grid.x = (grid.x + kGradWaves - 1) / kGradWaves;
-        if (vec)
-            adapter_grad_kernel<T, CT, true, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+        if (vec != kAnywhere)
+            adapter_grad_kernel<T, CT, kAligned, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
         else
-            adapter_grad_kernel<T, CT, false, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
-    } else if (vec) {
-        adapter_grad_kernel<T, CT, true, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+            adapter_grad_kernel<T, CT, kAnywhere, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+    } else if (vec == kStream) {
+        adapter_grad_kernel<T, CT, kStream, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+    } else if (vec == kAligned) {
+        adapter_grad_kernel<T, CT, kAligned, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
     } else {
-        adapter_grad_kernel<T, CT, false, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
+        adapter_grad_kernel<T, CT, kAnywhere, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
     }
 }
 template <typename T>
@@ -1124,7 +1208,8 @@ static int launch_grad(const GradArgs &a, int64_t rows, int count, int size, con
         const int ct = a.r > 32 ? 4 : a.r > 16 ? 2 : 1;
         const dim3 grid((unsigned)a.blocks, (unsigned)max_tiles(rows, count, size), (unsigned)ceil_div(a.r, ct * 16));
         Timed timed(KID_ADAPTER_GRAD, st);
-        const bool vec = a.prod[0].vec && a.prod[1].vec;
+        const int64_t longer = a.prod[0].len > a.prod[1].len ? a.prod[0].len : a.prod[1].len;
+        const int vec = access<T>(a.prod[0].vec && a.prod[1].vec, rows, longer);
         if (ct == 4) grad_kernel<T, 4>(a, vec, grid, v, size, st);
         else if (ct == 2) grad_kernel<T, 2>(a, vec, grid, v, size, st);
         else grad_kernel<T, 1>(a, vec, grid, v, size, st);

@@ -183,6 +183,12 @@ def test_few_rows_at_the_edges_of_their_forms(rows, m, n, r, count, dtype, pad, 
     inside(y, want["y"], "y")
 
 
+@pytest.mark.parametrize("dtype,rows", [("bf16", 1600), ("f32", 800)])
+@pytest.mark.parametrize("m,n,r", [(264, 8200, 20), (8200, 264, 64), (7752, 7752, 9)])
+def test_matrices_that_are_streamed(dtype, rows, m, n, r):
+    check(Case(rows, m, n, r, 3, dtype, ranks=r == 64, seed=2, pad=8))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_routes_and_workspaces_serve_what_they_promise(dtype):
     c = Case(700, 264, 520, 24, 6, dtype, ranks=True)
