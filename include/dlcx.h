@@ -310,10 +310,11 @@ typedef struct {
     int32_t dtype;   /* DLCX_F32 or DLCX_BF16: of x, y, dy, dx and of the factors                      */
 } dlcx_adapter_desc;
 
-/* Rows grouped by adapter: which rows each adapter has, in order, and how they are cut into tiles.
+/* Rows grouped by adapter: how many rows each adapter has, and which, in order.
  * ids: `rows` device ints, the adapter of each row; a value outside [0, count) is no adapter.  One
  * route serves every projection and both directions of a batch; dlcx_adapter_forward and
- * _backward make their own in the workspace where they get none.  rows 0 .. 2^24. */
+ * _backward make their own in the workspace where they get none.  One that they get has to be made
+ * from the same ids, rows and count: it is not checked.  rows 0 .. 2^24. */
 size_t dlcx_adapter_route_bytes(int64_t rows, int32_t count);
 int dlcx_adapter_route(int64_t rows, const int32_t *ids, int32_t count, void *route, void *stream);
 
@@ -329,8 +330,8 @@ size_t dlcx_adapter_workspace_bytes(const dlcx_adapter_desc *desc, int64_t rows)
  * scale (count floats) NULL: 1.  ranks (count ints) NULL: r; only the first ranks[a] columns of adapter a
  * are read, columns of h from there on are 0.  route NULL: formed here.  x, y and the factors may have any
  * alignment and stride that their type has; 16-byte aligned rows are faster.  bf16: products on
- * the bf16 matrix cores with fp32 sums, h rounded to bf16 as their operand (not in h_out), y rounded
- * once; fp32: fp32 matrix cores.  y_out, h_out and the workspace overlap nothing else. */
+ * the bf16 matrix cores with fp32 sums, h rounded to bf16 as their operand (not in h_out, and not
+ * where rows r <= 4096), y rounded once; fp32: fp32 matrix cores.  y_out, h_out and the workspace overlap nothing else. */
 int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
                          const int32_t *ids, const void *q, const void *p, const float *scale,
                          const int32_t *ranks, const void *route, const void *y_in, int64_t ldy_in,
