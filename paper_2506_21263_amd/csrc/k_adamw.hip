@@ -7,7 +7,7 @@
 //
 // Measured: AdamW with fp32 moments 5.3 TB/s (26.5 M fp32 elements in 140 tensors 148 us; 50 M with bf16
 // gradients 264 us), with 8-bit moments 5.8 TB/s (856 M bf16 elements 1.47 ms), where a copy of 2 GiB reaches
-// 4.9; the norm of 856 M bf16 gradients 257 us, 6.7 TB/s, of 26.5 M fp32 ones 24 + 3 us.
+// 4.9; the norm of 856 M bf16 gradients 257 us, 6.7 TB/s, of 26.5 M fp32 ones 20 + 3 us.
 #include <math.h>
 
 #include "common.h"
@@ -101,10 +101,11 @@ template <int DT>
 struct Raw {
     uint32_t w[DT == DLCX_F32 ? kVec : kVec / 2];
 };
-// STREAM: past the caches' order of use.  Against plain loads: 8-bit moments 1.47 (1.61) ms, a norm over
-// 1.7 GB 257 (303) us and over 106 MB 28 (25); but 32-bit moments, whose 12 or 14 bytes an element read and
-// written at the same places, 155 (148) and 278 (264) us, so those are plain.  Stores: all streamed, 1.47 (1.66) ms
-// and 278 (282) us.
+// STREAM: past the caches' order of use.  Against plain loads: 8-bit moments 1.47 (1.61) ms; a norm of bf16 gradients,
+// 1.7 GB 257 (303) us, 200 MB 34.9 (39.1); but of fp32 ones, which take twice the bytes a step, 1 GB 171 (169),
+// 300 MB that are read again 53 (47); and 32-bit moments, whose 12 or 14 bytes an element are read and written at
+// the same places, 155 (148) and 278 (264) us, so these two are plain.  Stores: all streamed, 1.47 (1.66) ms and
+// 278 (282) us.
 template <class T, bool STREAM>
 __device__ __forceinline__ T load_vector(AD_GLOBAL const T *p) {
     if constexpr (STREAM) return __builtin_nontemporal_load(p);
@@ -421,7 +422,7 @@ __device__ __forceinline__ double sum_squares(const void *grad, int64_t first, i
     Raw<DT> r[kSteps];
     if (numel - first >= kBlock) {
 #pragma unroll
-        for (int u = 0; u < kSteps; ++u) r[u] = load_whole<DT>(grad, first + u * kStep);
+        for (int u = 0; u < kSteps; ++u) r[u] = load_whole<DT, DT != DLCX_F32>(grad, first + u * kStep);
     } else {
 #pragma unroll
         for (int u = 0; u < kSteps; ++u)
