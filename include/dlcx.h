@@ -330,8 +330,8 @@ size_t dlcx_adapter_workspace_bytes(const dlcx_adapter_desc *desc, int64_t rows)
  * scale (count floats) NULL: 1.  ranks (count ints) NULL: r; only the first ranks[a] columns of adapter a
  * are read, columns of h from there on are 0.  route NULL: formed here.  x, y and the factors may have any
  * alignment and stride that their type has; 16-byte aligned rows are faster.  bf16: products on
- * the bf16 matrix cores with fp32 sums, h rounded to bf16 as their operand (not in h_out, and not
- * where rows r <= 4096), y rounded once; fp32: fp32 matrix cores.  y_out, h_out and the workspace overlap nothing else. */
+ * the bf16 matrix cores with fp32 sums, scale[a] h as an operand in three bf16 pieces that are its 24 bits, y rounded once;
+ * fp32: fp32 matrix cores.  y_out, h_out and the workspace overlap nothing else. */
 int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
                          const int32_t *ids, const void *q, const void *p, const float *scale,
                          const int32_t *ranks, const void *route, const void *y_in, int64_t ldy_in,
@@ -344,7 +344,7 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
  * dx_in (what the projection itself gives) may be dx_out, or NULL for zeros; dq_out (count x r x n) and
  * dp_out (count x r x m) are fp32 and overwritten, with zeros from column ranks[a] on and for adapters
  * without rows.  The order of a sum hangs on rows, count, sizes and the rows' ids alone.  bf16: as above;
- * the sums over rows take g and h in three bf16 pieces (error 2^-24 per product). */
+ * every product takes g and h in three pieces. */
 int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
                           const void *dy, int64_t lddy, const int32_t *ids, const void *q,
                           const void *p, const float *scale, const int32_t *ranks, const void *route,

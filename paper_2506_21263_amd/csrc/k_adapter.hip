@@ -47,7 +47,7 @@ struct Tile {
     int adapter;  // -1: rows without one; -2: there is no such tile
     int at, rows; // places in `order`
     int slab;     // number among the tiles of adapters that have several, -1: the only one
-    int block;    // number of its first 32 rows, when all buckets are cut into blocks of 32
+    int block;    // number of its first 16 rows, when all buckets are cut into blocks of 32 and these into two
 };
 // Tile `index` of the buckets' tiles of up to `size` rows; 64 buckets at a time, the same in every wavefront.
 // EVEN: a bucket's tiles have equal numbers of rows, in sixteens; else all but the last have `size`.
@@ -80,7 +80,7 @@ __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
             t.at = from;
             t.rows = min(each, stop - from);
             t.slab = several_l ? __builtin_amdgcn_readlane(slabs_upto, l) - several_l + k : -1;
-            t.block = __builtin_amdgcn_readlane(blocks_upto, l) - __builtin_amdgcn_readlane(n32, l) + k * (size / 32);
+            t.block = 2 * (__builtin_amdgcn_readlane(blocks_upto, l) - __builtin_amdgcn_readlane(n32, l)) + k * (each / 16);
             return t;
         }
         tiles = __builtin_amdgcn_readlane(upto, 63);
@@ -257,19 +257,30 @@ struct Bf16 {
     static __device__ __forceinline__ float at(const Frag &f, int i) {
         return i & 1 ? high_bf16(f.w[i / 2]) : low_bf16(f.w[i / 2]);
     }
-    // x as a sum of three bf16 numbers, to 2^-24
-    static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[3]) {
-        float rest[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rest[i] = x[i];
+    // x as a sum of three bf16 numbers, its 24 bits eight by eight: the sum is x itself.  All three have the sign of x, and
+    // what is not finite is that three times; a piece that would be zero is x / 2^32 instead (from 2^-80 on): so x times
+    // an infinity is that infinity in every piece, where 0 times it or two of different signs would be a NaN.
+    static __device__ __forceinline__ void parts(float x, elem (&e)[3]) {
+        const uint32_t bits = __float_as_uint(x), quiet = (bits & 0x007FFFFFu) ? 0x00400000u : 0u;
+        const uint32_t small = fabsf(x) >= 0x1p-80f ? __float_as_uint(x * 0x1p-32f) : 0u;
+        const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
+        float rest = x;
 #pragma unroll
         for (int h = 0; h < 3; ++h) {
-            f[h] = pack(rest);
+            uint32_t top = __float_as_uint(rest) & 0xFFFF0000u;
+            rest -= __uint_as_float(top);
+            if (h > 0 && (top & 0x7FFF0000u) == 0) top = small;
+            e[h] = (uint16_t)((finite ? top : bits | quiet) >> 16);
+        }
+    }
+    static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[3]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                rest[2 * i] -= low_bf16(f[h].w[i]);
-                rest[2 * i + 1] -= high_bf16(f[h].w[i]);
-            }
+        for (int i = 0; i < 8; i += 2) {
+            elem lo[3], hi[3];
+            parts(x[i], lo);
+            parts(x[i + 1], hi);
+#pragma unroll
+            for (int h = 0; h < 3; ++h) f[h].w[i / 2] = lo[h] | (uint32_t)hi[h] << 16;
         }
     }
     static constexpr int pieces = 3;
@@ -312,6 +323,7 @@ struct F32 {
         for (int i = 0; i < 8; ++i) f.x[i] = x[i];
         return f;
     }
+    static __device__ __forceinline__ void parts(float x, elem (&e)[1]) { e[0] = x; }
     static __device__ __forceinline__ void split(const float (&x)[8], Frag (&f)[1]) { f[0] = pack(x); }
     static __device__ __forceinline__ elem round(float x) { return x; }
     // the first n elements are zero
@@ -555,15 +567,15 @@ __global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapt
 
 // ---- operands ---------------------------------------------------------------------------------------
 // What the other two products read of h (or g): the sum of its splits, in 32 bits as it is and as two
-// operands, so that they are formed once and not by every workgroup that has other columns.  12 us for both of
-// 16384 rows at rank 64 (34 MB of shares, 4 of h, 15 of operands).
+// operands, so that they are formed once and not by every workgroup that has other columns.  14 us for both of
+// 16384 rows at rank 64 (34 MB of shares, 4 of h, 19 of operands).
 struct OperandJob {
     const float *splits;  // r columns each, `stride` floats apart
     int64_t stride;
     int n, placed;        // placed: their rows are in the order of the places
     const float *scale_out, *scale_up;  // what `out` and `turned`, and what `up` are multiplied with; nullptr: 1
     float *out;           // rows x r, or nullptr; zero from the adapter's rank on
-    void *up;             // places x steps 32, or nullptr: for the product with the factor
+    void *up;             // [block of 16 rows][step][piece][lane], or nullptr: for the product with the factor
     void *turned;         // [block of 32 rows][16 columns][piece][lane], or nullptr: for the sums over rows
 };
 struct OperandArgs {
@@ -581,6 +593,7 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
     const float s_out = j.scale_out && tile.adapter >= 0 ? j.scale_out[tile.adapter] : 1.f;
     const float s_up = j.scale_up && tile.adapter >= 0 ? j.scale_up[tile.adapter] : 1.f;
     const int c = blockIdx.z * 64 + threadIdx.x % 64, quad = threadIdx.x / 64;
+    __shared__ float to_up[32][65];
     if (c < cols) {
         int t[8];
         float x[8];
@@ -606,8 +619,8 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
             }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            to_up[quad * 8 + i][c % 64] = x[i] * s_up;
             if (t[i] < 0) continue;
-            if (j.up) ((typename T::elem *)j.up)[(int64_t)(place + i) * cols + c] = T::round(x[i] * s_up);
             x[i] *= s_out;
             if (j.out && c < a.r) j.out[(int64_t)t[i] * a.r + c] = x[i];
         }
@@ -616,15 +629,28 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
             T::split(x, f);
 #pragma unroll
             for (int h = 0; h < T::pieces; ++h)
-                ((typename T::Frag *)j.turned)[(((int64_t)tile.block * a.steps * 2 + c / 16) * T::pieces + h) * 64 +
+                ((typename T::Frag *)j.turned)[(((int64_t)(tile.block / 2) * a.steps * 2 + c / 16) * T::pieces + h) * 64 +
                                                quad * 16 + c % 16] = f[h];
         }
     }
+    if (!j.up) return;
+    __syncthreads();
+    // a thread has a row's eight columns of a step
+    const int lane = threadIdx.x % 64, half = threadIdx.x / 64 % 2, step = blockIdx.z * 2 + threadIdx.x / 128;
+    if (step >= a.steps) return;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = to_up[half * 16 + lane % 16][threadIdx.x / 128 * 32 + lane / 16 * 8 + i];
+    typename T::Frag f[T::pieces];
+    T::split(x, f);
+#pragma unroll
+    for (int h = 0; h < T::pieces; ++h)
+        ((typename T::Frag *)j.up)[(((int64_t)(tile.block + half) * a.steps + step) * T::pieces + h) * 64 + lane] = f[h];
 }
 
 // ---- up ---------------------------------------------------------------------------------------------
 struct UpArgs {
-    const void *h;       // places x steps 32, scaled
+    const void *h;       // [block of 16 rows][step][piece][lane], scaled
     const void *f;       // count x r x len
     const int32_t *ranks;
     const void *y_in;    // or nullptr
@@ -638,18 +664,15 @@ struct UpArgs {
 // columns into operand blocks in LDS once; then each wavefront takes 16 rows at a time: lane l has rows
 // 4 (l / 16) + 0 .. 3 and 16 bytes of each, so that 16 lanes make 256 in a row.  (With a row to
 // every lane of 16 an access is 64 pieces for the L1, not 16: 128 us for 16384 x 8192 at rank 64.)  HBM
-// bounds it: 104 us alone, 5.2 TB/s, what copies of this pattern reach (112 where it leaves grad its rows).
+// bounds it: 120 us where it leaves grad its rows, 4.5 TB/s.  bf16: scale h comes in all three of its pieces, so that a
+// row's result does not hang on the form that its number of rows takes; rounded to one piece it is 112 us, and at rank 256
+// (4133 rows) 54 instead of 104.  The pieces lie as the products take them: 1 KB of a row's own cache lines to a request,
+// where a row to each of 16 lanes took 128 us.
 constexpr int kUpWaves = 4;
-template <typename T, int KT, int VEC>
+template <typename T, int VEC>
 struct UpRows {
     ab_u32x4 y[4];
-    typename T::Frag h[KT];
-    __device__ __forceinline__ void load(const UpArgs &a, int64_t place, const int (&t)[4], int j) {
-        const int quad = (threadIdx.x & 63) >> 4;
-#pragma unroll
-        for (int s = 0; s < KT; ++s)
-            h[s] = T::template load8<true, true>((const typename T::elem *)a.h + place * (KT * 32), s * 32 + quad * 8,
-                                                 KT * 32);
+    __device__ __forceinline__ void load(const UpArgs &a, const int (&t)[4], int j) {
 #pragma unroll
         for (int v = 0; v < 4; ++v)
             y[v] = a.y_in ? load16<T, VEC>(row_at<typename T::elem>(a.y_in, t[v], a.pitch_in), j, a.len)
@@ -657,7 +680,7 @@ struct UpRows {
     }
 };
 template <typename T, int KT, int VEC>
-__global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 ? 3 : 2) void adapter_up_kernel(UpArgs a, Route route, int size) {
+__global__ __launch_bounds__(kUpWaves * 64, KT * T::pieces * sizeof(typename T::Frag) <= 96 ? 3 : 2) void adapter_up_kernel(UpArgs a, Route route, int size) {
     extern __shared__ __attribute__((aligned(16))) char up_lds[];
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
@@ -671,20 +694,29 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
     const int rank = adapter_rank(tile.adapter, a.ranks, a.r);
     const int steps = (rank + 31) / 32, last = tile.rows - 1;
     constexpr int round = kUpWaves * 16;
-    // Two rounds are on their way at any time; the row numbers of a later one go out before an earlier one's rows.
+    // Two rounds of rows are on their way at any time; the row numbers of a later one go out before an earlier one's rows,
+    // and so do the pieces of h of the next round, which take the places of this one's after the products.
     auto index_of = [&](int t0, int (&t)[4]) {
 #pragma unroll
         for (int v = 0; v < 4; ++v) t[v] = order[min(t0 + quad * 4 + v, last)];
     };
-    UpRows<T, KT, VEC> r0, r1;
-    auto load = [&](UpRows<T, KT, VEC> &r, int t0, const int (&t)[4]) { r.load(a, tile.at + min(t0 + row16, last), t, j); };
+    UpRows<T, VEC> r0, r1;
+    Frag h[KT][T::pieces];
+    auto load_h = [&](int t0) {
+        const Frag *from = (const Frag *)a.h + (int64_t)(tile.block + min(t0, last) / 16) * (KT * T::pieces * 64) + lane;
+#pragma unroll
+        for (int s = 0; s < KT; ++s)
+#pragma unroll
+            for (int k = 0; k < T::pieces; ++k) h[s][k] = from[(s * T::pieces + k) * 64];
+    };
     int t0 = wave * 16, i0[4], i1[4], n0[4], n1[4];
     index_of(t0, i0);
     index_of(t0 + round, i1);
     index_of(t0 + 2 * round, n0);
     index_of(t0 + 3 * round, n1);
-    load(r0, t0, i0);
-    load(r1, t0 + round, i1);
+    r0.load(a, i0, j);
+    load_h(t0);
+    r1.load(a, i1, j);
     for (int s = wave; s < steps; s += kUpWaves) {
         // (columns from the rank on meet zeros in h: the last one again does for them)
         const elem *f = (const elem *)a.f + (int64_t)tile.adapter * a.r * a.len;
@@ -698,7 +730,7 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
         for (int c = 0; c < T::lane; ++c) blocks[(s * T::lane + c) * 64 + lane] = turned[c];
     }
     __syncthreads();
-    auto products = [&](const UpRows<T, KT, VEC> &r, int t0, const int (&t)[4]) {
+    auto products = [&](const UpRows<T, VEC> &r, int t0, const int (&t)[4]) {
         f32x4_t acc[T::lane];
 #pragma unroll
         for (int c = 0; c < T::lane; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -706,8 +738,16 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
         for (int s = 0; s < KT; ++s)
             if (s < steps)
 #pragma unroll
-                for (int c = 0; c < T::lane; ++c)
-                    acc[c] = T::mma(r.h[s], blocks[(s * T::lane + c) * 64 + lane], acc[c]);
+                for (int c0 = 0; c0 < T::lane; c0 += 4) {
+                    Frag f[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) f[c] = blocks[(s * T::lane + c0 + c) * 64 + lane];
+#pragma unroll
+                    for (int k = 0; k < T::pieces; ++k)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[c0 + c] = T::mma(h[s][k], f[c], acc[c0 + c]);
+                }
+        load_h(t0 + round);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const bool valid = t0 + quad * 4 + v <= last;
@@ -732,12 +772,12 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * sizeof(typename T::Frag) <= 64 
         products(r0, t0, i0);
         copy(i0, n0);
         index_of(t0 + 4 * round, n0);
-        load(r0, t0 + 2 * round, i0);
+        r0.load(a, i0, j);
         if (t0 + round > last) break;
         products(r1, t0 + round, i1);
         copy(i1, n1);
         index_of(t0 + 5 * round, n1);
-        load(r1, t0 + 3 * round, i1);
+        r1.load(a, i1, j);
     }
 }
 
@@ -941,7 +981,7 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
 #pragma unroll
         for (int s = 0; s < T::lane; ++s) acc[c][s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const int j_row = j0 + T::lane * row16, j = column_base<T>(j_row, p.len);
-    const Frag *u = (const Frag *)p.u + ((int64_t)tile.block * steps * 2 + c0 / 16) * T::pieces * 64 + lane;
+    const Frag *u = (const Frag *)p.u + ((int64_t)(tile.block / 2) * steps * 2 + c0 / 16) * T::pieces * 64 + lane;
     const int64_t u_block = (int64_t)steps * 2 * T::pieces * 64;
     ab_u32x4 z[8];
     RowIndex at;
@@ -1248,8 +1288,8 @@ static size_t adapter_space(const dlcx_adapter_desc *d, int64_t rows, void *base
     const size_t row = (size_t)d->r * sizeof(float), steps = (size_t)up_steps(d->r);
     const int64_t longer = d->m > d->n ? d->m : d->n;
     w.split = take(row * (size_t)(rows * (low ? down_splits<Bf16>(longer, d->r) : down_splits<F32>(longer, d->r))));
-    w.up = take((size_t)rows * steps * 32 * (low ? 2 : 4));
-    const size_t turned = (size_t)max_tiles(rows, d->count, 32) * steps * 2 * 64 * frag;
+    const size_t turned = (size_t)max_tiles(rows, d->count, 32) * steps * 2 * 64 * frag;  // (of both forms)
+    w.up = take(turned);
     w.turned_h = take(turned);
     w.turned_g = take(turned);
     const int64_t small = 2 * (rows / 64), mid = ceil_div(kGradGroups * 4, cols), large = 2 * (rows / 4096);
