@@ -17,7 +17,7 @@ import argparse
 
 import torch
 
-from . import (BF16, F32, PHASE_P, PHASE_Q, STATE_GROUP, adapter_desc, desc, dlcx_adamw,
+from . import (BF16, F32, MMA_FMA, PHASE_P, PHASE_Q, STATE_GROUP, adapter_desc, desc, dlcx_adamw,
                dlcx_adapter_backward, dlcx_adapter_forward, dlcx_adapter_route,
                dlcx_adapter_route_bytes, dlcx_adapter_workspace_bytes, dlcx_compress_average,
                dlcx_decompress, dlcx_grad_norm, dlcx_orthonormalize, dlcx_outer_nesterov,
@@ -118,8 +118,15 @@ class AdapterProjection:
                               self.dp, self.workspace, scale=self.scale, route=route.table)
         return dx
 
+    def fold_workspace_bytes(self, group, mma):
+        """Scratch of `fold`: it packs both factors of an adapter, whatever rank the outer step compresses to."""
+        return 0 if mma == MMA_FMA else dlcx_workspace_bytes(desc(self.m, self.n, self.r, 8, group, mma), 1)
+
     def fold(self, ef, workspace, group, mma):
         """ef[a] <- ef[a] - s P_a Q_a^T for every worker: with e_a in ef[a], its pseudo-gradient."""
+        need = self.fold_workspace_bytes(group, mma)
+        if need and (workspace is None or workspace.numel() < need):
+            raise ValueError("workspace: %d bytes are wanted" % need)
         d = desc(self.m, self.n, self.r, 8, group, mma)
         for a in range(self.count):
             dlcx_decompress(d, self.p[a] * self.scale_value, self.q[a], None, [ef[a]],
@@ -148,7 +155,11 @@ class AdapterOuterStep:
                                      device=dev, dtype=torch.uint8)
 
     def step(self, proj):
-        M, ws = self.M, self.workspace
+        M = self.M
+        need = proj.fold_workspace_bytes(M.group, M.mma)
+        if self.workspace.numel() < need:  # adapters of a higher rank than the outer step's
+            self.workspace = torch.empty(need, device=self.workspace.device, dtype=torch.uint8)
+        ws = self.workspace
         self.t += 1
         if self.t >= 2:
             dlcx_decompress(M.desc(M.r_prev), M.p_hat, M.q_bar, self.delta_hat, M.ef, workspace=ws)
