@@ -969,7 +969,7 @@ __device__ __forceinline__ void load_rows(ab_u32x4 (&z)[8], const GradProduct &p
         z[i] = load16<T, VEC>(row_at<typename T::elem>(p.z, at.t[i], p.pitch), j, p.len);
 }
 template <typename T, int CT, int VEC, int SPLIT>
-__device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int steps, const Tile &tile,
+__device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, int rank, int steps, const Tile &tile,
                                                   const int32_t *__restrict__ order, int c0, int j0,
                                                   f32x4_t (*sums)[CT * T::lane][64]) {
     typedef typename T::Frag Frag;
@@ -1042,8 +1042,9 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
             float *row = out + (int64_t)col * p.len;
 #pragma unroll
             for (int s = 0; s < T::lane; s += 4) {
-                const f32x4_t w = {scale * acc[c][s][v], scale * acc[c][s + 1][v], scale * acc[c][s + 2][v],
-                                   scale * acc[c][s + 3][v]};
+                f32x4_t w = {scale * acc[c][s][v], scale * acc[c][s + 1][v], scale * acc[c][s + 2][v],
+                             scale * acc[c][s + 3][v]};
+                if (col >= rank) w = f32x4_t{0.f, 0.f, 0.f, 0.f};  // (zeros of u times what is not finite are none)
                 if (VEC || j_row + T::lane <= p.len) {
                     if (j_row >= p.len) continue;
                     if constexpr (VEC) *reinterpret_cast<f32x4_t *>(row + j + s) = w;
@@ -1069,7 +1070,7 @@ __global__ __launch_bounds__(kGradWaves * 64, 2) void adapter_grad_kernel(GradAr
     const int second = block >= a.blocks0;
     const GradProduct &p = a.prod[second];
     const int j0 = (block - (second ? a.blocks0 : 0)) * 16 * T::lane, c0 = blockIdx.z * CT * 16;
-    adapter_grad_rows<T, CT, VEC, SPLIT>(p, a.r, a.steps, tile, order, c0, j0,
+    adapter_grad_rows<T, CT, VEC, SPLIT>(p, a.r, adapter_rank(tile.adapter, a.ranks, a.r), a.steps, tile, order, c0, j0,
                                          reinterpret_cast<f32x4_t (*)[CT * T::lane][64]>(&sums));
 }
 
