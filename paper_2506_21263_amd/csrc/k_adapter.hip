@@ -470,7 +470,7 @@ __global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapt
     const int k0 = (share * kDownWaves + wave) * KS * 32;
     const bool whole = k0 + KS * 32 <= a.len;
     // The lane's elements of step s (with kQuads, after the exchange).  Where a row that is not read by 16 aligned bytes ends before them, its last
-    // eight, of which the factor's are zero as far as another lane has them (shorter rows are read by element).
+    // eight, of which the row's and the factor's are zero as far as another lane has them (shorter rows are read by element).
     constexpr bool kQuads = VEC && T::lane == 8;
     auto at = [&](int s) { return k0 + (kQuads ? s / 4 * 128 + quad * 32 + s % 4 * 8 : s * 32 + quad * 8); };
     auto load = [&](const elem *row, Frag (&f)[KS]) {
@@ -545,18 +545,27 @@ __global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapt
 #pragma unroll
     for (int c = 0; c < CT; ++c)  // columns from the rank on are the last one again: not stored
         load((const elem *)a.f + ((int64_t)tile.adapter * a.r + min(c0 + c * 16 + row16, rank - 1)) * a.len, f[c]);
-    if (!VEC && !whole && a.len >= 8)
+    const bool twice = !VEC && !whole && a.len >= 8;
+    auto drop = [&](Frag (&x)[KS]) {
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
+        for (int s = 0; s < KS; ++s) {
+            int n = at(s) - min(at(s), a.len - 8);
+            asm volatile("" : "+v"(n));  // (masks formed here and not kept through the loop: 151 registers, not 193)
+            T::drop(x[s], n);
+        }
+    };
+    if (twice)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) T::drop(f[c][s], at(s) - min(at(s), a.len - 8));
+        for (int c = 0; c < CT; ++c) drop(f[c]);
     for (int t0 = 0; t0 <= last; t0 += 32) {
+        if (twice) drop(x0);
         products(x0, 0);
         const int m0 = n0;
         n0 = index_of(t0 + 64);
         if (t0 + 32 <= last) load_row(m0, x0);
         join(t0, 0);
         if (t0 + 16 > last) break;
+        if (twice) drop(x1);
         products(x1, 1);
         const int m1 = n1;
         n1 = index_of(t0 + 80);
@@ -619,9 +628,9 @@ __global__ __launch_bounds__(256) void adapter_operand_kernel(OperandArgs a, Rou
             }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            to_up[quad * 8 + i][c % 64] = x[i] * s_up;
+            to_up[quad * 8 + i][c % 64] = c < rank ? x[i] * s_up : 0.f;
             if (t[i] < 0) continue;
-            x[i] *= s_out;
+            x[i] = c < rank ? x[i] * s_out : 0.f;
             if (j.out && c < a.r) j.out[(int64_t)t[i] * a.r + c] = x[i];
         }
         if (j.turned) {
@@ -718,12 +727,15 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * T::pieces * sizeof(typename T::
     load_h(t0);
     r1.load(a, i1, j);
     for (int s = wave; s < steps; s += kUpWaves) {
-        // (columns from the rank on meet zeros in h: the last one again does for them)
+        // (a column from the rank on is the last one again on its way, and zeros in the product)
         const elem *f = (const elem *)a.f + (int64_t)tile.adapter * a.r * a.len;
         ab_u32x4 rows[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             rows[i] = load16<T, VEC ? kAligned : kAnywhere>(f + (int64_t)min(s * 32 + quad * 8 + i, rank - 1) * a.len, j, a.len);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (s * 32 + quad * 8 + i >= rank) rows[i] = ab_u32x4{0u, 0u, 0u, 0u};
         Frag turned[T::lane];
         turn(rows, turned);
 #pragma unroll
@@ -959,7 +971,7 @@ struct RowIndex {
     __device__ __forceinline__ void load(const int32_t *__restrict__ order, int t0, int rows) {
         const int quad = (threadIdx.x & 63) >> 4;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = order[min(t0 + quad * 8 + i, rows - 1)];  // (rows beyond meet zeros in u)
+        for (int i = 0; i < 8; ++i) t[i] = order[min(t0 + quad * 8 + i, rows - 1)];
     }
 };
 template <typename T, int VEC>
@@ -997,6 +1009,10 @@ __device__ __forceinline__ void adapter_grad_rows(const GradProduct &p, int r, i
     if (wave * 32 < tile.rows) load_u(f[0], wave * 32, 0);
     for (int t0 = wave * 32; t0 < tile.rows; t0 += SPLIT * 32) {
         const int t1 = t0 + SPLIT * 32 < tile.rows ? t0 + SPLIT * 32 : t0;
+        if (t0 + 32 > tile.rows)  // zeros in the places of rows beyond the last one, as in u: 0 x Inf would not be 0
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (t0 + quad * 8 + i >= tile.rows) z[i] = ab_u32x4{0u, 0u, 0u, 0u};
         Frag turned[T::lane];
         turn(z, turned);
         load_rows<T, VEC>(z, p, at, j);
