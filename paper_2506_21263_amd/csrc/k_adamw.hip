@@ -6,7 +6,7 @@
 // table.start holds each tensor's first block, so a workgroup finds its tensor by searching there.
 //
 // Measured: AdamW with fp32 moments 5.3 TB/s (26.5 M fp32 elements in 140 tensors 148 us; 50 M with bf16
-// gradients 264 us), with 8-bit moments 5.8 TB/s (856 M bf16 elements 1.47 ms), where a copy of 2 GiB reaches
+// gradients 264 us), with 8-bit moments 5.6 TB/s (856 M bf16 elements 1.54 ms), where a copy of 2 GiB reaches
 // 4.9; the norm of 856 M bf16 gradients 257 us, 6.7 TB/s, of 26.5 M fp32 ones 20 + 3 us.
 #include <math.h>
 
@@ -235,8 +235,7 @@ __device__ __forceinline__ float group_scale(float amax, float top, float *inv) 
 }
 // The code of x >= 0 is the integer next to sqrt(x / scale), both operations rounded correctly, where x of a
 // second moment is a correctly rounded root itself.  With IEEE quotients and roots throughout the step was bound
-// by its arithmetic (4.2 TB/s; it still takes 55 vector instructions an element, nine tenths of the time that
-// 5.8 TB/s leave).  So a code is taken from a product and the hardware's roots and reciprocals (1 unit in the
+// by its arithmetic (4.2 TB/s; it still is, at 61 vector instructions an element).  So a code is taken from a product and the hardware's roots and reciprocals (1 unit in the
 // last place), together off by 1e-4 codes at most, and only where that lies within 1.25e-4 of the middle between
 // two codes is it decided by the definition: one code in 4000, hardly ever two of a thread's sixteen.
 __device__ __forceinline__ float near_root(float x, float inv) { return __builtin_amdgcn_sqrtf(x * inv); }
@@ -252,6 +251,9 @@ __device__ __forceinline__ void put_v(ad_u32x2 &w, int i, float root, float v) {
 }
 // Below this a group's largest v may have company whose hardware root is flushed to zero and whose code is not 1.
 constexpr float kTinyV = 0x1p-89f;
+// m below 2^60, v below 2^100 (bit patterns; a NaN is above) and eps between 2^-50 and 2^100.
+constexpr uint32_t kPlainM = (127u + 60) << 23, kPlainV = (127u + 100) << 23;
+constexpr float kPlainEpsLow = 0x1p-50f, kPlainEpsHigh = 0x1p100f;
 
 // a x + b y with every operation rounded: what the codes of the moments hang on is then the same wherever
 // the formula is evaluated.
@@ -316,13 +318,7 @@ __device__ __forceinline__ void adamw_elements(const dlcx_tensor &t, const Adamw
         const float gi = g[i] * gs;
         m[i] = weighted_sum(m[i], s.beta1, gi, s.one_minus_beta1);
         v[i] = weighted_sum(v[i], s.beta2, gi * gi, s.one_minus_beta2);
-        if constexpr (BITS == 32) {
-            p[i] = p[i] * decay - rate * (m[i] / (sqrtf(v[i]) * s.inv_sqrt_bc2 + s.eps));
-        } else {
-            // (a v that the hardware's root would flush counts as the smallest one that it does not)
-            root[i] = __builtin_amdgcn_sqrtf(__uint_as_float(max(__float_as_uint(v[i]), 0x00800000u)));
-            p[i] = p[i] * decay - rate * (m[i] * __builtin_amdgcn_rcpf(root[i] * s.inv_sqrt_bc2 + s.eps));
-        }
+        if constexpr (BITS == 32) p[i] = p[i] * decay - rate * (m[i] / (sqrtf(v[i]) * s.inv_sqrt_bc2 + s.eps));
     }
     if constexpr (BITS == 8) {
         uint32_t am = 0, av = 0;
@@ -330,6 +326,25 @@ __device__ __forceinline__ void adamw_elements(const dlcx_tensor &t, const Adamw
         for (int i = 0; i < kVec; ++i) {
             am = max(am, __float_as_uint(m[i]) & 0x7FFFFFFFu);
             av = max(av, __float_as_uint(v[i]));  // (v >= 0 or a NaN, whose sign makes it the larger)
+        }
+        // Root and quotient are the hardware's approximations with one correction each: at most 1e-4 units in the last
+        // place beyond the half of a correct rounding, 1.54 ms for 856 M elements where IEEE roots and quotients take
+        // 1.82 and approximations alone 1.43.  No step of them leaves fp32's range below these limits; beyond, IEEE.
+        if (am < kPlainM && av < kPlainV && s.eps >= kPlainEpsLow && s.eps <= kPlainEpsHigh) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const float y = __builtin_amdgcn_rsqf(__uint_as_float(max(__float_as_uint(v[i]), 0x00800000u)));
+                const float near = v[i] * y;
+                root[i] = fmaf(0.5f * y, fmaf(-near, near, v[i]), near);
+                const float d = root[i] * s.inv_sqrt_bc2 + s.eps, inv = __builtin_amdgcn_rcpf(d), q = m[i] * inv;
+                p[i] = p[i] * decay - rate * fmaf(inv, fmaf(-q, d, m[i]), q);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                root[i] = sqrtf(v[i]);
+                p[i] = p[i] * decay - rate * (m[i] / (root[i] * s.inv_sqrt_bc2 + s.eps));
+            }
         }
         float m_inv, v_inv;
         const float v_max = __uint_as_float(row_max(av));
