@@ -598,7 +598,7 @@ size_t dlcx_tensor_table_bytes(int32_t count) {
 }
 
 static int check_tensor(const dlcx_tensor &t) {
-    if (t.numel < 0 || t.reserved != 0) return DLCX_EINVAL;
+    if (t.numel < 0 || t.numel > (int64_t)0x7FFFFFFF * kBlock || t.reserved != 0) return DLCX_EINVAL;
     if (t.grad_dtype != DLCX_F32 && t.grad_dtype != DLCX_BF16) return DLCX_EINVAL;
     if (t.numel == 0) return DLCX_OK;
     if (!t.grad || !aligned16(t.grad)) return DLCX_EINVAL;
@@ -666,7 +666,7 @@ int dlcx_state_decode(int second, const void *codes, const float *scales, int64_
     if (numel == 0) return DLCX_OK;
     if (!codes || !scales || !out || !aligned16(codes) || !aligned16(out) || ((uintptr_t)scales & 3))
         return DLCX_EINVAL;
-    if (ceil_div(numel, kStep) > 0x7FFFFF) return DLCX_EINVAL;
+    if (numel > (int64_t)0x7FFFFF * kStep) return DLCX_EINVAL;
     return launch_state_decode(second, codes, scales, numel, out, out_dtype, as_stream(stream));
 }
 

@@ -1,0 +1,16 @@
+"""Numbers at the ends of their types that the calls of the optimizer refuse, on the host."""
+import ctypes as C
+
+import paper_2506_21263_amd as dlcx
+
+F = 0x10000  # aligned to 256, never read
+TOP = (1 << 63) - 1
+
+
+def test_lengths_whose_blocks_would_overflow():
+    L = dlcx.lib()
+    out = dlcx.Table()
+    for numel in (TOP, TOP - 4095, 1 << 62, (1 << 31) * 4096):
+        t = dlcx.Tensor(grad=F, numel=numel, grad_dtype=dlcx.F32)
+        assert L.dlcx_tensor_table(C.addressof(t), 1, F, C.addressof(out), None) == dlcx.EINVAL, numel
+        assert L.dlcx_state_decode(0, F, F, numel, F, 0, None) == dlcx.EINVAL, numel
