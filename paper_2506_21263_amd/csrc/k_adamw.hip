@@ -642,7 +642,9 @@ int dlcx_adamw(const dlcx_table *table_host, double lr, double beta1, double bet
     if (rc != DLCX_OK) return rc;
     if (!table_host->steps || step < 1) return DLCX_EINVAL;
     if (!isfinite(lr) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1)) return DLCX_EINVAL;
-    if (!(eps > 0) || !isfinite(eps) || !(grad_scale >= 0) || !isfinite(grad_scale)) return DLCX_EINVAL;
+    // (as the step has them, in fp32: an eps that is zero there divides zeros by zeros, a scale that is infinite zeros too)
+    if (!((float)eps > 0) || !isfinite((float)eps) || !(grad_scale >= 0) || !isfinite((float)grad_scale)) return DLCX_EINVAL;
+    if (!isfinite((float)lr)) return DLCX_EINVAL;
     if (norm && (((uintptr_t)norm & 3) || !(max_norm > 0))) return DLCX_EINVAL;
     AdamwStep s;
     s.beta1 = (float)beta1;

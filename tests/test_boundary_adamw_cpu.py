@@ -14,3 +14,13 @@ def test_lengths_whose_blocks_would_overflow():
         t = dlcx.Tensor(grad=F, numel=numel, grad_dtype=dlcx.F32)
         assert L.dlcx_tensor_table(C.addressof(t), 1, F, C.addressof(out), None) == dlcx.EINVAL, numel
         assert L.dlcx_state_decode(0, F, F, numel, F, 0, None) == dlcx.EINVAL, numel
+
+
+def test_hyperparameters_that_fp32_has_no_room_for():
+    t = dlcx.Table(memory=F, blocks=1, count=1, steps=1)
+
+    def adamw(lr=1e-3, eps=1e-8, gs=1.0):
+        return dlcx.lib().dlcx_adamw(C.addressof(t), lr, 0.9, 0.95, eps, 1, gs, None, 0.0, None)
+
+    for bad in (dict(eps=1e-46), dict(eps=1e39), dict(gs=1e39), dict(lr=1e39), dict(lr=-1e39)):
+        assert adamw(**bad) == dlcx.EINVAL, bad
