@@ -6,6 +6,7 @@ nothing else) and passes their addresses through.  There is no fallback: if the 
 missing or a call fails, an exception is raised.
 """
 import ctypes as C
+import math
 import os
 
 import torch
@@ -447,6 +448,17 @@ def _typed(t, dtype, numel, what):
     return t.data_ptr()
 
 
+def _packed(t, dtype, shape, what):
+    """Address of a packed device array of that shape: one with its last dimensions, or a flat one.  (Arrays of equal
+    shapes, as P and Q of a square projection, cannot be told apart.)"""
+    if t is not None and t.shape == shape and t.is_cuda and t.dtype == dtype and t.is_contiguous():
+        return t.data_ptr()
+    if t is not None and t.dim() > 1 and t.shape[-2:] != shape[-2:] and not (t.dim() == 2 and t.shape[1] == shape[-1]):
+        raise ValueError("%s: an array of %s is wanted, not of %s" % (what, " x ".join(map(str, shape)), " x ".join(
+            map(str, t.shape))))
+    return _typed(t, dtype, math.prod(shape), what)
+
+
 def _rows(t, rows, cols, dtype, what):
     """Address and row stride of a rows x cols device matrix whose rows are contiguous."""
     if t is None:
@@ -477,8 +489,8 @@ def dlcx_adapter_workspace_bytes(d, rows):
 
 def _adapter_common(d, rows, ids, q, p, scale, ranks, route, workspace):
     dt = torch.bfloat16 if d.dtype == BF16 else torch.float32
-    return (dt, _typed(ids, torch.int32, rows, "ids"), _typed(q, dt, d.count * d.r * d.n, "q"),
-            _typed(p, dt, d.count * d.r * d.m, "p"), _typed(scale, torch.float32, d.count, "scale"),
+    return (dt, _typed(ids, torch.int32, rows, "ids"), _packed(q, dt, (d.count, d.r, d.n), "q"),
+            _packed(p, dt, (d.count, d.r, d.m), "p"), _typed(scale, torch.float32, d.count, "scale"),
             _typed(ranks, torch.int32, d.count, "ranks"),
             None if route is None else _typed(route, torch.uint8, dlcx_adapter_route_bytes(rows, d.count), "route"),
             _typed(workspace, torch.uint8, dlcx_adapter_workspace_bytes(d, rows), "workspace"))
@@ -493,7 +505,7 @@ def dlcx_adapter_forward(d, x, ids, q, p, y_in, y_out, h_out, workspace, scale=N
     y_in, ldi = _rows(y_in, rows, d.m, dt, "y_in")
     y_out, ldo = _rows(y_out, rows, d.m, dt, "y_out")
     _check(lib().dlcx_adapter_forward(C.byref(d), rows, x, ldx, ids, q, p, scale, ranks, route, y_in, ldi,
-                                      y_out, ldo, _typed(h_out, torch.float32, rows * d.r, "h_out"), ws,
+                                      y_out, ldo, _packed(h_out, torch.float32, (rows, d.r), "h_out"), ws,
                                       _stream(stream)), "dlcx_adapter_forward")
 
 
@@ -507,9 +519,9 @@ def dlcx_adapter_backward(d, x, dy, ids, q, p, h, dx_in, dx_out, dq_out, dp_out,
     dx_in, ldi = _rows(dx_in, rows, d.n, dt, "dx_in")
     dx_out, ldo = _rows(dx_out, rows, d.n, dt, "dx_out")
     _check(lib().dlcx_adapter_backward(C.byref(d), rows, x, ldx, dy, lddy, ids, q, p, scale, ranks, route,
-                                       _typed(h, torch.float32, rows * d.r, "h"), dx_in, ldi, dx_out, ldo,
-                                       _typed(dq_out, torch.float32, d.count * d.r * d.n, "dq_out"),
-                                       _typed(dp_out, torch.float32, d.count * d.r * d.m, "dp_out"), ws,
+                                       _packed(h, torch.float32, (rows, d.r), "h"), dx_in, ldi, dx_out, ldo,
+                                       _packed(dq_out, torch.float32, (d.count, d.r, d.n), "dq_out"),
+                                       _packed(dp_out, torch.float32, (d.count, d.r, d.m), "dp_out"), ws,
                                        _stream(stream)), "dlcx_adapter_backward")
 
 
