@@ -531,6 +531,10 @@ def tensor(grad, param=None, m=None, v=None, m_scale=None, v_scale=None, copy=No
     and uint8 codes with a float32 scale per STATE_GROUP elements.  Returns the structure and what it
     points to."""
     numel = grad.numel()
+    if grad.dtype not in _CODE or (param is not None and param.dtype not in _CODE):
+        raise ValueError("gradients and parameters are float32 or bfloat16")
+    if param is not None and (m is None or v is None):
+        raise ValueError("a parameter has both of its moments")
     t = Tensor(grad=_typed(grad, grad.dtype, numel, "grad"), numel=numel, lr_scale=lr_scale,
                weight_decay=weight_decay, grad_dtype=_CODE[grad.dtype], state_bits=32)
     if param is not None:

@@ -1,6 +1,9 @@
 """Numbers at the ends of their types that the calls of the optimizer refuse, on the host."""
 import ctypes as C
 
+import pytest
+import torch
+
 import paper_2506_21263_amd as dlcx
 
 F = 0x10000  # aligned to 256, never read
@@ -24,3 +27,11 @@ def test_hyperparameters_that_fp32_has_no_room_for():
 
     for bad in (dict(eps=1e-46), dict(eps=1e39), dict(gs=1e39), dict(lr=1e39), dict(lr=-1e39)):
         assert adamw(**bad) == dlcx.EINVAL, bad
+
+
+def test_tensors_of_types_that_have_no_kernel():
+    g = torch.zeros(8)
+    for bad, says in ((dict(grad=g.half()), "float32 or bfloat16"), (dict(grad=g, param=g.double(), m=g, v=g), "float32 or bfloat16"),
+                      (dict(grad=g, param=g), "moments"), (dict(grad=g, param=g, m=g), "moments")):
+        with pytest.raises(ValueError, match=says):
+            dlcx.tensor(**bad)
