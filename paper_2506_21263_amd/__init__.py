@@ -163,9 +163,16 @@ def _ptr_array(ts):
     return C.cast(arr, C.c_void_p), arr  # keep `arr` alive with the caller
 
 
+# The handle of the current stream without the object around it (3 us of a call of 10), where torch has that; it is
+# no documented name of torch, so no call depends on it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
-    if stream is None:  # torch.cuda.current_stream().cuda_stream, without making the object (3 us)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if stream is None:
+        if _raw_stream is None:
+            return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
