@@ -14,6 +14,7 @@ stands beside it and the optimizer are entry points of the HIP library.
 teacher, outer step after outer step, and prints the losses.
 """
 import argparse
+import math
 
 import torch
 
@@ -22,6 +23,13 @@ from . import (BF16, F32, MMA_FMA, PHASE_P, PHASE_Q, STATE_GROUP, adapter_desc, 
                dlcx_adapter_route_bytes, dlcx_adapter_workspace_bytes, dlcx_compress_average,
                dlcx_decompress, dlcx_grad_norm, dlcx_orthonormalize, dlcx_outer_nesterov,
                dlcx_tensor_table, dlcx_tensor_table_bytes, dlcx_workspace_bytes, tensor)
+
+
+def _as_stream(stream):
+    """The stream of a call's `stream` argument: None (the current one), a handle or a stream."""
+    if stream is None:
+        return torch.cuda.current_stream()
+    return torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
 
 
 class Route:
@@ -37,13 +45,19 @@ class Route:
 class AdamW:
     """AdamW over a list of parameters with given gradient buffers: moments of 32 or 8 bits, clipping
     by the gradients' own norm (max_norm > 0), bf16 copies of fp32 parameters where wanted.
-    decays[i] is the weight decay of parameter i."""
+    decays[i] is the weight decay of parameter i.
+
+    With clipping, a step whose norm is not finite leaves everything as it was, and does not count: `step` looks at
+    the norm of the step before, which the GPU has long formed by then, `taken` at the last one's.  (Steps that
+    are captured into a graph are counted as they are captured.)"""
 
     def __init__(self, params, grads, lr, betas=(0.9, 0.95), eps=1e-8, decays=None, copies=None,
                  bits=32, max_norm=0.0):
         self.lr, self.betas, self.eps, self.max_norm, self.t = lr, betas, eps, max_norm, 0
         dev = params[0].device
         self.norm = torch.zeros(1, device=dev)
+        self.norm_host = torch.empty(1, pin_memory=True)
+        self.norm_there = None  # event: norm_host holds the norm of the last step
         self.moments = []
         tensors = []
         for i, p in enumerate(params):
@@ -63,18 +77,32 @@ class AdamW:
 
     def reset(self):
         """Moments and step count of a new run."""
-        self.t = 0
+        self.t, self.norm_there = 0, None
         for state in self.moments:
             for x in state.values():
                 x.zero_()
 
+    def taken(self):
+        """Steps that changed something."""
+        if self.norm_there is not None:
+            self.norm_there.synchronize()
+            self.norm_there = None
+            self.t -= not math.isfinite(float(self.norm_host))
+        return self.t
+
     def step(self, stream=None):
-        self.t += 1
+        self.t = self.taken() + 1
         clip = self.max_norm > 0
         if clip:
             dlcx_grad_norm(self.table, self.norm, stream=stream)
         dlcx_adamw(self.table, self.lr, self.betas[0], self.betas[1], self.eps, self.t,
                    norm=self.norm if clip else None, max_norm=self.max_norm, stream=stream)
+        if clip:
+            with torch.cuda.stream(_as_stream(stream)):
+                if not torch.cuda.is_current_stream_capturing():
+                    self.norm_host.copy_(self.norm, non_blocking=True)
+                    self.norm_there = torch.cuda.Event()
+                    self.norm_there.record()
 
 
 class AdapterProjection:
