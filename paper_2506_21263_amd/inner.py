@@ -32,14 +32,37 @@ def _as_stream(stream):
     return torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
 
 
+class Order:
+    """Buffers that are written on one stream and used on another: the other waits, and the memory is not given to
+    anybody else before it is through.  A graph is captured after whatever it uses is there."""
+
+    def __init__(self, stream=None):
+        self.stream = _as_stream(stream)
+
+    def enter(self, stream, buffers):
+        """The stream of a call that uses the buffers."""
+        stream = _as_stream(stream)
+        if stream != self.stream:
+            with torch.cuda.stream(stream):
+                if torch.cuda.is_current_stream_capturing():
+                    return stream
+            stream.wait_stream(self.stream)
+            for x in buffers:
+                x.record_stream(stream)
+            self.stream = stream
+        return stream
+
+
 class Route:
-    """Which rows of a batch belong to which adapter; one route serves every projection of the batch."""
+    """Which rows of a batch belong to which adapter; one route serves every projection of the batch.  With a stream
+    it is formed there (where `ids` has to be), and the calls that take it wait for it."""
 
     def __init__(self, ids, count, stream=None):
-        self.ids = ids
-        self.table = torch.empty(dlcx_adapter_route_bytes(ids.numel(), count), device=ids.device,
-                                 dtype=torch.uint8)
-        dlcx_adapter_route(ids, count, self.table, stream=stream)
+        self.ids, self.order = ids, Order(stream)
+        with torch.cuda.stream(self.order.stream):
+            self.table = torch.empty(dlcx_adapter_route_bytes(ids.numel(), count), device=ids.device,
+                                     dtype=torch.uint8)
+            dlcx_adapter_route(ids, count, self.table)
 
 
 class AdamW:
@@ -74,9 +97,12 @@ class AdamW:
                                   weight_decay=decays[i] if decays else 0.0, **state))
         memory = torch.empty(dlcx_tensor_table_bytes(len(tensors)), device=dev, dtype=torch.uint8)
         self.table = dlcx_tensor_table(tensors, memory)
+        self.order = Order()
+        self.own = [memory, self.norm] + [x for state in self.moments for x in state.values()]
 
     def reset(self):
         """Moments and step count of a new run."""
+        self.order.enter(None, self.own)
         self.t, self.norm_there = 0, None
         for state in self.moments:
             for x in state.values():
@@ -91,6 +117,8 @@ class AdamW:
         return self.t
 
     def step(self, stream=None):
+        """One step, on `stream` (gradients and parameters have to be there) after whatever came before."""
+        stream = self.order.enter(stream, self.own)
         self.t = self.taken() + 1
         clip = self.max_norm > 0
         if clip:
@@ -98,7 +126,7 @@ class AdamW:
         dlcx_adamw(self.table, self.lr, self.betas[0], self.betas[1], self.eps, self.t,
                    norm=self.norm if clip else None, max_norm=self.max_norm, stream=stream)
         if clip:
-            with torch.cuda.stream(_as_stream(stream)):
+            with torch.cuda.stream(stream):
                 if not torch.cuda.is_current_stream_capturing():
                     self.norm_host.copy_(self.norm, non_blocking=True)
                     self.norm_there = torch.cuda.Event()
@@ -134,6 +162,7 @@ class AdapterProjection:
 
     def forward(self, x, route):
         y = x @ self.base.t()
+        route.order.enter(None, [route.table])
         h = torch.empty(x.shape[0], self.r, device=x.device)
         dlcx_adapter_forward(self.d, x, route.ids, self.q_copy, self.p_copy, y, y, h, self.workspace,
                              scale=self.scale, route=route.table)
@@ -142,6 +171,7 @@ class AdapterProjection:
     def backward(self, x, h, dy, route):
         """dx; the gradients of the factors are left in dq and dp."""
         dx = dy @ self.base
+        route.order.enter(None, [route.table])
         dlcx_adapter_backward(self.d, x, dy, route.ids, self.q_copy, self.p_copy, h, dx, dx, self.dq,
                               self.dp, self.workspace, scale=self.scale, route=route.table)
         return dx

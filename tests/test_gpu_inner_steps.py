@@ -62,3 +62,92 @@ def test_a_step_that_is_left_out_does_not_count(bits, how):
     assert opt.taken() == 2
     opt.reset()
     assert opt.taken() == 0
+
+
+def test_an_optimizer_made_on_one_stream_steps_on_another():
+    gen = torch.Generator().manual_seed(7)
+    start, grad = (torch.randn(50001, generator=gen).to(DEV) for _ in range(2))
+    reference, buf = start.clone(), grad.clone()
+    opt = inner.AdamW([reference], [buf], 1e-2, max_norm=0.5)
+    for _ in range(3):
+        opt.step()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    param, buf = start.clone(), grad.clone()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)  # what follows on this stream is late
+    opt = inner.AdamW([param], [buf], 1e-2, max_norm=0.5)
+    opt.step(stream=streams[0])
+    with torch.cuda.stream(streams[0]):
+        torch.cuda._sleep(100_000_000)
+    opt.step(stream=streams[1].cuda_stream)
+    opt.step()
+    assert torch.equal(param, reference) and opt.taken() == 3
+    with torch.cuda.stream(streams[1]):
+        torch.cuda._sleep(100_000_000)
+        opt.step()
+    opt.reset()
+    assert not opt.moments[0]["m"].any() and not opt.moments[0]["v"].any()
+
+
+@pytest.mark.parametrize("late", ["route", "use"])
+def test_a_route_made_on_one_stream_serves_another(late):
+    gen = torch.Generator().manual_seed(8)
+    rnd = lambda *s: torch.randn(*s, generator=gen).to(DEV)  # noqa: E731
+    m, n, K, r, rows = 128, 192, 3, 32, 700
+    proj = inner.AdapterProjection(0.1 * rnd(m, n), rnd(K, r, n), 1.0, rows, torch.float32)
+    proj.p.copy_(rnd(K, r, m))
+    x, dy = rnd(rows, n), rnd(rows, m)
+    ids = torch.randint(0, K, (rows,), generator=gen).to(torch.int32).to(DEV)
+    route = inner.Route(ids, K)
+    y, h = proj.forward(x, route)
+    dx = proj.backward(x, h, dy, route)
+    grads = proj.dq.clone(), proj.dp.clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    if late == "route":
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(200_000_000)
+        route = inner.Route(ids, K, stream=side)
+        y2, h2 = proj.forward(x, route)
+        dx2 = proj.backward(x, h2, dy, route)
+    else:
+        torch.cuda._sleep(200_000_000)
+        route = inner.Route(ids, K)
+        with torch.cuda.stream(side):
+            y2, h2 = proj.forward(x, route)
+            dx2 = proj.backward(x, h2, dy, route)
+        torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip((y, h, dx) + grads, (y2, h2, dx2, proj.dq, proj.dp)):
+        assert torch.equal(a, b)
+
+
+def test_steps_and_routes_are_captured_into_a_graph():
+    gen = torch.Generator().manual_seed(9)
+    rnd = lambda *s: torch.randn(*s, generator=gen).to(DEV)  # noqa: E731
+    m, n, K, r, rows = 64, 64, 2, 32, 400
+    proj = inner.AdapterProjection(0.1 * rnd(m, n), rnd(K, r, n), 1.0, rows, torch.float32)
+    proj.p.copy_(rnd(K, r, m))
+    route = inner.Route((torch.arange(rows, device=DEV) % K).to(torch.int32), K)
+    x = rnd(rows, n)
+    param, grad = rnd(5000), rnd(5000)
+    opt = inner.AdamW([param], [grad], 1e-2, max_norm=0.5)
+    first = param.clone()
+    y, _ = proj.forward(x, route)
+    opt.step()
+    want = param.clone()
+    graph = torch.cuda.CUDAGraph()
+    opt.reset()
+    with torch.cuda.graph(graph):
+        y2, _ = proj.forward(x, route)
+        opt.step()
+    for _ in range(3):
+        param.copy_(first)
+        for t in opt.moments[0].values():
+            t.zero_()
+        y2.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(param, want) and torch.equal(y, y2)
+    assert opt.taken() == 1
