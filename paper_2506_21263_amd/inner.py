@@ -135,21 +135,34 @@ class AdamW:
 
 class AdapterProjection:
     """One projection y = x theta^T with an adapter per worker.  q0: count x r x n draws; P starts at zero,
-    so a new adapter changes nothing.  Masters are fp32; the products read copies in `dtype`."""
+    so a new adapter changes nothing.  Masters are fp32; the products read copies in `dtype`.
+
+    An optimizer's tensors begin at 16 bytes, so where r x m or r x n elements are not whole 16 bytes, the factors are
+    stored with up to seven more columns, which `ranks` leaves out of every product: p, q, dp and dq are the first r,
+    h has the stored ones."""
 
     def __init__(self, theta_g, q0, scale, max_rows, dtype=torch.bfloat16):
         self.m, self.n = theta_g.shape
         self.count, self.r = q0.shape[:2]
         dev = theta_g.device
         low = dtype == torch.bfloat16
-        self.d = adapter_desc(self.m, self.n, self.r, self.count, BF16 if low else F32)
+        whole = 8 if low else 4  # elements of 16 bytes
+        stored = self.r
+        while self.count > 1 and (stored * self.m % whole or stored * self.n % whole):
+            stored += 1
+        self.d = adapter_desc(self.m, self.n, stored, self.count, BF16 if low else F32)
+        self.ranks = None if stored == self.r else torch.full((self.count,), self.r, device=dev, dtype=torch.int32)
         self.dtype, self.q0 = dtype, q0
         self.base = theta_g.to(dtype)
-        self.q = q0.clone()
-        self.p = torch.zeros(self.count, self.r, self.m, device=dev)
-        self.q_copy = self.q.to(dtype) if low else self.q
-        self.p_copy = self.p.to(dtype) if low else self.p
-        self.dq, self.dp = torch.zeros_like(self.q), torch.zeros_like(self.p)
+        zeros = lambda k, dt=torch.float32: torch.zeros(self.count, stored, k, device=dev, dtype=dt)  # noqa: E731
+        self.stored = {name: zeros(k) for name, k in (("q", self.n), ("p", self.m), ("dq", self.n), ("dp", self.m))}
+        for name, k in (("q", self.n), ("p", self.m)):
+            self.stored[name + "_copy"] = zeros(k, dtype) if low else self.stored[name]
+        self.q, self.p, self.dq, self.dp, self.q_copy, self.p_copy = (
+            self.stored[name][:, :self.r] for name in ("q", "p", "dq", "dp", "q_copy", "p_copy"))
+        self.q.copy_(q0)
+        if low:
+            self.q_copy.copy_(q0)
         self.scale_value = scale
         self.scale = torch.full((self.count,), scale, device=dev)
         self.workspace = torch.empty(dlcx_adapter_workspace_bytes(self.d, max_rows), device=dev,
@@ -163,17 +176,18 @@ class AdapterProjection:
     def forward(self, x, route):
         y = x @ self.base.t()
         route.order.enter(None, [route.table])
-        h = torch.empty(x.shape[0], self.r, device=x.device)
-        dlcx_adapter_forward(self.d, x, route.ids, self.q_copy, self.p_copy, y, y, h, self.workspace,
-                             scale=self.scale, route=route.table)
+        h = torch.empty(x.shape[0], self.d.r, device=x.device)
+        dlcx_adapter_forward(self.d, x, route.ids, self.stored["q_copy"], self.stored["p_copy"], y, y, h,
+                             self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
         return y, h
 
     def backward(self, x, h, dy, route):
         """dx; the gradients of the factors are left in dq and dp."""
         dx = dy @ self.base
         route.order.enter(None, [route.table])
-        dlcx_adapter_backward(self.d, x, dy, route.ids, self.q_copy, self.p_copy, h, dx, dx, self.dq,
-                              self.dp, self.workspace, scale=self.scale, route=route.table)
+        dlcx_adapter_backward(self.d, x, dy, route.ids, self.stored["q_copy"], self.stored["p_copy"], h, dx, dx,
+                              self.stored["dq"], self.stored["dp"], self.workspace, scale=self.scale,
+                              ranks=self.ranks, route=route.table)
         return dx
 
     def fold_workspace_bytes(self, group, mma):

@@ -151,3 +151,41 @@ def test_steps_and_routes_are_captured_into_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(param, want) and torch.equal(y, y2)
     assert opt.taken() == 1
+
+
+@pytest.mark.parametrize("bits,dtype", [(32, torch.float32), (8, torch.float32), (32, torch.bfloat16), (8, torch.bfloat16)],
+                         ids=str)
+@pytest.mark.parametrize("m,n,K,r", [(51, 35, 3, 5), (1021, 2050, 2, 33), (64, 66, 4, 1), (17, 19, 1, 3), (33, 37, 2, 255)])
+def test_optimizers_of_adapters_of_any_size(m, n, K, r, bits, dtype):
+    gen = torch.Generator().manual_seed(m)
+    rnd = lambda *s: torch.randn(*s, generator=gen)  # noqa: E731
+    rows = 40
+    theta, q0, p0, x, dy = 0.1 * rnd(m, n), rnd(K, r, n) / n ** 0.5, rnd(K, r, m) * 0.1, rnd(K * rows, n), rnd(K * rows, m)
+    proj = inner.AdapterProjection(theta.to(DEV), q0.to(DEV), 2.0, K * rows, dtype)
+    proj.p.copy_(p0)
+    proj.p_copy.copy_(p0)
+    route = inner.Route((torch.arange(K * rows) // rows).to(torch.int32).to(DEV), K)
+    opts = [inner.AdamW(*(lambda p, g, c: (p, g, 1e-2, (0.9, 0.95), 1e-8, None, c, bits))(*proj.parameters(a)))
+            for a in range(K)]
+    xd, dyd = x.to(DEV).to(dtype), dy.to(DEV).to(dtype)
+    y, h = proj.forward(xd, route)
+    dx = proj.backward(xd, h, dyd, route)
+    for o in opts:
+        o.step()
+    # a few roundings to bf16 of operands and results, or sums of fp32
+    tol = 2e-2 if dtype == torch.bfloat16 else 1e-5
+    close = lambda g, v: float((g.double().cpu() - v).norm()) <= tol * float(v.norm())  # noqa: E731
+    for a in range(K):
+        at = slice(a * rows, (a + 1) * rows)
+        p, q, w = p0[a].to(dtype).double(), q0[a].to(dtype).double(), theta.to(dtype).double() + 0
+        xa, da = x[at].to(dtype).double(), dy[at].to(dtype).double()
+        g = 2.0 * da @ p.t()
+        assert close(y[at], xa @ w.t() + 2.0 * (xa @ q.t()) @ p) and close(dx[at], da @ w + g @ q)
+        assert close(proj.dq[a], g.t() @ xa) and close(proj.dp[a], 2.0 * (xa @ q.t()).t() @ da)
+        for master, copy, start, grad in ((proj.p[a], proj.p_copy[a], p0[a], proj.dp[a]), (proj.q[a], proj.q_copy[a], q0[a], proj.dq[a])):
+            step = grad.double().cpu()
+            want = start.double() - 1e-2 * step / (step.abs() + 1e-8)  # the first step of AdamW
+            assert float((master.double().cpu() - want).abs().max()) < 2e-6
+            assert torch.equal(copy, master.to(dtype))
+    for t in proj.stored.values():
+        assert not t[:, r:].any()  # nothing in the columns that are only stored
