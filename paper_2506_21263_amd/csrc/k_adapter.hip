@@ -1174,11 +1174,6 @@ static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st)
     return check_launch("adapter_down");
 }
 
-// A row to a workgroup reads the factors once a row, from L2 where rows share an adapter; tiles read them once for
-// 16 rows or more, but take two launches more and the sorting.  Measured at 8192 x 8192 (rows / tiles, us): rank 16
-// 64 rows 8.4 / 18.8, 256 rows 19.9 / 19.9, rank 64 64 rows 15.6 / 21.9, 128 rows 26 / 22.5, rank 256 16 rows
-// 20.8 / 28.6, 64 rows 47 / 39.
-static bool few_rows(int64_t rows, int r) { return rows * r <= 4096; }
 // Few rows in one launch, where forming h in every workgroup costs less than a second launch: Q_a up to 300 KB, read by all
 // workgroups together up to 20 MB, and not more of them than the GPU holds at once.  us alone on the GPU and called from
 // the host, in two launches -> one: 1 row of 2048 + 2048 columns at rank 8: 6.6, 13 -> 4.6, 10; 128 rows of 64 adapters
@@ -1188,6 +1183,40 @@ template <typename T>
 static bool one_launch(int64_t rows, int r, int64_t n, int64_t m) {
     const int64_t bytes = r * n * (int64_t)sizeof(typename T::elem), groups = rows * ceil_div(m, kRowCols);
     return bytes <= 300000 && groups <= 512 && groups * bytes <= 20000000;
+}
+
+// A row to a workgroup: its time grows with rows x (16 + r) (the matrix instructions take 16 rows at least) and the bytes of a
+// row, of which those of an fp32 row count half as much again in the first product and two thirds in the second.  Tiles read
+// a factor once for 16 rows or more, but take two launches more, the sorting, and a tile with its columns' blocks for every
+// adapter that has rows; which have is known on the device alone, so `count` stands for it, up to 64.  Both sides in us,
+// rows / tiles, of one adapter and of 64:
+//   8192 x 8192 bf16, forward    rank 1   256 rows 15 / 20, 15 / 33    1024 rows 46 / 28, 47 / 40
+//                                rank 16  128 rows 13 / 20, 15 / 34     512 rows 37 / 22, 40 / 40
+//                                rank 64   64 rows 17 / 23, 23 / 40     256 rows 50 / 24, 62 / 49
+//                     backward   rank 1   128 rows 27 / 28, 31 / 44     256 rows 35 / 31, 38 / 47
+//                                rank 64   32 rows 30 / 31, 88 / 93     128 rows 56 / 42, 130 / 134
+//   8192 x 8192 fp32, forward    rank 8   128 rows 18 / 23, 20 / 53     512 rows 54 / 32, 55 / 60
+//   2048 x 2048 bf16, forward    rank 16  512 rows 14 / 21, 14 / 23    1024 rows 23 / 22, 25 / 25
+//   28672 x 8192 bf16, forward   rank 16  128 rows 21 / 22, 28 / 72     512 rows 68 / 34, 78 / 90
+// Of 760 calls timed in both forms (64 x 64 to 8192 x 8192, ranks 1 to 64, 16 to 4096 rows, both types) the rule takes the
+// slower one by more than an eighth in six.
+constexpr int64_t kRowsForward = 250000000, kRowsBackward = 75000000;
+template <typename T>
+static bool few_rows(int64_t rows, const dlcx_adapter_desc &d, int64_t down, int64_t up, int64_t most) {
+    const bool low = T::lane == 8;
+    const int64_t one = low ? 2 * (down + up) : 6 * down + 8 * up / 3;
+    const int64_t n = rows < 64 ? rows : 64, adapters = d.count < n ? d.count : n;
+    return rows <= 4096 &&  // (the launch has them along y)
+           rows * (16 + d.r) * (one > 4800 ? one : 4800) <= most + adapters * 188 * up * (low ? 2 : 4);
+}
+
+template <typename T>
+static bool forward_by_rows(int64_t rows, const dlcx_adapter_desc &d) {
+    return one_launch<T>(rows, d.r, d.n, d.m) || few_rows<T>(rows, d, d.n, d.m, kRowsForward);
+}
+template <typename T>
+static bool backward_by_rows(int64_t rows, const dlcx_adapter_desc &d) {
+    return few_rows<T>(rows, d, d.m, d.n, kRowsBackward);
 }
 
 template <typename T>
@@ -1435,7 +1464,7 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
     AdapterSpace s;
     adapter_space(desc, rows, workspace, &s);
     const DownArgs down = {x, pitch(ldx), q, ranks, nullptr, 0, (int)desc->n, desc->r, 1};
-    if (few_rows(rows, desc->r)) {
+    if (desc->dtype == DLCX_BF16 ? forward_by_rows<Bf16>(rows, *desc) : forward_by_rows<F32>(rows, *desc)) {
         const RowsArgs a = {nullptr, 0, 0, ids, ranks, scale, p, y_in, y_out, h_out, pitch(ldy_in), pitch(ldy_out),
                             (int)desc->m, desc->r, desc->count};
         return desc->dtype == DLCX_BF16 ? down_and_rows<Bf16>(down, a, rows, nullptr, s, st)
@@ -1483,7 +1512,7 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
     else if ((rc = launch_route(rows, ids, s.route, st)) != DLCX_OK)
         return rc;
     if (rows > 0) {
-        const bool low = desc->dtype == DLCX_BF16, few = few_rows(rows, desc->r);
+        const bool low = desc->dtype == DLCX_BF16, few = low ? backward_by_rows<Bf16>(rows, *desc) : backward_by_rows<F32>(rows, *desc);
         const DownArgs down = {dy, pitch(lddy), p, ranks, nullptr, 0, (int)desc->m, desc->r, 1};
         const OperandJob g = {nullptr, 0, 0, few ? 0 : 1, scale, scale, nullptr, nullptr, s.turned_g};
         const OperandJob hj = {h, 0, 1, 0, nullptr, nullptr, nullptr, nullptr, s.turned_h};
