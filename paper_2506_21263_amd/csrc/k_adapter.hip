@@ -43,6 +43,11 @@ __device__ __forceinline__ int scan_wave(int x) {
     return x;
 }
 
+// A launch has at most 2^32 threads along x: workgroups beyond kGroupsX go on along the dimension that a kernel leaves free.
+constexpr int64_t kGroupsX = 1 << 22;
+static inline unsigned groups_x(int64_t groups) { return (unsigned)(groups < kGroupsX ? groups : kGroupsX); }
+static inline unsigned groups_on(int64_t groups) { return (unsigned)ceil_div(groups, kGroupsX); }
+
 struct Tile {
     int adapter;  // -1: rows without one; -2: there is no such tile
     int at, rows; // places in `order`
@@ -412,7 +417,7 @@ struct DownArgs {
     const int32_t *ranks;
     float *out;          // places x r, columns below the adapter's rank; shares of the reduction `stride` floats apart
     int64_t stride;
-    int len, r, shares;
+    int len, r, shares, tiles;
 };
 
 // A workgroup has a share of the reduction (its eight wavefronts 256 to 512 bytes of it each), CT x 16 columns and
@@ -458,8 +463,10 @@ __global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapt
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
     __shared__ f32x4_t sums[2][kDownWaves][CT][64];
-    const int share = (int)(blockIdx.x % (uint32_t)a.shares);
-    const Tile tile = find_tile<true>(route, size, (int)(blockIdx.x / (uint32_t)a.shares));
+    const uint32_t group = blockIdx.x + blockIdx.z * (uint32_t)kGroupsX;
+    const int share = (int)(group % (uint32_t)a.shares), index = (int)(group / (uint32_t)a.shares);
+    if (index >= a.tiles) return;
+    const Tile tile = find_tile<true>(route, size, index);
     if (tile.adapter < 0) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, row16 = lane & 15, quad = lane >> 4;
@@ -694,8 +701,9 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * T::pieces * sizeof(typename T::
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
     Frag *blocks = reinterpret_cast<Frag *>(up_lds);  // [step][tile of columns][lane]
-    const uint32_t block = blockIdx.x % (uint32_t)a.blocks;
-    const Tile tile = find_tile<true>(route, size, (int)(blockIdx.x / (uint32_t)a.blocks));
+    const uint32_t group = blockIdx.x + blockIdx.y * (uint32_t)kGroupsX;
+    const uint32_t block = group % (uint32_t)a.blocks;
+    const Tile tile = find_tile<true>(route, size, (int)(group / (uint32_t)a.blocks));  // (beyond the last: none)
     if (tile.adapter < (a.copy ? -1 : 0)) return;
     const int32_t *__restrict__ order = route.order + tile.at;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, row16 = lane & 15, quad = lane >> 4;
@@ -1163,10 +1171,11 @@ static int launch_down(DownArgs a, int64_t rows, const Route &v, hipStream_t st)
     const int64_t most = ceil_div(512, splits * cols), spare = v.count < most ? v.count / 2 : most / 2;
     int64_t fit = ceil_div(ceil_div(rows, most > spare ? most - spare : 1), 16) * 16;
     const int size = (int)(fit < kDownRows ? fit : kDownRows);
-    const int64_t groups = splits * (v.ids ? rows : max_tiles(rows, v.count, size));
+    const int64_t tiles = v.ids ? rows : max_tiles(rows, v.count, size), groups = splits * tiles;
     if (groups > 0x7FFFFFFF) return DLCX_EINVAL;
     a.shares = splits;
-    const dim3 grid((unsigned)groups, (unsigned)cols);
+    a.tiles = (int)tiles;
+    const dim3 grid(groups_x(groups), (unsigned)cols, groups_on(groups));
     Timed timed(KID_ADAPTER_DOWN, st);
     if (ct == 4) down_kernel<T, 4>(a, vec, grid, v, size, st);
     else if (ct == 2) down_kernel<T, 2>(a, vec, grid, v, size, st);
@@ -1228,7 +1237,7 @@ static int launch_operands(const OperandArgs &a, int jobs, int64_t rows, const R
 }
 
 template <typename T, int KT, int VEC>
-static int up_kernel(const UpArgs &a, unsigned grid, const Route &v, int size, hipStream_t st) {
+static int up_kernel(const UpArgs &a, dim3 grid, const Route &v, int size, hipStream_t st) {
     const size_t lds = (size_t)KT * T::lane * 64 * sizeof(typename T::Frag);
     static size_t granted = 0;
     const int rc = grant_dynamic_lds((const void *)adapter_up_kernel<T, KT, VEC>, lds, &granted, "adapter_up lds");
@@ -1238,7 +1247,7 @@ static int up_kernel(const UpArgs &a, unsigned grid, const Route &v, int size, h
     return check_launch("adapter_up");
 }
 template <typename T, int KT>
-static int up_kernel(const UpArgs &a, int vec, unsigned grid, const Route &v, int size, hipStream_t st) {
+static int up_kernel(const UpArgs &a, int vec, dim3 grid, const Route &v, int size, hipStream_t st) {
     return vec == kStream    ? up_kernel<T, KT, kStream>(a, grid, v, size, st)
            : vec == kAligned ? up_kernel<T, KT, kAligned>(a, grid, v, size, st)
                              : up_kernel<T, KT, kAnywhere>(a, grid, v, size, st);
@@ -1255,7 +1264,7 @@ static int launch_up(UpArgs a, int64_t rows, const Route &v, hipStream_t st) {
     const int64_t groups = cols * max_tiles(rows, v.count, size);
     if (groups > 0x7FFFFFFF) return DLCX_EINVAL;
     a.blocks = (int)cols;
-    const unsigned grid = (unsigned)groups;
+    const dim3 grid(groups_x(groups), groups_on(groups));
     switch (up_steps(a.r)) {
     case 1: return up_kernel<T, 1>(a, vec, grid, v, size, st);
     case 2: return up_kernel<T, 2>(a, vec, grid, v, size, st);
@@ -1463,7 +1472,7 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
     auto pitch = [es](int64_t ld) { return (uint32_t)(ld * es); };
     AdapterSpace s;
     adapter_space(desc, rows, workspace, &s);
-    const DownArgs down = {x, pitch(ldx), q, ranks, nullptr, 0, (int)desc->n, desc->r, 1};
+    const DownArgs down = {x, pitch(ldx), q, ranks, nullptr, 0, (int)desc->n, desc->r, 1, 0};
     if (desc->dtype == DLCX_BF16 ? forward_by_rows<Bf16>(rows, *desc) : forward_by_rows<F32>(rows, *desc)) {
         const RowsArgs a = {nullptr, 0, 0, ids, ranks, scale, p, y_in, y_out, h_out, pitch(ldy_in), pitch(ldy_out),
                             (int)desc->m, desc->r, desc->count};
@@ -1513,7 +1522,7 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
         return rc;
     if (rows > 0) {
         const bool low = desc->dtype == DLCX_BF16, few = low ? backward_by_rows<Bf16>(rows, *desc) : backward_by_rows<F32>(rows, *desc);
-        const DownArgs down = {dy, pitch(lddy), p, ranks, nullptr, 0, (int)desc->m, desc->r, 1};
+        const DownArgs down = {dy, pitch(lddy), p, ranks, nullptr, 0, (int)desc->m, desc->r, 1, 0};
         const OperandJob g = {nullptr, 0, 0, few ? 0 : 1, scale, scale, nullptr, nullptr, s.turned_g};
         const OperandJob hj = {h, 0, 1, 0, nullptr, nullptr, nullptr, nullptr, s.turned_h};
         if (few) {
