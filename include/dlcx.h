@@ -359,7 +359,12 @@ int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const voi
  *   sqrt(v) = c^2 v_scale,   c = 0 .. 255 (uint8),      v_scale = largest sqrt(v) of the group / 255^2
  * (squares of the codes: steps that shrink with the value, from 2/127 or 2/255 of the largest one near it
  * to 1/127^2 or 1/255^2 of it near zero; c of v is at least 1 where v > 0, so that a small v never turns
- * into a zero denominator).  copy (bf16, fp32 parameters only) or NULL receives the updated
+ * into a zero denominator).  Codes are the nearest ones, so one stays where a step moves it by less than a half: without
+ * gradient, and while the largest of its group stays, a code of m below 0.5 / (1 - beta1^(1/2)) and one of v below
+ * 0.5 / (1 - beta2^(1/4)) fall no further.  At beta1 = 0.9 m ends at 9^2/127^2 = 0.5 % of the group's largest; at
+ * beta2 = 0.95 sqrt(v) ends at 39^2/255^2 = 2.3 % of it, at 0.99 at 61 %, and from 0.9922 on no v falls but with its group's
+ * largest: where gradients of a group fade unevenly, beta2 = 0.999 wants moments of 32 bits.  Gradients that keep
+ * their distribution are followed at 0.999 as well, to 18 % of sqrt(v) in nine of ten elements (5 % at 0.95).  copy (bf16, fp32 parameters only) or NULL receives the updated
  * parameter rounded.  All but the scales are 16-byte aligned.  For dlcx_grad_norm alone, param NULL
  * and the rest ignored. */
 typedef struct {

@@ -68,7 +68,8 @@ class Route:
 class AdamW:
     """AdamW over a list of parameters with given gradient buffers: moments of 32 or 8 bits, clipping
     by the gradients' own norm (max_norm > 0), bf16 copies of fp32 parameters where wanted.
-    decays[i] is the weight decay of parameter i.
+    decays[i] is the weight decay of parameter i.  Moments of 8 bits (nearest codes) do not follow gradients of a
+    group of 128 that fade unevenly at betas[1] above 0.992: that wants bits=32.
 
     With clipping, a step whose norm is not finite leaves everything as it was, and does not count: `step` looks at
     the norm of the step before, which the GPU has long formed by then, `taken` at the last one's.  (Steps that
