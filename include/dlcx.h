@@ -343,7 +343,8 @@ int dlcx_adapter_forward(const dlcx_adapter_desc *desc, int64_t rows, const void
  *   dp_out[a][c][j] = scale[a] times the sum over the same rows of h[t][c] dy[t][j]
  * dx_in (what the projection itself gives) may be dx_out, or NULL for zeros; dq_out (count x r x n) and
  * dp_out (count x r x m) are fp32 and overwritten, with zeros from column ranks[a] on and for adapters
- * without rows.  The order of a sum hangs on rows, count, sizes and the rows' ids alone.  bf16: as above;
+ * without rows.  The order of a sum, here and above, hangs on rows, count, sizes, the rows' ids and, in bf16, on whether
+ * rows and factors are read by 16 aligned bytes (addresses, strides and lengths of whole 16 bytes).  bf16: as above;
  * every product takes g and h in three pieces. */
 int dlcx_adapter_backward(const dlcx_adapter_desc *desc, int64_t rows, const void *x, int64_t ldx,
                           const void *dy, int64_t lddy, const int32_t *ids, const void *q,
