@@ -681,9 +681,10 @@ struct UpArgs {
 // 4 (l / 16) + 0 .. 3 and 16 bytes of each, so that 16 lanes make 256 in a row.  (With a row to
 // every lane of 16 an access is 64 pieces for the L1, not 16: 128 us for 16384 x 8192 at rank 64.)  HBM
 // bounds it: 120 us where it leaves grad its rows, 4.5 TB/s.  bf16: scale h comes in all three of its pieces, so that a
-// row's result does not hang on the form that its number of rows takes; rounded to one piece it is 112 us, and at rank 256
-// (4133 rows) 54 instead of 104.  The pieces lie as the products take them: 1 KB of a row's own cache lines to a request,
-// where a row to each of 16 lanes took 128 us.
+// row's result does not hang on the form that its number of rows takes; rounded to one piece it is 112 us.  The pieces lie
+// as the products take them, 1 KB of consecutive memory to a request, where a row to each of 16 lanes took 128 us.  Above rank
+// 128 they take 96 registers: one workgroup to a compute unit, 91 us for 4133 rows at rank 256 where two, which spill, take
+// 111 (and one piece 54); up to there two, and three are no faster.
 constexpr int kUpWaves = 4;
 template <typename T, int VEC>
 struct UpRows {
@@ -696,7 +697,7 @@ struct UpRows {
     }
 };
 template <typename T, int KT, int VEC>
-__global__ __launch_bounds__(kUpWaves * 64, KT * T::pieces * sizeof(typename T::Frag) <= 96 ? 3 : 2) void adapter_up_kernel(UpArgs a, Route route, int size) {
+__global__ __launch_bounds__(kUpWaves * 64, KT * T::pieces * sizeof(typename T::Frag) <= 192 ? 2 : 1) void adapter_up_kernel(UpArgs a, Route route, int size) {
     extern __shared__ __attribute__((aligned(16))) char up_lds[];
     typedef typename T::Frag Frag;
     typedef typename T::elem elem;
