@@ -213,9 +213,10 @@ __device__ __forceinline__ ab_u32x4 load_any(const void *p) {
 
 // How rows are read and written: element by element where they begin anywhere, by 16 aligned bytes, or by these and past
 // the caches' order of use, for matrices of kStreamed bytes and more that pass by once.  A backward pass beside
-// 8192 + 8192 columns at rank 64, plain -> streamed, us: 16384 rows (268 MB a matrix) 339 -> 327 (down 73 -> 69, up 103 ->
-// 112, grad 146 -> 133: more of the rows of one product is in the cache for the next), 2000 rows (33 MB) 79 -> 77, 515
-// rows (8 MB) 56 -> 58; 4133 rows forward 76 -> 68.
+// 8192 + 8192 columns at rank 64, plain -> streamed, us: 16384 rows (268 MB a matrix) 350 -> 343 (down 74 -> 70, up 117 ->
+// 120, grad 140 -> 132: more of the rows of one product is in the cache for the next), 2000 rows (33 MB) 80 -> 80; 4133 rows
+// forward 80 -> 74.  Above 64 columns of a factor down and grad read the rows again for the next 64, plainly: 4133 rows at
+// rank 256, streamed -> plain, down 74 -> 62, grad 201 -> 173.
 constexpr int kAnywhere = 0, kAligned = 1, kStream = 2;
 constexpr int64_t kStreamed = 24000000;
 template <bool STREAM>
@@ -1157,7 +1158,7 @@ static void down_kernel(const DownArgs &a, int vec, dim3 grid, const Route &v, i
         return;
     }
     if constexpr (T::lane == 8)  // (fp32 rows: plain)
-        if (vec == kStream) {
+        if (vec == kStream && grid.y == 1) {
             adapter_down_kernel<T, CT, kStream><<<grid, kDownWaves * 64, 0, st>>>(a, v, size);
             return;
         }
@@ -1290,9 +1291,9 @@ static void grad_kernel(const GradArgs &a, int vec, dim3 grid, const Route &v, i
             adapter_grad_kernel<T, CT, kAligned, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
         else
             adapter_grad_kernel<T, CT, kAnywhere, 1><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
-    } else if (vec == kStream) {
+    } else if (vec == kStream && grid.z == 1) {
         adapter_grad_kernel<T, CT, kStream, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
-    } else if (vec == kAligned) {
+    } else if (vec != kAnywhere) {
         adapter_grad_kernel<T, CT, kAligned, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
     } else {
         adapter_grad_kernel<T, CT, kAnywhere, kGradWaves><<<grid, kGradWaves * 64, 0, st>>>(a, v, size);
