@@ -5,9 +5,9 @@
 // of a table: the elements are cut into blocks of kBlock, a tensor's last block may be shorter, and
 // table.start holds each tensor's first block, so a workgroup finds its tensor by searching there.
 //
-// Measured: AdamW with fp32 moments 5.3 TB/s (26.5 M fp32 elements in 140 tensors 148 us; 50 M with bf16
-// gradients 264 us), with 8-bit moments 5.6 TB/s (856 M bf16 elements 1.54 ms), where a copy of 2 GiB reaches
-// 4.9; the norm of 856 M bf16 gradients 257 us, 6.7 TB/s, of 26.5 M fp32 ones 20 + 3 us.
+// Measured: AdamW with fp32 moments 5.4 TB/s (26.5 M fp32 elements in 140 tensors 146 us; 50 M with bf16
+// gradients 262 us), with 8-bit moments 5.6 TB/s (856 M bf16 elements 1.54 ms), where a copy of 2 GiB reaches
+// 4.9; the norm of 856 M bf16 gradients 252 + 5 us, 6.7 TB/s, of 26.5 M fp32 ones 21 + 4 us.
 #include <math.h>
 
 #include "common.h"
@@ -101,10 +101,10 @@ template <int DT>
 struct Raw {
     uint32_t w[DT == DLCX_F32 ? kVec : kVec / 2];
 };
-// STREAM: past the caches' order of use.  Against plain loads: 8-bit moments 1.47 (1.61) ms; a norm of bf16 gradients,
+// STREAM: past the caches' order of use.  Against plain loads: 8-bit moments 1.56 (1.60) ms; a norm of bf16 gradients,
 // 1.7 GB 257 (303) us, 200 MB 34.9 (39.1); but of fp32 ones, which take twice the bytes a step, 1 GB 171 (169),
 // 300 MB that are read again 53 (47); and 32-bit moments, whose 12 or 14 bytes an element are read and written at
-// the same places, 155 (148) and 278 (264) us, so these two are plain.  Stores: all streamed, 1.47 (1.66) ms and
+// the same places, 155 (148) and 278 (264) us, so these two are plain.  Stores: all streamed, 1.56 (1.64) ms and
 // 278 (282) us.
 template <class T, bool STREAM>
 __device__ __forceinline__ T load_vector(AD_GLOBAL const T *p) {
@@ -235,7 +235,7 @@ __device__ __forceinline__ float group_scale(float amax, float top, float *inv) 
 }
 // The code of x >= 0 is the integer next to sqrt(x / scale), both operations rounded correctly, where x of a
 // second moment is a correctly rounded root itself.  With IEEE quotients and roots throughout the step was bound
-// by its arithmetic (4.2 TB/s; it still is, at 61 vector instructions an element).  So a code is taken from a product and the hardware's roots and reciprocals (1 unit in the
+// by its arithmetic (4.2 TB/s; it still is, at 64 vector instructions an element).  So a code is taken from a product and the hardware's roots and reciprocals (1 unit in the
 // last place), together off by 1e-4 codes at most, and only where that lies within 1.25e-4 of the middle between
 // two codes is it decided by the definition: one code in 4000, hardly ever two of a thread's sixteen.
 __device__ __forceinline__ float near_root(float x, float inv) { return __builtin_amdgcn_sqrtf(x * inv); }
@@ -391,7 +391,7 @@ __device__ __forceinline__ void adamw_elements(const dlcx_tensor &t, const Adamw
 }
 
 // A workgroup has 1 / PARTS of a block: with 32-bit moments one step, 264 us for the 50 M elements against 274 with
-// two, one after the other; with 8-bit ones two, 1.47 ms against 1.54, since what every thread does before its
+// two, one after the other; with 8-bit ones two, 1.56 ms against 1.61, since what every thread does before its
 // first element is worth the arithmetic of one.  A table with both kinds takes two launches.
 constexpr int kParts32 = 2, kParts8 = 1;
 template <int BITS, int PARTS>

@@ -98,7 +98,9 @@ __device__ __forceinline__ Tile find_tile(const Route &r, int size, int index) {
 // One workgroup sorts the rows by counting: every wavefront counts its own share, the counts become the
 // places where it writes, and the lanes of equal adapters find their order by ballots of the index's
 // bits, so the order within an adapter is that of the rows.  It runs alone, so the loops are kept short: the code
-// of an unrolled one came from memory for longer than it ran (16384 rows 18 us, now 12).
+// of an unrolled one came from memory for longer than it ran (16384 rows, one adapter after the other, 18 us, now 10).
+// One workgroup at any size: rows in any order of 64 adapters take 26 us for 16384, 1.5 ms for 2^20 (one after the other
+// 0.4), where the rows themselves, beside 8192 x 8192 in bf16, take 10 ms to read and write.
 __global__ __launch_bounds__(kRouteThreads) void adapter_route_kernel(int rows,
                                                                       const int32_t *__restrict__ ids, Route r) {
     extern __shared__ int cursor[];  // kRouteWaves x buckets, then kRouteKept buckets of every wavefront's rows
@@ -426,7 +428,7 @@ struct DownArgs {
 // at a time; the eight sums are joined in LDS, in turn in two places, so that one barrier a round is enough.
 // With whole rows to a workgroup instead, the factor comes from L2 as often as there are tiles of
 // rows, by the same few channels at a time: 91 us for 16384 x 8192 bf16 at rank 64, 88 us for 4133 rows.
-// This form: 69 us (3.9 TB/s of rows, and 34 MB of shares) and 25 us.
+// This form: 66 us (4.1 TB/s of rows, and 34 MB of shares) and 22 us.
 // In bf16 a load has 256 bytes of each of four rows, neighbouring lanes the same row; the four loads of sixteen rows
 // then change places within four lanes, into the layout of the matrix instructions.  With one row to each of 16
 // lanes instead (as fp32 rows are read): 79 and 31 us.
@@ -584,7 +586,7 @@ __global__ __launch_bounds__(kDownWaves * 64, CT == 4 && VEC ? 4 : 2) void adapt
 
 // ---- operands ---------------------------------------------------------------------------------------
 // What the other two products read of h (or g): the sum of its splits, in 32 bits as it is and as two
-// operands, so that they are formed once and not by every workgroup that has other columns.  14 us for both of
+// operands, so that they are formed once and not by every workgroup that has other columns.  13 us for both of
 // 16384 rows at rank 64 (34 MB of shares, 4 of h, 19 of operands).
 struct OperandJob {
     const float *splits;  // r columns each, `stride` floats apart
@@ -806,7 +808,7 @@ __global__ __launch_bounds__(kUpWaves * 64, KT * T::pieces * sizeof(typename T::
 // ---- few rows -----------------------------------------------------------------------------------------
 // Where each row has an adapter of its own there is nothing to share: a workgroup has one row and 512 columns, its
 // wavefronts every fourth column of the factor, and h stays in 32 bits.  The shares of h are added by every
-// workgroup for itself.  96 rows of 64 adapters beside 28672 columns at rank 16: 14 us for 88 MB of factors.
+// workgroup for itself.  96 rows of 64 adapters beside 28672 columns of ranks 16 and 8: 13 us for 44 MB of factors and 11 of y.
 struct RowsArgs {
     const float *splits;  // rows x r, `stride` floats apart
     int64_t stride;
@@ -972,9 +974,9 @@ struct GradArgs {
 // ones requested before the products of these.  In long tiles the workgroup's wavefronts take rows in
 // turn and join their sums in LDS; in tiles of up to kGradShort rows there is little to share (79 rows of 57
 // adapters, rank 45, fp32: 82 us that way, 39 this) and each has columns of its own.
-// 16384 rows of 8192 + 8192 columns at rank 64: 133 us, 4.0 TB/s.  128 accumulators leave a wavefront registers for
-// one set of rows on its way, 64 KB a compute unit, which carries 4.1 TB/s; two thirds of the matrix products
-// (the second and third piece of h and g) cost 13 us of the 145.
+// 16384 rows of 8192 + 8192 columns at rank 64: 132 us, 4.1 TB/s.  128 accumulators leave a wavefront registers for
+// one set of rows on its way, and requests come back in order: the operands of all but a round's first product are asked
+// for behind the rows of the next round and wait for them.
 constexpr int kGradWaves = 4;
 struct RowIndex {
     int t[8];
