@@ -119,19 +119,18 @@ class AdamW:
 
     def step(self, stream=None):
         """One step, on `stream` (gradients and parameters have to be there) after whatever came before."""
-        stream = self.order.enter(stream, self.own)
-        self.t = self.taken() + 1
         clip = self.max_norm > 0
-        if clip:
-            dlcx_grad_norm(self.table, self.norm, stream=stream)
-        dlcx_adamw(self.table, self.lr, self.betas[0], self.betas[1], self.eps, self.t,
-                   norm=self.norm if clip else None, max_norm=self.max_norm, stream=stream)
-        if clip:
-            with torch.cuda.stream(stream):
-                if not torch.cuda.is_current_stream_capturing():
-                    self.norm_host.copy_(self.norm, non_blocking=True)
-                    self.norm_there = torch.cuda.Event()
-                    self.norm_there.record()
+        with torch.cuda.stream(self.order.enter(stream, self.own)):
+            capturing = torch.cuda.is_current_stream_capturing()  # where no event is waited for
+            self.t = (self.t if capturing else self.taken()) + 1
+            if clip:
+                dlcx_grad_norm(self.table, self.norm)
+            dlcx_adamw(self.table, self.lr, self.betas[0], self.betas[1], self.eps, self.t,
+                       norm=self.norm if clip else None, max_norm=self.max_norm)
+            if clip and not capturing:
+                self.norm_host.copy_(self.norm, non_blocking=True)
+                self.norm_there = torch.cuda.Event()
+                self.norm_there.record()
 
 
 class AdapterProjection:

@@ -189,3 +189,23 @@ def test_optimizers_of_adapters_of_any_size(m, n, K, r, bits, dtype):
             assert torch.equal(copy, master.to(dtype))
     for t in proj.stored.values():
         assert not t[:, r:].any()  # nothing in the columns that are only stored
+
+
+def test_a_step_is_captured_while_the_norm_of_the_last_one_is_on_its_way():
+    gen = torch.Generator().manual_seed(10)
+    start, grad = (torch.randn(5000, generator=gen).to(DEV) for _ in range(2))
+    param, buf = start.clone(), grad.clone()
+    opt = inner.AdamW([param], [buf], 1e-2, max_norm=0.5)
+    for _ in range(3):
+        opt.step()
+    want = param.clone()
+    param, buf = start.clone(), grad.clone()
+    opt = inner.AdamW([param], [buf], 1e-2, max_norm=0.5)
+    opt.step()
+    assert opt.norm_there is not None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    graph.replay()
+    opt.step()
+    assert torch.equal(param, want) and opt.taken() == 3
