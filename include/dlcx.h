@@ -411,6 +411,72 @@ int dlcx_adamw(const dlcx_table *table_host, double lr, double beta1, double bet
 int dlcx_state_decode(int second, const void *codes, const float *scales, int64_t numel, void *out,
                       int out_dtype, void *stream);
 
+/* ---- the shared projection in 8 bits, the norm before it, and dropout -----------------------------------
+ *
+ * What else an inner step or a request does around the adapters: the shared projection itself with theta_g kept
+ * in 8 bits (one byte and one 128th of one for an element, read once for all workers), the norm of its inputs, and
+ * the dropout of what the adapters read.
+ *
+ * A matrix of rows x cols in 8 bits: e4m3 codes (largest 448), row-major, `ld` bytes between rows; a row's codes are
+ * padded with zeros to a multiple of 128 (dlcx_fp8_code_pitch(cols) bytes).  One byte s for every 128 consecutive
+ * elements of a row, `ldscale` bytes between rows, padded to a multiple of 4 (dlcx_fp8_scale_pitch(cols)):
+ * value = code * 2^(s - 127).  codes and ld are multiples of 16, scales and ldscale of 4; strides up to 2^29.  rows and
+ * cols 0 .. 2^24 each.  s is 0 .. 254 (255 makes a product's row NaN); the pad of the scales is not read as one. */
+typedef struct {
+    void *codes, *scales;
+    int64_t rows, cols, ld, ldscale;
+} dlcx_fp8;
+int64_t dlcx_fp8_code_pitch(int64_t cols);
+int64_t dlcx_fp8_scale_pitch(int64_t cols);
+
+/* x (rows x cols, DLCX_F32 or DLCX_BF16, ldx elements between rows) to 8 bits: `out` (rows x cols) with a scale for 128
+ * elements of a row, `out_t` (cols x rows), its transpose, with a scale for 128 elements of that one's rows; either
+ * may be NULL.  square: one scale for every 128 x 128 elements, so that out and out_t hold the same values.  A block's
+ * scale is the smallest power of two (from 2^-127; 1 for a block of zeros) that lets its largest finite magnitude be at
+ * most 448 of it; codes are rounded to nearest, ties to even.  Infinities and NaN become NaN. */
+int dlcx_fp8_quantize(int64_t rows, int64_t cols, const void *x, int64_t ldx, int dtype, int square,
+                      const dlcx_fp8 *out, const dlcx_fp8 *out_t, void *stream);
+
+/* What the codes stand for (bf16 holds it exactly in its range). */
+int dlcx_fp8_decode(const dlcx_fp8 *a, void *out, int64_t ldo, int out_dtype, void *stream);
+
+/* y_out = y_in + x w^T: x is rows x n, w m x n, both in 8 bits; y is rows x m, DLCX_F32 or DLCX_BF16.  y_in may be y_out,
+ * or NULL for zeros.  DLCX_F32: fp32 sums of exact products.  DLCX_BF16: the matrix cores' 8-bit products, which lose
+ * what is below 2^-13 of the largest of eight before they are added in fp32 (1.5e-5 of a result of normal inputs), y rounded
+ * once.  A projection's output from (x, theta_g), its
+ * inputs' gradient from (dy, the transpose of theta_g), its weights' from (transpose of dy, transpose of x) added to
+ * fp32 gradients.  The order of a sum hangs on rows, m and n.  The workspace serves up to `rows` rows. */
+size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n);
+int dlcx_fp8_product(const dlcx_fp8 *x, const dlcx_fp8 *w, const void *y_in, int64_t ldy_in, void *y_out,
+                     int64_t ldy_out, int dtype, void *workspace, void *stream);
+
+/* For every row: s = x + residual, rounded to the type and written to sum_out (both or neither; without them s = x);
+ * rstd = 1 / sqrt(mean(s^2) + eps); y = s rstd weight, to y_out (rounded once), to y8_out in 8 bits (from fp32, not from
+ * y_out), or to both.  weight: n elements of the same type.  rstd_out: `rows` floats for the gradient, or NULL.  sum_out
+ * may be x or residual.  Squares and their sum are fp32: rows whose sum of squares passes 2^128 give zeros. n 1 .. 2^24. */
+int dlcx_rms_norm(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *residual,
+                  int64_t ldr, const void *weight, float eps, void *sum_out, int64_t ldsum, void *y_out,
+                  int64_t ldy, const dlcx_fp8 *y8_out, float *rstd_out, void *stream);
+
+/* Its gradient, x being what was normalised (sum_out where there was a residual), with h = x rstd, g = dy weight:
+ *   dx_out = dx_in + rstd (g - h mean(g h)) ;  dw_out = sum over the rows of dy h  (n floats, overwritten)
+ * dx_in (the residual's gradient) may be NULL for zeros; dx_out may be dx_in, dy or x.  Sums of dw: fp32, in an order that
+ * hangs on rows and n.  The workspace serves up to `rows` rows. */
+size_t dlcx_rms_norm_workspace_bytes(int64_t rows, int64_t n);
+int dlcx_rms_norm_backward(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *weight,
+                           const float *rstd, const void *dy, int64_t lddy, const void *dx_in,
+                           int64_t lddx_in, void *dx_out, int64_t lddx_out, float *dw_out, void *workspace,
+                           void *stream);
+
+/* y_out = y_in + mask x / (1 - p), elements dropped with probability p, rounded to a multiple of 2^-16 (0 .. 65535 of
+ * them; also in 1 - p).  y_in NULL: zeros; y_out may be y_in or x.  Element i, counted along rows of `cols`, takes 16 bits
+ * of Philox 4x32 with ten rounds: key seed, counter (i / 8, offset + *offset_more), the (i % 8)th half word from the lowest
+ * up; it is kept where they are at least 65536 p.  The call on a gradient with the same numbers has the same mask.
+ * offset_more: a device 64-bit number (so that a captured graph draws anew), or NULL. */
+int dlcx_dropout(int64_t rows, int64_t cols, int dtype, const void *x, int64_t ldx, const void *y_in,
+                 int64_t ldy_in, void *y_out, int64_t ldy_out, double p, uint64_t seed, uint64_t offset,
+                 const uint64_t *offset_more, void *stream);
+
 /* ---- helpers: the steps the entry points above are made of ---------------------------- */
 
 /* Size of one worker's payload for one factor: what Alg. 1 hands to the AllReduce of Alg. 2 is

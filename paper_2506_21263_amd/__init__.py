@@ -62,6 +62,12 @@ class Table(C.Structure):
                 ("steps", C.c_int32)]
 
 
+class Fp8(C.Structure):
+    """A matrix in 8 bits; `held` keeps the tensors behind it."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld", C.c_int64), ("ldscale", C.c_int64)]
+
+
 _lib = None
 _vp, _i64, _i32, _int = C.c_void_p, C.c_int64, C.c_int32, C.c_int
 _dp = C.POINTER(Desc)
@@ -123,6 +129,19 @@ SYMBOLS = {
     "dlcx_adamw": (_int, [_vp, C.c_double, C.c_double, C.c_double, C.c_double, _i64, C.c_double,
                           _vp, C.c_double, _vp]),
     "dlcx_state_decode": (_int, [_int, _vp, _vp, _i64, _vp, _int, _vp]),
+    "dlcx_fp8_code_pitch": (_i64, [_i64]),
+    "dlcx_fp8_scale_pitch": (_i64, [_i64]),
+    "dlcx_fp8_quantize": (_int, [_i64, _i64, _vp, _i64, _int, _int, _vp, _vp, _vp]),
+    "dlcx_fp8_decode": (_int, [_vp, _vp, _i64, _int, _vp]),
+    "dlcx_fp8_product_workspace_bytes": (C.c_size_t, [_i64, _i64, _i64]),
+    "dlcx_fp8_product": (_int, [_vp, _vp, _vp, _i64, _vp, _i64, _int, _vp, _vp]),
+    "dlcx_rms_norm": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, C.c_float, _vp, _i64, _vp, _i64,
+                             _vp, _vp, _vp]),
+    "dlcx_rms_norm_workspace_bytes": (C.c_size_t, [_i64, _i64]),
+    "dlcx_rms_norm_backward": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64,
+                                      _vp, _vp, _vp]),
+    "dlcx_dropout": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, _i64, C.c_double, C.c_uint64,
+                            C.c_uint64, _vp, _vp]),
     "dlcx_profile_enable": (_int, [_int]),
     "dlcx_profile_kernels": (_int, []),
     "dlcx_profile_name": (C.c_char_p, [_int]),
@@ -594,6 +613,126 @@ def dlcx_state_decode(codes, scales, out, stream=None):
                                    _typed(scales, torch.float32, -(-n // STATE_GROUP), "scales"), n,
                                    _typed(out, out.dtype, n, "out"), _CODE[out.dtype], _stream(stream)),
            "dlcx_state_decode")
+
+
+def dlcx_fp8_code_pitch(cols):
+    return lib().dlcx_fp8_code_pitch(cols)
+
+
+def dlcx_fp8_scale_pitch(cols):
+    return lib().dlcx_fp8_scale_pitch(cols)
+
+
+def _bytes(t, kind, rows, pitch, what):
+    """Address and row stride of `rows` rows of at least `pitch` bytes on the device."""
+    if not (t.is_cuda and t.dtype in (kind, torch.uint8) and t.dim() == 2 and t.shape[0] == rows and t.shape[1] >= pitch):
+        raise ValueError("%s: a device matrix of %d rows of %d bytes (%s or uint8) is wanted" % (what, rows, pitch, kind))
+    step, inner = t.stride()
+    if (inner != 1 and t.shape[1] > 1) or (step < t.shape[1] and rows > 1):
+        raise ValueError("%s: the bytes of a row have to be consecutive, and rows apart" % what)
+    return t.data_ptr(), (step if rows > 1 else max(pitch, t.shape[1]))
+
+
+def fp8(codes, scales, cols):
+    """A matrix in 8 bits of `cols` columns, from its codes (float8_e4m3fn or uint8, dlcx_fp8_code_pitch(cols) of them to a
+    row, zeros from `cols` on) and its scales (uint8 or float8_e8m0fnu, dlcx_fp8_scale_pitch(cols) to a row)."""
+    rows = codes.shape[0]
+    c, ld = _bytes(codes, torch.float8_e4m3fn, rows, dlcx_fp8_code_pitch(cols), "codes")
+    s, lds = _bytes(scales, torch.float8_e8m0fnu, rows, dlcx_fp8_scale_pitch(cols), "scales")
+    a = Fp8(codes=c, scales=s, rows=rows, cols=cols, ld=ld, ldscale=lds)
+    a.held = (codes, scales)
+    return a
+
+
+def fp8_empty(rows, cols, device="cuda"):
+    """Memory for a matrix in 8 bits that dlcx_fp8_quantize or dlcx_rms_norm writes."""
+    return fp8(torch.empty(rows, dlcx_fp8_code_pitch(cols), device=device, dtype=torch.float8_e4m3fn),
+               torch.empty(rows, dlcx_fp8_scale_pitch(cols), device=device, dtype=torch.uint8), cols)
+
+
+def _ref(a):
+    return None if a is None else C.addressof(a)
+
+
+def _type_of(t, what):
+    if t.dtype not in _CODE:
+        raise ValueError("%s: float32 or bfloat16 is wanted" % what)
+    return t.dtype
+
+
+def dlcx_fp8_quantize(x, out=None, out_t=None, square=False, stream=None):
+    """x (a matrix, its rows may be apart) to `out` and its transpose to `out_t` (what `fp8` or `fp8_empty` made, or None)."""
+    dt = _type_of(x, "x")
+    rows, cols = x.shape
+    x, ldx = _rows(x, rows, cols, dt, "x")
+    _check(lib().dlcx_fp8_quantize(rows, cols, x, ldx, _CODE[dt], int(square), _ref(out), _ref(out_t), _stream(stream)),
+           "dlcx_fp8_quantize")
+
+
+def dlcx_fp8_decode(a, out, stream=None):
+    dt = _type_of(out, "out")
+    out, ldo = _rows(out, a.rows, a.cols, dt, "out")
+    _check(lib().dlcx_fp8_decode(C.addressof(a), out, ldo, _CODE[dt], _stream(stream)), "dlcx_fp8_decode")
+
+
+def dlcx_fp8_product_workspace_bytes(rows, m, n):
+    return lib().dlcx_fp8_product_workspace_bytes(rows, m, n)
+
+
+def dlcx_fp8_product(x, w, y_in, y_out, workspace, stream=None):
+    """y_out = y_in (None: zeros) + x w^T; y may be views with a row stride."""
+    dt = _type_of(y_out, "y_out")
+    y_in, ldi = _rows(y_in, x.rows, w.rows, dt, "y_in")
+    y_out, ldo = _rows(y_out, x.rows, w.rows, dt, "y_out")
+    ws = _typed(workspace, torch.uint8, dlcx_fp8_product_workspace_bytes(x.rows, w.rows, x.cols), "workspace")
+    _check(lib().dlcx_fp8_product(C.addressof(x), C.addressof(w), y_in, ldi, y_out, ldo, _CODE[dt], ws, _stream(stream)),
+           "dlcx_fp8_product")
+
+
+def dlcx_rms_norm(x, weight, eps, residual=None, sum_out=None, y_out=None, y8_out=None, rstd_out=None, stream=None):
+    """y_out and y8_out (a matrix in 8 bits): one of them or both; sum_out where there is a residual."""
+    dt = _type_of(x, "x")
+    rows, n = x.shape
+    x, ldx = _rows(x, rows, n, dt, "x")
+    residual, ldr = _rows(residual, rows, n, dt, "residual")
+    sum_out, lds = _rows(sum_out, rows, n, dt, "sum_out")
+    y_out, ldy = _rows(y_out, rows, n, dt, "y_out")
+    _check(lib().dlcx_rms_norm(rows, n, _CODE[dt], x, ldx, residual, ldr, _typed(weight, dt, n, "weight"), eps, sum_out,
+                               lds, y_out, ldy, _ref(y8_out), _typed(rstd_out, torch.float32, rows, "rstd_out"),
+                               _stream(stream)), "dlcx_rms_norm")
+
+
+def dlcx_rms_norm_workspace_bytes(rows, n):
+    return lib().dlcx_rms_norm_workspace_bytes(rows, n)
+
+
+def dlcx_rms_norm_backward(x, weight, rstd, dy, dx_in, dx_out, dw_out, workspace, stream=None):
+    """x: what was normalised (sum_out where there was a residual); dx_in None: zeros."""
+    dt = _type_of(x, "x")
+    rows, n = x.shape
+    x, ldx = _rows(x, rows, n, dt, "x")
+    dy, lddy = _rows(dy, rows, n, dt, "dy")
+    dx_in, ldi = _rows(dx_in, rows, n, dt, "dx_in")
+    dx_out, ldo = _rows(dx_out, rows, n, dt, "dx_out")
+    _check(lib().dlcx_rms_norm_backward(rows, n, _CODE[dt], x, ldx, _typed(weight, dt, n, "weight"),
+                                        _typed(rstd, torch.float32, rows, "rstd"), dy, lddy, dx_in, ldi, dx_out, ldo,
+                                        _typed(dw_out, torch.float32, n, "dw_out"),
+                                        _typed(workspace, torch.uint8, dlcx_rms_norm_workspace_bytes(rows, n), "workspace"),
+                                        _stream(stream)), "dlcx_rms_norm_backward")
+
+
+def dlcx_dropout(x, y_in, y_out, p, seed, offset=0, offset_more=None, stream=None):
+    """y_out = y_in (None: zeros) + mask x / (1 - p).  seed and offset: 64 bits; offset_more: an int64 device tensor of one
+    element that is added to offset when the call runs, or None."""
+    dt = _type_of(x, "x")
+    rows, cols = x.shape
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset: numbers of 64 bits are wanted")
+    x, ldx = _rows(x, rows, cols, dt, "x")
+    y_in, ldi = _rows(y_in, rows, cols, dt, "y_in")
+    y_out, ldo = _rows(y_out, rows, cols, dt, "y_out")
+    _check(lib().dlcx_dropout(rows, cols, _CODE[dt], x, ldx, y_in, ldi, y_out, ldo, p, seed, offset,
+                              _typed(offset_more, torch.int64, 1, "offset_more"), _stream(stream)), "dlcx_dropout")
 
 
 def dlcx_profile_enable(on):

@@ -35,7 +35,8 @@ enum KernelId {
     KID_ROUND, KID_QUANT_ROUND, KID_REQUANT, KID_EF_UPDATE,
     KID_MFMA_PEAK, KID_TRAFFIC_PROBE, KID_TENSOR_TABLE, KID_GRAD_NORM, KID_ADAMW,
     KID_STATE_DECODE, KID_ADAPTER_ROUTE, KID_ADAPTER_DOWN, KID_ADAPTER_OPERAND, KID_ADAPTER_UP,
-    KID_ADAPTER_ROWS, KID_ADAPTER_GRAD, KID_ADAPTER_SUM, KID_COUNT
+    KID_ADAPTER_ROWS, KID_ADAPTER_GRAD, KID_ADAPTER_SUM, KID_FP8_QUANTIZE, KID_FP8_DECODE, KID_FP8_PRODUCT,
+    KID_FP8_PRODUCT_SUM, KID_RMS_NORM, KID_RMS_NORM_GRAD, KID_RMS_NORM_SUM, KID_DROPOUT, KID_COUNT
 };
 struct Timed {
     Timed(int kid, hipStream_t st);

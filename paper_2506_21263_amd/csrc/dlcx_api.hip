@@ -163,7 +163,9 @@ static const char *const kKernelNames[KID_COUNT] = {
     "project_q", "sum_slabs", "reconstruct", "gram_partials", "chol_inverse", "apply_w",
     "effective_rank", "round_fused", "quant_round", "requantize", "ef_update",
     "mfma_peak", "traffic_probe", "tensor_table", "grad_norm", "adamw", "state_decode",
-    "adapter_route", "adapter_down", "adapter_operand", "adapter_up", "adapter_rows", "adapter_grad", "adapter_sum"};
+    "adapter_route", "adapter_down", "adapter_operand", "adapter_up", "adapter_rows", "adapter_grad", "adapter_sum",
+    "fp8_quantize", "fp8_decode", "fp8_product", "fp8_product_sum", "rms_norm", "rms_norm_backward", "rms_norm_sum",
+    "dropout"};
 
 int dlcx_profile_enable(int on) {
     std::lock_guard<std::mutex> lock(g_prof_mutex);

@@ -1,0 +1,207 @@
+// A matrix to 8 bits with a power of two for every 128 elements of a row, and back.
+//
+// Both are streams, bound by HBM.  The quantiser takes tiles of 128 x 128: a lane holds 8 x 8 elements, sixteen
+// lanes a row's 128 columns, so a row's largest is found among a row of lanes and a column's among the sixteen
+// such rows of the workgroup; both layouts come from one reading of x.
+#include "eight.h"
+
+namespace dlcx {
+
+int check_fp8(const dlcx_fp8 *a) {
+    if (!a || a->rows < 0 || a->rows > kMaxSide || a->cols < 0 || a->cols > kMaxSide) return DLCX_EINVAL;
+    if (a->rows == 0 || a->cols == 0) return DLCX_OK;
+    if (!a->codes || off_by(a->codes, 16) || !a->scales || off_by(a->scales, 4)) return DLCX_EINVAL;
+    if (a->ld < code_pitch(a->cols) || a->ld % 16 || a->ld > kMaxRowStride) return DLCX_EINVAL;
+    if (a->ldscale < scale_pitch(a->cols) || a->ldscale % 4 || a->ldscale > kMaxRowStride) return DLCX_EINVAL;
+    return DLCX_OK;
+}
+
+struct QuantArgs {
+    const void *x;
+    int64_t ldx;
+    int rows, cols, row_tiles, col_tiles;
+    uint8_t *codes, *scales, *codes_t, *scales_t;
+    int64_t ld, lds, ld_t, lds_t;
+};
+
+// ROWS: codes along the rows; COLS: the transpose's; SQUARE: one scale for the tile.
+template <typename T, bool ROWS, bool COLS, bool SQUARE>
+__global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
+    __shared__ uint32_t s_max[COLS && !SQUARE ? 16 * 128 : 4];
+    __shared__ __attribute__((aligned(16))) uint8_t s_t[COLS ? 128 * 128 : 16];
+    const int tid = threadIdx.x, lane16 = tid & 15, part = tid >> 4;
+    for (int64_t tile = blockIdx.x; tile < (int64_t)a.row_tiles * a.col_tiles; tile += gridDim.x) {
+        const int tr = (int)(tile / a.col_tiles), tc = (int)(tile % a.col_tiles);
+        const int row0 = tr * 128 + part * 8, col0 = tc * 128 + lane16 * 8;
+        const int there = min(max(a.cols - col0, 0), 8);
+        float v[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            load8<T>((const typename T::elem *)a.x + (int64_t)(row0 + i) * a.ldx + col0, row0 + i < a.rows ? there : 0, v[i]);
+        uint32_t top[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[i] = finite_max8(v[i]);
+        uint32_t shared = 0;
+        if constexpr (SQUARE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) shared = max(shared, top[i]);
+            shared = max16(shared);
+            shared = max(shared, (uint32_t)__shfl_xor((int)shared, 16, 64));
+            shared = max(shared, (uint32_t)__shfl_xor((int)shared, 32, 64));
+            if ((tid & 63) == 0) s_max[tid >> 6] = shared;
+            __syncthreads();
+            shared = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+        }
+        if constexpr (ROWS) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t s = scale_byte(SQUARE ? shared : max16(top[i]));
+                const uint2 c = codes8(v[i], scale_inverse(s));
+                if (row0 + i < a.rows) {
+                    *reinterpret_cast<uint2 *>(a.codes + (int64_t)(row0 + i) * a.ld + col0) = c;
+                    if (lane16 == 0) a.scales[(int64_t)(row0 + i) * a.lds + tc] = (uint8_t)s;
+                }
+            }
+        }
+        if constexpr (COLS) {
+            if constexpr (!SQUARE) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) m = max(m, finite_bits(v[i][j]));
+                    s_max[part * 128 + lane16 * 8 + j] = m;
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t m = shared;
+                if constexpr (!SQUARE) {
+                    m = 0;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) m = max(m, s_max[k * 128 + lane16 * 8 + j]);
+                }
+                const uint32_t s = scale_byte(m);
+                float u[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = v[i][j];
+                *reinterpret_cast<uint2 *>(s_t + (lane16 * 8 + j) * 128 + part * 8) = codes8(u, scale_inverse(s));
+                if (part == 0 && col0 + j < a.cols) a.scales_t[(int64_t)(col0 + j) * a.lds_t + tr] = (uint8_t)s;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = k * 32 + (tid >> 3);
+                const uint4 w = *reinterpret_cast<const uint4 *>(s_t + c * 128 + (tid & 7) * 16);
+                if (tc * 128 + c < a.cols)
+                    *reinterpret_cast<uint4 *>(a.codes_t + (int64_t)(tc * 128 + c) * a.ld_t + tr * 128 + (tid & 7) * 16) = w;
+            }
+        }
+        if constexpr (COLS || SQUARE) __syncthreads();
+    }
+}
+
+template <typename T>
+static int launch_quantize8(const QuantArgs &a, bool rows, bool cols, bool square, hipStream_t st) {
+    const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles;
+    const dim3 grid((unsigned)(tiles < kMostGroups ? tiles : kMostGroups));
+    Timed timed(KID_FP8_QUANTIZE, st);
+    if (square) {
+        if (rows && cols) quantize_kernel<T, true, true, true><<<grid, 256, 0, st>>>(a);
+        else if (rows) quantize_kernel<T, true, false, true><<<grid, 256, 0, st>>>(a);
+        else quantize_kernel<T, false, true, true><<<grid, 256, 0, st>>>(a);
+    } else {
+        if (rows && cols) quantize_kernel<T, true, true, false><<<grid, 256, 0, st>>>(a);
+        else if (rows) quantize_kernel<T, true, false, false><<<grid, 256, 0, st>>>(a);
+        else quantize_kernel<T, false, true, false><<<grid, 256, 0, st>>>(a);
+    }
+    return check_launch("fp8_quantize");
+}
+
+struct DecodeArgs {
+    const uint8_t *codes, *scales;
+    int64_t ld, lds;
+    void *out;
+    int64_t ldo;
+    int rows, cols, groups;  // groups: of 8 columns in a row
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void decode_kernel(DecodeArgs a) {
+    const int64_t total = (int64_t)a.rows * a.groups;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
+        const int64_t row = at / a.groups;
+        const int g = (int)(at - row * a.groups);
+        const uint2 c = *reinterpret_cast<const uint2 *>(a.codes + row * a.ld + g * 8);
+        const float s = scale_value(a.scales[row * a.lds + g / 16]);
+        typedef float v2 __attribute__((ext_vector_type(2)));
+        const uint32_t w[2] = {c.x, c.y};
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const v2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], true);
+            v[4 * h] = lo[0] * s;
+            v[4 * h + 1] = lo[1] * s;
+            v[4 * h + 2] = hi[0] * s;
+            v[4 * h + 3] = hi[1] * s;
+        }
+        store8<T>((typename T::elem *)a.out + row * a.ldo + g * 8, a.cols - g * 8, v);
+    }
+}
+
+}  // namespace dlcx
+
+using namespace dlcx;
+
+extern "C" {
+
+int64_t dlcx_fp8_code_pitch(int64_t cols) { return cols < 0 || cols > kMaxSide ? 0 : code_pitch(cols); }
+int64_t dlcx_fp8_scale_pitch(int64_t cols) { return cols < 0 || cols > kMaxSide ? 0 : scale_pitch(cols); }
+
+int dlcx_fp8_quantize(int64_t rows, int64_t cols, const void *x, int64_t ldx, int dtype, int square, const dlcx_fp8 *out,
+                      const dlcx_fp8 *out_t, void *stream) {
+    if (rows < 0 || rows > kMaxSide || cols < 0 || cols > kMaxSide) return DLCX_EINVAL;
+    if ((dtype != DLCX_F32 && dtype != DLCX_BF16) || square < 0 || square > 1 || (!out && !out_t)) return DLCX_EINVAL;
+    if (out && (check_fp8(out) != DLCX_OK || out->rows != rows || out->cols != cols)) return DLCX_EINVAL;
+    if (out_t && (check_fp8(out_t) != DLCX_OK || out_t->rows != cols || out_t->cols != rows)) return DLCX_EINVAL;
+    if (rows == 0 || cols == 0) return DLCX_OK;
+    if (bad_rows(x, ldx, cols, dtype)) return DLCX_EINVAL;
+    QuantArgs a = {};
+    a.x = x;
+    a.ldx = ldx;
+    a.rows = (int)rows;
+    a.cols = (int)cols;
+    a.row_tiles = (int)ceil_div(rows, 128);
+    a.col_tiles = (int)ceil_div(cols, 128);
+    if (out) {
+        a.codes = (uint8_t *)out->codes;
+        a.scales = (uint8_t *)out->scales;
+        a.ld = out->ld;
+        a.lds = out->ldscale;
+    }
+    if (out_t) {
+        a.codes_t = (uint8_t *)out_t->codes;
+        a.scales_t = (uint8_t *)out_t->scales;
+        a.ld_t = out_t->ld;
+        a.lds_t = out_t->ldscale;
+    }
+    return dtype == DLCX_BF16 ? launch_quantize8<TypeBf16>(a, out, out_t, square, as_stream(stream))
+                              : launch_quantize8<TypeF32>(a, out, out_t, square, as_stream(stream));
+}
+
+int dlcx_fp8_decode(const dlcx_fp8 *a, void *out, int64_t ldo, int out_dtype, void *stream) {
+    if (check_fp8(a) != DLCX_OK || (out_dtype != DLCX_F32 && out_dtype != DLCX_BF16)) return DLCX_EINVAL;
+    if (a->rows == 0 || a->cols == 0) return DLCX_OK;
+    if (bad_rows(out, ldo, a->cols, out_dtype)) return DLCX_EINVAL;
+    const DecodeArgs d = {(const uint8_t *)a->codes, (const uint8_t *)a->scales, a->ld, a->ldscale, out, ldo, (int)a->rows,
+                          (int)a->cols, (int)ceil_div(a->cols, 8)};
+    const int64_t blocks = ceil_div((int64_t)d.rows * d.groups, 256);
+    const dim3 grid((unsigned)(blocks < kMostGroups ? blocks : kMostGroups));
+    Timed timed(KID_FP8_DECODE, as_stream(stream));
+    if (out_dtype == DLCX_BF16) decode_kernel<TypeBf16><<<grid, 256, 0, as_stream(stream)>>>(d);
+    else decode_kernel<TypeF32><<<grid, 256, 0, as_stream(stream)>>>(d);
+    return check_launch("fp8_decode");
+}
+
+}  // extern "C"

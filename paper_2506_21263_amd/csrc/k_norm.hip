@@ -1,0 +1,378 @@
+// Root-mean-square norm of the rows of a matrix, with the residual's addition before it and an output in 8 bits
+// behind it, and its gradient.
+//
+//   s = x + residual (as it is stored) ;  rstd = 1 / sqrt(mean s^2 + eps) ;  y = s rstd w
+//   dx = dx_in + rstd (g - h mean(g h)),  g = dy w,  h = s rstd ;  dw = sum over rows of dy h
+//
+// Streams over the rows, bound by HBM.  Up to kInRegisters columns a row is read once and held in the registers of
+// its workgroup (a wavefront for short rows); longer rows are read twice.  Sums are fp32, in an order that hangs on
+// n and, for dw, on the number of rows.
+#include "eight.h"
+
+namespace dlcx {
+
+constexpr int kInRegisters = 32768;  // 1024 lanes x 4 times 8 elements
+
+struct NormArgs {
+    const void *x, *residual, *weight;
+    void *sum, *y;
+    uint8_t *codes, *scales;
+    float *rstd;
+    int64_t ldx, ldr, ldsum, ldy, ld8, lds;
+    int rows, n;
+    float eps;
+};
+
+// The sum over the LANES lanes of a row's group, in all of them: LANES = 64, or a workgroup.
+template <int LANES>
+__device__ __forceinline__ float sum_lanes(float x, float *s_part) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
+    if constexpr (LANES > 64) {
+        if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = 0.f;
+#pragma unroll
+        for (int k = 0; k < LANES / 64; ++k) x += s_part[k];
+    }
+    return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void put_eight(const NormArgs &a, int64_t row, int col, const float (&v)[8], int lane) {
+    const uint32_t s = scale_byte(max16(finite_max8(v)));
+    const uint2 c = codes8(v, scale_inverse(s));
+    if (col < (a.n + 127) / 128 * 128) {
+        *reinterpret_cast<uint2 *>(a.codes + row * a.ld8 + col) = c;
+        if ((lane & 15) == 0) a.scales[row * a.lds + col / 128] = (uint8_t)s;
+    }
+}
+
+// LANES to a row, each with CH times 8 elements of it.
+template <typename T, int LANES, int CH>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArgs a) {
+    typedef typename T::elem elem;
+    __shared__ float s_part[16];
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
+    const int lane = threadIdx.x % LANES;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * kRows) {
+        float v[CH][8], w[CH][8];
+        float ss = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+            load8<T>((const elem *)a.x + row * a.ldx + col, there, v[c]);
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+                load8<T>((const elem *)a.residual + row * a.ldr + col, there, w[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] += w[c][i];
+                round8<T>(v[c]);
+                if (a.sum) store8<T>((elem *)a.sum + row * a.ldsum + col, there, v[c]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+            load8<T>((const elem *)a.weight + col, there, w[c]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss += v[c][i] * v[c][i];
+        }
+        ss = sum_lanes<LANES>(ss, s_part);
+        const float rstd = 1.f / sqrtf(ss / (float)a.n + a.eps);
+        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * w[c][i];
+            if (a.y) store8<T>((elem *)a.y + row * a.ldy + col, there, v[c]);
+            if (a.codes) put_eight<T>(a, row, col, v[c], lane);
+        }
+        if constexpr (LANES > 64) __syncthreads();
+    }
+}
+
+// Rows of any length: read twice, the sum (where there is a residual) from where it was written by the same lane.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
+    typedef typename T::elem elem;
+    __shared__ float s_part[16];
+    const int lane = threadIdx.x;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const elem *x = (const elem *)a.x + row * a.ldx;
+        elem *sum = (elem *)a.sum + row * a.ldsum;
+        float ss = 0.f;
+        for (int64_t col = lane * 8; col < a.n; col += 8192) {
+            const int there = (int)min((int64_t)8, a.n - col);
+            float v[8], r[8];
+            load8<T>(x + col, there, v);
+            if (a.residual) {
+                load8<T>((const elem *)a.residual + row * a.ldr + col, there, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += r[i];
+                round8<T>(v);
+                store8<T>(sum + col, there, v);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss += v[i] * v[i];
+        }
+        ss = sum_lanes<1024>(ss, s_part);
+        const float rstd = 1.f / sqrtf(ss / (float)a.n + a.eps);
+        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+        const int64_t end = a.codes ? ((int64_t)a.n + 127) / 128 * 128 : a.n;  // (whole rows of 16 lanes)
+        for (int64_t col = lane * 8; col < end; col += 8192) {
+            const int there = (int)min((int64_t)8, a.n - col);
+            float v[8], w[8];
+            if (a.residual) load8<T>(sum + col, there, v);
+            else load8<T>(x + col, there, v);
+            load8<T>((const elem *)a.weight + col, there, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * w[i];
+            if (a.y) store8<T>((elem *)a.y + row * a.ldy + col, there, v);
+            if (a.codes) put_eight<T>(a, row, (int)col, v, lane);
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T>
+static int launch_norm(const NormArgs &a, hipStream_t st) {
+    auto grid = [&a](int per) { return dim3((unsigned)(ceil_div(a.rows, per) < (1 << 22) ? ceil_div(a.rows, per) : (1 << 22))); };
+    Timed timed(KID_RMS_NORM, st);
+    if (a.n <= 512) norm_kernel<T, 64, 1><<<grid(4), 256, 0, st>>>(a);
+    else if (a.n <= 2048) norm_kernel<T, 256, 1><<<grid(1), 256, 0, st>>>(a);
+    else if (a.n <= 4096) norm_kernel<T, 256, 2><<<grid(1), 256, 0, st>>>(a);
+    else if (a.n <= 8192) norm_kernel<T, 256, 4><<<grid(1), 256, 0, st>>>(a);
+    else if (a.n <= 16384) norm_kernel<T, 512, 4><<<grid(1), 512, 0, st>>>(a);
+    else if (a.n <= kInRegisters) norm_kernel<T, 1024, 4><<<grid(1), 1024, 0, st>>>(a);
+    else norm_long_kernel<T><<<grid(1), 1024, 0, st>>>(a);
+    return check_launch("rms_norm");
+}
+
+// ---- the gradient --------------------------------------------------------------------------------------
+// A workgroup takes every gridDim'th row and keeps its part of dw in registers; the parts are added by a second
+// kernel, in order.
+struct NormGradArgs {
+    const void *x, *weight, *dy, *dx_in;
+    const float *rstd;
+    void *dx;
+    float *part, *dw, *dot;  // parts x n ; n ; rows (long rows)
+    int64_t ldx, lddy, ldi, ldo;
+    int rows, n, parts;
+};
+
+template <typename T, int LANES, int CH>
+__global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
+    typedef typename T::elem elem;
+    __shared__ float s_part[2][16];
+    const int lane = threadIdx.x;
+    float w[CH][8], dw[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * LANES + lane) * 8;
+        load8<T>((const elem *)a.weight + col, min(a.n - col, 8), w[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        float h[CH][8], g[CH][8];
+        const float rstd = a.rstd[row];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+            load8<T>((const elem *)a.x + row * a.ldx + col, there, h[c]);
+            load8<T>((const elem *)a.dy + row * a.lddy + col, there, g[c]);
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[c][i] *= rstd;
+                dw[c][i] += g[c][i] * h[c][i];
+                g[c][i] *= w[c][i];
+                dot += g[c][i] * h[c][i];
+            }
+        dot = sum_lanes<LANES>(dot, s_part[turn]) / (float)a.n;  // (two places, so one barrier a row)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+            float r[8] = {};
+            if (a.dx_in) load8<T>((const elem *)a.dx_in + row * a.ldi + col, there, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] += rstd * (g[c][i] - h[c][i] * dot);
+            store8<T>((elem *)a.dx + row * a.ldo + col, there, r);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (c * LANES + lane) * 8;
+        store8<TypeF32>(a.part + (int64_t)blockIdx.x * a.n + col, min(a.n - col, 8), dw[c]);
+    }
+}
+
+// Long rows: first mean(g h) of each ...
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_dot_kernel(NormGradArgs a) {
+    typedef typename T::elem elem;
+    __shared__ float s_part[16];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const float rstd = a.rstd[row];
+        float dot = 0.f;
+        for (int64_t col = threadIdx.x * 8; col < a.n; col += 8192) {
+            const int there = (int)min((int64_t)8, a.n - col);
+            float x[8], g[8], w[8];
+            load8<T>((const elem *)a.x + row * a.ldx + col, there, x);
+            load8<T>((const elem *)a.dy + row * a.lddy + col, there, g);
+            load8<T>((const elem *)a.weight + col, there, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dot += g[i] * w[i] * (x[i] * rstd);
+        }
+        dot = sum_lanes<1024>(dot, s_part) / (float)a.n;
+        if (threadIdx.x == 0) a.dot[row] = dot;
+        __syncthreads();
+    }
+}
+// ... then columns: a workgroup has 2048 of them and every parts'th row.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_grad_long_kernel(NormGradArgs a) {
+    typedef typename T::elem elem;
+    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    const int there = (int)max((int64_t)0, min((int64_t)8, a.n - col));
+    if (there == 0) return;
+    float w[8], dw[8] = {};
+    load8<T>((const elem *)a.weight + col, there, w);
+    for (int64_t row = blockIdx.y; row < a.rows; row += a.parts) {
+        const float rstd = a.rstd[row], dot = a.dot[row];
+        float h[8], g[8], r[8] = {};
+        load8<T>((const elem *)a.x + row * a.ldx + col, there, h);
+        load8<T>((const elem *)a.dy + row * a.lddy + col, there, g);
+        if (a.dx_in) load8<T>((const elem *)a.dx_in + row * a.ldi + col, there, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[i] *= rstd;
+            dw[i] += g[i] * h[i];
+            r[i] += rstd * (g[i] * w[i] - h[i] * dot);
+        }
+        store8<T>((elem *)a.dx + row * a.ldo + col, there, r);
+    }
+    store8<TypeF32>(a.part + blockIdx.y * (int64_t)a.n + col, there, dw);
+}
+
+// dw from its parts: 16 columns and 16 shares of the parts to a workgroup.
+__global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__ part, int parts, int n, float *__restrict__ dw) {
+    __shared__ float s[16][17];
+    const int c = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int64_t col = (int64_t)blockIdx.x * 16 + c;
+    float t = 0.f;
+    if (col < n)
+        for (int p = share; p < parts; p += 16) t += part[(int64_t)p * n + col];
+    s[share][c] = t;
+    __syncthreads();
+    if (share == 0 && col < n) {
+        t = 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) t += s[k][c];
+        dw[col] = t;
+    }
+}
+
+// Workgroups of the gradient, each with a part of dw.
+static int norm_parts(int64_t rows, int64_t n) {
+    const int64_t most = n <= 2048 ? 2048 : n <= 8192 ? 1024 : n <= 16384 ? 512 : 256;
+    return (int)(rows < most ? rows : most);
+}
+
+template <typename T>
+static int launch_norm_grad(const NormGradArgs &a, hipStream_t st) {
+    {
+        Timed timed(KID_RMS_NORM_GRAD, st);
+        const dim3 grid((unsigned)a.parts);
+        if (a.n <= 512) norm_grad_kernel<T, 64, 1><<<grid, 64, 0, st>>>(a);
+        else if (a.n <= 2048) norm_grad_kernel<T, 256, 1><<<grid, 256, 0, st>>>(a);
+        else if (a.n <= 4096) norm_grad_kernel<T, 256, 2><<<grid, 256, 0, st>>>(a);
+        else if (a.n <= 8192) norm_grad_kernel<T, 256, 4><<<grid, 256, 0, st>>>(a);
+        else if (a.n <= 16384) norm_grad_kernel<T, 512, 4><<<grid, 512, 0, st>>>(a);
+        else if (a.n <= kInRegisters) norm_grad_kernel<T, 1024, 4><<<grid, 1024, 0, st>>>(a);
+        else {
+            norm_dot_kernel<T><<<dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))), 1024, 0, st>>>(a);
+            norm_grad_long_kernel<T><<<dim3((unsigned)ceil_div(a.n, 2048), (unsigned)a.parts), 256, 0, st>>>(a);
+        }
+        const int rc = check_launch("rms_norm_backward");
+        if (rc != DLCX_OK) return rc;
+    }
+    Timed timed(KID_RMS_NORM_SUM, st);
+    norm_sum_kernel<<<dim3((unsigned)ceil_div(a.n, 16)), 256, 0, st>>>(a.part, a.parts, a.n, a.dw);
+    return check_launch("rms_norm_sum");
+}
+
+}  // namespace dlcx
+
+using namespace dlcx;
+
+extern "C" {
+
+static int check_norm(int64_t rows, int64_t n, int dtype) {
+    if (rows < 0 || rows > kMaxSide || n < 1 || n > kMaxSide) return DLCX_EINVAL;
+    return dtype == DLCX_F32 || dtype == DLCX_BF16 ? DLCX_OK : DLCX_EINVAL;
+}
+
+int dlcx_rms_norm(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                  const void *weight, float eps, void *sum_out, int64_t ldsum, void *y_out, int64_t ldy,
+                  const dlcx_fp8 *y8_out, float *rstd_out, void *stream) {
+    if (check_norm(rows, n, dtype) != DLCX_OK || !(eps >= 0.f) || eps > 1e30f) return DLCX_EINVAL;
+    if (y8_out && (check_fp8(y8_out) != DLCX_OK || y8_out->rows != rows || y8_out->cols != n)) return DLCX_EINVAL;
+    if ((residual != nullptr) != (sum_out != nullptr) || (!y_out && !y8_out)) return DLCX_EINVAL;
+    if (rows == 0) return DLCX_OK;
+    if (bad_rows(x, ldx, n, dtype) || !weight || off_by(weight, dtype == DLCX_BF16 ? 2 : 4) || off_by(rstd_out, 4)) return DLCX_EINVAL;
+    if (residual && (bad_rows(residual, ldr, n, dtype) || bad_rows(sum_out, ldsum, n, dtype))) return DLCX_EINVAL;
+    if (y_out && bad_rows(y_out, ldy, n, dtype)) return DLCX_EINVAL;
+    if ((sum_out == x && sum_out && ldsum != ldx) || (sum_out == residual && sum_out && ldsum != ldr)) return DLCX_EINVAL;
+    NormArgs a = {x, residual, weight, sum_out, y_out, nullptr, nullptr, rstd_out, ldx, ldr, ldsum, ldy, 0, 0, (int)rows, (int)n, eps};
+    if (y8_out) {
+        a.codes = (uint8_t *)y8_out->codes;
+        a.scales = (uint8_t *)y8_out->scales;
+        a.ld8 = y8_out->ld;
+        a.lds = y8_out->ldscale;
+    }
+    return dtype == DLCX_BF16 ? launch_norm<TypeBf16>(a, as_stream(stream)) : launch_norm<TypeF32>(a, as_stream(stream));
+}
+
+size_t dlcx_rms_norm_workspace_bytes(int64_t rows, int64_t n) {
+    if (check_norm(rows, n, DLCX_F32) != DLCX_OK) return 0;
+    return a256x((size_t)norm_parts(rows, n) * n * sizeof(float)) + a256x(n > kInRegisters ? (size_t)rows * sizeof(float) : 0) + 256;
+}
+
+int dlcx_rms_norm_backward(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *weight,
+                           const float *rstd, const void *dy, int64_t lddy, const void *dx_in, int64_t lddx_in,
+                           void *dx_out, int64_t lddx_out, float *dw_out, void *workspace, void *stream) {
+    if (check_norm(rows, n, dtype) != DLCX_OK) return DLCX_EINVAL;
+    if (!dw_out || off_by(dw_out, 4) || !workspace || off_by(workspace, 256)) return DLCX_EINVAL;
+    if (rows > 0) {
+        if (bad_rows(x, ldx, n, dtype) || bad_rows(dy, lddy, n, dtype) || bad_rows(dx_out, lddx_out, n, dtype)) return DLCX_EINVAL;
+        if (dx_in && bad_rows(dx_in, lddx_in, n, dtype)) return DLCX_EINVAL;
+        if (!weight || off_by(weight, dtype == DLCX_BF16 ? 2 : 4) || !rstd || off_by(rstd, 4)) return DLCX_EINVAL;
+        if ((dx_in == dx_out && lddx_in != lddx_out) || (dy == dx_out && lddy != lddx_out) || (x == dx_out && ldx != lddx_out))
+            return DLCX_EINVAL;
+    }
+    NormGradArgs a = {x, weight, dy, dx_in, rstd, dx_out, (float *)workspace, dw_out, nullptr, ldx, lddy, lddx_in, lddx_out,
+                      (int)rows, (int)n, norm_parts(rows, n)};
+    a.dot = (float *)((char *)workspace + a256x((size_t)a.parts * n * sizeof(float)));
+    if (rows == 0) {
+        Timed timed(KID_RMS_NORM_SUM, as_stream(stream));
+        norm_sum_kernel<<<dim3((unsigned)ceil_div(n, 16)), 256, 0, as_stream(stream)>>>(a.part, 0, a.n, dw_out);
+        return check_launch("rms_norm_sum");
+    }
+    return dtype == DLCX_BF16 ? launch_norm_grad<TypeBf16>(a, as_stream(stream)) : launch_norm_grad<TypeF32>(a, as_stream(stream));
+}
+
+}  // extern "C"
