@@ -9,6 +9,8 @@
 // whose instruction keeps all of a product; a block's sum is scaled by an exponent's addition and added in fp32.
 //
 // w is the instructions' first operand and x the second: a lane then has four consecutive outputs of one row.
+#include <algorithm>
+
 #include "eight.h"
 
 namespace dlcx {
@@ -16,6 +18,7 @@ namespace dlcx {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 struct ProductArgs {
@@ -187,6 +190,225 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
     }
 }
 
+// ---- large products with bf16 results -----------------------------------------------------------------
+// 256 x 256 outputs to a workgroup of four wavefronts, one to a SIMD, 128 x 128 to each in 32 x 32 x 64 products: the
+// accumulators take 256 of its registers, a half stage's operands 64 and the next half's 64 more.  A stage is 512 rows
+// of 128 bytes, straight to LDS, two of them; a row's 16-byte pieces lie at piece ^ (row / 2 & 7), so that the sixteen
+// lanes that read at once hit all banks.  One barrier a stage, in its middle: from there on its operands are in
+// registers, so its place is fetched anew while the second half is multiplied, and the next stage is there to be read.
+// Scales go through LDS, too (four stages' to a dword): read by every lane that needs them they were 40 % of all
+// requests to the cache.  Results leave through LDS as whole lines.  Edge tiles are moved inside the matrix and write
+// only what is theirs, so no address is checked.
+// Consecutive workgroups go to different XCDs: each XCD gets a contiguous range of tiles, in groups of four rows of
+// tiles, whose operands its L2 holds.
+// 16384 x 8192 x 8192: 0.82 ms, 2.7 PFLOP/s (0.64 without the fetches, 1.44 with 128 x 128 tiles); 8192^3 0.41 ms.
+constexpr int kWideTile = 256, kWideStage = 512 * 128, kWideLds = 2 * kWideStage + 2 * 2048;
+
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+template <typename V>
+__device__ __forceinline__ V lds_read(uint32_t at) { return *(const __attribute__((address_space(3))) V *)(uintptr_t)at; }
+
+struct TilePlace {
+    int row, col;
+};
+// The tile of this workgroup.
+__device__ __forceinline__ TilePlace tile_place(int row_tiles, int col_tiles, int group) {
+    const int total = row_tiles * col_tiles, id = blockIdx.x, share = total / 8, more = total % 8, xcd = id & 7;
+    const int t = xcd * share + min(xcd, more) + (id >> 3);
+    const int per = group * col_tiles, first = t / per * group, rows = min(group, row_tiles - first), in = t % per;
+    return {__builtin_amdgcn_readfirstlane(first + in % rows), __builtin_amdgcn_readfirstlane(in / rows)};
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, -1, 0x00020000);
+}
+// 16 or 4 bytes to a lane from a buffer to LDS, lane after lane.
+__device__ __forceinline__ void fetch_lds16(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t lane_at, uint32_t at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(lds_byte *)to, 16, lane_at, at, 0, 0);
+}
+__device__ __forceinline__ void fetch_lds4(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t lane_at, uint32_t at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(lds_byte *)to, 4, lane_at, at, 0, 0);
+}
+
+template <bool ADD>
+__global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_wide[];
+    uint8_t *const s_scale = s_wide + 2 * kWideStage;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const TilePlace place = tile_place(a.row_tiles, a.col_tiles, 4);
+    const int row0 = min(place.row * kWideTile, a.rows - kWideTile), col0 = min(place.col * kWideTile, a.m - kWideTile);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte *)s_wide;
+    const auto from_w = buffer_at(a.w + col0 * a.ldw), from_x = buffer_at(a.x + row0 * a.ldx);
+    const bool of_w = wave < 2;  // whose scales this wavefront fetches, 128 rows
+    const auto from_s = buffer_at(of_w ? a.ws + col0 * a.ldws : a.xs + row0 * a.ldxs);
+    const uint32_t pitch_s = (uint32_t)(of_w ? a.ldws : a.ldxs), lane_s = ((wave & 1) * 128 + lane) * pitch_s;
+    uint32_t lane_w[2], lane_x[2];  // 64 rows of either operand to a wavefront, eight to a load
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+        const uint32_t r = wave * 64 + o * 8 + (lane >> 3), piece = ((lane & 7) ^ (o * 4 + (lane >> 4))) * 16;
+        lane_w[o] = r * (uint32_t)a.ldw + piece;
+        lane_x[o] = r * (uint32_t)a.ldx + piece;
+    }
+    const uint32_t w16 = (uint32_t)a.ldw * 16, x16 = (uint32_t)a.ldx * 16;
+    auto fetch = [&](int buf, int block, int i) {
+        uint8_t *to = s_wide + buf * kWideStage + (wave * 8 + (i & 7)) * 1024;
+        if (i < 8) fetch_lds16(from_w, to, lane_w[i & 1], block * 128 + (i >> 1) * w16);
+        else fetch_lds16(from_x, to + 256 * 128, lane_x[i & 1], block * 128 + ((i - 8) >> 1) * x16);
+    };
+    auto fetch_scales = [&](int buf, int block, int i) {
+        fetch_lds4(from_s, s_scale + buf * 2048 + (wave * 2 + i) * 256, lane_s, block + i * 64 * pitch_s);
+    };
+    const int r32 = lane & 31, g = lane >> 5, wm = (wave & 1) * 128, wn = (wave >> 1) * 128;
+    uint32_t at_w[2][2][2], at_x[2][2][2];  // buffer, half, piece
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const uint32_t piece = ((4 * h + 2 * g + p) ^ ((r32 >> 1) & 7)) * 16;
+                at_w[b][h][p] = lds0 + b * kWideStage + (wm + r32) * 128 + piece;
+                at_x[b][h][p] = lds0 + b * kWideStage + (256 + wn + r32) * 128 + piece;
+                asm volatile("" : "+v"(at_w[b][h][p]), "+v"(at_x[b][h][p]));  // (kept, with offsets in the reads)
+            }
+    uint32_t at_sw = lds0 + 2 * kWideStage + (wm + r32) * 4, at_sx = lds0 + 2 * kWideStage + (256 + wn + r32) * 4;
+    asm volatile("" : "+v"(at_sw), "+v"(at_sx));
+    auto read_w = [&](int b, int h, int i) { return join(lds_read<i32x4>(at_w[b][h][0] + i * 4096), lds_read<i32x4>(at_w[b][h][1] + i * 4096)); };
+    auto read_x = [&](int b, int h, int i) { return join(lds_read<i32x4>(at_x[b][h][0] + i * 4096), lds_read<i32x4>(at_x[b][h][1] + i * 4096)); };
+
+    const int last = a.blocks - 1;
+    f32x16 acc[4][4] = {};
+    int scale_w[4], scale_x[4], next_w[4], next_x[4];
+    i32x8 fw[2][4], fx[2][4];
+    fetch_scales(0, 0, 0);
+    fetch_scales(0, 0, 1);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) fetch(0, 0, i);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) fetch(1, min(1, last), i);
+    asm volatile("s_waitcnt vmcnt(16)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        fw[0][i] = read_w(0, 0, i);
+        fx[0][i] = read_x(0, 0, i);
+        scale_w[i] = next_w[i] = lds_read<int>(at_sw + i * 128);
+        scale_x[i] = next_x[i] = lds_read<int>(at_sx + i * 128);
+    }
+    // Four matrix instructions' worth of issue between reads and fetches is given, not found: the compiler would put
+    // them all in front.  (masks: 8 matrix, 0x100 LDS reads, 0x20 loads)
+    auto step = [&](auto s, int block, int scales) {
+        constexpr int S = decltype(s)::value, B = S & 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            fx[1][i] = read_x(B, 1, i);
+            fw[1][i] = read_w(B, 1, i);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[0][i], fx[0][j], acc[i][j], 0, 0, S, scale_w[i], S, scale_x[j]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            __builtin_amdgcn_sched_group_barrier(8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(8, 8, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        const int next = min(block + S + 2, last);  // (past the last one it comes again, and is not used)
+        if constexpr (S == 0) {
+            fetch_scales(scales ^ 1, min(block + 4, last & ~3), 0);
+            fetch_scales(scales ^ 1, min(block + 4, last & ~3), 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            fx[0][i] = read_x(B ^ 1, 0, i);
+            fw[0][i] = read_w(B ^ 1, 0, i);
+        }
+        if constexpr (S == 3) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                next_w[i] = lds_read<int>(at_sw + (scales ^ 1) * 2048 + i * 128);
+                next_x[i] = lds_read<int>(at_sx + (scales ^ 1) * 2048 + i * 128);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) fetch(B, next, i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[1][i], fx[1][j], acc[i][j], 0, 0, S, scale_w[i], S, scale_x[j]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            __builtin_amdgcn_sched_group_barrier(8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            __builtin_amdgcn_sched_group_barrier(8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x20, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(8, 4, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int block = 0, scales = 0;
+    for (; block + 4 <= a.blocks; block += 4, scales ^= 1) {
+        unrolled<4>([&](auto s) { step(s, block, scales); });
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            scale_w[i] = next_w[i];
+            scale_x[i] = next_x[i];
+        }
+    }
+    if (block < a.blocks) step(std::integral_constant<int, 0>(), block, scales);
+    if (block + 1 < a.blocks) step(std::integral_constant<int, 1>(), block, scales);
+    if (block + 2 < a.blocks) step(std::integral_constant<int, 2>(), block, scales);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // no stage is on its way or read any more
+
+    // A wavefront's 128 rows of x by 128 columns, rows of 256 bytes in its own quarter of the stages.
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const uint32_t mine = lds0 + wave * 32768;
+    const int keep_row = place.row * kWideTile, keep_col = place.col * kWideTile;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = j * 32 + r32, piece = i * 4 + q;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+                if constexpr (ADD) {
+                    const uint16_t *p = (const uint16_t *)a.y_in + (int64_t)(row0 + wn + r) * a.ldi + col0 + wm + piece * 8 + g * 4;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += TypeBf16::get(p[e]);
+                }
+                *(__attribute__((address_space(3))) u32x2 *)(uintptr_t)(mine + r * 256 + ((piece ^ (r32 & 15)) * 16) + g * 8) =
+                    u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 8
+    for (int k = 0; k < 32; ++k) {
+        const int r = k * 4 + (lane >> 4), piece = lane & 15, row = row0 + wn + r, col = col0 + wm + piece * 8;
+        const i32x4 v = lds_read<i32x4>(mine + r * 256 + ((piece ^ (r & 15)) * 16));
+        uint16_t *to = (uint16_t *)a.y + (int64_t)row * a.ldo + col;
+        if (row >= keep_row && col >= keep_col) {
+            Loose16 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w.w[e] = (uint32_t)v[e];
+            *reinterpret_cast<Loose16 *>(to) = w;
+        } else if (row >= keep_row) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e >= keep_col) to[e] = (uint16_t)((uint32_t)v[e / 2] >> (16 * (e & 1)));
+        }
+    }
+}
+
 // y from the splits' sums, added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void product_sum_kernel(ProductArgs a, int splits) {
@@ -206,22 +428,37 @@ __global__ __launch_bounds__(256) void product_sum_kernel(ProductArgs a, int spl
 
 struct ProductPlan {
     int splits, per_split;
+    bool wide;
 };
 // The sum is split where the tiles do not fill the GPU.
-static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n) {
+static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, int64_t most_stride) {
+    // Tiles of 256 x 256 run one to a compute unit: they lose by a last round that is nearly empty.
+    const int64_t wide = ceil_div(rows, kWideTile) * ceil_div(m, kWideTile);
+    if (dtype == DLCX_BF16 && rows >= kWideTile && m >= kWideTile && wide >= 128 && most_stride <= (1 << 23))  // (256 rows: 32 bits)
+        return {1, (int)(ceil_div(n, 512) * 4), true};
     const int64_t tiles = ceil_div(rows, 128) * ceil_div(m, 128), blocks = ceil_div(n, 128);
     int64_t splits = 1;
     if (tiles < 512 && tiles > 0) splits = ceil_div(512, tiles);
     if (splits > blocks / 4) splits = blocks / 4;
     if (splits < 1) splits = 1;
     const int64_t per = (ceil_div(blocks, splits) + 3) / 4 * 4;
-    return {(int)(blocks ? ceil_div(blocks, per) : 1), (int)per};
+    return {(int)(blocks ? ceil_div(blocks, per) : 1), (int)per, false};
 }
 
 template <typename T>
 static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st) {
     {
         Timed timed(KID_FP8_PRODUCT, st);
+        if (plan.wide) {
+            static size_t granted[2] = {0, 0};
+            const auto kernel = a.y_in ? product_wide_kernel<true> : product_wide_kernel<false>;
+            int rc = grant_dynamic_lds((const void *)kernel, kWideLds, &granted[a.y_in ? 1 : 0], "fp8_product");
+            if (rc != DLCX_OK) return rc;
+            a.row_tiles = (int)ceil_div(a.rows, kWideTile);
+            a.col_tiles = (int)ceil_div(a.m, kWideTile);
+            kernel<<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles)), 256, kWideLds, st>>>(a);
+            return check_launch("fp8_product");
+        }
         product_kernel<T><<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits), 256, 0, st>>>(a);
         const int rc = check_launch("fp8_product");
         if (rc != DLCX_OK || plan.splits == 1) return rc;
@@ -247,7 +484,7 @@ size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
     size_t most = 0;  // of fewer rows, too: these may be split further
     for (int64_t tiles = 1; tiles <= ceil_div(rows, 128) && tiles <= 512; ++tiles) {
         const int64_t r = tiles * 128 < rows ? tiles * 128 : rows;
-        const ProductPlan plan = product_plan(r, m, n);
+        const ProductPlan plan = product_plan(r, m, n, DLCX_F32, 0);  // (bf16 results never need more)
         const size_t need = plan.splits > 1 ? (size_t)plan.splits * r * m * sizeof(float) : 0;
         if (need > most) most = need;
     }
@@ -261,7 +498,8 @@ int dlcx_fp8_product(const dlcx_fp8 *x, const dlcx_fp8 *w, const void *y_in, int
     if (x->rows == 0 || w->rows == 0) return DLCX_OK;
     if (bad_rows(y_out, ldy_out, w->rows, dtype) || (y_in && bad_rows(y_in, ldy_in, w->rows, dtype))) return DLCX_EINVAL;
     if ((y_in == y_out && ldy_in != ldy_out) || !workspace || off_by(workspace, 256)) return DLCX_EINVAL;
-    const ProductPlan plan = product_plan(x->rows, w->rows, x->cols);
+    const int64_t stride = std::max({x->ld, w->ld, x->ldscale, w->ldscale});
+    const ProductPlan plan = product_plan(x->rows, w->rows, x->cols, dtype, stride);
     ProductArgs a = {(const uint8_t *)x->codes, (const uint8_t *)x->scales, (const uint8_t *)w->codes, (const uint8_t *)w->scales,
                      y_in, y_out, plan.splits > 1 ? (float *)workspace : nullptr, x->ld, x->ldscale, w->ld, w->ldscale,
                      ldy_in, ldy_out, (int)x->rows, (int)w->rows, (int)ceil_div(x->cols, 128), plan.per_split,

@@ -164,6 +164,15 @@ def test_product_of_views(rows, m, n, dtype):
     check_product(rows, m, n, dtype, False, pad=5, shift=2)
 
 
+@pytest.mark.parametrize("rows,m,n", [(2817, 3001, 129), (3000, 2816, 1700), (256, 32769, 515), (33000, 257, 640), (4096, 2048, 100)])
+def test_large_product(rows, m, n):
+    """Tiles at the edges are moved inside: every output once, in place too, and nothing around them."""
+    check_product(rows, m, n, "bf16", False)
+    check_product(rows, m, n, "bf16", True, pad=3, shift=1, alias=True)
+    check_product(rows, m, n, "bf16", False, pad=8, shift=8)
+    check_product(rows, m, n, "f32", True)
+
+
 def test_product_without_terms():
     """A sum of no terms is zero: y_in comes back."""
     x, w = dlcx.fp8_empty(5, 0, DEV), dlcx.fp8_empty(7, 0, DEV)
