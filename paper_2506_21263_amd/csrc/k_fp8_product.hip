@@ -409,6 +409,187 @@ __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs a) {
     }
 }
 
+// ---- few rows -------------------------------------------------------------------------------------------
+// w is read once and straight into registers; what bounds this is HBM, or the launch.  Sixteen rows of w to a
+// wavefront; the sum is cut into quads of four blocks (whose scales are one dword), and where m alone does not fill
+// the GPU, KW wavefronts of a workgroup take every KW'th quad and their sums are added through LDS, in order.
+//
+// A lane's part of a 16 x 128 operand: 16 bytes at 16 g and 16 at 64 + 16 g of its row (the order of a sum's terms
+// is free, as long as both operands have it).
+struct Quad {
+    i32x4 lo[4], hi[4];
+    int scale;
+};
+// Blocks `block` .. `block` + 3 of a row, those before `end`; others, and all without `there`: zeros.
+__device__ __forceinline__ void load_quad(Quad &q, const uint8_t *row, const uint8_t *scales, int block, int end, bool there) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        q.lo[k] = q.hi[k] = i32x4{0, 0, 0, 0};
+        if (there && block + k < end) {
+            q.lo[k] = *(const i32x4 *)(row + (int64_t)(block + k) * 128);
+            q.hi[k] = *(const i32x4 *)(row + (int64_t)(block + k) * 128 + 64);
+        }
+    }
+    q.scale = 0x7f7f7f7f;
+    if (there && block < end) q.scale = *(const int *)(scales + block);
+}
+
+// acc + w x^T for one block of 128; S: the byte of the scales.  ew: the scales of the lane's four outputs' rows (fp32).
+template <typename T, int S>
+__device__ __forceinline__ f32x4 block_product(const i32x8 &w, const i32x8 &x, const f32x4 &acc, int sw, int sx, const int (&ew)[4]) {
+    if constexpr (T::size == 2) {
+        return scaled_mma<S>(w, x, acc, sw, sx);
+    } else {
+        f32x4 sum = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w[2 * k], w[2 * k + 1]), widen(x[2 * k], x[2 * k + 1]), sum, 0, 0, 0);
+        int e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = (ew[i] >> (8 * S)) & 255;
+        return add_scaled(acc, sum, e, (sx >> (8 * S)) & 255);
+    }
+}
+
+// Up to 16 rows of x.
+template <typename T, int KW>
+__global__ __launch_bounds__(512, 2) void product_few_kernel(ProductArgs a) {
+    constexpr int WR = 8 / KW;
+    __shared__ f32x4 s_sum[KW > 1 ? 8 * 64 : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, g = lane >> 4, kw = wave % KW;
+    const int64_t col0 = ((int64_t)blockIdx.x * WR + wave / KW) * 16, wrow = min(col0 + r16, (int64_t)a.m - 1);
+    const uint8_t *w = a.w + wrow * a.ldw + g * 16, *ws = a.ws + wrow * a.ldws;
+    const bool there = r16 < a.rows;
+    const uint8_t *x = a.x + (there ? r16 : 0) * a.ldx + g * 16, *xs = a.xs + (there ? r16 : 0) * a.ldxs;
+    f32x4 acc = {};
+    Quad qw[2], qx[2];
+    const int stride = KW * 4;
+    load_quad(qw[0], w, ws, kw * 4, a.blocks, true);
+    load_quad(qx[0], x, xs, kw * 4, a.blocks, there);
+    auto quad = [&](int at, int block) {
+        load_quad(qw[at ^ 1], w, ws, block + stride, a.blocks, true);
+        load_quad(qx[at ^ 1], x, xs, block + stride, a.blocks, there);
+        int ew[4] = {};
+        if constexpr (T::size == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ew[e] = __shfl(qw[at].scale, g * 4 + e, 64);
+        }
+        unrolled<4>([&](auto k) {
+            constexpr int K = decltype(k)::value;
+            if (block + K < a.blocks)  // (a scale behind the last block's may be anything)
+                acc = block_product<T, K>(join(qw[at].lo[K], qw[at].hi[K]), join(qx[at].lo[K], qx[at].hi[K]), acc, qw[at].scale, qx[at].scale, ew);
+        });
+    };
+    for (int block = kw * 4; block < a.blocks; block += 2 * stride) {
+        quad(0, block);
+        if (block + stride < a.blocks) quad(1, block + stride);
+    }
+    if constexpr (KW > 1) {
+        s_sum[threadIdx.x] = acc;
+        __syncthreads();
+        if (kw > 0) return;
+        acc = f32x4{};
+#pragma unroll
+        for (int k = 0; k < KW; ++k) acc += s_sum[(wave + k) * 64 + lane];
+    }
+    const int64_t col = col0 + g * 4;
+    if (there && col < a.m) put4<T>(a, r16, col, acc);
+}
+
+// 17 .. 128 rows: 16 NX of them, whose blocks four wavefronts (64 rows of w) share through LDS, two blocks at a time.
+template <typename T, int NX>
+__global__ __launch_bounds__(256, 2) void product_some_kernel(ProductArgs a) {
+    constexpr int kStage = NX * 16 * 256;  // two blocks of a row after each other
+    __shared__ __attribute__((aligned(16))) uint8_t s_x[2 * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, g = lane >> 4;
+    const int64_t col0 = (int64_t)blockIdx.x * 64 + wave * 16, wrow = min(col0 + r16, (int64_t)a.m - 1);
+    const uint8_t *w = a.w + wrow * a.ldw + g * 16, *ws = a.ws + wrow * a.ldws;
+    const int first = blockIdx.y * a.per_split, last = min(first + a.per_split, a.blocks);
+    // Fetches: four rows of 256 bytes to a load, 16-byte pieces at piece ^ (row & 15); NX of them to a wavefront.
+    const uint8_t *from[NX];
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+        const int r = (wave * NX + i) * 4 + (lane >> 4), piece = (lane & 15) ^ (r & 15);
+        from[i] = a.x + min(r, a.rows - 1) * a.ldx + piece * 16;
+    }
+    // (the second block of the last pair may lie behind the row: then the first one comes twice)
+    auto fetch = [&](int buf, int block) {
+#pragma unroll
+        for (int i = 0; i < NX; ++i) {
+            const int piece = (lane & 15) ^ (((wave * NX + i) * 4 + (lane >> 4)) & 15);
+            const int back = block + 1 < a.blocks || piece < 8 ? 0 : 128;
+            load_lds16(from[i] + (int64_t)block * 128 - back, &s_x[buf * kStage + (wave * NX + i) * 1024]);
+        }
+    };
+    const uint8_t *xs[NX];
+#pragma unroll
+    for (int j = 0; j < NX; ++j) xs[j] = a.xs + min(j * 16 + r16, a.rows - 1) * a.ldxs;
+    f32x4 acc[NX] = {};
+    int scale_w = 0, scale_x[NX] = {}, ew[4] = {};
+    i32x4 lo[2][2], hi[2][2];
+    auto load_w = [&](int at, int block) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int b = min(block + k, last - 1);
+            lo[at][k] = *(const i32x4 *)(w + (int64_t)b * 128);
+            hi[at][k] = *(const i32x4 *)(w + (int64_t)b * 128 + 64);
+        }
+    };
+    fetch(0, first);
+    load_w(0, first);
+    auto pair = [&](auto p, int block) {
+        constexpr int P = decltype(p)::value;
+        if constexpr (P == 0) {
+            scale_w = *(const int *)(ws + block);
+#pragma unroll
+            for (int j = 0; j < NX; ++j) scale_x[j] = *(const int *)(xs[j] + block);
+            if constexpr (T::size == 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ew[e] = __shfl(scale_w, g * 4 + e, 64);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (block + 2 < last) {
+            fetch(P ^ 1, block + 2);
+            load_w(P ^ 1, block + 2);
+        }
+        unrolled<2>([&](auto k) {
+            constexpr int K = decltype(k)::value;
+            if (block + K < last) {
+                const i32x8 fw = join(lo[P][K], hi[P][K]);
+#pragma unroll
+                for (int j = 0; j < NX; ++j) {
+                    const uint8_t *row = &s_x[P * kStage + (j * 16 + r16) * 256];
+                    const i32x8 fx = join(*(const i32x4 *)(row + (((K * 8 + g) ^ r16) * 16)), *(const i32x4 *)(row + (((K * 8 + g + 4) ^ r16) * 16)));
+                    acc[j] = block_product<T, 2 * P + K>(fw, fx, acc[j], scale_w, scale_x[j], ew);
+                }
+            }
+        });
+    };
+    for (int block = first; block < last; block += 4) {
+        pair(std::integral_constant<int, 0>(), block);
+        if (block + 2 < last) pair(std::integral_constant<int, 1>(), block + 2);
+    }
+    const int64_t col = col0 + g * 4;
+    if (col >= a.m) return;
+#pragma unroll
+    for (int j = 0; j < NX; ++j) {
+        const int row = j * 16 + r16;
+        if (row >= a.rows) continue;
+        if (a.part) {
+            float *p = a.part + ((int64_t)blockIdx.y * a.rows + row) * a.m + col;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < a.m) p[e] = acc[j][e];
+        } else {
+            put4<T>(a, row, col, acc[j]);
+        }
+    }
+}
+
 // y from the splits' sums, added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void product_sum_kernel(ProductArgs a, int splits) {
@@ -426,30 +607,43 @@ __global__ __launch_bounds__(256) void product_sum_kernel(ProductArgs a, int spl
     }
 }
 
+enum ProductForm { kFew, kSome, kTiles, kWide };
 struct ProductPlan {
-    int splits, per_split;
-    bool wide;
+    ProductForm form;
+    int splits, per_split;  // of the sum, and its blocks in one
+    int kw;
 };
-// The sum is split where the tiles do not fill the GPU.
+// Which form, and how the sum is split where the outputs alone do not fill the GPU.
 static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, int64_t most_stride) {
+    const int64_t blocks = ceil_div(n, 128), quads = ceil_div(blocks, 4);
+    if (rows <= 16) {
+        int kw = 1;
+        while (kw < 8 && ceil_div(m, 16) * kw < 2048 && kw * 2 <= quads) kw *= 2;
+        return {kFew, 1, 0, kw};
+    }
+    if (blocks == 0) return {kTiles, 1, 4, 0};  // (the others begin with a fetch)
     // Tiles of 256 x 256 run one to a compute unit: they lose by a last round that is nearly empty.
     const int64_t wide = ceil_div(rows, kWideTile) * ceil_div(m, kWideTile);
     if (dtype == DLCX_BF16 && rows >= kWideTile && m >= kWideTile && wide >= 128 && most_stride <= (1 << 23))  // (256 rows: 32 bits)
-        return {1, (int)(ceil_div(n, 512) * 4), true};
-    const int64_t tiles = ceil_div(rows, 128) * ceil_div(m, 128), blocks = ceil_div(n, 128);
-    int64_t splits = 1;
-    if (tiles < 512 && tiles > 0) splits = ceil_div(512, tiles);
-    if (splits > blocks / 4) splits = blocks / 4;
-    if (splits < 1) splits = 1;
-    const int64_t per = (ceil_div(blocks, splits) + 3) / 4 * 4;
-    return {(int)(blocks ? ceil_div(blocks, per) : 1), (int)per, false};
+        return {kWide, 1, 0, 0};
+    const bool some = rows <= 128;
+    const int64_t tiles = some ? ceil_div(m, 64) : ceil_div(rows, 128) * ceil_div(m, 128);
+    int64_t splits = some ? (tiles < 384 ? ceil_div(512, tiles) : 1) : tiles < 512 ? ceil_div(512, tiles) : 1;
+    splits = std::max((int64_t)1, std::min(splits, blocks / 4));
+    const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
+    return {some ? kSome : kTiles, (int)(blocks ? ceil_div(blocks, per) : 1), (int)per, 0};
+}
+
+template <typename T, int NX>
+static void run_some(const ProductArgs &a, int splits, hipStream_t st) {
+    product_some_kernel<T, NX><<<dim3((unsigned)ceil_div(a.m, 64), splits), 256, 0, st>>>(a);
 }
 
 template <typename T>
 static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st) {
     {
         Timed timed(KID_FP8_PRODUCT, st);
-        if (plan.wide) {
+        if (plan.form == kWide) {
             static size_t granted[2] = {0, 0};
             const auto kernel = a.y_in ? product_wide_kernel<true> : product_wide_kernel<false>;
             int rc = grant_dynamic_lds((const void *)kernel, kWideLds, &granted[a.y_in ? 1 : 0], "fp8_product");
@@ -457,9 +651,20 @@ static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st
             a.row_tiles = (int)ceil_div(a.rows, kWideTile);
             a.col_tiles = (int)ceil_div(a.m, kWideTile);
             kernel<<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles)), 256, kWideLds, st>>>(a);
-            return check_launch("fp8_product");
+        } else if (plan.form == kFew) {
+            const dim3 grid((unsigned)ceil_div(a.m, 16 * (8 / plan.kw)));
+            if (plan.kw == 1) product_few_kernel<T, 1><<<grid, 512, 0, st>>>(a);
+            else if (plan.kw == 2) product_few_kernel<T, 2><<<grid, 512, 0, st>>>(a);
+            else if (plan.kw == 4) product_few_kernel<T, 4><<<grid, 512, 0, st>>>(a);
+            else product_few_kernel<T, 8><<<grid, 512, 0, st>>>(a);
+        } else if (plan.form == kSome) {
+            if (a.rows <= 32) run_some<T, 2>(a, plan.splits, st);
+            else if (a.rows <= 64) run_some<T, 4>(a, plan.splits, st);
+            else if (a.rows <= 96) run_some<T, 6>(a, plan.splits, st);
+            else run_some<T, 8>(a, plan.splits, st);
+        } else {
+            product_kernel<T><<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits), 256, 0, st>>>(a);
         }
-        product_kernel<T><<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits), 256, 0, st>>>(a);
         const int rc = check_launch("fp8_product");
         if (rc != DLCX_OK || plan.splits == 1) return rc;
     }
@@ -482,12 +687,12 @@ static bool bad_product(int64_t rows, int64_t m, int64_t n) {
 size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
     if (bad_product(rows, m, n)) return 0;
     size_t most = 0;  // of fewer rows, too: these may be split further
-    for (int64_t tiles = 1; tiles <= ceil_div(rows, 128) && tiles <= 512; ++tiles) {
-        const int64_t r = tiles * 128 < rows ? tiles * 128 : rows;
+    auto look = [&](int64_t r) {
         const ProductPlan plan = product_plan(r, m, n, DLCX_F32, 0);  // (bf16 results never need more)
-        const size_t need = plan.splits > 1 ? (size_t)plan.splits * r * m * sizeof(float) : 0;
-        if (need > most) most = need;
-    }
+        if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * r * m * sizeof(float));
+    };
+    look(std::min(rows, (int64_t)128));
+    for (int64_t tiles = 2; tiles <= ceil_div(rows, 128) && tiles <= 512; ++tiles) look(std::min(tiles * 128, rows));
     return a256x(most) + 256;
 }
 

@@ -175,13 +175,14 @@ def test_large_product(rows, m, n):
 
 def test_product_without_terms():
     """A sum of no terms is zero: y_in comes back."""
-    x, w = dlcx.fp8_empty(5, 0, DEV), dlcx.fp8_empty(7, 0, DEV)
-    ws = torch.empty(dlcx.dlcx_fp8_product_workspace_bytes(5, 7, 0), device=DEV, dtype=torch.uint8)
-    y_in, y = torch.randn(5, 7, device=DEV), torch.full((5, 7), 9.0, device=DEV)
-    dlcx.dlcx_fp8_product(x, w, y_in, y, ws)
-    assert torch.equal(y, y_in)
-    dlcx.dlcx_fp8_product(x, w, None, y, ws)
-    assert not bool(y.any())
+    for rows, m, dt in ((5, 7, torch.float32), (50, 70, torch.bfloat16), (3000, 3000, torch.bfloat16)):
+        x, w = dlcx.fp8_empty(rows, 0, DEV), dlcx.fp8_empty(m, 0, DEV)
+        ws = torch.empty(dlcx.dlcx_fp8_product_workspace_bytes(rows, m, 0), device=DEV, dtype=torch.uint8)
+        y_in, y = torch.randn(rows, m, device=DEV).to(dt), torch.full((rows, m), 9.0, device=DEV, dtype=dt)
+        dlcx.dlcx_fp8_product(x, w, y_in, y, ws)
+        assert torch.equal(y, y_in)
+        dlcx.dlcx_fp8_product(x, w, None, y, ws)
+        assert not bool(y.any())
 
 
 @pytest.mark.parametrize("rows", [1, 20, 300])
