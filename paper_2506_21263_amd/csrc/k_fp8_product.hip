@@ -64,102 +64,130 @@ __device__ __forceinline__ f32x4 scaled_mma(const i32x8 &a, const i32x8 &b, cons
 template <typename T>
 __device__ __forceinline__ void put4(const ProductArgs &a, int64_t row, int64_t col, f32x4 v) {
     typedef typename T::elem elem;
+    struct __attribute__((packed, aligned(T::size))) Four { elem e[4]; };
     const int there = (int)min((int64_t)4, a.m - col);
-    if (a.y_in) {
-        const elem *p = (const elem *)a.y_in + row * a.ldi + col;
+    const elem *in = (const elem *)a.y_in + row * a.ldi + col;
+    elem *out = (elem *)a.y + row * a.ldo + col;
+    if (there == 4) {
+        if (a.y_in) {
+            const Four f = *(const Four *)in;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < there) v[i] += T::get(p[i]);
+            for (int i = 0; i < 4; ++i) v[i] += T::get(f.e[i]);
+        }
+        Four f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.e[i] = T::put(v[i]);
+        *(Four *)out = f;
+        return;
     }
-    elem *p = (elem *)a.y + row * a.ldo + col;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (i < there) p[i] = T::put(v[i]);
+        if (i < there) out[i] = T::put(a.y_in ? v[i] + T::get(in[i]) : v[i]);
+}
+// Partial sums of a split, rows padded to a multiple of four.
+__device__ __forceinline__ int64_t part_pitch(int m) { return (m + 3) / 4 * 4; }
+__device__ __forceinline__ void put_part(const ProductArgs &a, int64_t split, int64_t row, int64_t col, const f32x4 &v) {
+    *(f32x4 *)(a.part + (split * a.rows + row) * part_pitch(a.m) + col) = v;
 }
 
-// 128 x 128 outputs to a workgroup of four wavefronts, 64 x 64 to each.  Tiles of 128 rows x 128 bytes, twice, straight
-// to LDS; the 16-byte pieces of a row lie at piece ^ (row & 7), so that eight rows' same piece lies in all banks.
-// Rows past the end are read as the last one and not written.
-template <typename T>
+struct TilePlace {
+    int row, col;
+};
+// The tile of workgroup `id`.  Consecutive ones go to different XCDs: each XCD gets a contiguous range of tiles, in
+// groups of `group` rows of tiles, whose operands its L2 holds.
+__device__ __forceinline__ TilePlace tile_place(int id, int row_tiles, int col_tiles, int group) {
+    const int total = row_tiles * col_tiles, share = total / 8, more = total % 8, xcd = id & 7;
+    const int t = xcd * share + min(xcd, more) + (id >> 3);
+    const int per = group * col_tiles, first = t / per * group, rows = min(group, row_tiles - first), in = t % per;
+    return {__builtin_amdgcn_readfirstlane(first + in % rows), __builtin_amdgcn_readfirstlane(in / rows)};
+}
+
+// ---- tiles --------------------------------------------------------------------------------------------
+// 128 columns x 32 FN rows of outputs to a workgroup of four wavefronts, 64 x 16 FN to each.  128 bytes of the tile's
+// rows at a time, twice, straight to LDS; the 16-byte pieces of a row lie at piece ^ (row & 7), so that what is read at
+// once lies in all banks.  Rows past the end are read as the last one and not written.
+template <typename T, int FN>
 __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
-    __shared__ __attribute__((aligned(16))) uint8_t s_tile[2][2][128 * 128];
+    constexpr int kRows = 32 * FN, kStage = (128 + kRows) * 128, kFetchX = kRows / 32;
+    constexpr bool kWiden = T::size == 4;       // fp32 results
+    constexpr int kScaleRows = kWiden ? 4 : 1;  // of w, to a lane: its outputs' or its operand's
+    __shared__ __attribute__((aligned(16))) uint8_t s_tile[2 * kStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t row0 = (int64_t)(blockIdx.x % a.row_tiles) * 128, col0 = (int64_t)(blockIdx.x / a.row_tiles) * 128;
+    const TilePlace place = tile_place(blockIdx.x, a.row_tiles, a.col_tiles, 8);
+    const int64_t row0 = (int64_t)place.row * kRows, col0 = (int64_t)place.col * 128;
     const int split = blockIdx.y, first = split * a.per_split, last = min(first + a.per_split, a.blocks);
-    const uint8_t *from[2][4];
+    const uint8_t *from_w[4], *from_x[kFetchX];
+    const int piece = (lane & 7) ^ (lane >> 3);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = wave * 32 + i * 8 + (lane >> 3), piece = (lane & 7) ^ (r & 7);
-        from[0][i] = a.w + min(col0 + r, (int64_t)a.m - 1) * a.ldw + piece * 16;
-        from[1][i] = a.x + min(row0 + r, (int64_t)a.rows - 1) * a.ldx + piece * 16;
-    }
+    for (int i = 0; i < 4; ++i) from_w[i] = a.w + min(col0 + wave * 32 + i * 8 + (lane >> 3), (int64_t)a.m - 1) * a.ldw + piece * 16;
+#pragma unroll
+    for (int i = 0; i < kFetchX; ++i)
+        from_x[i] = a.x + min(row0 + (wave * kFetchX + i) * 8 + (lane >> 3), (int64_t)a.rows - 1) * a.ldx + piece * 16;
     auto fetch = [&](int buf, int block) {
+        uint8_t *to = s_tile + buf * kStage;
 #pragma unroll
-        for (int o = 0; o < 2; ++o)
+        for (int i = 0; i < 4; ++i) load_lds16(from_w[i] + (int64_t)block * 128, to + (wave * 4 + i) * 1024);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_lds16(from[o][i] + (int64_t)block * 128, &s_tile[buf][o][(wave * 32 + i * 8) * 128]);
+        for (int i = 0; i < kFetchX; ++i) load_lds16(from_x[i] + (int64_t)block * 128, to + 128 * 128 + (wave * kFetchX + i) * 1024);
     };
-    const int r16 = lane & 15, g = lane >> 4, wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
-    constexpr bool kWide = T::size == 4;      // fp32 results
-    constexpr int kScaleRows = kWide ? 4 : 1;  // of w, to a lane: its outputs' or its operand's
-    const uint8_t *sw[4][kScaleRows], *sx[4];
+    const int r16 = lane & 15, g = lane >> 4, wm = (wave & 1) * 64, wn = (wave >> 1) * 16 * FN;
+    const uint8_t *sw[4][kScaleRows], *sx[FN];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int e = 0; e < kScaleRows; ++e)
-            sw[i][e] = a.ws + min(col0 + wm + i * 16 + (kWide ? g * 4 + e : r16), (int64_t)a.m - 1) * a.ldws;
-        sx[i] = a.xs + min(row0 + wn + i * 16 + r16, (int64_t)a.rows - 1) * a.ldxs;
-    }
-    f32x4 acc[4][4] = {};
-    int scale_w[4][kScaleRows], scale_x[4];
+            sw[i][e] = a.ws + min(col0 + wm + i * 16 + (kWiden ? g * 4 + e : r16), (int64_t)a.m - 1) * a.ldws;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) sx[j] = a.xs + min(row0 + wn + j * 16 + r16, (int64_t)a.rows - 1) * a.ldxs;
+    const int p0 = (g ^ (lane & 7)) * 16, p1 = ((g + 4) ^ (lane & 7)) * 16;
+    f32x4 acc[4][FN] = {};
+    int scale_w[4][kScaleRows], scale_x[FN];
     auto step = [&](int buf, auto s) {
-        i32x8 fw[4], fx[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int rw = wm + i * 16 + r16, rx = wn + i * 16 + r16;
-            const uint8_t *pw = &s_tile[buf][0][rw * 128], *px = &s_tile[buf][1][rx * 128];
-            fw[i] = join(*(const i32x4 *)(pw + ((g ^ (rw & 7)) * 16)), *(const i32x4 *)(pw + (((g + 4) ^ (rw & 7)) * 16)));
-            fx[i] = join(*(const i32x4 *)(px + ((g ^ (rx & 7)) * 16)), *(const i32x4 *)(px + (((g + 4) ^ (rx & 7)) * 16)));
-        }
         constexpr int S = decltype(s)::value;
-        if constexpr (kWide) {
-            f32x4 sum[4][4] = {};
+        const uint8_t *pw = s_tile + buf * kStage + (wm + r16) * 128, *px = s_tile + buf * kStage + (128 + wn + r16) * 128;
+        i32x8 fw[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                bf16x8 bw[4], bx[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    bw[i] = widen(fw[i][2 * k], fw[i][2 * k + 1]);
-                    bx[i] = widen(fx[i][2 * k], fx[i][2 * k + 1]);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i], bx[j], sum[i][j], 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                int ew[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) ew[e] = (scale_w[i][e] >> (8 * S)) & 255;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = add_scaled(acc[i][j], sum[i][j], ew, (scale_x[j] >> (8 * S)) & 255);
-            }
-        } else {
+        for (int i = 0; i < 4; ++i) fw[i] = join(*(const i32x4 *)(pw + i * 2048 + p0), *(const i32x4 *)(pw + i * 2048 + p1));
+        if constexpr (kWiden) {
+            bf16x8 bw[4][4];
+            int ew[4][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = scaled_mma<S>(fw[i], fx[j], acc[i][j], scale_w[i][0], scale_x[j]);
+                for (int k = 0; k < 4; ++k) {
+                    bw[i][k] = widen(fw[i][2 * k], fw[i][2 * k + 1]);
+                    ew[i][k] = (scale_w[i][k] >> (8 * S)) & 255;
+                }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
+                f32x4 sum[4] = {};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bf16x8 bx = widen(fx[2 * k], fx[2 * k + 1]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i][k], bx, sum[i], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][j] = add_scaled(acc[i][j], sum[i], ew[i], (scale_x[j] >> (8 * S)) & 255);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][j] = scaled_mma<S>(fw[i], fx, acc[i][j], scale_w[i][0], scale_x[j]);
+            }
         }
     };
     if (first < last) fetch(0, first);
     for (int block = first; block < last; block += 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < kScaleRows; ++e) scale_w[i][e] = *(const int *)(sw[i][e] + block);
-            scale_x[i] = *(const int *)(sx[i] + block);
-        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j) scale_x[j] = *(const int *)(sx[j] + block);
         unrolled<4>([&](auto s) {
             constexpr int S = decltype(s)::value;
             if (block + S < last) {
@@ -171,21 +199,15 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
         });
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < FN; ++j) {
         const int64_t row = row0 + wn + j * 16 + r16;
         if (row >= a.rows) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t col = col0 + wm + i * 16 + g * 4;
             if (col >= a.m) continue;
-            if (a.part) {
-                float *p = a.part + ((int64_t)split * a.rows + row) * a.m + col;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col + e < a.m) p[e] = acc[i][j][e];
-            } else {
-                put4<T>(a, row, col, acc[i][j]);
-            }
+            if (a.part) put_part(a, split, row, col, acc[i][j]);
+            else put4<T>(a, row, col, acc[i][j]);
         }
     }
 }
@@ -199,25 +221,12 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
 // Scales go through LDS, too (four stages' to a dword): read by every lane that needs them they were 40 % of all
 // requests to the cache.  Results leave through LDS as whole lines.  Edge tiles are moved inside the matrix and write
 // only what is theirs, so no address is checked.
-// Consecutive workgroups go to different XCDs: each XCD gets a contiguous range of tiles, in groups of four rows of
-// tiles, whose operands its L2 holds.
 // 16384 x 8192 x 8192: 0.82 ms, 2.7 PFLOP/s (0.64 without the fetches, 1.44 with 128 x 128 tiles); 8192^3 0.41 ms.
 constexpr int kWideTile = 256, kWideStage = 512 * 128, kWideLds = 2 * kWideStage + 2 * 2048;
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 template <typename V>
 __device__ __forceinline__ V lds_read(uint32_t at) { return *(const __attribute__((address_space(3))) V *)(uintptr_t)at; }
-
-struct TilePlace {
-    int row, col;
-};
-// The tile of this workgroup.
-__device__ __forceinline__ TilePlace tile_place(int row_tiles, int col_tiles, int group) {
-    const int total = row_tiles * col_tiles, id = blockIdx.x, share = total / 8, more = total % 8, xcd = id & 7;
-    const int t = xcd * share + min(xcd, more) + (id >> 3);
-    const int per = group * col_tiles, first = t / per * group, rows = min(group, row_tiles - first), in = t % per;
-    return {__builtin_amdgcn_readfirstlane(first + in % rows), __builtin_amdgcn_readfirstlane(in / rows)};
-}
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *p) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, -1, 0x00020000);
@@ -235,7 +244,7 @@ __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t s_wide[];
     uint8_t *const s_scale = s_wide + 2 * kWideStage;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const TilePlace place = tile_place(a.row_tiles, a.col_tiles, 4);
+    const TilePlace place = tile_place(blockIdx.x, a.row_tiles, a.col_tiles, 4);
     const int row0 = min(place.row * kWideTile, a.rows - kWideTile), col0 = min(place.col * kWideTile, a.m - kWideTile);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte *)s_wide;
     const auto from_w = buffer_at(a.w + col0 * a.ldw), from_x = buffer_at(a.x + row0 * a.ldx);
@@ -579,14 +588,8 @@ __global__ __launch_bounds__(256, 2) void product_some_kernel(ProductArgs a) {
     for (int j = 0; j < NX; ++j) {
         const int row = j * 16 + r16;
         if (row >= a.rows) continue;
-        if (a.part) {
-            float *p = a.part + ((int64_t)blockIdx.y * a.rows + row) * a.m + col;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (col + e < a.m) p[e] = acc[j][e];
-        } else {
-            put4<T>(a, row, col, acc[j]);
-        }
+        if (a.part) put_part(a, blockIdx.y, row, col, acc[j]);
+        else put4<T>(a, row, col, acc[j]);
     }
 }
 
@@ -595,15 +598,11 @@ template <typename T>
 __global__ __launch_bounds__(256) void product_sum_kernel(ProductArgs a, int splits) {
     const int64_t quads = (a.m + 3) / 4, total = quads * a.rows;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
-        const int64_t row = at / quads, col = (at - row * quads) * 4;
         f32x4 v = {};
-        for (int s = 0; s < splits; ++s) {
-            const float *p = a.part + ((int64_t)s * a.rows + row) * a.m + col;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (col + e < a.m) v[e] += p[e];
-        }
-        put4<T>(a, row, col, v);
+        const f32x4 *p = (const f32x4 *)a.part + at;
+        for (int s = 0; s < splits; ++s) v += p[s * total];
+        const int64_t row = at / quads;
+        put4<T>(a, row, (at - row * quads) * 4, v);
     }
 }
 
@@ -611,7 +610,7 @@ enum ProductForm { kFew, kSome, kTiles, kWide };
 struct ProductPlan {
     ProductForm form;
     int splits, per_split;  // of the sum, and its blocks in one
-    int kw;
+    int kw;  // kFew: wavefronts along the sum; kTiles: fragments of x
 };
 // Which form, and how the sum is split where the outputs alone do not fill the GPU.
 static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, int64_t most_stride) {
@@ -621,17 +620,20 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
         while (kw < 8 && ceil_div(m, 16) * kw < 2048 && kw * 2 <= quads) kw *= 2;
         return {kFew, 1, 0, kw};
     }
-    if (blocks == 0) return {kTiles, 1, 4, 0};  // (the others begin with a fetch)
+    if (blocks == 0) return {kTiles, 1, 4, 4};  // (the others begin with a fetch)
     // Tiles of 256 x 256 run one to a compute unit: they lose by a last round that is nearly empty.
     const int64_t wide = ceil_div(rows, kWideTile) * ceil_div(m, kWideTile);
     if (dtype == DLCX_BF16 && rows >= kWideTile && m >= kWideTile && wide >= 128 && most_stride <= (1 << 23))  // (256 rows: 32 bits)
         return {kWide, 1, 0, 0};
     const bool some = rows <= 128;
-    const int64_t tiles = some ? ceil_div(m, 64) : ceil_div(rows, 128) * ceil_div(m, 128);
-    int64_t splits = some ? (tiles < 384 ? ceil_div(512, tiles) : 1) : tiles < 512 ? ceil_div(512, tiles) : 1;
+    const int64_t col_tiles = ceil_div(m, some ? 64 : 128);
+    // Tiles of 64 rows where those of 128 leave compute units without work.
+    const int fn = some || ceil_div(rows, 128) * col_tiles >= 512 ? 4 : 2;
+    const int64_t tiles = some ? col_tiles : ceil_div(rows, 32 * fn) * col_tiles;
+    int64_t splits = tiles < 384 ? ceil_div(512, tiles) : 1;
     splits = std::max((int64_t)1, std::min(splits, blocks / 4));
     const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
-    return {some ? kSome : kTiles, (int)(blocks ? ceil_div(blocks, per) : 1), (int)per, 0};
+    return {some ? kSome : kTiles, (int)ceil_div(blocks, per), (int)per, fn};
 }
 
 template <typename T, int NX>
@@ -663,7 +665,10 @@ static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st
             else if (a.rows <= 96) run_some<T, 6>(a, plan.splits, st);
             else run_some<T, 8>(a, plan.splits, st);
         } else {
-            product_kernel<T><<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits), 256, 0, st>>>(a);
+            a.row_tiles = (int)ceil_div(a.rows, 32 * plan.kw);
+            const dim3 grid((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits);
+            if (plan.kw == 4) product_kernel<T, 4><<<grid, 256, 0, st>>>(a);
+            else product_kernel<T, 2><<<grid, 256, 0, st>>>(a);
         }
         const int rc = check_launch("fp8_product");
         if (rc != DLCX_OK || plan.splits == 1) return rc;
@@ -689,10 +694,10 @@ size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
     size_t most = 0;  // of fewer rows, too: these may be split further
     auto look = [&](int64_t r) {
         const ProductPlan plan = product_plan(r, m, n, DLCX_F32, 0);  // (bf16 results never need more)
-        if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * r * m * sizeof(float));
+        if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * r * ceil_div(m, 4) * 16);
     };
     look(std::min(rows, (int64_t)128));
-    for (int64_t tiles = 2; tiles <= ceil_div(rows, 128) && tiles <= 512; ++tiles) look(std::min(tiles * 128, rows));
+    for (int64_t tiles = 3; tiles <= ceil_div(rows, 64) && tiles <= 1024; ++tiles) look(std::min(tiles * 64, rows));
     return a256x(most) + 256;
 }
 
@@ -709,7 +714,7 @@ int dlcx_fp8_product(const dlcx_fp8 *x, const dlcx_fp8 *w, const void *y_in, int
                      y_in, y_out, plan.splits > 1 ? (float *)workspace : nullptr, x->ld, x->ldscale, w->ld, w->ldscale,
                      ldy_in, ldy_out, (int)x->rows, (int)w->rows, (int)ceil_div(x->cols, 128), plan.per_split,
                      (int)ceil_div(x->rows, 128), (int)ceil_div(w->rows, 128)};
-    if ((int64_t)a.row_tiles * a.col_tiles >= kMostGroups) return DLCX_EUNSUPPORTED;
+    if ((int64_t)a.row_tiles * a.col_tiles >= kMostGroups / 2) return DLCX_EUNSUPPORTED;  // 2^51 outputs
     return dtype == DLCX_BF16 ? launch_product<TypeBf16>(a, plan, as_stream(stream)) : launch_product<TypeF32>(a, plan, as_stream(stream));
 }
 
