@@ -506,90 +506,115 @@ __global__ __launch_bounds__(512, 2) void product_few_kernel(ProductArgs a) {
     if (there && col < a.m) put4<T>(a, r16, col, acc);
 }
 
-// 17 .. 128 rows: 16 NX of them, whose blocks four wavefronts (64 rows of w) share through LDS, two blocks at a time.
-template <typename T, int NX>
-__global__ __launch_bounds__(256, 2) void product_some_kernel(ProductArgs a) {
-    constexpr int kStage = NX * 16 * 256;  // two blocks of a row after each other
-    __shared__ __attribute__((aligned(16))) uint8_t s_x[2 * kStage];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r16 = lane & 15, g = lane >> 4;
-    const int64_t col0 = (int64_t)blockIdx.x * 64 + wave * 16, wrow = min(col0 + r16, (int64_t)a.m - 1);
-    const uint8_t *w = a.w + wrow * a.ldw + g * 16, *ws = a.ws + wrow * a.ldws;
-    const int first = blockIdx.y * a.per_split, last = min(first + a.per_split, a.blocks);
-    // Fetches: four rows of 256 bytes to a load, 16-byte pieces at piece ^ (row & 15); NX of them to a wavefront.
-    const uint8_t *from[NX];
+// 17 .. 128 rows: 32 FN of them beside 128 rows of w, one workgroup to a compute unit.  Bound by the reading of w, so what
+// counts is how much of it is on its way: a ring of as many stages as LDS holds (128 bytes of each row, straight to LDS;
+// pieces at piece ^ (row & 7)), all but one of them in flight, 64 KB of w to a compute unit beside 96 rows.  Scales
+// come four stages to a dword, two dwords ahead, 256 rows (w's, then x's) to a load of the workgroup.
+template <typename T, int FN>
+struct SomeShape {
+    static constexpr int kRows = 32 * FN, kStage = (128 + kRows) * 128, kRing = 152 * 1024 / kStage;
+    static constexpr int kLds = kRing * kStage + 4 * 1024;
+};
+template <typename T, int FN>
+__global__ __launch_bounds__(256, 1) void product_some_kernel(ProductArgs a) {
+    typedef SomeShape<T, FN> Shape;
+    constexpr int kStage = Shape::kStage, kRing = Shape::kRing;
+    constexpr bool kWiden = T::size == 4;
+    constexpr int kScaleRows = kWiden ? 4 : 1;
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];
+    uint8_t *const s_scale = s_ring + kRing * kStage;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t col0 = (int64_t)blockIdx.x * 128;
+    const int split = blockIdx.y, first = split * a.per_split, last = min(first + a.per_split, a.blocks);
+    const int piece = (lane & 7) ^ (lane >> 3);
+    const uint8_t *from_w[4], *from_x[FN];
 #pragma unroll
-    for (int i = 0; i < NX; ++i) {
-        const int r = (wave * NX + i) * 4 + (lane >> 4), piece = (lane & 15) ^ (r & 15);
-        from[i] = a.x + min(r, a.rows - 1) * a.ldx + piece * 16;
-    }
-    // (the second block of the last pair may lie behind the row: then the first one comes twice)
-    auto fetch = [&](int buf, int block) {
+    for (int i = 0; i < 4; ++i) from_w[i] = a.w + min(col0 + (wave * 4 + i) * 8 + (lane >> 3), (int64_t)a.m - 1) * a.ldw + piece * 16;
 #pragma unroll
-        for (int i = 0; i < NX; ++i) {
-            const int piece = (lane & 15) ^ (((wave * NX + i) * 4 + (lane >> 4)) & 15);
-            const int back = block + 1 < a.blocks || piece < 8 ? 0 : 128;
-            load_lds16(from[i] + (int64_t)block * 128 - back, &s_x[buf * kStage + (wave * NX + i) * 1024]);
-        }
+    for (int i = 0; i < FN; ++i) from_x[i] = a.x + min((wave * FN + i) * 8 + (lane >> 3), a.rows - 1) * a.ldx + piece * 16;
+    const uint8_t *from_s = wave < 2 ? a.ws + min(col0 + tid, (int64_t)a.m - 1) * a.ldws : a.xs + min(tid - 128, a.rows - 1) * a.ldxs;
+    // (past the last stage it comes again, and is not used: every wavefront always has the same number under way)
+    auto fetch = [&](int slot, int block) {
+        const int64_t at = (int64_t)min(block, last - 1) * 128;
+        uint8_t *to = s_ring + slot * kStage;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_lds16(from_w[i] + at, to + (wave * 4 + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < FN; ++i) load_lds16(from_x[i] + at, to + 128 * 128 + (wave * FN + i) * 1024);
     };
-    const uint8_t *xs[NX];
-#pragma unroll
-    for (int j = 0; j < NX; ++j) xs[j] = a.xs + min(j * 16 + r16, a.rows - 1) * a.ldxs;
-    f32x4 acc[NX] = {};
-    int scale_w = 0, scale_x[NX] = {}, ew[4] = {};
-    i32x4 lo[2][2], hi[2][2];
-    auto load_w = [&](int at, int block) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int b = min(block + k, last - 1);
-            lo[at][k] = *(const i32x4 *)(w + (int64_t)b * 128);
-            hi[at][k] = *(const i32x4 *)(w + (int64_t)b * 128 + 64);
-        }
+    auto fetch_scales = [&](int block) {  // (first is a multiple of four)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from_s + min(block, (last - 1) & ~3)),
+                                         (__attribute__((address_space(3))) void *)(s_scale + (block >> 2 & 3) * 1024 + wave * 256), 4, 0, 0);
     };
-    fetch(0, first);
-    load_w(0, first);
-    auto pair = [&](auto p, int block) {
-        constexpr int P = decltype(p)::value;
-        if constexpr (P == 0) {
-            scale_w = *(const int *)(ws + block);
+    fetch_scales(first);
+    fetch_scales(first + 4);
 #pragma unroll
-            for (int j = 0; j < NX; ++j) scale_x[j] = *(const int *)(xs[j] + block);
-            if constexpr (T::size == 4) {
+    for (int k = 0; k < kRing - 1; ++k) fetch(k, first + k);
+    const int r16 = lane & 15, g = lane >> 4, wm = (wave & 1) * 64, wn = (wave >> 1) * 16 * FN;
+    const int p0 = (g ^ (lane & 7)) * 16, p1 = ((g + 4) ^ (lane & 7)) * 16;
+    f32x4 acc[4][FN] = {};
+    int scale_w[4][kScaleRows], scale_x[FN], slot = 0;
+    for (int block = first; block < last; block += 4) {
+        unrolled<4>([&](auto s) {
+            constexpr int S = decltype(s)::value;
+            if (block + S < last) {
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRing - 2) * (4 + FN)) : "memory");  // this stage is there,
+                __syncthreads();                                                              // and the last one has been read
+                if constexpr (S == 0) {
+                    fetch_scales(block + 8);
+                    const int *at = (const int *)(s_scale + (block >> 2 & 3) * 1024);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) ew[e] = __shfl(scale_w, g * 4 + e, 64);
-            }
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (block + 2 < last) {
-            fetch(P ^ 1, block + 2);
-            load_w(P ^ 1, block + 2);
-        }
-        unrolled<2>([&](auto k) {
-            constexpr int K = decltype(k)::value;
-            if (block + K < last) {
-                const i32x8 fw = join(lo[P][K], hi[P][K]);
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < NX; ++j) {
-                    const uint8_t *row = &s_x[P * kStage + (j * 16 + r16) * 256];
-                    const i32x8 fx = join(*(const i32x4 *)(row + (((K * 8 + g) ^ r16) * 16)), *(const i32x4 *)(row + (((K * 8 + g + 4) ^ r16) * 16)));
-                    acc[j] = block_product<T, 2 * P + K>(fw, fx, acc[j], scale_w, scale_x[j], ew);
+                        for (int e = 0; e < kScaleRows; ++e) scale_w[i][e] = at[wm + i * 16 + (kWiden ? g * 4 + e : r16)];
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) scale_x[j] = at[128 + wn + j * 16 + r16];
+                }
+                fetch(slot == 0 ? kRing - 1 : slot - 1, block + S + kRing - 1);
+                const uint8_t *pw = s_ring + slot * kStage + (wm + r16) * 128, *px = s_ring + slot * kStage + (128 + wn + r16) * 128;
+                slot = slot + 1 == kRing ? 0 : slot + 1;
+                i32x8 fw[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fw[i] = join(*(const i32x4 *)(pw + i * 2048 + p0), *(const i32x4 *)(pw + i * 2048 + p1));
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
+                    if constexpr (kWiden) {
+                        f32x4 sum[4] = {};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const bf16x8 bx = widen(fx[2 * k], fx[2 * k + 1]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(fw[i][2 * k], fw[i][2 * k + 1]), bx, sum[i], 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            int ew[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) ew[e] = (scale_w[i][e] >> (8 * S)) & 255;
+                            acc[i][j] = add_scaled(acc[i][j], sum[i], ew, (scale_x[j] >> (8 * S)) & 255);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[i][j] = scaled_mma<S>(fw[i], fx, acc[i][j], scale_w[i][0], scale_x[j]);
+                    }
                 }
             }
         });
-    };
-    for (int block = first; block < last; block += 4) {
-        pair(std::integral_constant<int, 0>(), block);
-        if (block + 2 < last) pair(std::integral_constant<int, 1>(), block + 2);
     }
-    const int64_t col = col0 + g * 4;
-    if (col >= a.m) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is on its way to LDS that is no longer this workgroup's)
 #pragma unroll
-    for (int j = 0; j < NX; ++j) {
-        const int row = j * 16 + r16;
+    for (int j = 0; j < FN; ++j) {
+        const int row = wn + j * 16 + r16;
         if (row >= a.rows) continue;
-        if (a.part) put_part(a, blockIdx.y, row, col, acc[j]);
-        else put4<T>(a, row, col, acc[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t col = col0 + wm + i * 16 + g * 4;
+            if (col >= a.m) continue;
+            if (a.part) put_part(a, split, row, col, acc[i][j]);
+            else put4<T>(a, row, col, acc[i][j]);
+        }
     }
 }
 
@@ -626,19 +651,24 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
     if (dtype == DLCX_BF16 && rows >= kWideTile && m >= kWideTile && wide >= 128 && most_stride <= (1 << 23))  // (256 rows: 32 bits)
         return {kWide, 1, 0, 0};
     const bool some = rows <= 128;
-    const int64_t col_tiles = ceil_div(m, some ? 64 : 128);
+    const int64_t col_tiles = ceil_div(m, 128);
     // Tiles of 64 rows where those of 128 leave compute units without work.
     const int fn = some || ceil_div(rows, 128) * col_tiles >= 512 ? 4 : 2;
     const int64_t tiles = some ? col_tiles : ceil_div(rows, 32 * fn) * col_tiles;
-    int64_t splits = tiles < 384 ? ceil_div(512, tiles) : 1;
+    int64_t splits = some ? (tiles < 160 ? 256 / tiles : 1) : tiles < 384 ? ceil_div(512, tiles) : 1;
     splits = std::max((int64_t)1, std::min(splits, blocks / 4));
     const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
     return {some ? kSome : kTiles, (int)ceil_div(blocks, per), (int)per, fn};
 }
 
-template <typename T, int NX>
-static void run_some(const ProductArgs &a, int splits, hipStream_t st) {
-    product_some_kernel<T, NX><<<dim3((unsigned)ceil_div(a.m, 64), splits), 256, 0, st>>>(a);
+template <typename T, int FN>
+static int run_some(const ProductArgs &a, int splits, hipStream_t st) {
+    static size_t granted = 0;
+    const int lds = SomeShape<T, FN>::kLds;
+    const int rc = grant_dynamic_lds((const void *)product_some_kernel<T, FN>, lds, &granted, "fp8_product");
+    if (rc != DLCX_OK) return rc;
+    product_some_kernel<T, FN><<<dim3((unsigned)ceil_div(a.m, 128), splits), 256, lds, st>>>(a);
+    return DLCX_OK;
 }
 
 template <typename T>
@@ -660,10 +690,11 @@ static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st
             else if (plan.kw == 4) product_few_kernel<T, 4><<<grid, 512, 0, st>>>(a);
             else product_few_kernel<T, 8><<<grid, 512, 0, st>>>(a);
         } else if (plan.form == kSome) {
-            if (a.rows <= 32) run_some<T, 2>(a, plan.splits, st);
-            else if (a.rows <= 64) run_some<T, 4>(a, plan.splits, st);
-            else if (a.rows <= 96) run_some<T, 6>(a, plan.splits, st);
-            else run_some<T, 8>(a, plan.splits, st);
+            const int rc = a.rows <= 32   ? run_some<T, 1>(a, plan.splits, st)
+                           : a.rows <= 64 ? run_some<T, 2>(a, plan.splits, st)
+                           : a.rows <= 96 ? run_some<T, 3>(a, plan.splits, st)
+                                          : run_some<T, 4>(a, plan.splits, st);
+            if (rc != DLCX_OK) return rc;
         } else {
             a.row_tiles = (int)ceil_div(a.rows, 32 * plan.kw);
             const dim3 grid((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits);
