@@ -420,8 +420,7 @@ __global__ __launch_bounds__(256, 1) void product_wide_kernel(ProductArgs a) {
 
 // ---- few rows -------------------------------------------------------------------------------------------
 // w is read once and straight into registers; what bounds this is HBM, or the launch.  Sixteen rows of w to a
-// wavefront; the sum is cut into quads of four blocks (whose scales are one dword), and where m alone does not fill
-// the GPU, KW wavefronts of a workgroup take every KW'th quad and their sums are added through LDS, in order.
+// wavefront; the sum is cut into quads of four blocks (whose scales are one dword), two of them on their way.
 //
 // A lane's part of a 16 x 128 operand: 16 bytes at 16 g and 16 at 64 + 16 g of its row (the order of a sum's terms
 // is free, as long as both operands have it).
@@ -429,18 +428,15 @@ struct Quad {
     i32x4 lo[4], hi[4];
     int scale;
 };
-// Blocks `block` .. `block` + 3 of a row, those before `end`; others, and all without `there`: zeros.
-__device__ __forceinline__ void load_quad(Quad &q, const uint8_t *row, const uint8_t *scales, int block, int end, bool there) {
+// Blocks `block` .. `block` + 3 of a row, none past the last one (which comes again, and is not used).
+__device__ __forceinline__ void load_quad(Quad &q, const uint8_t *row, const uint8_t *scales, int block, int last) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        q.lo[k] = q.hi[k] = i32x4{0, 0, 0, 0};
-        if (there && block + k < end) {
-            q.lo[k] = *(const i32x4 *)(row + (int64_t)(block + k) * 128);
-            q.hi[k] = *(const i32x4 *)(row + (int64_t)(block + k) * 128 + 64);
-        }
+        const uint8_t *p = row + (int64_t)min(block + k, last) * 128;
+        q.lo[k] = *(const i32x4 *)p;
+        q.hi[k] = *(const i32x4 *)(p + 64);
     }
-    q.scale = 0x7f7f7f7f;
-    if (there && block < end) q.scale = *(const int *)(scales + block);
+    q.scale = *(const int *)(scales + block);
 }
 
 // acc + w x^T for one block of 128; S: the byte of the scales.  ew: the scales of the lane's four outputs' rows (fp32).
@@ -460,39 +456,59 @@ __device__ __forceinline__ f32x4 block_product(const i32x8 &w, const i32x8 &x, c
     }
 }
 
-// Up to 16 rows of x.
+// Up to 16 rows of x (a lane whose row is not there has the last one's, and writes nothing).  Where m alone does not
+// fill the GPU, KW wavefronts of a workgroup take every KW'th quad and their sums are added through LDS, in order.
+// 1 row of 28672 x 8192: 48 us (5.0 TB/s); 16 rows: 65.
 template <typename T, int KW>
-__global__ __launch_bounds__(512, 2) void product_few_kernel(ProductArgs a) {
-    constexpr int WR = 8 / KW;
-    __shared__ f32x4 s_sum[KW > 1 ? 8 * 64 : 1];
+__global__ __launch_bounds__(256, 2) void product_few_kernel(ProductArgs a) {
+    constexpr int WR = 4 / KW;
+    __shared__ f32x4 s_sum[KW > 1 ? 4 * 64 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r16 = lane & 15, g = lane >> 4, kw = wave % KW;
+    const int r16 = lane & 15, g = lane >> 4, kw = wave % KW, xrow = min(r16, a.rows - 1);
     const int64_t col0 = ((int64_t)blockIdx.x * WR + wave / KW) * 16, wrow = min(col0 + r16, (int64_t)a.m - 1);
     const uint8_t *w = a.w + wrow * a.ldw + g * 16, *ws = a.ws + wrow * a.ldws;
-    const bool there = r16 < a.rows;
-    const uint8_t *x = a.x + (there ? r16 : 0) * a.ldx + g * 16, *xs = a.xs + (there ? r16 : 0) * a.ldxs;
+    const uint8_t *x = a.x + xrow * a.ldx + g * 16, *xs = a.xs + xrow * a.ldxs;
+    const int last = a.blocks - 1;
     f32x4 acc = {};
     Quad qw[2], qx[2];
-    const int stride = KW * 4;
-    load_quad(qw[0], w, ws, kw * 4, a.blocks, true);
-    load_quad(qx[0], x, xs, kw * 4, a.blocks, there);
-    auto quad = [&](int at, int block) {
-        load_quad(qw[at ^ 1], w, ws, block + stride, a.blocks, true);
-        load_quad(qx[at ^ 1], x, xs, block + stride, a.blocks, there);
+    auto load = [&](auto at, int block) {
+        load_quad(qw[decltype(at)::value], w, ws, block, last);
+        load_quad(qx[decltype(at)::value], x, xs, block, last);
+    };
+    auto multiply = [&](auto at, int block) {
+        constexpr int A = decltype(at)::value;
         int ew[4] = {};
         if constexpr (T::size == 4) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ew[e] = __shfl(qw[at].scale, g * 4 + e, 64);
+            for (int e = 0; e < 4; ++e) ew[e] = __shfl(qw[A].scale, g * 4 + e, 64);
         }
         unrolled<4>([&](auto k) {
             constexpr int K = decltype(k)::value;
-            if (block + K < a.blocks)  // (a scale behind the last block's may be anything)
-                acc = block_product<T, K>(join(qw[at].lo[K], qw[at].hi[K]), join(qx[at].lo[K], qx[at].hi[K]), acc, qw[at].scale, qx[at].scale, ew);
+            if (block + K <= last)
+                acc = block_product<T, K>(join(qw[A].lo[K], qw[A].hi[K]), join(qx[A].lo[K], qx[A].hi[K]), acc, qw[A].scale, qx[A].scale, ew);
         });
     };
-    for (int block = kw * 4; block < a.blocks; block += 2 * stride) {
-        quad(0, block);
-        if (block + stride < a.blocks) quad(1, block + stride);
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    int block = kw * 4;
+    if (block <= last) {
+        load(even, block);
+        for (;;) {
+            if (block + KW * 4 > last) {
+                multiply(even, block);
+                break;
+            }
+            load(odd, block + KW * 4);
+            multiply(even, block);
+            block += KW * 4;
+            if (block + KW * 4 > last) {
+                multiply(odd, block);
+                break;
+            }
+            load(even, block + KW * 4);
+            multiply(odd, block);
+            block += KW * 4;
+        }
     }
     if constexpr (KW > 1) {
         s_sum[threadIdx.x] = acc;
@@ -503,12 +519,14 @@ __global__ __launch_bounds__(512, 2) void product_few_kernel(ProductArgs a) {
         for (int k = 0; k < KW; ++k) acc += s_sum[(wave + k) * 64 + lane];
     }
     const int64_t col = col0 + g * 4;
-    if (there && col < a.m) put4<T>(a, r16, col, acc);
+    if (r16 < a.rows && col < a.m) put4<T>(a, r16, col, acc);
 }
 
 // 17 .. 128 rows: 32 FN of them beside 128 rows of w, one workgroup to a compute unit.  Bound by the reading of w, so what
 // counts is how much of it is on its way: a ring of as many stages as LDS holds (128 bytes of each row, straight to LDS;
-// pieces at piece ^ (row & 7)), all but one of them in flight, 64 KB of w to a compute unit beside 96 rows.  Scales
+// pieces at piece ^ (row & 7)), all but one of them in flight, 64 KB of w to a compute unit beside 96 rows.  (Twice as much,
+// in registers and with a barrier only every four blocks, measured the same: a compute unit takes in 24 - 28 bytes a ns
+// from HBM, and x's are among them.)  96 rows of 28672 x 8192: 77 us, 3.1 TB/s of w, 5.4 of both.  Scales
 // come four stages to a dword, two dwords ahead, 256 rows (w's, then x's) to a load of the workgroup.
 template <typename T, int FN>
 struct SomeShape {
@@ -642,7 +660,7 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
     const int64_t blocks = ceil_div(n, 128), quads = ceil_div(blocks, 4);
     if (rows <= 16) {
         int kw = 1;
-        while (kw < 8 && ceil_div(m, 16) * kw < 2048 && kw * 2 <= quads) kw *= 2;
+        while (kw < 4 && ceil_div(m, 16) * kw < 4096 && kw * 2 <= quads) kw *= 2;
         return {kFew, 1, 0, kw};
     }
     if (blocks == 0) return {kTiles, 1, 4, 4};  // (the others begin with a fetch)
@@ -684,11 +702,10 @@ static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st
             a.col_tiles = (int)ceil_div(a.m, kWideTile);
             kernel<<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles)), 256, kWideLds, st>>>(a);
         } else if (plan.form == kFew) {
-            const dim3 grid((unsigned)ceil_div(a.m, 16 * (8 / plan.kw)));
-            if (plan.kw == 1) product_few_kernel<T, 1><<<grid, 512, 0, st>>>(a);
-            else if (plan.kw == 2) product_few_kernel<T, 2><<<grid, 512, 0, st>>>(a);
-            else if (plan.kw == 4) product_few_kernel<T, 4><<<grid, 512, 0, st>>>(a);
-            else product_few_kernel<T, 8><<<grid, 512, 0, st>>>(a);
+            const dim3 grid((unsigned)ceil_div(a.m, 16 * (4 / plan.kw)));
+            if (plan.kw == 1) product_few_kernel<T, 1><<<grid, 256, 0, st>>>(a);
+            else if (plan.kw == 2) product_few_kernel<T, 2><<<grid, 256, 0, st>>>(a);
+            else product_few_kernel<T, 4><<<grid, 256, 0, st>>>(a);
         } else if (plan.form == kSome) {
             const int rc = a.rows <= 32   ? run_some<T, 1>(a, plan.splits, st)
                            : a.rows <= 64 ? run_some<T, 2>(a, plan.splits, st)
