@@ -40,10 +40,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, p);
 }
 
-// Eight elements from p on, of which `count` are there (the others: 0).
-template <typename T>
+// Eight elements from p on, of which `count` are there (the others: 0).  ENDS: rows may end within the eight; where
+// their length is a multiple of eight, the code for that is left out (its registers would be there all the time).
+template <typename T, bool ENDS = true>
 __device__ __forceinline__ void load8(const typename T::elem *p, int count, float (&v)[8]) {
-    if (count >= 8) {
+    if (ENDS ? count >= 8 : count > 0) {
         if constexpr (T::size == 2) {
             const Loose16 a = *reinterpret_cast<const Loose16 *>(p);
 #pragma unroll
@@ -59,14 +60,55 @@ __device__ __forceinline__ void load8(const typename T::elem *p, int count, floa
                 v[4 + i] = b.f[i];
             }
         }
+    } else if (ENDS && count > 0) {  // (all of them asked for at once: one wait, not eight)
+        typename T::elem e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = p[min(i, count - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < count ? T::get(e[i]) : 0.f;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? T::get(p[i]) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
     }
 }
+// The same as it lies in memory, for later.
 template <typename T>
+struct Raw8 {
+    uint32_t w[2 * T::size];
+    template <bool ENDS>
+    __device__ __forceinline__ void load(const typename T::elem *p, int count) {
+        if (ENDS ? count >= 8 : count > 0) {
+#pragma unroll
+            for (int h = 0; h < T::size / 2; ++h) {
+                const Loose16 a = reinterpret_cast<const Loose16 *>(p)[h];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[4 * h + i] = a.w[i];
+            }
+        } else if (ENDS && count > 0) {
+            typename T::elem e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = p[min(i, count - 1)];
+            if constexpr (T::size == 2) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = (2 * i < count ? (uint32_t)e[2 * i] : 0u) | (2 * i + 1 < count ? (uint32_t)e[2 * i + 1] << 16 : 0u);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = i < count ? __float_as_uint(e[i]) : 0u;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * T::size; ++i) w[i] = 0;
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (T::size == 2) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else return __uint_as_float(w[i]);
+    }
+};
+template <typename T, bool ENDS = true>
 __device__ __forceinline__ void store8(typename T::elem *p, int count, const float (&v)[8]) {
-    if (count >= 8) {
+    if (ENDS ? count >= 8 : count > 0) {
         if constexpr (T::size == 2) {
             Loose16 a;
 #pragma unroll
@@ -81,7 +123,7 @@ __device__ __forceinline__ void store8(typename T::elem *p, int count, const flo
                 reinterpret_cast<Loose16f *>(p)[h] = a;
             }
         }
-    } else {
+    } else if constexpr (ENDS) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < count) p[i] = T::put(v[i]);

@@ -4,14 +4,12 @@
 //   s = x + residual (as it is stored) ;  rstd = 1 / sqrt(mean s^2 + eps) ;  y = s rstd w
 //   dx = dx_in + rstd (g - h mean(g h)),  g = dy w,  h = s rstd ;  dw = sum over rows of dy h
 //
-// Streams over the rows, bound by HBM.  Up to kInRegisters columns a row is read once and held in the registers of
-// its workgroup (a wavefront for short rows); longer rows are read twice.  Sums are fp32, in an order that hangs on
-// n and, for dw, on the number of rows.
+// Streams over the rows, bound by HBM.  Up to 8192 columns (and, where n is a multiple of eight, 32768; bf16 gradients:
+// 16384) a row is read once and held in the registers of its workgroup (a wavefront for short rows); longer rows are
+// read twice.  Sums are fp32, in an order that hangs on n and, for dw, on the number of rows.
 #include "eight.h"
 
 namespace dlcx {
-
-constexpr int kInRegisters = 32768;  // 1024 lanes x 4 times 8 elements
 
 struct NormArgs {
     const void *x, *residual, *weight;
@@ -48,8 +46,11 @@ __device__ __forceinline__ void put_eight(const NormArgs &a, int64_t row, int co
     }
 }
 
+// Floats between the parts of dw.
+__host__ __device__ __forceinline__ int64_t part_pitch(int64_t n) { return (n + 7) / 8 * 8; }
+
 // LANES to a row, each with CH times 8 elements of it.
-template <typename T, int LANES, int CH>
+template <typename T, int LANES, int CH, bool ENDS>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArgs a) {
     typedef typename T::elem elem;
     __shared__ float s_part[16];
@@ -61,13 +62,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-            load8<T>((const elem *)a.x + row * a.ldx + col, there, v[c]);
+            load8<T, ENDS>((const elem *)a.x + row * a.ldx + col, there, v[c]);
         }
         if (a.residual) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-                load8<T>((const elem *)a.residual + row * a.ldr + col, there, w[c]);
+                load8<T, ENDS>((const elem *)a.residual + row * a.ldr + col, there, w[c]);
             }
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -75,13 +76,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[c][i] += w[c][i];
                 round8<T>(v[c]);
-                if (a.sum) store8<T>((elem *)a.sum + row * a.ldsum + col, there, v[c]);
+                if (a.sum) store8<T, ENDS>((elem *)a.sum + row * a.ldsum + col, there, v[c]);
             }
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-            load8<T>((const elem *)a.weight + col, there, w[c]);
+            load8<T, ENDS>((const elem *)a.weight + col, there, w[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss += v[c][i] * v[c][i];
         }
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
             const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * w[c][i];
-            if (a.y) store8<T>((elem *)a.y + row * a.ldy + col, there, v[c]);
+            if (a.y) store8<T, ENDS>((elem *)a.y + row * a.ldy + col, there, v[c]);
             if (a.codes) put_eight<T>(a, row, col, v[c], lane);
         }
         if constexpr (LANES > 64) __syncthreads();
@@ -143,17 +144,22 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     }
 }
 
+template <typename T, bool ENDS>
+static void run_norm(const NormArgs &a, hipStream_t st) {
+    auto grid = [&a](int per) { return dim3((unsigned)(ceil_div(a.rows, per) < (1 << 22) ? ceil_div(a.rows, per) : (1 << 22))); };
+    if (a.n <= 512) norm_kernel<T, 64, 1, ENDS><<<grid(4), 256, 0, st>>>(a);
+    else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1), 256, 0, st>>>(a);
+    else if (a.n <= 4096) norm_kernel<T, 256, 2, ENDS><<<grid(1), 256, 0, st>>>(a);
+    else if (a.n <= 8192) norm_kernel<T, 512, 2, ENDS><<<grid(1), 512, 0, st>>>(a);
+    else if (!ENDS && a.n <= 16384) norm_kernel<T, 1024, 2, false><<<grid(1), 1024, 0, st>>>(a);
+    else if (!ENDS && a.n <= 32768) norm_kernel<T, 1024, 4, false><<<grid(1), 1024, 0, st>>>(a);
+    else norm_long_kernel<T><<<grid(1), 1024, 0, st>>>(a);
+}
 template <typename T>
 static int launch_norm(const NormArgs &a, hipStream_t st) {
-    auto grid = [&a](int per) { return dim3((unsigned)(ceil_div(a.rows, per) < (1 << 22) ? ceil_div(a.rows, per) : (1 << 22))); };
     Timed timed(KID_RMS_NORM, st);
-    if (a.n <= 512) norm_kernel<T, 64, 1><<<grid(4), 256, 0, st>>>(a);
-    else if (a.n <= 2048) norm_kernel<T, 256, 1><<<grid(1), 256, 0, st>>>(a);
-    else if (a.n <= 4096) norm_kernel<T, 256, 2><<<grid(1), 256, 0, st>>>(a);
-    else if (a.n <= 8192) norm_kernel<T, 256, 4><<<grid(1), 256, 0, st>>>(a);
-    else if (a.n <= 16384) norm_kernel<T, 512, 4><<<grid(1), 512, 0, st>>>(a);
-    else if (a.n <= kInRegisters) norm_kernel<T, 1024, 4><<<grid(1), 1024, 0, st>>>(a);
-    else norm_long_kernel<T><<<grid(1), 1024, 0, st>>>(a);
+    if (a.n % 8) run_norm<T, true>(a, st);
+    else run_norm<T, false>(a, st);
     return check_launch("rms_norm");
 }
 
@@ -169,54 +175,72 @@ struct NormGradArgs {
     int rows, n, parts;
 };
 
-template <typename T, int LANES, int CH>
+// A row's x and dy are asked for while the row before is worked on, and dx_in before the row's sum is formed, so that
+// neither the sum nor its barrier is waited for with nothing on its way; they stay packed until they are used.
+template <typename T, int LANES, int CH, bool ENDS>
 __global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
     typedef typename T::elem elem;
     __shared__ float s_part[2][16];
     const int lane = threadIdx.x;
-    float w[CH][8], dw[CH][8];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int col = (c * LANES + lane) * 8;
-        load8<T>((const elem *)a.weight + col, min(a.n - col, 8), w[c]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
-    }
-    int turn = 0;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        float h[CH][8], g[CH][8];
-        const float rstd = a.rstd[row];
+    Raw8<T> w[CH], x[CH], dy[CH];
+    float dw[CH][8];
+    auto load = [&](Raw8<T>(&to)[CH], const void *p, int64_t at) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-            load8<T>((const elem *)a.x + row * a.ldx + col, there, h[c]);
-            load8<T>((const elem *)a.dy + row * a.lddy + col, there, g[c]);
+            const int col = (c * LANES + lane) * 8;
+            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col);
         }
+    };
+    load(w, a.weight, 0);
+    int64_t row = blockIdx.x;
+    load(x, a.x, row * a.ldx);
+    load(dy, a.dy, row * a.lddy);
+    float rstd = a.rstd[row];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
+    for (int turn = 0; row < a.rows; turn ^= 1) {
+        const int64_t next = row + gridDim.x, there = next < a.rows ? next : row;
+        Raw8<T> r[CH], nx[CH], ndy[CH];
+        if (a.dx_in) load(r, a.dx_in, row * a.ldi);
+        load(nx, a.x, there * a.ldx);
+        load(ndy, a.dy, there * a.lddy);
+        const float nrstd = a.rstd[there];
         float dot = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                h[c][i] *= rstd;
-                dw[c][i] += g[c][i] * h[c][i];
-                g[c][i] *= w[c][i];
-                dot += g[c][i] * h[c][i];
+                const float h = x[c][i] * rstd;
+                dw[c][i] += dy[c][i] * h;
+                dot += dy[c][i] * w[c][i] * h;
             }
         dot = sum_lanes<LANES>(dot, s_part[turn]) / (float)a.n;  // (two places, so one barrier a row)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-            float r[8] = {};
-            if (a.dx_in) load8<T>((const elem *)a.dx_in + row * a.ldi + col, there, r);
+            const int col = (c * LANES + lane) * 8;
+            float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] += rstd * (g[c][i] - h[c][i] * dot);
-            store8<T>((elem *)a.dx + row * a.ldo + col, there, r);
+            for (int i = 0; i < 8; ++i) {
+                v[i] = rstd * (dy[c][i] * w[c][i] - x[c][i] * rstd * dot);
+                if (a.dx_in) v[i] += r[c][i];
+            }
+            store8<T, ENDS>((elem *)a.dx + row * a.ldo + col, a.n - col, v);
+            x[c] = nx[c];
+            dy[c] = ndy[c];
         }
+        row = next;
+        rstd = nrstd;
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * LANES + lane) * 8;
-        store8<TypeF32>(a.part + (int64_t)blockIdx.x * a.n + col, min(a.n - col, 8), dw[c]);
+        if (col < a.n) {
+            float *p = a.part + (int64_t)blockIdx.x * part_pitch(a.n) + col;
+            *reinterpret_cast<float4 *>(p) = make_float4(dw[c][0], dw[c][1], dw[c][2], dw[c][3]);
+            *reinterpret_cast<float4 *>(p + 4) = make_float4(dw[c][4], dw[c][5], dw[c][6], dw[c][7]);
+        }
     }
 }
 
@@ -265,53 +289,71 @@ __global__ __launch_bounds__(256) void norm_grad_long_kernel(NormGradArgs a) {
         }
         store8<T>((elem *)a.dx + row * a.ldo + col, there, r);
     }
-    store8<TypeF32>(a.part + blockIdx.y * (int64_t)a.n + col, there, dw);
+    float *p = a.part + blockIdx.y * part_pitch(a.n) + col;
+    *reinterpret_cast<float4 *>(p) = make_float4(dw[0], dw[1], dw[2], dw[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(dw[4], dw[5], dw[6], dw[7]);
 }
 
-// dw from its parts: 16 columns and 16 shares of the parts to a workgroup.
+// dw from its parts: 64 columns to a workgroup, sixteen shares of the parts to them, eight parts at a time.
 __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__ part, int parts, int n, float *__restrict__ dw) {
-    __shared__ float s[16][17];
+    __shared__ float4 s[16][17];
     const int c = threadIdx.x & 15, share = threadIdx.x >> 4;
-    const int64_t col = (int64_t)blockIdx.x * 16 + c;
-    float t = 0.f;
+    const int64_t col = (int64_t)blockIdx.x * 64 + c * 4, pitch = part_pitch(n);
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
     if (col < n)
-        for (int p = share; p < parts; p += 16) t += part[(int64_t)p * n + col];
+        for (int p = share; p < parts; p += 128) {
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const float4 *>(part + min(p + 16 * k, parts - 1) * pitch + col);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool on = p + 16 * k < parts;
+                t.x += on ? v[k].x : 0.f;
+                t.y += on ? v[k].y : 0.f;
+                t.z += on ? v[k].z : 0.f;
+                t.w += on ? v[k].w : 0.f;
+            }
+        }
     s[share][c] = t;
     __syncthreads();
-    if (share == 0 && col < n) {
-        t = 0.f;
+    if (share < 4) {  // (a component to each)
+        float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) t += s[k][c];
-        dw[col] = t;
+        for (int k = 0; k < 16; ++k) sum += reinterpret_cast<const float *>(&s[k][c])[share];
+        if (col + share < n) dw[col + share] = sum;
     }
 }
 
-// Workgroups of the gradient, each with a part of dw.
+// Workgroups of the gradient, each with a part of dw: as many as the GPU holds at once.
 static int norm_parts(int64_t rows, int64_t n) {
-    const int64_t most = n <= 2048 ? 2048 : n <= 8192 ? 1024 : n <= 16384 ? 512 : 256;
+    const int64_t most = n <= 512 ? 4096 : n <= 2048 ? 1536 : n <= 4096 ? 1024 : n <= 8192 ? 512 : 256;
     return (int)(rows < most ? rows : most);
 }
 
+template <typename T, bool ENDS>
+static void run_norm_grad(const NormGradArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)a.parts);
+    if (a.n <= 512) norm_grad_kernel<T, 64, 1, ENDS><<<grid, 64, 0, st>>>(a);
+    else if (a.n <= 2048) norm_grad_kernel<T, 256, 1, ENDS><<<grid, 256, 0, st>>>(a);
+    else if (a.n <= 4096) norm_grad_kernel<T, 256, 2, ENDS><<<grid, 256, 0, st>>>(a);
+    else if (a.n <= 8192) norm_grad_kernel<T, 512, 2, ENDS><<<grid, 512, 0, st>>>(a);
+    else if (T::size == 2 && !ENDS && a.n <= 16384) norm_grad_kernel<TypeBf16, 1024, 2, false><<<grid, 1024, 0, st>>>(a);
+    else {
+        norm_dot_kernel<T><<<dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))), 1024, 0, st>>>(a);
+        norm_grad_long_kernel<T><<<dim3((unsigned)ceil_div(a.n, 2048), (unsigned)a.parts), 256, 0, st>>>(a);
+    }
+}
 template <typename T>
 static int launch_norm_grad(const NormGradArgs &a, hipStream_t st) {
     {
         Timed timed(KID_RMS_NORM_GRAD, st);
-        const dim3 grid((unsigned)a.parts);
-        if (a.n <= 512) norm_grad_kernel<T, 64, 1><<<grid, 64, 0, st>>>(a);
-        else if (a.n <= 2048) norm_grad_kernel<T, 256, 1><<<grid, 256, 0, st>>>(a);
-        else if (a.n <= 4096) norm_grad_kernel<T, 256, 2><<<grid, 256, 0, st>>>(a);
-        else if (a.n <= 8192) norm_grad_kernel<T, 256, 4><<<grid, 256, 0, st>>>(a);
-        else if (a.n <= 16384) norm_grad_kernel<T, 512, 4><<<grid, 512, 0, st>>>(a);
-        else if (a.n <= kInRegisters) norm_grad_kernel<T, 1024, 4><<<grid, 1024, 0, st>>>(a);
-        else {
-            norm_dot_kernel<T><<<dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))), 1024, 0, st>>>(a);
-            norm_grad_long_kernel<T><<<dim3((unsigned)ceil_div(a.n, 2048), (unsigned)a.parts), 256, 0, st>>>(a);
-        }
+        if (a.n % 8) run_norm_grad<T, true>(a, st);
+        else run_norm_grad<T, false>(a, st);
         const int rc = check_launch("rms_norm_backward");
         if (rc != DLCX_OK) return rc;
     }
     Timed timed(KID_RMS_NORM_SUM, st);
-    norm_sum_kernel<<<dim3((unsigned)ceil_div(a.n, 16)), 256, 0, st>>>(a.part, a.parts, a.n, a.dw);
+    norm_sum_kernel<<<dim3((unsigned)ceil_div(a.n, 64)), 256, 0, st>>>(a.part, a.parts, a.n, a.dw);
     return check_launch("rms_norm_sum");
 }
 
@@ -349,7 +391,7 @@ int dlcx_rms_norm(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx
 
 size_t dlcx_rms_norm_workspace_bytes(int64_t rows, int64_t n) {
     if (check_norm(rows, n, DLCX_F32) != DLCX_OK) return 0;
-    return a256x((size_t)norm_parts(rows, n) * n * sizeof(float)) + a256x(n > kInRegisters ? (size_t)rows * sizeof(float) : 0) + 256;
+    return a256x((size_t)norm_parts(rows, n) * part_pitch(n) * sizeof(float)) + a256x(n > 8192 ? (size_t)rows * sizeof(float) : 0) + 256;
 }
 
 int dlcx_rms_norm_backward(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *weight,
@@ -366,10 +408,10 @@ int dlcx_rms_norm_backward(int64_t rows, int64_t n, int dtype, const void *x, in
     }
     NormGradArgs a = {x, weight, dy, dx_in, rstd, dx_out, (float *)workspace, dw_out, nullptr, ldx, lddy, lddx_in, lddx_out,
                       (int)rows, (int)n, norm_parts(rows, n)};
-    a.dot = (float *)((char *)workspace + a256x((size_t)a.parts * n * sizeof(float)));
+    a.dot = (float *)((char *)workspace + a256x((size_t)a.parts * part_pitch(n) * sizeof(float)));
     if (rows == 0) {
         Timed timed(KID_RMS_NORM_SUM, as_stream(stream));
-        norm_sum_kernel<<<dim3((unsigned)ceil_div(n, 16)), 256, 0, as_stream(stream)>>>(a.part, 0, a.n, dw_out);
+        norm_sum_kernel<<<dim3((unsigned)ceil_div(n, 64)), 256, 0, as_stream(stream)>>>(a.part, 0, a.n, dw_out);
         return check_launch("rms_norm_sum");
     }
     return dtype == DLCX_BF16 ? launch_norm_grad<TypeBf16>(a, as_stream(stream)) : launch_norm_grad<TypeF32>(a, as_stream(stream));
