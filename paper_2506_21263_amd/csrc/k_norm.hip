@@ -4,9 +4,11 @@
 //   s = x + residual (as it is stored) ;  rstd = 1 / sqrt(mean s^2 + eps) ;  y = s rstd w
 //   dx = dx_in + rstd (g - h mean(g h)),  g = dy w,  h = s rstd ;  dw = sum over rows of dy h
 //
-// Streams over the rows, bound by HBM.  Up to 8192 columns (and, where n is a multiple of eight, 32768; bf16 gradients:
-// 16384) a row is read once and held in the registers of its workgroup (a wavefront for short rows); longer rows are
+// Streams over the rows, bound by HBM.  Up to 8192 columns (and, where n is a multiple of eight, 16384, of bf16 32768;
+// gradients of bf16 16384) a row is read once and held in the registers of its workgroup (a wavefront for short rows); longer rows are
 // read twice.  Sums are fp32, in an order that hangs on n and, for dw, on the number of rows.
+#include <algorithm>
+
 #include "eight.h"
 
 namespace dlcx {
@@ -49,55 +51,62 @@ __device__ __forceinline__ void put_eight(const NormArgs &a, int64_t row, int co
 // Floats between the parts of dw.
 __host__ __device__ __forceinline__ int64_t part_pitch(int64_t n) { return (n + 7) / 8 * 8; }
 
-// LANES to a row, each with CH times 8 elements of it.
+// LANES to a row, each with CH times 8 elements of it; the next row is asked for before this one's sum is formed.
 template <typename T, int LANES, int CH, bool ENDS>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArgs a) {
     typedef typename T::elem elem;
-    __shared__ float s_part[16];
+    __shared__ float s_part[2][16];
     constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
     const int lane = threadIdx.x % LANES;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * kRows) {
-        float v[CH][8], w[CH][8];
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    if (row >= a.rows) return;  // (a wavefront of its own: rows share workgroups only where no barrier is met)
+    Raw8<T> w[CH], x[CH], r[CH];
+    auto load = [&](Raw8<T>(&to)[CH], const void *p, int64_t at) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * LANES + lane) * 8;
+            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col);
+        }
+    };
+    load(x, a.x, row * a.ldx);
+    if (a.residual) load(r, a.residual, row * a.ldr);
+    load(w, a.weight, 0);
+    for (int turn = 0;; turn ^= 1) {
+        const int64_t next = row + stride;
+        float v[CH][8];
         float ss = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-            load8<T, ENDS>((const elem *)a.x + row * a.ldx + col, there, v[c]);
-        }
-        if (a.residual) {
+            const int col = (c * LANES + lane) * 8;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-                load8<T, ENDS>((const elem *)a.residual + row * a.ldr + col, there, w[c]);
-            }
+            for (int i = 0; i < 8; ++i) v[c][i] = x[c][i];
+            if (a.residual) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[c][i] += w[c][i];
+                for (int i = 0; i < 8; ++i) v[c][i] += r[c][i];
                 round8<T>(v[c]);
-                if (a.sum) store8<T, ENDS>((elem *)a.sum + row * a.ldsum + col, there, v[c]);
+                store8<T, ENDS>((elem *)a.sum + row * a.ldsum + col, a.n - col, v[c]);
             }
-        }
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
-            load8<T, ENDS>((const elem *)a.weight + col, there, w[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss += v[c][i] * v[c][i];
         }
-        ss = sum_lanes<LANES>(ss, s_part);
+        if (next < a.rows) {
+            load(x, a.x, next * a.ldx);
+            if (a.residual) load(r, a.residual, next * a.ldr);
+        }
+        ss = sum_lanes<LANES>(ss, s_part[turn]);
         const float rstd = 1.f / sqrtf(ss / (float)a.n + a.eps);
         if (a.rstd && lane == 0) a.rstd[row] = rstd;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int col = (c * LANES + lane) * 8, there = min(a.n - col, 8);
+            const int col = (c * LANES + lane) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * w[c][i];
-            if (a.y) store8<T, ENDS>((elem *)a.y + row * a.ldy + col, there, v[c]);
+            if (a.y) store8<T, ENDS>((elem *)a.y + row * a.ldy + col, a.n - col, v[c]);
             if (a.codes) put_eight<T>(a, row, col, v[c], lane);
         }
-        if constexpr (LANES > 64) __syncthreads();
+        if (next >= a.rows) break;
+        row = next;
     }
 }
 
@@ -146,14 +155,14 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
 
 template <typename T, bool ENDS>
 static void run_norm(const NormArgs &a, hipStream_t st) {
-    auto grid = [&a](int per) { return dim3((unsigned)(ceil_div(a.rows, per) < (1 << 22) ? ceil_div(a.rows, per) : (1 << 22))); };
-    if (a.n <= 512) norm_kernel<T, 64, 1, ENDS><<<grid(4), 256, 0, st>>>(a);
-    else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1), 256, 0, st>>>(a);
-    else if (a.n <= 4096) norm_kernel<T, 256, 2, ENDS><<<grid(1), 256, 0, st>>>(a);
-    else if (a.n <= 8192) norm_kernel<T, 512, 2, ENDS><<<grid(1), 512, 0, st>>>(a);
-    else if (!ENDS && a.n <= 16384) norm_kernel<T, 1024, 2, false><<<grid(1), 1024, 0, st>>>(a);
-    else if (!ENDS && a.n <= 32768) norm_kernel<T, 1024, 4, false><<<grid(1), 1024, 0, st>>>(a);
-    else norm_long_kernel<T><<<grid(1), 1024, 0, st>>>(a);
+    auto grid = [&a](int per, int most) { return dim3((unsigned)std::min(ceil_div(a.rows, per), (int64_t)most)); };
+    if (a.n <= 512) norm_kernel<T, 64, 1, ENDS><<<grid(4, 2048), 256, 0, st>>>(a);
+    else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1, 2048), 256, 0, st>>>(a);
+    else if (a.n <= 4096) norm_kernel<T, 256, 2, ENDS><<<grid(1, 1536), 256, 0, st>>>(a);
+    else if (a.n <= 8192) norm_kernel<T, 512, 2, ENDS><<<grid(1, 768), 512, 0, st>>>(a);
+    else if (!ENDS && a.n <= 16384) norm_kernel<T, 1024, 2, false><<<grid(1, 512), 1024, 0, st>>>(a);
+    else if (T::size == 2 && !ENDS && a.n <= 32768) norm_kernel<TypeBf16, 1024, 4, false><<<grid(1, 256), 1024, 0, st>>>(a);
+    else norm_long_kernel<T><<<grid(1, 1 << 22), 1024, 0, st>>>(a);
 }
 template <typename T>
 static int launch_norm(const NormArgs &a, hipStream_t st) {
@@ -201,12 +210,15 @@ __global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
     for (int turn = 0; row < a.rows; turn ^= 1) {
-        const int64_t next = row + gridDim.x, there = next < a.rows ? next : row;
+        const int64_t next = row + gridDim.x;
         Raw8<T> r[CH], nx[CH], ndy[CH];
+        float nrstd = 0.f;
         if (a.dx_in) load(r, a.dx_in, row * a.ldi);
-        load(nx, a.x, there * a.ldx);
-        load(ndy, a.dy, there * a.lddy);
-        const float nrstd = a.rstd[there];
+        if (next < a.rows) {
+            load(nx, a.x, next * a.ldx);
+            load(ndy, a.dy, next * a.lddy);
+            nrstd = a.rstd[next];
+        }
         float dot = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
