@@ -489,6 +489,10 @@ def _rows(t, rows, cols, dtype, what):
     """Address and row stride of a rows x cols device matrix whose rows are contiguous."""
     if t is None:
         return None, cols
+    if t.is_cuda and t.dtype == dtype and t.shape == (rows, cols):  # the usual case, with few questions
+        step, inner = t.stride()
+        if inner == 1 and step >= cols:
+            return t.data_ptr(), (step if rows > 1 else cols)
     if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols):
         raise ValueError("%s: a %d x %d device matrix of %s is wanted" % (what, rows, cols, dtype))
     step, inner = t.stride()

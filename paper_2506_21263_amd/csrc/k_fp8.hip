@@ -24,38 +24,65 @@ struct QuantArgs {
     int64_t ld, lds, ld_t, lds_t;
 };
 
-// ROWS: codes along the rows; COLS: the transpose's; SQUARE: one scale for the tile.
-template <typename T, bool ROWS, bool COLS, bool SQUARE>
+// The largest of the four lanes 16 apart, in all of them.
+__device__ __forceinline__ uint32_t max_over_rows(uint32_t x) {
+    x = max(x, (uint32_t)__shfl_xor((int)x, 16, 64));
+    return max(x, (uint32_t)__shfl_xor((int)x, 32, 64));
+}
+
+// ROWS: codes along the rows; COLS: the transpose's; SQUARE: one scale for the tile.  Each XCD has a contiguous range of
+// tiles, along the rows, so that the bytes of a line of scales meet in one L2.
+// In LDS the transpose's 128 rows of 128 bytes have their 16-byte pieces at piece ^ (row / 8 & 7) and change places with
+// the next row in the upper half, so that the lanes that write at once (rows eight apart) use all banks.
+template <typename T, bool ROWS, bool COLS, bool SQUARE, bool ENDS>
 __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
-    __shared__ uint32_t s_max[COLS && !SQUARE ? 16 * 128 : 4];
+    __shared__ __attribute__((aligned(16))) uint32_t s_max[4 * 128];
     __shared__ __attribute__((aligned(16))) uint8_t s_t[COLS ? 128 * 128 : 16];
-    const int tid = threadIdx.x, lane16 = tid & 15, part = tid >> 4;
-    for (int64_t tile = blockIdx.x; tile < (int64_t)a.row_tiles * a.col_tiles; tile += gridDim.x) {
+    const int tid = threadIdx.x, lane16 = tid & 15, part = tid >> 4, wave = tid >> 6;
+    const int64_t total = (int64_t)a.row_tiles * a.col_tiles, share = (total + 7) / 8;
+    for (int64_t id = blockIdx.x; id < share * 8; id += gridDim.x) {
+        const int64_t tile = (id & 7) * share + (id >> 3);
+        if (tile >= total) continue;
         const int tr = (int)(tile / a.col_tiles), tc = (int)(tile % a.col_tiles);
         const int row0 = tr * 128 + part * 8, col0 = tc * 128 + lane16 * 8;
-        const int there = min(max(a.cols - col0, 0), 8);
+        const int there = a.cols - col0;
+        Raw8<T> raw[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            raw[i].template load<ENDS>((const typename T::elem *)a.x + (int64_t)(row0 + i) * a.ldx + col0, row0 + i < a.rows ? there : 0);
         float v[8][8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            load8<T>((const typename T::elem *)a.x + (int64_t)(row0 + i) * a.ldx + col0, row0 + i < a.rows ? there : 0, v[i]);
-        uint32_t top[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top[i] = finite_max8(v[i]);
+            for (int j = 0; j < 8; ++j) v[i][j] = raw[i][j];
         uint32_t shared = 0;
         if constexpr (SQUARE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) shared = max(shared, top[i]);
-            shared = max16(shared);
-            shared = max(shared, (uint32_t)__shfl_xor((int)shared, 16, 64));
-            shared = max(shared, (uint32_t)__shfl_xor((int)shared, 32, 64));
-            if ((tid & 63) == 0) s_max[tid >> 6] = shared;
+            for (int i = 0; i < 8; ++i) shared = max(shared, finite_max8(v[i]));
+            shared = max_over_rows(max16(shared));
+            if ((tid & 63) == 0) s_max[wave] = shared;
             __syncthreads();
             shared = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+        }
+        uint32_t top[8];  // of the columns
+        if constexpr (COLS && !SQUARE) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                top[j] = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top[j] = max(top[j], finite_bits(v[i][j]));
+                top[j] = max_over_rows(top[j]);
+            }
+            if ((tid & 63) < 16) {
+                uint4 *to = reinterpret_cast<uint4 *>(s_max + wave * 128 + lane16 * 8);
+                to[0] = make_uint4(top[0], top[1], top[2], top[3]);
+                to[1] = make_uint4(top[4], top[5], top[6], top[7]);
+            }
         }
         if constexpr (ROWS) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t s = scale_byte(SQUARE ? shared : max16(top[i]));
+                const uint32_t s = scale_byte(SQUARE ? shared : max16(finite_max8(v[i])));
                 const uint2 c = codes8(v[i], scale_inverse(s));
                 if (row0 + i < a.rows) {
                     *reinterpret_cast<uint2 *>(a.codes + (int64_t)(row0 + i) * a.ld + col0) = c;
@@ -65,35 +92,33 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
         }
         if constexpr (COLS) {
             if constexpr (!SQUARE) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint32_t m = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) m = max(m, finite_bits(v[i][j]));
-                    s_max[part * 128 + lane16 * 8 + j] = m;
-                }
                 __syncthreads();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top[j] = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint4 lo = *reinterpret_cast<const uint4 *>(s_max + k * 128 + lane16 * 8);
+                    const uint4 hi = *reinterpret_cast<const uint4 *>(s_max + k * 128 + lane16 * 8 + 4);
+                    const uint32_t m[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) top[j] = max(top[j], m[j]);
+                }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t m = shared;
-                if constexpr (!SQUARE) {
-                    m = 0;
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) m = max(m, s_max[k * 128 + lane16 * 8 + j]);
-                }
-                const uint32_t s = scale_byte(m);
+                const uint32_t s = scale_byte(SQUARE ? shared : top[j]);
                 float u[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) u[i] = v[i][j];
-                *reinterpret_cast<uint2 *>(s_t + (lane16 * 8 + j) * 128 + part * 8) = codes8(u, scale_inverse(s));
+                const int c = lane16 * 8 + j;
+                *reinterpret_cast<uint2 *>(s_t + (c ^ (lane16 >> 3)) * 128 + ((part >> 1) ^ (lane16 & 7)) * 16 + (part & 1) * 8) = codes8(u, scale_inverse(s));
                 if (part == 0 && col0 + j < a.cols) a.scales_t[(int64_t)(col0 + j) * a.lds_t + tr] = (uint8_t)s;
             }
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int c = k * 32 + (tid >> 3);
-                const uint4 w = *reinterpret_cast<const uint4 *>(s_t + c * 128 + (tid & 7) * 16);
+                const uint4 w = *reinterpret_cast<const uint4 *>(s_t + (c ^ (c >> 6)) * 128 + ((tid & 7) ^ (c >> 3 & 7)) * 16);
                 if (tc * 128 + c < a.cols)
                     *reinterpret_cast<uint4 *>(a.codes_t + (int64_t)(tc * 128 + c) * a.ld_t + tr * 128 + (tid & 7) * 16) = w;
             }
@@ -102,19 +127,24 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
     }
 }
 
+template <typename T, bool ROWS, bool COLS, bool SQUARE>
+static void run_quantize(const QuantArgs &a, hipStream_t st) {
+    const int64_t ids = ceil_div((int64_t)a.row_tiles * a.col_tiles, 8) * 8;
+    const dim3 grid((unsigned)(ids < kMostGroups ? ids : kMostGroups));
+    if (a.cols % 8) quantize_kernel<T, ROWS, COLS, SQUARE, true><<<grid, 256, 0, st>>>(a);
+    else quantize_kernel<T, ROWS, COLS, SQUARE, false><<<grid, 256, 0, st>>>(a);
+}
 template <typename T>
 static int launch_quantize8(const QuantArgs &a, bool rows, bool cols, bool square, hipStream_t st) {
-    const int64_t tiles = (int64_t)a.row_tiles * a.col_tiles;
-    const dim3 grid((unsigned)(tiles < kMostGroups ? tiles : kMostGroups));
     Timed timed(KID_FP8_QUANTIZE, st);
     if (square) {
-        if (rows && cols) quantize_kernel<T, true, true, true><<<grid, 256, 0, st>>>(a);
-        else if (rows) quantize_kernel<T, true, false, true><<<grid, 256, 0, st>>>(a);
-        else quantize_kernel<T, false, true, true><<<grid, 256, 0, st>>>(a);
+        if (rows && cols) run_quantize<T, true, true, true>(a, st);
+        else if (rows) run_quantize<T, true, false, true>(a, st);
+        else run_quantize<T, false, true, true>(a, st);
     } else {
-        if (rows && cols) quantize_kernel<T, true, true, false><<<grid, 256, 0, st>>>(a);
-        else if (rows) quantize_kernel<T, true, false, false><<<grid, 256, 0, st>>>(a);
-        else quantize_kernel<T, false, true, false><<<grid, 256, 0, st>>>(a);
+        if (rows && cols) run_quantize<T, true, true, false>(a, st);
+        else if (rows) run_quantize<T, true, false, false>(a, st);
+        else run_quantize<T, false, true, false>(a, st);
     }
     return check_launch("fp8_quantize");
 }

@@ -745,7 +745,10 @@ size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
         if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * r * ceil_div(m, 4) * 16);
     };
     look(std::min(rows, (int64_t)128));
-    for (int64_t tiles = 3; tiles <= ceil_div(rows, 64) && tiles <= 1024; ++tiles) look(std::min(tiles * 64, rows));
+    for (int64_t r = 192; r < rows + 64 && r <= 65536; r += 64) {
+        look(std::min(r, rows));
+        if (ceil_div(r, 128) * ceil_div(m, 128) >= 512) break;  // (never split)
+    }
     return a256x(most) + 256;
 }
 
