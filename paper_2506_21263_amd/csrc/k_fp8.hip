@@ -50,15 +50,25 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             raw[i].template load<ENDS>((const typename T::elem *)a.x + (int64_t)(row0 + i) * a.ldx + col0, row0 + i < a.rows ? there : 0);
-        float v[8][8];
+        // Elements stay packed between their uses: left to itself, the compiler keeps all of them unpacked, in 190 registers.
+        auto packed = [&] {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = raw[i][j];
+                for (int k = 0; k < 2 * T::size; ++k) asm volatile("" : "+v"(raw[i].w[k]));
+        };
+        auto row = [&](int i, float(&v)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = raw[i][j];
+        };
         uint32_t shared = 0;
         if constexpr (SQUARE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) shared = max(shared, finite_max8(v[i]));
+            for (int i = 0; i < 8; ++i) {
+                float v[8];
+                row(i, v);
+                shared = max(shared, finite_max8(v));
+            }
             shared = max_over_rows(max16(shared));
             if ((tid & 63) == 0) s_max[wave] = shared;
             __syncthreads();
@@ -70,7 +80,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
             for (int j = 0; j < 8; ++j) {
                 top[j] = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top[j] = max(top[j], finite_bits(v[i][j]));
+                for (int i = 0; i < 8; ++i) top[j] = max(top[j], finite_bits(raw[i][j]));
                 top[j] = max_over_rows(top[j]);
             }
             if ((tid & 63) < 16) {
@@ -80,10 +90,13 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
             }
         }
         if constexpr (ROWS) {
+            packed();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t s = scale_byte(SQUARE ? shared : max16(finite_max8(v[i])));
-                const uint2 c = codes8(v[i], scale_inverse(s));
+                float v[8];
+                row(i, v);
+                const uint32_t s = scale_byte(SQUARE ? shared : max16(finite_max8(v)));
+                const uint2 c = codes8(v, scale_inverse(s));
                 if (row0 + i < a.rows) {
                     *reinterpret_cast<uint2 *>(a.codes + (int64_t)(row0 + i) * a.ld + col0) = c;
                     if (lane16 == 0) a.scales[(int64_t)(row0 + i) * a.lds + tc] = (uint8_t)s;
@@ -91,6 +104,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
             }
         }
         if constexpr (COLS) {
+            packed();
             if constexpr (!SQUARE) {
                 __syncthreads();
 #pragma unroll
@@ -109,7 +123,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
                 const uint32_t s = scale_byte(SQUARE ? shared : top[j]);
                 float u[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] = v[i][j];
+                for (int i = 0; i < 8; ++i) u[i] = raw[i][j];
                 const int c = lane16 * 8 + j;
                 *reinterpret_cast<uint2 *>(s_t + (c ^ (lane16 >> 3)) * 128 + ((part >> 1) ^ (lane16 & 7)) * 16 + (part & 1) * 8) = codes8(u, scale_inverse(s));
                 if (part == 0 && col0 + j < a.cols) a.scales_t[(int64_t)(col0 + j) * a.lds_t + tr] = (uint8_t)s;
