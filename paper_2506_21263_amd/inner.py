@@ -10,6 +10,10 @@ stands beside it and the optimizer are entry points of the HIP library.
     outer     delta_a = e_a - s_a P_a Q_a^T                      dlcx_decompress
               and on as in Alg. 2: the replicas theta_l,a = theta_g + s_a P_a Q_a^T are never formed
 
+With the shared weights in 8 bits the plain products become dlcx_fp8_quantize and dlcx_fp8_product, a norm in front of
+them (dlcx_rms_norm) writes its output in both forms, and the adapters may read their rows with dropout (dlcx_dropout),
+whose mask is drawn again in the backward pass.
+
 `python -m paper_2506_21263_amd.inner` trains two workers beside a 512 x 512 matrix towards a synthetic
 teacher, outer step after outer step, and prints the losses.
 """
@@ -21,8 +25,10 @@ import torch
 from . import (BF16, F32, MMA_FMA, PHASE_P, PHASE_Q, STATE_GROUP, adapter_desc, desc, dlcx_adamw,
                dlcx_adapter_backward, dlcx_adapter_forward, dlcx_adapter_route,
                dlcx_adapter_route_bytes, dlcx_adapter_workspace_bytes, dlcx_compress_average,
-               dlcx_decompress, dlcx_grad_norm, dlcx_orthonormalize, dlcx_outer_nesterov,
-               dlcx_tensor_table, dlcx_tensor_table_bytes, dlcx_workspace_bytes, tensor)
+               dlcx_decompress, dlcx_dropout, dlcx_fp8_product, dlcx_fp8_product_workspace_bytes, dlcx_fp8_quantize,
+               dlcx_grad_norm, dlcx_orthonormalize, dlcx_outer_nesterov, dlcx_rms_norm, dlcx_rms_norm_backward,
+               dlcx_rms_norm_workspace_bytes, dlcx_tensor_table, dlcx_tensor_table_bytes, dlcx_workspace_bytes,
+               fp8_empty, tensor)
 
 
 def _as_stream(stream):
@@ -133,15 +139,48 @@ class AdamW:
                 self.norm_there.record()
 
 
+class Norm:
+    """Root-mean-square norm in front of projections, with the addition of a residual.  What the backward pass needs
+    is returned by the forward pass; the weights' gradient is left in dw."""
+
+    def __init__(self, n, dtype=torch.bfloat16, eps=1e-5, device="cuda"):
+        self.n, self.eps = n, eps
+        self.weight = torch.ones(n, device=device, dtype=dtype)
+        self.dw = torch.zeros(n, device=device)
+
+    def forward(self, x, residual=None, eight=False):
+        """The normalised rows, the same in 8 bits (eight; else None), and (sum, rstd) for the backward pass."""
+        y = torch.empty_like(x)
+        y8 = fp8_empty(x.shape[0], self.n, x.device) if eight else None
+        total = torch.empty_like(x) if residual is not None else None
+        rstd = torch.empty(x.shape[0], device=x.device)
+        dlcx_rms_norm(x, self.weight, self.eps, residual=residual, sum_out=total, y_out=y, y8_out=y8, rstd_out=rstd)
+        return y, y8, (x if residual is None else total, rstd)
+
+    def backward(self, saved, dy, dx_in=None):
+        """dx (of x and of the residual); dx_in: the gradient of the sum itself."""
+        x, rstd = saved
+        dx = torch.empty_like(x)
+        workspace = torch.empty(dlcx_rms_norm_workspace_bytes(*x.shape), device=x.device, dtype=torch.uint8)
+        dlcx_rms_norm_backward(x, self.weight, rstd, dy, dx_in, dx, self.dw, workspace)
+        return dx
+
+
 class AdapterProjection:
     """One projection y = x theta^T with an adapter per worker.  q0: count x r x n draws; P starts at zero,
     so a new adapter changes nothing.  Masters are fp32; the products read copies in `dtype`.
+
+    base_bits=8 keeps theta_g in 8 bits (twice: its transpose is the backward pass's), with a scale for 128 x 128 elements;
+    the rows it is multiplied by are brought to 8 bits, too.  dropout: of the rows that the adapters read; the mask hangs
+    on `seed` and the number `draw` that both passes of a step are given.
 
     An optimizer's tensors begin at 16 bytes, so where r x m or r x n elements are not whole 16 bytes, the factors are
     stored with up to seven more columns, which `ranks` leaves out of every product: p, q, dp and dq are the first r,
     h has the stored ones."""
 
-    def __init__(self, theta_g, q0, scale, max_rows, dtype=torch.bfloat16):
+    def __init__(self, theta_g, q0, scale, max_rows, dtype=torch.bfloat16, base_bits=16, dropout=0.0, seed=0):
+        if base_bits not in (8, 16) or not 0.0 <= dropout < 1.0:
+            raise ValueError("base_bits: 8 or 16 (the adapters' own type); dropout: from 0 up to 1")
         self.m, self.n = theta_g.shape
         self.count, self.r = q0.shape[:2]
         dev = theta_g.device
@@ -153,7 +192,13 @@ class AdapterProjection:
         self.d = adapter_desc(self.m, self.n, stored, self.count, BF16 if low else F32)
         self.ranks = None if stored == self.r else torch.full((self.count,), self.r, device=dev, dtype=torch.int32)
         self.dtype, self.q0 = dtype, q0
-        self.base = theta_g.to(dtype)
+        self.dropout, self.seed = dropout, seed
+        self.base = self.base8 = self.base8_t = None
+        if base_bits == 8:
+            self.base8, self.base8_t = fp8_empty(self.m, self.n, dev), fp8_empty(self.n, self.m, dev)
+            dlcx_fp8_quantize(theta_g, self.base8, self.base8_t, square=True)
+        else:
+            self.base = theta_g.to(dtype)
         zeros = lambda k, dt=torch.float32: torch.zeros(self.count, stored, k, device=dev, dtype=dt)  # noqa: E731
         self.stored = {name: zeros(k) for name, k in (("q", self.n), ("p", self.m), ("dq", self.n), ("dp", self.m))}
         for name, k in (("q", self.n), ("p", self.m)):
@@ -173,21 +218,44 @@ class AdapterProjection:
         copies = [self.p_copy[a], self.q_copy[a]] if self.dtype == torch.bfloat16 else None
         return [self.p[a], self.q[a]], [self.dp[a], self.dq[a]], copies
 
-    def forward(self, x, route):
-        y = x @ self.base.t()
+    def _product(self, x, w, x8=None):
+        """x w^T with w in 8 bits."""
+        if x8 is None:
+            x8 = fp8_empty(*x.shape, x.device)
+            dlcx_fp8_quantize(x, x8)
+        y = torch.empty(x.shape[0], w.rows, device=x.device, dtype=x.dtype)
+        workspace = torch.empty(dlcx_fp8_product_workspace_bytes(x.shape[0], w.rows, w.cols), device=x.device,
+                                dtype=torch.uint8)
+        dlcx_fp8_product(x8, w, None, y, workspace)
+        return y
+
+    def _dropped(self, x, draw):
+        """The rows that the adapters read."""
+        if not self.dropout:
+            return x
+        out = torch.empty_like(x)
+        dlcx_dropout(x, None, out, self.dropout, self.seed, draw)
+        return out
+
+    def forward(self, x, route, x8=None, draw=0):
+        """x8: x in 8 bits, where a norm has written it already."""
+        y = x @ self.base.t() if self.base is not None else self._product(x, self.base8, x8)
         route.order.enter(None, [route.table])
         h = torch.empty(x.shape[0], self.d.r, device=x.device)
-        dlcx_adapter_forward(self.d, x, route.ids, self.stored["q_copy"], self.stored["p_copy"], y, y, h,
-                             self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
+        dlcx_adapter_forward(self.d, self._dropped(x, draw), route.ids, self.stored["q_copy"], self.stored["p_copy"], y,
+                             y, h, self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
         return y, h
 
-    def backward(self, x, h, dy, route):
+    def backward(self, x, h, dy, route, draw=0):
         """dx; the gradients of the factors are left in dq and dp."""
-        dx = dy @ self.base
+        dx = dy @ self.base if self.base is not None else self._product(dy, self.base8_t)
         route.order.enter(None, [route.table])
-        dlcx_adapter_backward(self.d, x, dy, route.ids, self.stored["q_copy"], self.stored["p_copy"], h, dx, dx,
-                              self.stored["dq"], self.stored["dp"], self.workspace, scale=self.scale,
-                              ranks=self.ranks, route=route.table)
+        own = torch.empty_like(dx) if self.dropout else dx      # what comes through the adapters, or the whole
+        dlcx_adapter_backward(self.d, self._dropped(x, draw), dy, route.ids, self.stored["q_copy"], self.stored["p_copy"],
+                              h, None if self.dropout else dx, own, self.stored["dq"], self.stored["dp"], self.workspace,
+                              scale=self.scale, ranks=self.ranks, route=route.table)
+        if self.dropout:
+            dlcx_dropout(own, dx, dx, self.dropout, self.seed, draw)
         return dx
 
     def fold_workspace_bytes(self, group, mma):
@@ -206,7 +274,10 @@ class AdapterProjection:
 
     def restart(self, theta_g):
         """The adapters of the next inner phase, beside the updated weights."""
-        self.base.copy_(theta_g)
+        if self.base is not None:
+            self.base.copy_(theta_g)
+        else:
+            dlcx_fp8_quantize(theta_g, self.base8, self.base8_t, square=True)
         self.q.copy_(self.q0)
         self.p.zero_()
         if self.dtype == torch.bfloat16:
@@ -248,9 +319,11 @@ class AdapterOuterStep:
 
 
 def train(m=512, n=512, workers=2, r=8, rows=256, inner=20, outer=8, bits=32, dtype=torch.bfloat16,
-          lr=2e-2, outer_lr=0.3, outer_mu=0.0, max_norm=1.0, seed=0, device="cuda", say=None):
+          lr=2e-2, outer_lr=0.3, outer_mu=0.0, max_norm=1.0, seed=0, device="cuda", say=None, base_bits=16,
+          dropout=0.0, norm=False):
     """Workers train adapters of rank r towards a teacher that is a rank-r step away from the shared
-    weights; every `inner` steps an outer step.  Every phase goes nearly the whole way, so with the step of
+    weights; every `inner` steps an outer step.  base_bits, dropout: AdapterProjection's; norm: rows are normalised
+    before they are projected.  Every phase goes nearly the whole way, so with the step of
     delay an outer rate above 1/4 already overshoots a little.  Returns the losses at the phases' starts."""
     from .stage import MatrixState
     from . import MMA_F32
@@ -259,7 +332,9 @@ def train(m=512, n=512, workers=2, r=8, rows=256, inner=20, outer=8, bits=32, dt
     theta = 0.02 * normal(m, n)
     teacher = theta + 0.1 * normal(m, r) @ normal(r, n) / n ** 0.5
     M = MatrixState(theta, workers, normal(2 * r, n), 8, 64, MMA_F32)
-    proj = AdapterProjection(theta, normal(workers, r, n) / n ** 0.5, 1.0, workers * rows, dtype)
+    proj = AdapterProjection(theta, normal(workers, r, n) / n ** 0.5, 1.0, workers * rows, dtype, base_bits,
+                             dropout, seed)
+    front = Norm(n, dtype, device=device) if norm else None
     optimizers = []
     for a in range(workers):
         params, grads, copies = proj.parameters(a)
@@ -272,11 +347,16 @@ def train(m=512, n=512, workers=2, r=8, rows=256, inner=20, outer=8, bits=32, dt
             opt.reset()
         for k in range(inner):
             x = normal(workers * rows, n).to(dtype)      # every worker's own batch
+            x8, draw = None, t * inner + k
+            if norm:
+                x, x8, saved = front.forward(x, eight=base_bits == 8)
             want = x.float() @ teacher.t()
-            y, h = proj.forward(x, route)
+            y, h = proj.forward(x, route, x8, draw)
             off = y.float() - want
             loss = (off * off).sum(1).view(workers, rows).mean(1) / m
-            proj.backward(x, h, (off * (2.0 / (rows * m))).to(dtype), route)
+            dx = proj.backward(x, h, (off * (2.0 / (rows * m))).to(dtype), route, draw)
+            if norm:
+                front.backward(saved, dx)
             for opt in optimizers:
                 opt.step()
             if k == 0:
@@ -293,5 +373,8 @@ if __name__ == "__main__":
     ap.add_argument("--bits", type=int, default=32, choices=(8, 32), help="of the optimizer's moments")
     ap.add_argument("--outer", type=int, default=8)
     ap.add_argument("--inner", type=int, default=20)
+    ap.add_argument("--base", type=int, default=16, choices=(8, 16), help="bits of the shared weights")
+    ap.add_argument("--dropout", type=float, default=0.0, help="of the rows that the adapters read")
+    ap.add_argument("--norm", action="store_true", help="rows are normalised before they are projected")
     a = ap.parse_args()
-    train(bits=a.bits, outer=a.outer, inner=a.inner, say=lambda s: print(s, flush=True))
+    train(bits=a.bits, outer=a.outer, inner=a.inner, base_bits=a.base, dropout=a.dropout, norm=a.norm, say=lambda s: print(s, flush=True))
