@@ -40,13 +40,24 @@ __device__ __forceinline__ void load_lds16(const uint8_t *from, uint8_t *lds) {
 
 __device__ __forceinline__ i32x8 join(const i32x4 &a, const i32x4 &b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// Eight codes to bf16.
-__device__ __forceinline__ bf16x8 widen(int lo, int hi) {
+// Eight codes to bf16, times a power of two.
+__device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale = 1.f) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, 1.f, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, 1.f, true);
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)hi, scale, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// Where all scales of a quad are from 2^-63 to 2^64, they are applied as the codes are widened (bf16 has the exponents of
+// fp32, so that is exact, too) and blocks add up in one accumulator; products below 2^-126, whose sum no fp32 result holds
+// in full, are all that may be lost.  `outside` collects the quad's dwords: bit 7 of a byte from 64 to 191 differs from bit 6.
+__device__ __forceinline__ uint32_t outside(int scales) { return ~((uint32_t)scales ^ (uint32_t)scales << 1) & 0x80808080u; }
+// true for the whole wavefront if none of the first `count` blocks' scales is outside
+__device__ __forceinline__ bool all_inside(uint32_t collected, int count) {
+    const uint32_t valid = count >= 4 ? 0xffffffffu : (1u << 8 * count) - 1u;
+    return __ballot((collected & valid) != 0) == 0;
+}
+template <int S>
+__device__ __forceinline__ float scale_of(int scales) { return __uint_as_float(((uint32_t)scales >> (8 * S) & 255u) << 23); }
 // c + the block's sum, whose scales' bytes add up to e
 __device__ __forceinline__ f32x4 add_scaled(const f32x4 &c, const f32x4 &sum, const int (&ew)[4], int ex) {
     f32x4 r;
@@ -109,8 +120,7 @@ __device__ __forceinline__ TilePlace tile_place(int id, int row_tiles, int col_t
 template <typename T, int FN>
 __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
     constexpr int kRows = 32 * FN, kStage = (128 + kRows) * 128, kFetchX = kRows / 32;
-    constexpr bool kWiden = T::size == 4;       // fp32 results
-    constexpr int kScaleRows = kWiden ? 4 : 1;  // of w, to a lane: its outputs' or its operand's
+    constexpr bool kWiden = T::size == 4;  // fp32 results
     __shared__ __attribute__((aligned(16))) uint8_t s_tile[2 * kStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const TilePlace place = tile_place(blockIdx.x, a.row_tiles, a.col_tiles, 8);
@@ -131,17 +141,15 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
         for (int i = 0; i < kFetchX; ++i) load_lds16(from_x[i] + (int64_t)block * 128, to + 128 * 128 + (wave * kFetchX + i) * 1024);
     };
     const int r16 = lane & 15, g = lane >> 4, wm = (wave & 1) * 64, wn = (wave >> 1) * 16 * FN;
-    const uint8_t *sw[4][kScaleRows], *sx[FN];
+    const uint8_t *sw[4], *sx[FN];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < kScaleRows; ++e)
-            sw[i][e] = a.ws + min(col0 + wm + i * 16 + (kWiden ? g * 4 + e : r16), (int64_t)a.m - 1) * a.ldws;
+    for (int i = 0; i < 4; ++i) sw[i] = a.ws + min(col0 + wm + i * 16 + r16, (int64_t)a.m - 1) * a.ldws;
 #pragma unroll
     for (int j = 0; j < FN; ++j) sx[j] = a.xs + min(row0 + wn + j * 16 + r16, (int64_t)a.rows - 1) * a.ldxs;
     const int p0 = (g ^ (lane & 7)) * 16, p1 = ((g + 4) ^ (lane & 7)) * 16;
     f32x4 acc[4][FN] = {};
-    int scale_w[4][kScaleRows], scale_x[FN];
+    int scale_w[4], scale_x[FN];
+    bool inside = false;
     auto step = [&](int buf, auto s) {
         constexpr int S = decltype(s)::value;
         const uint8_t *pw = s_tile + buf * kStage + (wm + r16) * 128, *px = s_tile + buf * kStage + (128 + wn + r16) * 128;
@@ -150,44 +158,60 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
         for (int i = 0; i < 4; ++i) fw[i] = join(*(const i32x4 *)(pw + i * 2048 + p0), *(const i32x4 *)(pw + i * 2048 + p1));
         if constexpr (kWiden) {
             bf16x8 bw[4][4];
-            int ew[4][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
+                const float s = inside ? scale_of<S>(scale_w[i]) : 1.f;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    bw[i][k] = widen(fw[i][2 * k], fw[i][2 * k + 1]);
-                    ew[i][k] = (scale_w[i][k] >> (8 * S)) & 255;
-                }
+                for (int k = 0; k < 4; ++k) bw[i][k] = widen(fw[i][2 * k], fw[i][2 * k + 1], s);
+            }
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
-                f32x4 sum[4] = {};
+                const float s = inside ? scale_of<S>(scale_x[j]) : 1.f;
+                if (inside) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bf16x8 bx = widen(fx[2 * k], fx[2 * k + 1]);
+                    for (int k = 0; k < 4; ++k) {
+                        const bf16x8 bx = widen(fx[2 * k], fx[2 * k + 1], s);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i][k], bx, sum[i], 0, 0, 0);
+                        for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i][k], bx, acc[i][j], 0, 0, 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f32x4 sum = {};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i][k], widen(fx[2 * k], fx[2 * k + 1]), sum, 0, 0, 0);
+                        int ew[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) ew[e] = (__shfl(scale_w[i], g * 4 + e, 64) >> (8 * S)) & 255;
+                        acc[i][j] = add_scaled(acc[i][j], sum, ew, (scale_x[j] >> (8 * S)) & 255);
+                    }
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][j] = add_scaled(acc[i][j], sum[i], ew[i], (scale_x[j] >> (8 * S)) & 255);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][j] = scaled_mma<S>(fw[i], fx, acc[i][j], scale_w[i][0], scale_x[j]);
+                for (int i = 0; i < 4; ++i) acc[i][j] = scaled_mma<S>(fw[i], fx, acc[i][j], scale_w[i], scale_x[j]);
             }
         }
     };
     if (first < last) fetch(0, first);
     for (int block = first; block < last; block += 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int e = 0; e < kScaleRows; ++e) scale_w[i][e] = *(const int *)(sw[i][e] + block);
+        for (int i = 0; i < 4; ++i) scale_w[i] = *(const int *)(sw[i] + block);
 #pragma unroll
         for (int j = 0; j < FN; ++j) scale_x[j] = *(const int *)(sx[j] + block);
+        if constexpr (kWiden) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bad |= outside(scale_w[i]);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) bad |= outside(scale_x[j]);
+            inside = all_inside(bad, last - block);
+        }
         unrolled<4>([&](auto s) {
             constexpr int S = decltype(s)::value;
             if (block + S < last) {
@@ -663,20 +687,37 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
         while (kw < 4 && ceil_div(m, 16) * kw < 4096 && kw * 2 <= quads) kw *= 2;
         return {kFew, 1, 0, kw};
     }
-    if (blocks == 0) return {kTiles, 1, 4, 4};  // (the others begin with a fetch)
+    if (blocks == 0) return {kTiles, 1, 4, 2};  // (the others begin with a fetch)
     // Tiles of 256 x 256 run one to a compute unit: they lose by a last round that is nearly empty.
     const int64_t wide = ceil_div(rows, kWideTile) * ceil_div(m, kWideTile);
     if (dtype == DLCX_BF16 && rows >= kWideTile && m >= kWideTile && wide >= 128 && most_stride <= (1 << 23))  // (256 rows: 32 bits)
         return {kWide, 1, 0, 0};
     const bool some = rows <= 128;
     const int64_t col_tiles = ceil_div(m, 128);
-    // Tiles of 64 rows where those of 128 leave compute units without work.
-    const int fn = some || ceil_div(rows, 128) * col_tiles >= 512 ? 4 : 2;
-    const int64_t tiles = some ? col_tiles : ceil_div(rows, 32 * fn) * col_tiles;
-    int64_t splits = some ? (tiles < 160 ? 256 / tiles : 1) : tiles < 384 ? ceil_div(512, tiles) : 1;
-    splits = std::max((int64_t)1, std::min(splits, blocks / 4));
-    const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
-    return {some ? kSome : kTiles, (int)ceil_div(blocks, per), (int)per, fn};
+    if (some) {
+        int64_t splits = col_tiles < 160 ? 256 / col_tiles : 1;
+        splits = std::max((int64_t)1, std::min(splits, blocks / 4));
+        const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
+        return {kSome, (int)ceil_div(blocks, per), (int)per, 0};
+    }
+    // Tiles of 128 rows (not of fp32 results, which have no registers for them) or 64, and splits: what the busiest compute
+    // unit has to do, in blocks of 64 rows, a little more for those of 64 (which read w twice as often), and what it costs
+    // to write and add the splits' sums (about as much as four blocks for each).
+    ProductPlan best = {};
+    int64_t least = INT64_MAX;
+    for (int fn = dtype == DLCX_BF16 ? 4 : 2; fn >= 2; fn -= 2) {
+        const int64_t tiles = ceil_div(rows, 32 * fn) * col_tiles;
+        for (int64_t splits = 1; splits <= std::max((int64_t)1, std::min(blocks / 4, (int64_t)16)); ++splits) {
+            const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4, used = ceil_div(blocks, per);
+            const int64_t cost = ceil_div(tiles * used, 256) * std::min(per, blocks) * (fn == 4 ? 8 : 5) + (used > 1 ? 16 * used + 32 : 0);
+            if (cost < least) {
+                least = cost;
+                best = {kTiles, (int)used, (int)per, fn};
+            }
+            if (tiles >= 512) break;  // (no split)
+        }
+    }
+    return best;
 }
 
 template <typename T, int FN>
@@ -715,7 +756,7 @@ static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st
         } else {
             a.row_tiles = (int)ceil_div(a.rows, 32 * plan.kw);
             const dim3 grid((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits);
-            if (plan.kw == 4) product_kernel<T, 4><<<grid, 256, 0, st>>>(a);
+            if (T::size == 2 && plan.kw == 4) product_kernel<TypeBf16, 4><<<grid, 256, 0, st>>>(a);
             else product_kernel<T, 2><<<grid, 256, 0, st>>>(a);
         }
         const int rc = check_launch("fp8_product");
@@ -741,8 +782,10 @@ size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
     if (bad_product(rows, m, n)) return 0;
     size_t most = 0;  // of fewer rows, too: these may be split further
     auto look = [&](int64_t r) {
-        const ProductPlan plan = product_plan(r, m, n, DLCX_F32, 0);  // (bf16 results never need more)
-        if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * r * ceil_div(m, 4) * 16);
+        for (int dtype : {DLCX_F32, DLCX_BF16}) {
+            const ProductPlan plan = product_plan(r, m, n, dtype, INT64_MAX);
+            if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * r * ceil_div(m, 4) * 16);
+        }
     };
     look(std::min(rows, (int64_t)128));
     for (int64_t r = 192; r < rows + 64 && r <= 65536; r += 64) {
