@@ -546,8 +546,8 @@ __global__ __launch_bounds__(256, 2) void product_few_kernel(ProductArgs a) {
     if (r16 < a.rows && col < a.m) put4<T>(a, r16, col, acc);
 }
 
-// 17 .. 128 rows: 32 FN of them beside 128 rows of w, one workgroup to a compute unit.  Bound by the reading of w, so what
-// counts is how much of it is on its way: a ring of as many stages as LDS holds (128 bytes of each row, straight to LDS;
+// Tiles of 128 columns x 32 FN rows, one workgroup to a compute unit: 17 .. 128 rows, and as many tiles of 128 as there are
+// compute units.  Few rows are bound by the reading of w, so what counts is how much of it is on its way: a ring of as many stages as LDS holds (128 bytes of each row, straight to LDS;
 // pieces at piece ^ (row & 7)), all but one of them in flight, 64 KB of w to a compute unit beside 96 rows.  (Twice as much,
 // in registers and with a barrier only every four blocks, measured the same: a compute unit takes in 24 - 28 bytes a ns
 // from HBM, and x's are among them.)  96 rows of 28672 x 8192: 77 us, 3.1 TB/s of w, 5.4 of both.  Scales
@@ -566,15 +566,16 @@ __global__ __launch_bounds__(256, 1) void product_some_kernel(ProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];
     uint8_t *const s_scale = s_ring + kRing * kStage;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t col0 = (int64_t)blockIdx.x * 128;
+    const TilePlace place = tile_place(blockIdx.x, a.row_tiles, a.col_tiles, 8);
+    const int64_t row0 = (int64_t)place.row * Shape::kRows, col0 = (int64_t)place.col * 128;
     const int split = blockIdx.y, first = split * a.per_split, last = min(first + a.per_split, a.blocks);
     const int piece = (lane & 7) ^ (lane >> 3);
     const uint8_t *from_w[4], *from_x[FN];
 #pragma unroll
     for (int i = 0; i < 4; ++i) from_w[i] = a.w + min(col0 + (wave * 4 + i) * 8 + (lane >> 3), (int64_t)a.m - 1) * a.ldw + piece * 16;
 #pragma unroll
-    for (int i = 0; i < FN; ++i) from_x[i] = a.x + min((wave * FN + i) * 8 + (lane >> 3), a.rows - 1) * a.ldx + piece * 16;
-    const uint8_t *from_s = wave < 2 ? a.ws + min(col0 + tid, (int64_t)a.m - 1) * a.ldws : a.xs + min(tid - 128, a.rows - 1) * a.ldxs;
+    for (int i = 0; i < FN; ++i) from_x[i] = a.x + min(row0 + (wave * FN + i) * 8 + (lane >> 3), (int64_t)a.rows - 1) * a.ldx + piece * 16;
+    const uint8_t *from_s = wave < 2 ? a.ws + min(col0 + tid, (int64_t)a.m - 1) * a.ldws : a.xs + min(row0 + tid - 128, (int64_t)a.rows - 1) * a.ldxs;
     // (past the last stage it comes again, and is not used: every wavefront always has the same number under way)
     auto fetch = [&](int slot, int block) {
         const int64_t at = (int64_t)min(block, last - 1) * 128;
@@ -648,7 +649,7 @@ __global__ __launch_bounds__(256, 1) void product_some_kernel(ProductArgs a) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (nothing is on its way to LDS that is no longer this workgroup's)
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-        const int row = wn + j * 16 + r16;
+        const int64_t row = row0 + wn + j * 16 + r16;
         if (row >= a.rows) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -677,7 +678,7 @@ enum ProductForm { kFew, kSome, kTiles, kWide };
 struct ProductPlan {
     ProductForm form;
     int splits, per_split;  // of the sum, and its blocks in one
-    int kw;  // kFew: wavefronts along the sum; kTiles: fragments of x
+    int kw;  // kFew: wavefronts along the sum; others: 32nds of a tile's rows
 };
 // Which form, and how the sum is split where the outputs alone do not fill the GPU.
 static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, int64_t most_stride) {
@@ -698,35 +699,45 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
         int64_t splits = col_tiles < 160 ? 256 / col_tiles : 1;
         splits = std::max((int64_t)1, std::min(splits, blocks / 4));
         const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
-        return {kSome, (int)ceil_div(blocks, per), (int)per, 0};
+        return {kSome, (int)ceil_div(blocks, per), (int)per, (int)ceil_div(rows, 32)};
     }
-    // Tiles of 128 rows (not of fp32 results, which have no registers for them) or 64, and splits: what the busiest compute
-    // unit has to do, in blocks of 64 rows, a little more for those of 64 (which read w twice as often), and what it costs
-    // to write and add the splits' sums (about as much as four blocks for each).
+    // Tiles of 128 rows (not of fp32 results, which have no registers for them) or 64, in pairs that share a compute unit,
+    // or of 128 rows alone on it with a ring of stages; and splits.  The least of what the busiest compute unit takes, as
+    // measured in us for a block of a tile, and of writing and adding the splits' sums.  (1024 x 4096 x 4096 bf16: ring 25.8,
+    // 128 rows 31.7 and 34.5 in two splits, 64 rows 31.5; 3000 x 700 x 6000: 128 rows in three splits 29.0, ring 35.0; 2050 x
+    // 1021 x 4133 fp32: 46.6, 44.1, 40.0, 40.2 in one to four splits.)
     ProductPlan best = {};
-    int64_t least = INT64_MAX;
-    for (int fn = dtype == DLCX_BF16 ? 4 : 2; fn >= 2; fn -= 2) {
+    double least = 1e300;
+    auto consider = [&](ProductForm form, int fn, int64_t splits, double alone, double paired) {
         const int64_t tiles = ceil_div(rows, 32 * fn) * col_tiles;
-        for (int64_t splits = 1; splits <= std::max((int64_t)1, std::min(blocks / 4, (int64_t)16)); ++splits) {
-            const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4, used = ceil_div(blocks, per);
-            const int64_t cost = ceil_div(tiles * used, 256) * std::min(per, blocks) * (fn == 4 ? 8 : 5) + (used > 1 ? 16 * used + 32 : 0);
-            if (cost < least) {
-                least = cost;
-                best = {kTiles, (int)used, (int)per, fn};
-            }
-            if (tiles >= 512) break;  // (no split)
+        if (splits > 1 && tiles >= 512) return;
+        const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4, used = ceil_div(blocks, per), busiest = ceil_div(tiles * used, 256);
+        double cost = (double)(busiest * std::min(per, blocks)) * (busiest == 1 ? alone : paired);
+        if (used > 1) cost += 3.0 + 1e-6 * (double)(used * ceil_div(rows, 64) * 64 * m);  // (rows of whole tiles: see the workspace)
+        if (cost >= least) return;
+        least = cost;
+        best = {form, (int)used, (int)per, fn};
+    };
+    for (int64_t splits = 1; splits <= std::max((int64_t)1, std::min(blocks / 4, (int64_t)16)); ++splits) {
+        if (dtype == DLCX_BF16) {
+            consider(kTiles, 4, splits, 1.0, 0.8);
+            consider(kTiles, 2, splits, 0.6, 0.47);
+        } else {
+            consider(kTiles, 2, splits, 0.85, 0.7);
         }
     }
+    if (dtype == DLCX_BF16) consider(kSome, 4, 1, 0.77, 0.8);
     return best;
 }
 
 template <typename T, int FN>
-static int run_some(const ProductArgs &a, int splits, hipStream_t st) {
+static int run_some(ProductArgs a, int splits, hipStream_t st) {
     static size_t granted = 0;
     const int lds = SomeShape<T, FN>::kLds;
     const int rc = grant_dynamic_lds((const void *)product_some_kernel<T, FN>, lds, &granted, "fp8_product");
     if (rc != DLCX_OK) return rc;
-    product_some_kernel<T, FN><<<dim3((unsigned)ceil_div(a.m, 128), splits), 256, lds, st>>>(a);
+    a.row_tiles = (int)ceil_div(a.rows, 32 * FN);
+    product_some_kernel<T, FN><<<dim3((unsigned)(a.row_tiles * (int64_t)a.col_tiles), splits), 256, lds, st>>>(a);
     return DLCX_OK;
 }
 
@@ -748,9 +759,9 @@ static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st
             else if (plan.kw == 2) product_few_kernel<T, 2><<<grid, 256, 0, st>>>(a);
             else product_few_kernel<T, 4><<<grid, 256, 0, st>>>(a);
         } else if (plan.form == kSome) {
-            const int rc = a.rows <= 32   ? run_some<T, 1>(a, plan.splits, st)
-                           : a.rows <= 64 ? run_some<T, 2>(a, plan.splits, st)
-                           : a.rows <= 96 ? run_some<T, 3>(a, plan.splits, st)
+            const int rc = plan.kw == 1   ? run_some<T, 1>(a, plan.splits, st)
+                           : plan.kw == 2 ? run_some<T, 2>(a, plan.splits, st)
+                           : plan.kw == 3 ? run_some<T, 3>(a, plan.splits, st)
                                           : run_some<T, 4>(a, plan.splits, st);
             if (rc != DLCX_OK) return rc;
         } else {
@@ -780,7 +791,7 @@ static bool bad_product(int64_t rows, int64_t m, int64_t n) {
 
 size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
     if (bad_product(rows, m, n)) return 0;
-    size_t most = 0;  // of fewer rows, too: these may be split further
+    size_t most = 0;  // of fewer rows, too: these may be split further (above 128 the plan is the same for 64 rows each)
     auto look = [&](int64_t r) {
         for (int dtype : {DLCX_F32, DLCX_BF16}) {
             const ProductPlan plan = product_plan(r, m, n, dtype, INT64_MAX);
