@@ -49,7 +49,11 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
         Raw8<T> raw[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            raw[i].template load<ENDS>((const typename T::elem *)a.x + (int64_t)(row0 + i) * a.ldx + col0, row0 + i < a.rows ? there : 0);
+            raw[i].template load<ENDS>((const typename T::elem *)a.x + (int64_t)(row0 + i) * a.ldx + col0, row0 + i < a.rows ? there : 0, a.cols);
+        if constexpr (ENDS) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[i].template settle<ENDS>(row0 + i < a.rows ? there : 0, a.cols);
+        }
         // Elements stay packed between their uses: left to itself, the compiler keeps all of them unpacked, in 190 registers.
         auto packed = [&] {
 #pragma unroll

@@ -66,12 +66,14 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
-            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col);
+            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col, a.n);
         }
     };
     load(x, a.x, row * a.ldx);
     if (a.residual) load(r, a.residual, row * a.ldr);
     load(w, a.weight, 0);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) w[c].template settle<ENDS>(a.n - (c * LANES + lane) * 8, a.n);
     for (int turn = 0;; turn ^= 1) {
         const int64_t next = row + stride;
         float v[CH][8];
@@ -79,9 +81,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
+            x[c].template settle<ENDS>(a.n - col, a.n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = x[c][i];
             if (a.residual) {
+                r[c].template settle<ENDS>(a.n - col, a.n);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[c][i] += r[c][i];
                 round8<T>(v[c]);
@@ -155,12 +159,15 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
 
 template <typename T, bool ENDS>
 static void run_norm(const NormArgs &a, hipStream_t st) {
-    auto grid = [&a](int per, int most) { return dim3((unsigned)std::min(ceil_div(a.rows, per), (int64_t)most)); };
+    // Workgroups: no more than the GPU holds at once, and rows shared out evenly.
+    auto grid = [&a](int per, int most) { return dim3((unsigned)ceil_div(a.rows, per * ceil_div(a.rows, (int64_t)per * most))); };
     if (a.n <= 512) norm_kernel<T, 64, 1, ENDS><<<grid(4, 2048), 256, 0, st>>>(a);
-    else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1, 2048), 256, 0, st>>>(a);
-    else if (a.n <= 4096) norm_kernel<T, 256, 2, ENDS><<<grid(1, 1536), 256, 0, st>>>(a);
-    else if (a.n <= 8192) norm_kernel<T, 512, 2, ENDS><<<grid(1, 768), 512, 0, st>>>(a);
-    else if (!ENDS && a.n <= 16384) norm_kernel<T, 1024, 2, false><<<grid(1, 512), 1024, 0, st>>>(a);
+    else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1, ENDS ? 1024 : 2048), 256, 0, st>>>(a);
+    else if (ENDS && a.n <= 4096) norm_kernel<T, 512, 1, true><<<grid(1, 512), 512, 0, st>>>(a);
+    else if (ENDS && a.n <= 8192) norm_kernel<T, 1024, 1, true><<<grid(1, 256), 1024, 0, st>>>(a);
+    else if (!ENDS && a.n <= 4096) norm_kernel<T, 256, 2, false><<<grid(1, 1280), 256, 0, st>>>(a);
+    else if (!ENDS && a.n <= 8192) norm_kernel<T, 512, 2, false><<<grid(1, 768), 512, 0, st>>>(a);
+    else if (!ENDS && a.n <= 16384) norm_kernel<T, 1024, 2, false><<<grid(1, 256), 1024, 0, st>>>(a);
     else if (T::size == 2 && !ENDS && a.n <= 32768) norm_kernel<TypeBf16, 1024, 4, false><<<grid(1, 256), 1024, 0, st>>>(a);
     else norm_long_kernel<T><<<grid(1, 1 << 22), 1024, 0, st>>>(a);
 }
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
-            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col);
+            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col, a.n);
         }
     };
     load(w, a.weight, 0);
@@ -206,9 +213,11 @@ __global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
     load(dy, a.dy, row * a.lddy);
     float rstd = a.rstd[row];
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+        w[c].template settle<ENDS>(a.n - (c * LANES + lane) * 8, a.n);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
+    }
     for (int turn = 0; row < a.rows; turn ^= 1) {
         const int64_t next = row + gridDim.x;
         Raw8<T> r[CH], nx[CH], ndy[CH];
@@ -221,18 +230,23 @@ __global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
         }
         float dot = 0.f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c) {
+            const int count = a.n - (c * LANES + lane) * 8;
+            x[c].template settle<ENDS>(count, a.n);
+            dy[c].template settle<ENDS>(count, a.n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float h = x[c][i] * rstd;
                 dw[c][i] += dy[c][i] * h;
                 dot += dy[c][i] * w[c][i] * h;
             }
+        }
         dot = sum_lanes<LANES>(dot, s_part[turn]) / (float)a.n;  // (two places, so one barrier a row)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
             float v[8];
+            if (a.dx_in) r[c].template settle<ENDS>(a.n - col, a.n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 v[i] = rstd * (dy[c][i] * w[c][i] - x[c][i] * rstd * dot);
@@ -306,20 +320,21 @@ __global__ __launch_bounds__(256) void norm_grad_long_kernel(NormGradArgs a) {
     *reinterpret_cast<float4 *>(p + 4) = make_float4(dw[4], dw[5], dw[6], dw[7]);
 }
 
-// dw from its parts: 64 columns to a workgroup, sixteen shares of the parts to them, eight parts at a time.
+// dw from its parts: 32 columns to a workgroup, 32 shares of the parts to them, eight parts at a time.
+constexpr int kSumCols = 32;
 __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__ part, int parts, int n, float *__restrict__ dw) {
-    __shared__ float4 s[16][17];
-    const int c = threadIdx.x & 15, share = threadIdx.x >> 4;
-    const int64_t col = (int64_t)blockIdx.x * 64 + c * 4, pitch = part_pitch(n);
+    __shared__ float4 s[32][9];
+    const int c = threadIdx.x & 7, share = threadIdx.x >> 3;
+    const int64_t col = (int64_t)blockIdx.x * kSumCols + c * 4, pitch = part_pitch(n);
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
     if (col < n)
-        for (int p = share; p < parts; p += 128) {
+        for (int p = share; p < parts; p += 256) {
             float4 v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const float4 *>(part + min(p + 16 * k, parts - 1) * pitch + col);
+            for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const float4 *>(part + min(p + 32 * k, parts - 1) * pitch + col);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const bool on = p + 16 * k < parts;
+                const bool on = p + 32 * k < parts;
                 t.x += on ? v[k].x : 0.f;
                 t.y += on ? v[k].y : 0.f;
                 t.z += on ? v[k].z : 0.f;
@@ -331,15 +346,20 @@ __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__
     if (share < 4) {  // (a component to each)
         float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) sum += reinterpret_cast<const float *>(&s[k][c])[share];
+        for (int k = 0; k < 32; ++k) sum += reinterpret_cast<const float *>(&s[k][c])[share];
         if (col + share < n) dw[col + share] = sum;
     }
 }
 
-// Workgroups of the gradient, each with a part of dw: as many as the GPU holds at once.
+// Workgroups of the gradient, each with a part of dw: no more than the GPU holds at once, and rows shared out evenly.
+// (515 rows of 2050 fp32: 515 of them, of which the GPU held 512, took 12 us, 258 of two rows 7.)
+static int64_t most_norm_parts(int64_t n) {
+    const bool ends = n % 8 != 0;
+    return n <= 512 ? 4096 : n <= 2048 ? 1024 : n <= 4096 ? (ends ? 512 : 768) : n <= 8192 ? (ends ? 256 : 512) : 256;
+}
 static int norm_parts(int64_t rows, int64_t n) {
-    const int64_t most = n <= 512 ? 4096 : n <= 2048 ? 1536 : n <= 4096 ? 1024 : n <= 8192 ? 512 : 256;
-    return (int)(rows < most ? rows : most);
+    const int64_t turns = ceil_div(rows, most_norm_parts(n));
+    return turns ? (int)ceil_div(rows, turns) : 0;
 }
 
 template <typename T, bool ENDS>
@@ -347,8 +367,10 @@ static void run_norm_grad(const NormGradArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)a.parts);
     if (a.n <= 512) norm_grad_kernel<T, 64, 1, ENDS><<<grid, 64, 0, st>>>(a);
     else if (a.n <= 2048) norm_grad_kernel<T, 256, 1, ENDS><<<grid, 256, 0, st>>>(a);
-    else if (a.n <= 4096) norm_grad_kernel<T, 256, 2, ENDS><<<grid, 256, 0, st>>>(a);
-    else if (a.n <= 8192) norm_grad_kernel<T, 512, 2, ENDS><<<grid, 512, 0, st>>>(a);
+    else if (ENDS && a.n <= 4096) norm_grad_kernel<T, 512, 1, true><<<grid, 512, 0, st>>>(a);
+    else if (ENDS && a.n <= 8192) norm_grad_kernel<T, 1024, 1, true><<<grid, 1024, 0, st>>>(a);
+    else if (!ENDS && a.n <= 4096) norm_grad_kernel<T, 256, 2, false><<<grid, 256, 0, st>>>(a);
+    else if (!ENDS && a.n <= 8192) norm_grad_kernel<T, 512, 2, false><<<grid, 512, 0, st>>>(a);
     else if (T::size == 2 && !ENDS && a.n <= 16384) norm_grad_kernel<TypeBf16, 1024, 2, false><<<grid, 1024, 0, st>>>(a);
     else {
         norm_dot_kernel<T><<<dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))), 1024, 0, st>>>(a);
@@ -365,7 +387,7 @@ static int launch_norm_grad(const NormGradArgs &a, hipStream_t st) {
         if (rc != DLCX_OK) return rc;
     }
     Timed timed(KID_RMS_NORM_SUM, st);
-    norm_sum_kernel<<<dim3((unsigned)ceil_div(a.n, 64)), 256, 0, st>>>(a.part, a.parts, a.n, a.dw);
+    norm_sum_kernel<<<dim3((unsigned)ceil_div(a.n, kSumCols)), 256, 0, st>>>(a.part, a.parts, a.n, a.dw);
     return check_launch("rms_norm_sum");
 }
 
@@ -403,7 +425,8 @@ int dlcx_rms_norm(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx
 
 size_t dlcx_rms_norm_workspace_bytes(int64_t rows, int64_t n) {
     if (check_norm(rows, n, DLCX_F32) != DLCX_OK) return 0;
-    return a256x((size_t)norm_parts(rows, n) * part_pitch(n) * sizeof(float)) + a256x(n > 8192 ? (size_t)rows * sizeof(float) : 0) + 256;
+    const int64_t parts = std::min(rows, most_norm_parts(n));  // (no fewer than of fewer rows)
+    return a256x((size_t)parts * part_pitch(n) * sizeof(float)) + a256x(n > 8192 ? (size_t)rows * sizeof(float) : 0) + 256;
 }
 
 int dlcx_rms_norm_backward(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *weight,
@@ -423,7 +446,7 @@ int dlcx_rms_norm_backward(int64_t rows, int64_t n, int dtype, const void *x, in
     a.dot = (float *)((char *)workspace + a256x((size_t)a.parts * part_pitch(n) * sizeof(float)));
     if (rows == 0) {
         Timed timed(KID_RMS_NORM_SUM, as_stream(stream));
-        norm_sum_kernel<<<dim3((unsigned)ceil_div(n, 64)), 256, 0, as_stream(stream)>>>(a.part, 0, a.n, dw_out);
+        norm_sum_kernel<<<dim3((unsigned)ceil_div(n, kSumCols)), 256, 0, as_stream(stream)>>>(a.part, 0, a.n, dw_out);
         return check_launch("rms_norm_sum");
     }
     return dtype == DLCX_BF16 ? launch_norm_grad<TypeBf16>(a, as_stream(stream)) : launch_norm_grad<TypeF32>(a, as_stream(stream));
