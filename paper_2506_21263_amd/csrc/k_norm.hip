@@ -407,8 +407,8 @@ int dlcx_rms_norm(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx
                   const dlcx_fp8 *y8_out, float *rstd_out, void *stream) {
     if (check_norm(rows, n, dtype) != DLCX_OK || !(eps >= 0.f) || eps > 1e30f) return DLCX_EINVAL;
     if (y8_out && (check_fp8(y8_out) != DLCX_OK || y8_out->rows != rows || y8_out->cols != n)) return DLCX_EINVAL;
+    if (rows == 0) return DLCX_OK;  // (tensors without elements have no address)
     if ((residual != nullptr) != (sum_out != nullptr) || (!y_out && !y8_out)) return DLCX_EINVAL;
-    if (rows == 0) return DLCX_OK;
     if (bad_rows(x, ldx, n, dtype) || !weight || off_by(weight, dtype == DLCX_BF16 ? 2 : 4) || off_by(rstd_out, 4)) return DLCX_EINVAL;
     if (residual && (bad_rows(residual, ldr, n, dtype) || bad_rows(sum_out, ldsum, n, dtype))) return DLCX_EINVAL;
     if (y_out && bad_rows(y_out, ldy, n, dtype)) return DLCX_EINVAL;

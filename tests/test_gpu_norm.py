@@ -139,6 +139,19 @@ def test_gradient_of_views_in_place(n, alias):
     check_backward(5, n, "f32", True, pad=1, shift=3, alias=alias)
 
 
+def test_no_rows():
+    """An empty batch: tensors without elements have no address."""
+    x, w = torch.empty(0, 300, device=DEV), torch.ones(300, device=DEV)
+    out = forward(x, w, torch.empty(0, 300, device=DEV), y8=True)
+    assert out["y"].shape == (0, 300)
+    y = torch.empty(0, 7, device=DEV)
+    w8 = dlcx.fp8_empty(7, 300, DEV)
+    ws = torch.empty(dlcx.dlcx_fp8_product_workspace_bytes(0, 7, 300), device=DEV, dtype=torch.uint8)
+    dlcx.dlcx_fp8_quantize(x, out["y8"], dlcx.fp8_empty(300, 0, DEV))
+    dlcx.dlcx_fp8_product(out["y8"], w8, None, y, ws)
+    dlcx.dlcx_dropout(x, None, x, 0.5, 1)
+
+
 def test_gradient_without_rows():
     dw = torch.full((300,), 9.0, device=DEV)
     x = torch.empty(0, 300, device=DEV)
