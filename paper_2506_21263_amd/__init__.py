@@ -469,7 +469,7 @@ def _typed(t, dtype, numel, what):
     """Address of a contiguous device tensor of that type with at least `numel` elements, or None."""
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype == dtype and t.numel() >= numel and t.is_contiguous()):
+    if not (t.is_cuda and t.dtype is dtype and t.numel() >= numel and t.is_contiguous()):
         raise ValueError("%s: a contiguous device tensor of %d elements of %s is wanted" % (what, numel, dtype))
     return t.data_ptr()
 
@@ -489,7 +489,7 @@ def _rows(t, rows, cols, dtype, what):
     """Address and row stride of a rows x cols device matrix whose rows are contiguous."""
     if t is None:
         return None, cols
-    if t.is_cuda and t.dtype == dtype and t.shape == (rows, cols):  # the usual case, with few questions
+    if t.is_cuda and t.dtype is dtype and t.shape == (rows, cols):  # the usual case, with few questions
         step, inner = t.stride()
         if inner == 1 and step >= cols:
             return t.data_ptr(), (step if rows > 1 else cols)
@@ -659,9 +659,10 @@ def _ref(a):
 
 
 def _type_of(t, what):
-    if t.dtype not in _CODE:
-        raise ValueError("%s: float32 or bfloat16 is wanted" % what)
-    return t.dtype
+    dt = t.dtype
+    if dt is torch.bfloat16 or dt is torch.float32:
+        return dt
+    raise ValueError("%s: float32 or bfloat16 is wanted" % what)
 
 
 def dlcx_fp8_quantize(x, out=None, out_t=None, square=False, stream=None):
