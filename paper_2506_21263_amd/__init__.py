@@ -6,6 +6,7 @@ nothing else) and passes their addresses through.  There is no fallback: if the 
 missing or a call fails, an exception is raised.
 """
 import ctypes as C
+import functools
 import math
 import os
 
@@ -680,6 +681,7 @@ def dlcx_fp8_decode(a, out, stream=None):
     _check(lib().dlcx_fp8_decode(C.addressof(a), out, ldo, _CODE[dt], _stream(stream)), "dlcx_fp8_decode")
 
 
+@functools.lru_cache(maxsize=4096)  # (it looks at every smaller number of rows: up to 40 us, and every product asks)
 def dlcx_fp8_product_workspace_bytes(rows, m, n):
     return lib().dlcx_fp8_product_workspace_bytes(rows, m, n)
 
