@@ -71,53 +71,36 @@ __device__ __forceinline__ void load8(const typename T::elem *p, int count, floa
         for (int i = 0; i < 8; ++i) v[i] = 0.f;
     }
 }
-// The same as it lies in memory, for later: `load` asks for it and `settle` makes it what is meant, where the row ends
-// within the eight.  In a row of at least eight elements the last eight are asked for then, by the same instruction as
-// everywhere, and moved down by `settle`: nothing is waited for before everything is asked for.
+// The same as it lies in memory, for later: `load` asks for it and `settle` makes it what is meant, where the row (of at
+// least eight elements) ends within the eight: then its last eight are asked for, by the same instruction as everywhere, and
+// moved down by `settle`.  So nothing is waited for before everything is asked for.
 template <typename T>
 struct Raw8 {
     uint32_t w[2 * T::size];
-    __device__ __forceinline__ void zero() {
+    __device__ __forceinline__ void load(const typename T::elem *p) {
 #pragma unroll
-        for (int i = 0; i < 2 * T::size; ++i) w[i] = 0;
-    }
-    // n: the row's length
-    template <bool ENDS>
-    __device__ __forceinline__ void load(const typename T::elem *p, int count, int n) {
-        if (!ENDS || n >= 8) {
-            if (count > 0) {
-                if constexpr (ENDS) p += min(count - 8, 0);
+        for (int h = 0; h < T::size / 2; ++h) {
+            const Loose16 a = reinterpret_cast<const Loose16 *>(p)[h];
 #pragma unroll
-                for (int h = 0; h < T::size / 2; ++h) {
-                    const Loose16 a = reinterpret_cast<const Loose16 *>(p)[h];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[4 * h + i] = a.w[i];
-                }
-            } else {
-                zero();
-            }
-        } else {
-            typename T::elem e[8];
-            zero();
-            if (count > 0) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = p[min(i, count - 1)];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if constexpr (T::size == 2) w[i / 2] |= (uint32_t)e[i] << (16 * (i & 1));
-                    else w[i] = __float_as_uint(e[i]);
-                }
-                cut(count);
-            }
+            for (int i = 0; i < 4; ++i) w[4 * h + i] = a.w[i];
         }
     }
     template <bool ENDS>
-    __device__ __forceinline__ void settle(int count, int n) {
-        if (ENDS && n >= 8 && count > 0 && count < 8) {
+    __device__ __forceinline__ void load(const typename T::elem *p, int count) {
+        if (count > 0) {
+            load(ENDS ? p + min(count - 8, 0) : p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * T::size; ++i) w[i] = 0;
+        }
+    }
+    template <bool ENDS>
+    __device__ __forceinline__ void settle(int count) {
+        if (ENDS && count > 0 && count < 8) {
             const int by = 8 - count;
             if constexpr (T::size == 2) {
-                if (by & 4) w[0] = w[2], w[1] = w[3];
-                if (by & 2) w[0] = w[1], w[1] = w[2], w[2] = w[3];
+                if (by & 4) w[0] = w[2], w[1] = w[3], w[2] = w[3] = 0;
+                if (by & 2) w[0] = w[1], w[1] = w[2], w[2] = w[3], w[3] = 0;
                 if (by & 1) {
 #pragma unroll
                     for (int i = 0; i < 3; ++i) w[i] = w[i] >> 16 | w[i + 1] << 16;
@@ -128,19 +111,8 @@ struct Raw8 {
                 for (int d = 4; d > 0; d >>= 1)
                     if (by & d)
 #pragma unroll
-                        for (int i = 0; i + d < 8; ++i) w[i] = w[i + d];
+                        for (int i = 0; i < 8; ++i) w[i] = i + d < 8 ? w[i + d] : 0u;
             }
-            cut(count);
-        }
-    }
-    // nothing from element `count` on
-    __device__ __forceinline__ void cut(int count) {
-        if constexpr (T::size == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = 2 * i + 1 < count ? w[i] : 2 * i < count ? w[i] & 0xffffu : 0u;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = i < count ? w[i] : 0u;
         }
     }
     __device__ __forceinline__ float operator[](int i) const {

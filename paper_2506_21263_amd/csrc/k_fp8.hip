@@ -47,12 +47,28 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
         const int row0 = tr * 128 + part * 8, col0 = tc * 128 + lane16 * 8;
         const int there = a.cols - col0;
         Raw8<T> raw[8];
+        const typename T::elem *x = (const typename T::elem *)a.x + (int64_t)row0 * a.ldx + col0;
+        if (!ENDS || a.cols >= 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            raw[i].template load<ENDS>((const typename T::elem *)a.x + (int64_t)(row0 + i) * a.ldx + col0, row0 + i < a.rows ? there : 0, a.cols);
-        if constexpr (ENDS) {
+            for (int i = 0; i < 8; ++i) raw[i].template load<ENDS>(x + i * a.ldx, row0 + i < a.rows ? there : 0);
+            if constexpr (ENDS) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) raw[i].template settle<ENDS>(row0 + i < a.rows ? there : 0, a.cols);
+                for (int i = 0; i < 8; ++i) raw[i].template settle<ENDS>(row0 + i < a.rows ? there : 0);
+            }
+        } else {  // (rows of fewer than eight elements)
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+                float v[8];
+                load8<T>(x + i * a.ldx, row0 + i < a.rows ? there : 0, v);
+                Raw8<T> r;
+#pragma unroll
+                for (int k = 0; k < 2 * T::size; ++k)
+                    r.w[k] = T::size == 4 ? __float_as_uint(v[k]) : __float_as_uint(v[2 * k & 7]) >> 16 | (__float_as_uint(v[2 * k + 1 & 7]) & 0xffff0000u);
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+#pragma unroll
+                    for (int k = 0; k < 2 * T::size; ++k) raw[n].w[k] = n == i ? r.w[k] : raw[n].w[k];
+            }
         }
         // Elements stay packed between their uses: left to itself, the compiler keeps all of them unpacked, in 190 registers.
         auto packed = [&] {

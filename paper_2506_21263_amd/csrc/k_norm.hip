@@ -66,26 +66,30 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
-            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col, a.n);
+            if (c < CH / 2) to[c].load((const elem *)p + at + col);  // (n is more than LANES * 4 * CH)
+            else to[c].template load<ENDS>((const elem *)p + at + col, a.n - col);
         }
+    };
+    auto settle = [&](Raw8<T>(&x)[CH]) {
+#pragma unroll
+        for (int c = CH / 2; c < CH; ++c) x[c].template settle<ENDS>(a.n - (c * LANES + lane) * 8);
     };
     load(x, a.x, row * a.ldx);
     if (a.residual) load(r, a.residual, row * a.ldr);
     load(w, a.weight, 0);
-#pragma unroll
-    for (int c = 0; c < CH; ++c) w[c].template settle<ENDS>(a.n - (c * LANES + lane) * 8, a.n);
+    settle(w);
     for (int turn = 0;; turn ^= 1) {
         const int64_t next = row + stride;
+        settle(x);
+        if (a.residual) settle(r);
         float v[CH][8];
         float ss = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
-            x[c].template settle<ENDS>(a.n - col, a.n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = x[c][i];
             if (a.residual) {
-                r[c].template settle<ENDS>(a.n - col, a.n);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[c][i] += r[c][i];
                 round8<T>(v[c]);
@@ -161,12 +165,11 @@ template <typename T, bool ENDS>
 static void run_norm(const NormArgs &a, hipStream_t st) {
     // Workgroups: no more than the GPU holds at once, and rows shared out evenly.
     auto grid = [&a](int per, int most) { return dim3((unsigned)ceil_div(a.rows, per * ceil_div(a.rows, (int64_t)per * most))); };
-    if (a.n <= 512) norm_kernel<T, 64, 1, ENDS><<<grid(4, 2048), 256, 0, st>>>(a);
-    else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1, ENDS ? 1024 : 2048), 256, 0, st>>>(a);
-    else if (ENDS && a.n <= 4096) norm_kernel<T, 512, 1, true><<<grid(1, 512), 512, 0, st>>>(a);
-    else if (ENDS && a.n <= 8192) norm_kernel<T, 1024, 1, true><<<grid(1, 256), 1024, 0, st>>>(a);
-    else if (!ENDS && a.n <= 4096) norm_kernel<T, 256, 2, false><<<grid(1, 1280), 256, 0, st>>>(a);
-    else if (!ENDS && a.n <= 8192) norm_kernel<T, 512, 2, false><<<grid(1, 768), 512, 0, st>>>(a);
+    if (ENDS && a.n < 8) norm_long_kernel<T><<<grid(1, 1 << 22), 1024, 0, st>>>(a);
+    else if (a.n <= 512) norm_kernel<T, 64, 1, ENDS><<<grid(4, 2048), 256, 0, st>>>(a);
+    else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1, 2048), 256, 0, st>>>(a);
+    else if (a.n <= 4096) norm_kernel<T, 256, 2, ENDS><<<grid(1, 1280), 256, 0, st>>>(a);
+    else if (a.n <= 8192) norm_kernel<T, 512, 2, ENDS><<<grid(1, 768), 512, 0, st>>>(a);
     else if (!ENDS && a.n <= 16384) norm_kernel<T, 1024, 2, false><<<grid(1, 256), 1024, 0, st>>>(a);
     else if (T::size == 2 && !ENDS && a.n <= 32768) norm_kernel<TypeBf16, 1024, 4, false><<<grid(1, 256), 1024, 0, st>>>(a);
     else norm_long_kernel<T><<<grid(1, 1 << 22), 1024, 0, st>>>(a);
@@ -191,62 +194,73 @@ struct NormGradArgs {
     int rows, n, parts;
 };
 
-// A row's x and dy are asked for while the row before is worked on, and dx_in before the row's sum is formed, so that
-// neither the sum nor its barrier is waited for with nothing on its way; they stay packed until they are used.
+// A row's x and dy (and, where there are registers for it, dx_in) are asked for while the row before is worked on, so that
+// neither the sum nor its barrier is waited for with nothing on its way; they stay packed until they are used.  Short rows
+// have a wavefront each, whose parts of dw are added in LDS.
 template <typename T, int LANES, int CH, bool ENDS>
-__global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_kernel(NormGradArgs a) {
     typedef typename T::elem elem;
+    constexpr int kRows = LANES < 256 ? 256 / LANES : 1;
+    constexpr bool kAhead = CH == 1;
     __shared__ float s_part[2][16];
-    const int lane = threadIdx.x;
-    Raw8<T> w[CH], x[CH], dy[CH];
-    float dw[CH][8];
+    __shared__ __attribute__((aligned(16))) float s_dw[kRows > 1 ? kRows * LANES * 8 : 4];
+    const int lane = threadIdx.x % LANES;
+    Raw8<T> w[CH], x[CH], dy[CH], r[CH];
+    float dw[CH][8], rstd = 0.f;
     auto load = [&](Raw8<T>(&to)[CH], const void *p, int64_t at) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
-            to[c].template load<ENDS>((const elem *)p + at + col, a.n - col, a.n);
+            if (c < CH / 2) to[c].load((const elem *)p + at + col);  // (n is more than LANES * 4 * CH)
+            else to[c].template load<ENDS>((const elem *)p + at + col, a.n - col);
         }
     };
-    load(w, a.weight, 0);
-    int64_t row = blockIdx.x;
-    load(x, a.x, row * a.ldx);
-    load(dy, a.dy, row * a.lddy);
-    float rstd = a.rstd[row];
+    auto settle = [&](Raw8<T>(&x)[CH]) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        w[c].template settle<ENDS>(a.n - (c * LANES + lane) * 8, a.n);
+        for (int c = CH / 2; c < CH; ++c) x[c].template settle<ENDS>(a.n - (c * LANES + lane) * 8);
+    };
+    load(w, a.weight, 0);
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    if (row < a.rows) {
+        load(x, a.x, row * a.ldx);
+        load(dy, a.dy, row * a.lddy);
+        if (kAhead && a.dx_in) load(r, a.dx_in, row * a.ldi);
+        rstd = a.rstd[row];
+    }
+    settle(w);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
-    }
     for (int turn = 0; row < a.rows; turn ^= 1) {
-        const int64_t next = row + gridDim.x;
-        Raw8<T> r[CH], nx[CH], ndy[CH];
+        const int64_t next = row + stride;
+        Raw8<T> nx[CH], ndy[CH], nr[CH];
         float nrstd = 0.f;
-        if (a.dx_in) load(r, a.dx_in, row * a.ldi);
+        if (!kAhead && a.dx_in) load(r, a.dx_in, row * a.ldi);
         if (next < a.rows) {
             load(nx, a.x, next * a.ldx);
             load(ndy, a.dy, next * a.lddy);
+            if (kAhead && a.dx_in) load(nr, a.dx_in, next * a.ldi);
             nrstd = a.rstd[next];
         }
+        settle(x);
+        settle(dy);
         float dot = 0.f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int count = a.n - (c * LANES + lane) * 8;
-            x[c].template settle<ENDS>(count, a.n);
-            dy[c].template settle<ENDS>(count, a.n);
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float h = x[c][i] * rstd;
                 dw[c][i] += dy[c][i] * h;
                 dot += dy[c][i] * w[c][i] * h;
             }
-        }
         dot = sum_lanes<LANES>(dot, s_part[turn]) / (float)a.n;  // (two places, so one barrier a row)
+        if (a.dx_in) settle(r);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * LANES + lane) * 8;
             float v[8];
-            if (a.dx_in) r[c].template settle<ENDS>(a.n - col, a.n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 v[i] = rstd * (dy[c][i] * w[c][i] - x[c][i] * rstd * dot);
@@ -255,9 +269,24 @@ __global__ __launch_bounds__(LANES) void norm_grad_kernel(NormGradArgs a) {
             store8<T, ENDS>((elem *)a.dx + row * a.ldo + col, a.n - col, v);
             x[c] = nx[c];
             dy[c] = ndy[c];
+            if constexpr (kAhead) r[c] = nr[c];
         }
         row = next;
         rstd = nrstd;
+    }
+    if constexpr (kRows > 1) {
+        const int wave = threadIdx.x / LANES;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_dw[(wave * 8 + i) * LANES + lane] = dw[0][i];
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float t = 0.f;
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) t += s_dw[(k * 8 + i) * LANES + lane];
+            dw[0][i] = t;
+        }
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -352,30 +381,28 @@ __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__
 }
 
 // Workgroups of the gradient, each with a part of dw: no more than the GPU holds at once, and rows shared out evenly.
-// (515 rows of 2050 fp32: 515 of them, of which the GPU held 512, took 12 us, 258 of two rows 7.)
-static int64_t most_norm_parts(int64_t n) {
-    const bool ends = n % 8 != 0;
-    return n <= 512 ? 4096 : n <= 2048 ? 1024 : n <= 4096 ? (ends ? 512 : 768) : n <= 8192 ? (ends ? 256 : 512) : 256;
-}
+static int64_t most_norm_parts(int64_t n) { return n <= 2048 ? 1024 : n <= 4096 ? 768 : n <= 8192 ? 512 : 256; }
 static int norm_parts(int64_t rows, int64_t n) {
-    const int64_t turns = ceil_div(rows, most_norm_parts(n));
-    return turns ? (int)ceil_div(rows, turns) : 0;
+    const int64_t units = n >= 8 && n <= 512 ? ceil_div(rows, 4) : rows;  // (four rows to a workgroup)
+    const int64_t turns = ceil_div(units, most_norm_parts(n));
+    return turns ? (int)ceil_div(units, turns) : 0;
 }
 
+template <typename T>
+static void long_norm_grad(const NormGradArgs &a, hipStream_t st) {
+    norm_dot_kernel<T><<<dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))), 1024, 0, st>>>(a);
+    norm_grad_long_kernel<T><<<dim3((unsigned)ceil_div(a.n, 2048), (unsigned)a.parts), 256, 0, st>>>(a);
+}
 template <typename T, bool ENDS>
 static void run_norm_grad(const NormGradArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)a.parts);
-    if (a.n <= 512) norm_grad_kernel<T, 64, 1, ENDS><<<grid, 64, 0, st>>>(a);
+    if (ENDS && a.n < 8) long_norm_grad<T>(a, st);
+    else if (a.n <= 512) norm_grad_kernel<T, 64, 1, ENDS><<<grid, 256, 0, st>>>(a);
     else if (a.n <= 2048) norm_grad_kernel<T, 256, 1, ENDS><<<grid, 256, 0, st>>>(a);
-    else if (ENDS && a.n <= 4096) norm_grad_kernel<T, 512, 1, true><<<grid, 512, 0, st>>>(a);
-    else if (ENDS && a.n <= 8192) norm_grad_kernel<T, 1024, 1, true><<<grid, 1024, 0, st>>>(a);
-    else if (!ENDS && a.n <= 4096) norm_grad_kernel<T, 256, 2, false><<<grid, 256, 0, st>>>(a);
-    else if (!ENDS && a.n <= 8192) norm_grad_kernel<T, 512, 2, false><<<grid, 512, 0, st>>>(a);
+    else if (a.n <= 4096) norm_grad_kernel<T, 256, 2, ENDS><<<grid, 256, 0, st>>>(a);
+    else if (a.n <= 8192) norm_grad_kernel<T, 512, 2, ENDS><<<grid, 512, 0, st>>>(a);
     else if (T::size == 2 && !ENDS && a.n <= 16384) norm_grad_kernel<TypeBf16, 1024, 2, false><<<grid, 1024, 0, st>>>(a);
-    else {
-        norm_dot_kernel<T><<<dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))), 1024, 0, st>>>(a);
-        norm_grad_long_kernel<T><<<dim3((unsigned)ceil_div(a.n, 2048), (unsigned)a.parts), 256, 0, st>>>(a);
-    }
+    else long_norm_grad<T>(a, st);
 }
 template <typename T>
 static int launch_norm_grad(const NormGradArgs &a, hipStream_t st) {
@@ -426,7 +453,7 @@ int dlcx_rms_norm(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx
 size_t dlcx_rms_norm_workspace_bytes(int64_t rows, int64_t n) {
     if (check_norm(rows, n, DLCX_F32) != DLCX_OK) return 0;
     const int64_t parts = std::min(rows, most_norm_parts(n));  // (no fewer than of fewer rows)
-    return a256x((size_t)parts * part_pitch(n) * sizeof(float)) + a256x(n > 8192 ? (size_t)rows * sizeof(float) : 0) + 256;
+    return a256x((size_t)parts * part_pitch(n) * sizeof(float)) + a256x(n > 8192 || n < 8 ? (size_t)rows * sizeof(float) : 0) + 256;
 }
 
 int dlcx_rms_norm_backward(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *weight,

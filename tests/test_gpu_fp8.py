@@ -62,6 +62,13 @@ def test_quantize(rows, cols, dtype, form):
                 assert np.array_equal(f64(v[:, :cols_]), decode(c, s, cols_)) and bool((v[:, cols_:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", ["both", "square"])
+@pytest.mark.parametrize("rows,cols", [(200, 3), (130, 7), (300, 8), (133, 9), (257, 135)])
+def test_quantize_narrow(rows, cols, form, dtype):
+    test_quantize(rows, cols, dtype, form)
+
+
 def test_every_code_and_what_is_between_them():
     """Codes come back as they are, and values between two of them go to the nearest, ties to the even one."""
     v = np.sort(CODES[np.isfinite(CODES) & (CODES >= 0)])

@@ -132,6 +132,12 @@ def test_gradient(rows, n, dtype, residual):
     check_backward(rows, n, dtype, residual)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(9001, 5), (5003, 8), (9001, 130), (4099, 512), (2500, 1023)])
+def test_gradient_of_many_short_rows(rows, n, dtype):
+    check_backward(rows, n, dtype, True, pad=1, shift=1)
+
+
 @pytest.mark.parametrize("alias", ["x", "dy", "dx_in"])
 @pytest.mark.parametrize("n", [5, 600, 2050, 9001, 33001])
 def test_gradient_of_views_in_place(n, alias):
