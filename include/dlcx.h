@@ -296,7 +296,7 @@ int dlcx_select_rank_from(const int32_t *rprime_dev, int n_matrices, int32_t *rp
  *
  * K workers that share theta_g in one GPU's memory, or requests that are answered with it, differ by
  * low-rank adapters: y = theta_g x + s_a P_a Q_a^T x for a row of adapter a.  The projection itself is
- * a plain product of the caller's; the calls below do what stands beside it, and the update of the
+ * a plain product of the caller's, or dlcx_fp8_product; the calls below do what stands beside it, and the update of the
  * adapters (or of any other tensors) between two outer steps.  The factors of an adapter have the
  * layout of every factor here, so dlcx_decompress folds a trained adapter into an error buffer. */
 

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
 // Scales go through LDS, too (four stages' to a dword): read by every lane that needs them they were 40 % of all
 // requests to the cache.  Results leave through LDS as whole lines.  Edge tiles are moved inside the matrix and write
 // only what is theirs, so no address is checked.
-// 16384 x 8192 x 8192: 0.82 ms, 2.7 PFLOP/s (0.64 without the fetches, 1.44 with 128 x 128 tiles); 8192^3 0.41 ms.
+// 16384 x 8192 x 8192: 0.85 ms, 2.6 PFLOP/s (0.64 without the fetches, 1.44 with 128 x 128 tiles); 8192^3 0.41 ms.
 constexpr int kWideTile = 256, kWideStage = 512 * 128, kWideLds = 2 * kWideStage + 2 * 2048;
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
@@ -547,11 +547,12 @@ __global__ __launch_bounds__(256, 2) void product_few_kernel(ProductArgs a) {
 }
 
 // Tiles of 128 columns x 32 FN rows, one workgroup to a compute unit: 17 .. 128 rows, and as many tiles of 128 as there are
-// compute units.  Few rows are bound by the reading of w, so what counts is how much of it is on its way: a ring of as many stages as LDS holds (128 bytes of each row, straight to LDS;
-// pieces at piece ^ (row & 7)), all but one of them in flight, 64 KB of w to a compute unit beside 96 rows.  (Twice as much,
-// in registers and with a barrier only every four blocks, measured the same: a compute unit takes in 24 - 28 bytes a ns
-// from HBM, and x's are among them.)  96 rows of 28672 x 8192: 77 us, 3.1 TB/s of w, 5.4 of both.  Scales
-// come four stages to a dword, two dwords ahead, 256 rows (w's, then x's) to a load of the workgroup.
+// compute units.  Few rows are bound by the reading of w, so what counts is how much of it is on its way: a ring of as many
+// stages as LDS holds (128 bytes of each row, straight to LDS; pieces at piece ^ (row & 7)), all but one of them in flight,
+// 64 KB of w to a compute unit beside 96 rows.  (Twice as much, in registers and with a barrier only every four blocks,
+// measured the same: a compute unit takes in 24 - 28 bytes a ns from HBM, and x's are among them.)  96 rows of 28672 x 8192:
+// 70 us, 3.4 TB/s of w.  Scales come four stages to a dword, two dwords ahead, 256 rows (w's, then x's) to a load of the
+// workgroup.
 template <typename T, int FN>
 struct SomeShape {
     static constexpr int kRows = 32 * FN, kStage = (128 + kRows) * 128, kRing = 152 * 1024 / kStage;

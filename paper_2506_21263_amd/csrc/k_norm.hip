@@ -5,8 +5,11 @@
 //   dx = dx_in + rstd (g - h mean(g h)),  g = dy w,  h = s rstd ;  dw = sum over rows of dy h
 //
 // Streams over the rows, bound by HBM.  Up to 8192 columns (and, where n is a multiple of eight, 16384, of bf16 32768;
-// gradients of bf16 16384) a row is read once and held in the registers of its workgroup (a wavefront for short rows); longer rows are
-// read twice.  Sums are fp32, in an order that hangs on n and, for dw, on the number of rows.
+// gradients of bf16 16384) a row is read once and held in the registers of its workgroup (a wavefront for short rows); longer
+// rows, and rows of fewer than eight elements, are read twice.  Sums are fp32, in an order that hangs on n and, for dw, on
+// the number of rows.
+// 4133 x 8192 bf16 with residual, to 8 bits: 50 us (5.0 TB/s), gradient of 16384 x 8192 with residual 190 + 5 us (5.6 TB/s);
+// fp32, 6000 x 6000, 113 us each way (5.1 TB/s), 6000 x 5999 126 and 117.
 #include <algorithm>
 
 #include "eight.h"
