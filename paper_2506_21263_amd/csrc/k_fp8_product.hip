@@ -113,6 +113,83 @@ __device__ __forceinline__ TilePlace tile_place(int id, int row_tiles, int col_t
     return {__builtin_amdgcn_readfirstlane(first + in % rows), __builtin_amdgcn_readfirstlane(in / rows)};
 }
 
+// A wavefront's 64 x 16 FN outputs and one block of 128: lane r16 has row r16 of each 16 of w's (from pw) and x's (from px) in
+// LDS, pieces of 16 bytes at p0 and p1; S: the byte of their scales.
+template <int S, int FN>
+__device__ __forceinline__ void multiply_scaled(const uint8_t *pw, const uint8_t *px, int p0, int p1, const int (&scale_w)[4],
+                                                const int (&scale_x)[FN], f32x4 (&acc)[4][FN]) {
+    i32x8 fw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fw[i] = join(*(const i32x4 *)(pw + i * 2048 + p0), *(const i32x4 *)(pw + i * 2048 + p1));
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][j] = scaled_mma<S>(fw[i], fx, acc[i][j], scale_w[i], scale_x[j]);
+    }
+}
+// The same of widened codes, scaled as they are widened.  TIGHT: half of them at a time (two wavefronts to a SIMD have no
+// registers for more).  Widening takes as many cycles as three eighths of the products (64 rows) or a quarter (128 rows), and they
+// hardly overlap: 8192 x 8192 x 4096 takes 577 us (0.95 PFLOP/s) in tiles of 128 rows, 659 in tiles of 64.
+template <int S, int FN, bool TIGHT = false>
+__device__ __forceinline__ void multiply_widened(const uint8_t *pw, const uint8_t *px, int p0, int p1, const int (&scale_w)[4],
+                                                 const int (&scale_x)[FN], f32x4 (&acc)[4][FN]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int at = h ? p1 : p0;
+        bf16x8 bw[4][2];
+        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const i32x4 f = *(const i32x4 *)(pw + i * 2048 + at);
+            bw[i][0] = widen(f[0], f[1], scale_of<S>(scale_w[i]));
+            bw[i][1] = widen(f[2], f[3], scale_of<S>(scale_w[i]));
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const i32x4 f = *(const i32x4 *)(px + j * 2048 + at);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 bx = widen(f[2 * k], f[2 * k + 1], scale_of<S>(scale_x[j]));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i][k], bx, acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+    if (!TIGHT) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 8 + 2 * FN, 0);  // all reads, the first half of w widened, ...
+        __builtin_amdgcn_sched_group_barrier(0x002, 28, 0);
+#pragma unroll
+        for (int k = 0; k < 16 * FN; ++k) {  // ... and the rest between the products
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+        }
+    }
+}
+// The same of scales that bf16 does not hold: a block's sum is scaled.
+template <int S, int FN>
+__device__ __forceinline__ void multiply_apart(const uint8_t *pw, const uint8_t *px, int p0, int p1, const int (&scale_w)[4],
+                                               const int (&scale_x)[FN], f32x4 (&acc)[4][FN]) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        asm volatile("" ::: "memory");  // (else x's columns stay in registers from one i to the next)
+        const i32x8 fw = join(*(const i32x4 *)(pw + i * 2048 + p0), *(const i32x4 *)(pw + i * 2048 + p1));
+        int ew[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ew[e] = (__shfl(scale_w[i], g * 4 + e, 64) >> (8 * S)) & 255;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
+            f32x4 sum = {};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(fw[2 * k], fw[2 * k + 1]), widen(fx[2 * k], fx[2 * k + 1]), sum, 0, 0, 0);
+            acc[i][j] = add_scaled(acc[i][j], sum, ew, (scale_x[j] >> (8 * S)) & 255);
+        }
+    }
+}
+
 // ---- tiles --------------------------------------------------------------------------------------------
 // 128 columns x 32 FN rows of outputs to a workgroup of four wavefronts, 64 x 16 FN to each.  128 bytes of the tile's
 // rows at a time, twice, straight to LDS; the 16-byte pieces of a row lie at piece ^ (row & 7), so that what is read at
@@ -121,7 +198,8 @@ template <typename T, int FN>
 __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
     constexpr int kRows = 32 * FN, kStage = (128 + kRows) * 128, kFetchX = kRows / 32;
     constexpr bool kWiden = T::size == 4;  // fp32 results
-    __shared__ __attribute__((aligned(16))) uint8_t s_tile[2 * kStage];
+    // (Widened, two workgroups to a compute unit are 3 - 5 % faster than the three that would fit: 2048^3 26.0 us, not 27.0.)
+    __shared__ __attribute__((aligned(16))) uint8_t s_tile[kWiden && 2 * kStage < 56 * 1024 ? 56 * 1024 : 2 * kStage];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const TilePlace place = tile_place(blockIdx.x, a.row_tiles, a.col_tiles, 8);
     const int64_t row0 = (int64_t)place.row * kRows, col0 = (int64_t)place.col * 128;
@@ -148,62 +226,33 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
     for (int j = 0; j < FN; ++j) sx[j] = a.xs + min(row0 + wn + j * 16 + r16, (int64_t)a.rows - 1) * a.ldxs;
     const int p0 = (g ^ (lane & 7)) * 16, p1 = ((g + 4) ^ (lane & 7)) * 16;
     f32x4 acc[4][FN] = {};
-    int scale_w[4], scale_x[FN];
+    int scale_w[4], scale_x[FN], next_w[4], next_x[FN];
+    auto fetch_scales = [&](int block) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) next_w[i] = *(const int *)(sw[i] + block);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) next_x[j] = *(const int *)(sx[j] + block);
+    };
     bool inside = false;
     auto step = [&](int buf, auto s) {
         constexpr int S = decltype(s)::value;
         const uint8_t *pw = s_tile + buf * kStage + (wm + r16) * 128, *px = s_tile + buf * kStage + (128 + wn + r16) * 128;
-        i32x8 fw[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) fw[i] = join(*(const i32x4 *)(pw + i * 2048 + p0), *(const i32x4 *)(pw + i * 2048 + p1));
         if constexpr (kWiden) {
-            bf16x8 bw[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float s = inside ? scale_of<S>(scale_w[i]) : 1.f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) bw[i][k] = widen(fw[i][2 * k], fw[i][2 * k + 1], s);
-            }
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
-                const float s = inside ? scale_of<S>(scale_x[j]) : 1.f;
-                if (inside) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const bf16x8 bx = widen(fx[2 * k], fx[2 * k + 1], s);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i][k], bx, acc[i][j], 0, 0, 0);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        f32x4 sum = {};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i][k], widen(fx[2 * k], fx[2 * k + 1]), sum, 0, 0, 0);
-                        int ew[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) ew[e] = (__shfl(scale_w[i], g * 4 + e, 64) >> (8 * S)) & 255;
-                        acc[i][j] = add_scaled(acc[i][j], sum, ew, (scale_x[j] >> (8 * S)) & 255);
-                    }
-                }
-            }
+            if (inside) multiply_widened<S, FN, FN == 4>(pw, px, p0, p1, scale_w, scale_x, acc);
+            else multiply_apart<S, FN>(pw, px, p0, p1, scale_w, scale_x, acc);
         } else {
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i][j] = scaled_mma<S>(fw[i], fx, acc[i][j], scale_w[i], scale_x[j]);
-            }
+            multiply_scaled<S, FN>(pw, px, p0, p1, scale_w, scale_x, acc);
         }
     };
-    if (first < last) fetch(0, first);
+    if (first < last) {
+        fetch_scales(first);
+        fetch(0, first);
+    }
     for (int block = first; block < last; block += 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) scale_w[i] = *(const int *)(sw[i] + block);
+        for (int i = 0; i < 4; ++i) scale_w[i] = next_w[i];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) scale_x[j] = *(const int *)(sx[j] + block);
+        for (int j = 0; j < FN; ++j) scale_x[j] = next_x[j];
         if constexpr (kWiden) {
             uint32_t bad = 0;
 #pragma unroll
@@ -218,6 +267,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the tile is there ...
                 __syncthreads();                                  // ... all of it, and the other one has been read
                 if (block + S + 1 < last) fetch((S + 1) & 1, block + S + 1);
+                if (S == 0 && block + 4 < last) fetch_scales(block + 4);
                 step(S & 1, s);
             }
         });
@@ -563,7 +613,6 @@ __global__ __launch_bounds__(256, 1) void product_some_kernel(ProductArgs a) {
     typedef SomeShape<T, FN> Shape;
     constexpr int kStage = Shape::kStage, kRing = Shape::kRing;
     constexpr bool kWiden = T::size == 4;
-    constexpr int kScaleRows = kWiden ? 4 : 1;
     extern __shared__ __attribute__((aligned(16))) uint8_t s_ring[];
     uint8_t *const s_scale = s_ring + kRing * kStage;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -597,7 +646,8 @@ __global__ __launch_bounds__(256, 1) void product_some_kernel(ProductArgs a) {
     const int r16 = lane & 15, g = lane >> 4, wm = (wave & 1) * 64, wn = (wave >> 1) * 16 * FN;
     const int p0 = (g ^ (lane & 7)) * 16, p1 = ((g + 4) ^ (lane & 7)) * 16;
     f32x4 acc[4][FN] = {};
-    int scale_w[4][kScaleRows], scale_x[FN], slot = 0;
+    int scale_w[4], scale_x[FN], slot = 0;
+    bool inside = false;
     for (int block = first; block < last; block += 4) {
         unrolled<4>([&](auto s) {
             constexpr int S = decltype(s)::value;
@@ -607,42 +657,21 @@ __global__ __launch_bounds__(256, 1) void product_some_kernel(ProductArgs a) {
                 if constexpr (S == 0) {
                     fetch_scales(block + 8);
                     const int *at = (const int *)(s_scale + (block >> 2 & 3) * 1024);
+                    uint32_t bad = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i) bad |= outside(scale_w[i] = at[wm + i * 16 + r16]);
 #pragma unroll
-                        for (int e = 0; e < kScaleRows; ++e) scale_w[i][e] = at[wm + i * 16 + (kWiden ? g * 4 + e : r16)];
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) scale_x[j] = at[128 + wn + j * 16 + r16];
+                    for (int j = 0; j < FN; ++j) bad |= outside(scale_x[j] = at[128 + wn + j * 16 + r16]);
+                    if constexpr (kWiden) inside = all_inside(bad, last - block);
                 }
                 fetch(slot == 0 ? kRing - 1 : slot - 1, block + S + kRing - 1);
                 const uint8_t *pw = s_ring + slot * kStage + (wm + r16) * 128, *px = s_ring + slot * kStage + (128 + wn + r16) * 128;
                 slot = slot + 1 == kRing ? 0 : slot + 1;
-                i32x8 fw[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) fw[i] = join(*(const i32x4 *)(pw + i * 2048 + p0), *(const i32x4 *)(pw + i * 2048 + p1));
-#pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    const i32x8 fx = join(*(const i32x4 *)(px + j * 2048 + p0), *(const i32x4 *)(px + j * 2048 + p1));
-                    if constexpr (kWiden) {
-                        f32x4 sum[4] = {};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const bf16x8 bx = widen(fx[2 * k], fx[2 * k + 1]);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(fw[i][2 * k], fw[i][2 * k + 1]), bx, sum[i], 0, 0, 0);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            int ew[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) ew[e] = (scale_w[i][e] >> (8 * S)) & 255;
-                            acc[i][j] = add_scaled(acc[i][j], sum[i], ew, (scale_x[j] >> (8 * S)) & 255);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[i][j] = scaled_mma<S>(fw[i], fx, acc[i][j], scale_w[i][0], scale_x[j]);
-                    }
+                if constexpr (kWiden) {
+                    if (inside) multiply_widened<S, FN>(pw, px, p0, p1, scale_w, scale_x, acc);
+                    else multiply_apart<S, FN>(pw, px, p0, p1, scale_w, scale_x, acc);
+                } else {
+                    multiply_scaled<S, FN>(pw, px, p0, p1, scale_w, scale_x, acc);
                 }
             }
         });
@@ -702,11 +731,11 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
         const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
         return {kSome, (int)ceil_div(blocks, per), (int)per, (int)ceil_div(rows, 32)};
     }
-    // Tiles of 128 rows (not of fp32 results, which have no registers for them) or 64, in pairs that share a compute unit,
-    // or of 128 rows alone on it with a ring of stages; and splits.  The least of what the busiest compute unit takes, as
+    // Tiles of 128 rows or 64, in pairs that share a compute unit, or (bf16) of 128 rows alone on it with a ring of stages;
+    // and splits.  The least of what the busiest compute unit takes, as
     // measured in us for a block of a tile, and of writing and adding the splits' sums.  (1024 x 4096 x 4096 bf16: ring 25.8,
     // 128 rows 31.7 and 34.5 in two splits, 64 rows 31.5; 3000 x 700 x 6000: 128 rows in three splits 29.0, ring 35.0; 2050 x
-    // 1021 x 4133 fp32: 46.6, 44.1, 40.0, 40.2 in one to four splits.)
+    // 1021 x 4133 fp32: 64 rows 46.6, 44.1, 40.0, 40.2 in one to four splits, 128 rows 37.9 in three.)
     ProductPlan best = {};
     double least = 1e300;
     auto consider = [&](ProductForm form, int fn, int64_t splits, double alone, double paired) {
@@ -714,7 +743,8 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
         if (splits > 1 && tiles >= 512) return;
         const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4, used = ceil_div(blocks, per), busiest = ceil_div(tiles * used, 256);
         double cost = (double)(busiest * std::min(per, blocks)) * (busiest == 1 ? alone : paired);
-        if (used > 1) cost += 3.0 + 1e-6 * (double)(used * ceil_div(rows, 64) * 64 * m);  // (rows of whole tiles: see the workspace)
+        const int f32 = dtype == DLCX_F32 ? 1 : 0;  // (the sums' launch reads and writes y, too)
+        if (used > 1) cost += 3.0 - f32 + 1e-6 * (double)((used + f32) * ceil_div(rows, 64) * 64 * m);  // (rows of whole tiles: see the workspace)
         if (cost >= least) return;
         least = cost;
         best = {form, (int)used, (int)per, fn};
@@ -724,6 +754,7 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
             consider(kTiles, 4, splits, 1.0, 0.8);
             consider(kTiles, 2, splits, 0.6, 0.47);
         } else {
+            consider(kTiles, 4, splits, 1.6, 1.18);
             consider(kTiles, 2, splits, 0.85, 0.7);
         }
     }
@@ -768,7 +799,7 @@ static int launch_product(ProductArgs a, const ProductPlan &plan, hipStream_t st
         } else {
             a.row_tiles = (int)ceil_div(a.rows, 32 * plan.kw);
             const dim3 grid((unsigned)(a.row_tiles * (int64_t)a.col_tiles), plan.splits);
-            if (T::size == 2 && plan.kw == 4) product_kernel<TypeBf16, 4><<<grid, 256, 0, st>>>(a);
+            if (plan.kw == 4) product_kernel<T, 4><<<grid, 256, 0, st>>>(a);
             else product_kernel<T, 2><<<grid, 256, 0, st>>>(a);
         }
         const int rc = check_launch("fp8_product");

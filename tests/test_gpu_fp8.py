@@ -212,6 +212,29 @@ def test_extreme_scales(rows):
     assert bool((y == float("inf")).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,m,n", [(1, 90, 1100), (20, 90, 1100), (300, 130, 1100), (700, 700, 1100), (4096, 2048, 300)])
+def test_scales_far_apart(rows, m, n, dtype):
+    """Scales from 2^-117 to 2^73, another for every block of a row: the smallest products vanish beside the largest.  What
+    fp32 cannot hold (below 2^-126 each) is in the bound's last term."""
+    gen = torch.Generator().manual_seed(4)
+    x, _ = operand(gen, rows, n)
+    w, _ = operand(gen, m, n)
+    for a, low, high in ((x, 10, 121), (w, 40, 201)):
+        s = a.held[1]
+        s.copy_(torch.randint(low, high, s.shape, generator=gen, dtype=torch.uint8))
+        s[::3] = 127                                               # some rows' are all near 1
+    xv, wv = (decode(*bytes_of(a), n) for a in (x, w))
+    y = torch.empty(rows, m, device=DEV, dtype=TYPES[dtype])
+    ws = torch.empty(dlcx.dlcx_fp8_product_workspace_bytes(rows, m, n), device=DEV, dtype=torch.uint8)
+    dlcx.dlcx_fp8_product(x, w, None, y, ws)
+    want, most = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    bound = (n + 8) * 2.0 ** -23 * most + n * 2.0 ** -126
+    if dtype == "bf16":
+        bound += 2.0 ** -10 * most + HALF[y.dtype] * np.abs(want) * 1.01
+    assert (np.abs(f64(y) - want) <= bound).all()
+
+
 @pytest.mark.parametrize("rows", [1, 20, 300])
 def test_a_nan_stays_in_its_row_and_column(rows):
     gen = torch.Generator().manual_seed(2)
