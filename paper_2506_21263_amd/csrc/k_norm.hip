@@ -197,6 +197,17 @@ struct NormGradArgs {
     int rows, n, parts;
 };
 
+// Eight elements of a part of dw; a part that is all of it goes where it belongs.
+__device__ __forceinline__ void put_part(const NormGradArgs &a, int part, int64_t col, const float (&dw)[8]) {
+    if (a.parts == 1) {
+        store8<TypeF32>(a.dw + col, (int)(a.n - col), dw);
+        return;
+    }
+    float *p = a.part + (int64_t)part * part_pitch(a.n) + col;
+    *reinterpret_cast<float4 *>(p) = make_float4(dw[0], dw[1], dw[2], dw[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(dw[4], dw[5], dw[6], dw[7]);
+}
+
 // A row's x and dy (and, where there are registers for it, dx_in) are asked for while the row before is worked on, so that
 // neither the sum nor its barrier is waited for with nothing on its way; they stay packed until they are used.  Short rows
 // have a wavefront each, whose parts of dw are added in LDS.
@@ -294,11 +305,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_kernel(No
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * LANES + lane) * 8;
-        if (col < a.n) {
-            float *p = a.part + (int64_t)blockIdx.x * part_pitch(a.n) + col;
-            *reinterpret_cast<float4 *>(p) = make_float4(dw[c][0], dw[c][1], dw[c][2], dw[c][3]);
-            *reinterpret_cast<float4 *>(p + 4) = make_float4(dw[c][4], dw[c][5], dw[c][6], dw[c][7]);
-        }
+        if (col < a.n) put_part(a, blockIdx.x, col, dw[c]);
     }
 }
 
@@ -347,9 +354,7 @@ __global__ __launch_bounds__(256) void norm_grad_long_kernel(NormGradArgs a) {
         }
         store8<T>((elem *)a.dx + row * a.ldo + col, there, r);
     }
-    float *p = a.part + blockIdx.y * part_pitch(a.n) + col;
-    *reinterpret_cast<float4 *>(p) = make_float4(dw[0], dw[1], dw[2], dw[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(dw[4], dw[5], dw[6], dw[7]);
+    put_part(a, blockIdx.y, col, dw);
 }
 
 // dw from its parts: 32 columns to a workgroup, 32 shares of the parts to them, eight parts at a time.
@@ -383,10 +388,12 @@ __global__ __launch_bounds__(256) void norm_sum_kernel(const float *__restrict__
     }
 }
 
-// Workgroups of the gradient, each with a part of dw: no more than the GPU holds at once, and rows shared out evenly.
+// Workgroups of the gradient, each with a part of dw: no more than the GPU holds at once, and rows shared out evenly.  Few
+// rows are one's, which saves the second launch: a turn takes 0.7 us (8192 columns: 1.2), the launch 2 and the host 3.
 static int64_t most_norm_parts(int64_t n) { return n <= 2048 ? 1024 : n <= 4096 ? 768 : n <= 8192 ? 512 : 256; }
 static int norm_parts(int64_t rows, int64_t n) {
     const int64_t units = n >= 8 && n <= 512 ? ceil_div(rows, 4) : rows;  // (four rows to a workgroup)
+    if (units <= (n <= 512 ? 4 : n <= 2048 ? 3 : n <= 8192 ? 2 : 1)) return units ? 1 : 0;
     const int64_t turns = ceil_div(units, most_norm_parts(n));
     return turns ? (int)ceil_div(units, turns) : 0;
 }
@@ -414,7 +421,7 @@ static int launch_norm_grad(const NormGradArgs &a, hipStream_t st) {
         if (a.n % 8) run_norm_grad<T, true>(a, st);
         else run_norm_grad<T, false>(a, st);
         const int rc = check_launch("rms_norm_backward");
-        if (rc != DLCX_OK) return rc;
+        if (rc != DLCX_OK || a.parts == 1) return rc;
     }
     Timed timed(KID_RMS_NORM_SUM, st);
     norm_sum_kernel<<<dim3((unsigned)ceil_div(a.n, kSumCols)), 256, 0, st>>>(a.part, a.parts, a.n, a.dw);
