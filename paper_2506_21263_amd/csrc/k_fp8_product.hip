@@ -723,13 +723,23 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
     const int64_t wide = ceil_div(rows, kWideTile) * ceil_div(m, kWideTile);
     if (dtype == DLCX_BF16 && rows >= kWideTile && m >= kWideTile && wide >= 128 && most_stride <= (1 << 23))  // (256 rows: 32 bits)
         return {kWide, 1, 0, 0};
-    const bool some = rows <= 128;
     const int64_t col_tiles = ceil_div(m, 128);
-    if (some) {
-        int64_t splits = col_tiles < 160 ? 256 / col_tiles : 1;
-        splits = std::max((int64_t)1, std::min(splits, blocks / 4));
-        const int64_t per = ceil_div(ceil_div(blocks, splits), 4) * 4;
-        return {kSome, (int)ceil_div(blocks, per), (int)per, (int)ceil_div(rows, 32)};
+    if (rows <= 128) {
+        // Splits as far as they fill the GPU, by the us that a block, a split and its sums were measured to take.  (100 x 2050 x
+        // 4133 fp32: nine splits 16.7, five 20.1; 40 x 700 x 20000 bf16: 20 splits 16.1, 40 20.7.)
+        const int fn = (int)ceil_div(rows, 32);
+        const double block = dtype == DLCX_F32 ? 0.5 + 0.3 * fn : 0.25 + 0.13 * fn, split = 0.25 + 5e-5 * (double)(fn * m);
+        ProductPlan best = {kSome, 1, (int)(quads * 4), fn};
+        double least = (double)blocks * block;
+        const int64_t most = col_tiles < 160 ? 256 / col_tiles : 1;
+        for (int64_t per = ceil_div(ceil_div(blocks, most), 4) * 4; per < blocks && (double)per * block < least; per += 4) {
+            const int64_t used = ceil_div(blocks, per);
+            const double cost = (double)per * block + 2.0 + (double)used * split;
+            if (cost >= least) continue;
+            least = cost;
+            best = {kSome, (int)used, (int)per, fn};
+        }
+        return best;
     }
     // Tiles of 128 rows or 64, in pairs that share a compute unit, or (bf16) of 128 rows alone on it with a ring of stages;
     // and splits.  The least of what the busiest compute unit takes, as
@@ -823,14 +833,14 @@ static bool bad_product(int64_t rows, int64_t m, int64_t n) {
 
 size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
     if (bad_product(rows, m, n)) return 0;
-    size_t most = 0;  // of fewer rows, too: these may be split further (above 128 the plan is the same for 64 rows each)
+    size_t most = 0;  // of fewer rows, too: these may be split further (the plan is the same for 32 rows each, above 128 for 64)
     auto look = [&](int64_t r) {
         for (int dtype : {DLCX_F32, DLCX_BF16}) {
             const ProductPlan plan = product_plan(r, m, n, dtype, INT64_MAX);
             if (plan.splits > 1) most = std::max(most, (size_t)plan.splits * r * ceil_div(m, 4) * 16);
         }
     };
-    look(std::min(rows, (int64_t)128));
+    for (int64_t r = 32; r < rows + 32 && r <= 128; r += 32) look(std::min(r, rows));
     for (int64_t r = 192; r < rows + 64 && r <= 65536; r += 64) {
         look(std::min(r, rows));
         if (ceil_div(r, 128) * ceil_div(m, 128) >= 512) break;  // (never split)
