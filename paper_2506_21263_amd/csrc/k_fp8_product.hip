@@ -691,16 +691,23 @@ __global__ __launch_bounds__(256, 1) void product_some_kernel(ProductArgs a) {
     }
 }
 
-// y from the splits' sums, added in order.
+// y from the splits' sums, added in order, four of them asked for at a time.  (Outputs that are split are fewer than 2^23.)
 template <typename T>
 __global__ __launch_bounds__(256) void product_sum_kernel(ProductArgs a, int splits) {
-    const int64_t quads = (a.m + 3) / 4, total = quads * a.rows;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
+    const uint32_t quads = (uint32_t)(a.m + 3) / 4, total = quads * (uint32_t)a.rows;
+    for (uint32_t at = blockIdx.x * 256 + threadIdx.x; at < total; at += gridDim.x * 256) {
         f32x4 v = {};
         const f32x4 *p = (const f32x4 *)a.part + at;
-        for (int s = 0; s < splits; ++s) v += p[s * total];
-        const int64_t row = at / quads;
-        put4<T>(a, row, (at - row * quads) * 4, v);
+        for (int s = 0; s < splits; s += 4) {
+            f32x4 u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = p[(int64_t)min(s + k, splits - 1) * total];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (s + k < splits) v += u[k];
+        }
+        const uint32_t row = at / quads;
+        put4<T>(a, row, (int64_t)(at - row * quads) * 4, v);
     }
 }
 
