@@ -733,7 +733,7 @@ static ProductPlan product_plan(int64_t rows, int64_t m, int64_t n, int dtype, i
     const int64_t col_tiles = ceil_div(m, 128);
     if (rows <= 128) {
         // Splits as far as they fill the GPU, by the us that a block, a split and its sums were measured to take.  (100 x 2050 x
-        // 4133 fp32: nine splits 16.7, five 20.1; 40 x 700 x 20000 bf16: 20 splits 16.1, 40 20.7.)
+        // 4133 fp32: nine splits 16.7, five 20.1; 40 x 700 x 20000 bf16: 20 splits 13.1, and 40 were 4.7 more before sums were read four at a time.)
         const int fn = (int)ceil_div(rows, 32);
         const double block = dtype == DLCX_F32 ? 0.5 + 0.3 * fn : 0.25 + 0.13 * fn, split = 0.25 + 5e-5 * (double)(fn * m);
         ProductPlan best = {kSome, 1, (int)(quads * 4), fn};
