@@ -421,7 +421,8 @@ int dlcx_state_decode(int second, const void *codes, const float *scales, int64_
  * padded with zeros to a multiple of 128 (dlcx_fp8_code_pitch(cols) bytes).  One byte s for every 128 consecutive
  * elements of a row, `ldscale` bytes between rows, padded to a multiple of 4 (dlcx_fp8_scale_pitch(cols)):
  * value = code * 2^(s - 127).  codes and ld are multiples of 16, scales and ldscale of 4; strides up to 2^29.  rows and
- * cols 0 .. 2^24 each.  s is 0 .. 254 (255 makes a product's row NaN); the pad of the scales is not read as one. */
+ * cols 0 .. 2^24 each.  s is 0 .. 254, or 255 for NaN: its block decodes to NaN, and outputs of a product that sum over
+ * the block are NaN, whatever its codes.  The library writes no 255.  The pad of the scales is not read as one. */
 typedef struct {
     void *codes, *scales;
     int64_t rows, cols, ld, ldscale;

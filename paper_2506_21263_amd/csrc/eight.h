@@ -184,8 +184,11 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t largest) {
 }
 // 2^(127 - s): what a value is multiplied by before it becomes a code (s <= 247, so this is a normal number)
 __device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - s) << 23); }
-// 2^(s - 127); s = 0 is the only one below the normal range
-__device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x400000u); }
+// 2^(s - 127); s = 0 is the only one below the normal range, 255 is NaN
+constexpr uint32_t kScaleNan = 255;
+__device__ __forceinline__ float scale_value(uint32_t s) {
+    return __uint_as_float(s == kScaleNan ? 0x7fc00000u : s ? s << 23 : 0x400000u);
+}
 
 __device__ __forceinline__ uint2 codes8(const float (&v)[8], float inverse) {
     int w[2];

@@ -58,11 +58,14 @@ __device__ __forceinline__ bool all_inside(uint32_t collected, int count) {
 }
 template <int S>
 __device__ __forceinline__ float scale_of(int scales) { return __uint_as_float(((uint32_t)scales >> (8 * S) & 255u) << 23); }
-// c + the block's sum, whose scales' bytes add up to e
+// c + the block's sum, whose scales' bytes are ew and ex (the scaled instruction takes 255 for NaN by itself)
 __device__ __forceinline__ f32x4 add_scaled(const f32x4 &c, const f32x4 &sum, const int (&ew)[4], int ex) {
     f32x4 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = c[i] + __builtin_amdgcn_ldexpf(sum[i], ew[i] + ex - 254);
+    for (int i = 0; i < 4; ++i) {
+        const float scaled = __builtin_amdgcn_ldexpf(sum[i], ew[i] + ex - 254);
+        r[i] = c[i] + (max(ew[i], ex) == (int)kScaleNan ? __builtin_nanf("") : scaled);
+    }
     return r;
 }
 
