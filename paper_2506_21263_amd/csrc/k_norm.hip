@@ -164,18 +164,20 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     }
 }
 
+constexpr int kMostLong = 1 << 20;  // workgroups of 1024 threads in a launch: 2^32 threads are too many
+
 template <typename T, bool ENDS>
 static void run_norm(const NormArgs &a, hipStream_t st) {
     // Workgroups: no more than the GPU holds at once, and rows shared out evenly.
     auto grid = [&a](int per, int most) { return dim3((unsigned)ceil_div(a.rows, per * ceil_div(a.rows, (int64_t)per * most))); };
-    if (ENDS && a.n < 8) norm_long_kernel<T><<<grid(1, 1 << 22), 1024, 0, st>>>(a);
+    if (ENDS && a.n < 8) norm_long_kernel<T><<<grid(1, kMostLong), 1024, 0, st>>>(a);
     else if (a.n <= 512) norm_kernel<T, 64, 1, ENDS><<<grid(4, 2048), 256, 0, st>>>(a);
     else if (a.n <= 2048) norm_kernel<T, 256, 1, ENDS><<<grid(1, 2048), 256, 0, st>>>(a);
     else if (a.n <= 4096) norm_kernel<T, 256, 2, ENDS><<<grid(1, 1280), 256, 0, st>>>(a);
     else if (a.n <= 8192) norm_kernel<T, 512, 2, ENDS><<<grid(1, 768), 512, 0, st>>>(a);
     else if (!ENDS && a.n <= 16384) norm_kernel<T, 1024, 2, false><<<grid(1, 256), 1024, 0, st>>>(a);
     else if (T::size == 2 && !ENDS && a.n <= 32768) norm_kernel<TypeBf16, 1024, 4, false><<<grid(1, 256), 1024, 0, st>>>(a);
-    else norm_long_kernel<T><<<grid(1, 1 << 22), 1024, 0, st>>>(a);
+    else norm_long_kernel<T><<<grid(1, kMostLong), 1024, 0, st>>>(a);
 }
 template <typename T>
 static int launch_norm(const NormArgs &a, hipStream_t st) {
@@ -400,7 +402,7 @@ static int norm_parts(int64_t rows, int64_t n) {
 
 template <typename T>
 static void long_norm_grad(const NormGradArgs &a, hipStream_t st) {
-    norm_dot_kernel<T><<<dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))), 1024, 0, st>>>(a);
+    norm_dot_kernel<T><<<dim3((unsigned)(a.rows < kMostLong ? a.rows : kMostLong)), 1024, 0, st>>>(a);
     norm_grad_long_kernel<T><<<dim3((unsigned)ceil_div(a.n, 2048), (unsigned)a.parts), 256, 0, st>>>(a);
 }
 template <typename T, bool ENDS>
