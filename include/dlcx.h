@@ -446,7 +446,8 @@ int dlcx_fp8_decode(const dlcx_fp8 *a, void *out, int64_t ldo, int out_dtype, vo
  * what is below 2^-13 of the largest of eight before they are added in fp32 (1.5e-5 of a result of normal inputs), y rounded
  * once.  A projection's output from (x, theta_g), its
  * inputs' gradient from (dy, the transpose of theta_g), its weights' from (transpose of dy, transpose of x) added to
- * fp32 gradients.  The order of a sum hangs on rows, m and n.  The workspace serves up to `rows` rows. */
+ * fp32 gradients.  The order of a sum hangs on rows, m and n.  The workspace serves up to `rows` rows.  One call has fewer
+ * than 2^22 squares of 128 x 128 outputs, begun ones counted (2^36 outputs); DLCX_EUNSUPPORTED from there on. */
 size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n);
 int dlcx_fp8_product(const dlcx_fp8 *x, const dlcx_fp8 *w, const void *y_in, int64_t ldy_in, void *y_out,
                      int64_t ldy_out, int dtype, void *workspace, void *stream);

@@ -871,7 +871,8 @@ int dlcx_fp8_product(const dlcx_fp8 *x, const dlcx_fp8 *w, const void *y_in, int
                      y_in, y_out, plan.splits > 1 ? (float *)workspace : nullptr, x->ld, x->ldscale, w->ld, w->ldscale,
                      ldy_in, ldy_out, (int)x->rows, (int)w->rows, (int)ceil_div(x->cols, 128), plan.per_split,
                      (int)ceil_div(x->rows, 128), (int)ceil_div(w->rows, 128)};
-    if ((int64_t)a.row_tiles * a.col_tiles >= kMostGroups / 2) return DLCX_EUNSUPPORTED;  // 2^51 outputs
+    // tiles of 128 x 128, in 2^36 outputs: the form with tiles of 64 rows has twice as many workgroups
+    if ((int64_t)a.row_tiles * a.col_tiles >= kMostGroups / 2) return DLCX_EUNSUPPORTED;
     return dtype == DLCX_BF16 ? launch_product<TypeBf16>(a, plan, as_stream(stream)) : launch_product<TypeF32>(a, plan, as_stream(stream));
 }
 
