@@ -171,8 +171,9 @@ class AdapterProjection:
     so a new adapter changes nothing.  Masters are fp32; the products read copies in `dtype`.
 
     base_bits=8 keeps theta_g in 8 bits (twice: its transpose is the backward pass's), with a scale for 128 x 128 elements;
-    the rows it is multiplied by are brought to 8 bits, too.  dropout: of the rows that the adapters read; the mask hangs
-    on `seed` and the number `draw` that both passes of a step are given.
+    the rows it is multiplied by are brought to 8 bits, too.  dropout: of the rows that the adapters read in training; the
+    mask hangs on `seed` and the number `draw`, another one for every step, that both passes of a step are given.
+    Evaluation and serving pass training=False and read the rows as they are.
 
     An optimizer's tensors begin at 16 bytes, so where r x m or r x n elements are not whole 16 bytes, the factors are
     stored with up to seven more columns, which `ranks` leaves out of every product: p, q, dp and dq are the first r,
@@ -229,32 +230,42 @@ class AdapterProjection:
         dlcx_fp8_product(x8, w, None, y, workspace)
         return y
 
-    def _dropped(self, x, draw):
+    def _drops(self, draw, training):
+        """Whether the adapters read their rows with dropout."""
+        if not (self.dropout and training):
+            return False
+        if draw is None:
+            raise ValueError("draw: dropout wants a number of the step in training, the same in both passes; or training=False")
+        return True
+
+    def _dropped(self, x, draw, drops):
         """The rows that the adapters read."""
-        if not self.dropout:
+        if not drops:
             return x
         out = torch.empty_like(x)
         dlcx_dropout(x, None, out, self.dropout, self.seed, draw)
         return out
 
-    def forward(self, x, route, x8=None, draw=0):
+    def forward(self, x, route, x8=None, draw=None, training=True):
         """x8: x in 8 bits, where a norm has written it already."""
+        drops = self._drops(draw, training)
         y = x @ self.base.t() if self.base is not None else self._product(x, self.base8, x8)
         route.order.enter(None, [route.table])
         h = torch.empty(x.shape[0], self.d.r, device=x.device)
-        dlcx_adapter_forward(self.d, self._dropped(x, draw), route.ids, self.stored["q_copy"], self.stored["p_copy"], y,
-                             y, h, self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
+        dlcx_adapter_forward(self.d, self._dropped(x, draw, drops), route.ids, self.stored["q_copy"],
+                             self.stored["p_copy"], y, y, h, self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
         return y, h
 
-    def backward(self, x, h, dy, route, draw=0):
+    def backward(self, x, h, dy, route, draw=None, training=True):
         """dx; the gradients of the factors are left in dq and dp."""
+        drops = self._drops(draw, training)
         dx = dy @ self.base if self.base is not None else self._product(dy, self.base8_t)
         route.order.enter(None, [route.table])
-        own = torch.empty_like(dx) if self.dropout else dx      # what comes through the adapters, or the whole
-        dlcx_adapter_backward(self.d, self._dropped(x, draw), dy, route.ids, self.stored["q_copy"], self.stored["p_copy"],
-                              h, None if self.dropout else dx, own, self.stored["dq"], self.stored["dp"], self.workspace,
-                              scale=self.scale, ranks=self.ranks, route=route.table)
-        if self.dropout:
+        own = torch.empty_like(dx) if drops else dx      # what comes through the adapters, or the whole
+        dlcx_adapter_backward(self.d, self._dropped(x, draw, drops), dy, route.ids, self.stored["q_copy"],
+                              self.stored["p_copy"], h, None if drops else dx, own, self.stored["dq"], self.stored["dp"],
+                              self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
+        if drops:
             dlcx_dropout(own, dx, dx, self.dropout, self.seed, draw)
         return dx
 
