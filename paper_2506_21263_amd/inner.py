@@ -18,6 +18,7 @@ whose mask is drawn again in the backward pass.
 teacher, outer step after outer step, and prints the losses.
 """
 import argparse
+import itertools
 import math
 
 import torch
@@ -173,13 +174,17 @@ class AdapterProjection:
     base_bits=8 keeps theta_g in 8 bits (twice: its transpose is the backward pass's), with a scale for 128 x 128 elements;
     the rows it is multiplied by are brought to 8 bits, too.  dropout: of the rows that the adapters read in training; the
     mask hangs on `seed` and the number `draw`, another one for every step, that both passes of a step are given.
+    Without a seed, projections with dropout are numbered as a process makes them, so that no two of them have the same
+    masks; pass one where processes are to differ, or where masks are not to hang on what was made before.
     Evaluation and serving pass training=False and read the rows as they are.
 
     An optimizer's tensors begin at 16 bytes, so where r x m or r x n elements are not whole 16 bytes, the factors are
     stored with up to seven more columns, which `ranks` leaves out of every product: p, q, dp and dq are the first r,
     h has the stored ones."""
 
-    def __init__(self, theta_g, q0, scale, max_rows, dtype=torch.bfloat16, base_bits=16, dropout=0.0, seed=0):
+    _seeds = itertools.count()
+
+    def __init__(self, theta_g, q0, scale, max_rows, dtype=torch.bfloat16, base_bits=16, dropout=0.0, seed=None):
         if base_bits not in (8, 16) or not 0.0 <= dropout < 1.0:
             raise ValueError("base_bits: 8 or 16 (the adapters' own type); dropout: from 0 up to 1")
         self.m, self.n = theta_g.shape
@@ -194,6 +199,8 @@ class AdapterProjection:
         self.ranks = None if stored == self.r else torch.full((self.count,), self.r, device=dev, dtype=torch.int32)
         self.dtype, self.q0 = dtype, q0
         self.dropout, self.seed = dropout, seed
+        if seed is None:
+            self.seed = next(AdapterProjection._seeds) if dropout else 0
         self.base = self.base8 = self.base8_t = None
         if base_bits == 8:
             self.base8, self.base8_t = fp8_empty(self.m, self.n, dev), fp8_empty(self.n, self.m, dev)

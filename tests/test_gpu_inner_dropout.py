@@ -36,3 +36,12 @@ def test_evaluation_drops_nothing(base_bits, dtype):
     proj, route, x, dy = projection(dtype, base_bits, 0.3)
     y, h = proj.forward(x, route, draw=1)
     assert not torch.equal(y, results[0][0])
+
+
+def test_two_projections_have_masks_of_their_own():
+    """Two of one shape, in the same step; with one seed they have one mask."""
+    ys = []
+    for kw in ({}, {}, dict(seed=3), dict(seed=3)):
+        proj, route, x, _ = projection("f32", 16, 0.3, **kw)
+        ys.append(proj.forward(x, route, draw=7)[0])
+    assert not torch.equal(ys[0], ys[1]) and torch.equal(ys[2], ys[3])
