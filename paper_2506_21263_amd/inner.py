@@ -173,7 +173,8 @@ class AdapterProjection:
 
     base_bits=8 keeps theta_g in 8 bits (twice: its transpose is the backward pass's), with a scale for 128 x 128 elements;
     the rows it is multiplied by are brought to 8 bits, too.  dropout: of the rows that the adapters read in training; the
-    mask hangs on `seed` and the number `draw`, another one for every step, that both passes of a step are given.
+    mask hangs on `seed` and the number `draw`, another one for every step, that both passes of a step are given: an int,
+    or for a step that is captured into a graph an int64 tensor of one element on the device, which the program counts up.
     Without a seed, projections with dropout are numbered as a process makes them, so that no two of them have the same
     masks; pass one where processes are to differ, or where masks are not to hang on what was made before.
     Evaluation and serving pass training=False and read the rows as they are.
@@ -245,12 +246,16 @@ class AdapterProjection:
             raise ValueError("draw: dropout wants a number of the step in training, the same in both passes; or training=False")
         return True
 
+    def _drop(self, x, y_in, y_out, draw):
+        number, more = (0, draw) if isinstance(draw, torch.Tensor) else (draw, None)
+        dlcx_dropout(x, y_in, y_out, self.dropout, self.seed, number, more)
+
     def _dropped(self, x, draw, drops):
         """The rows that the adapters read."""
         if not drops:
             return x
         out = torch.empty_like(x)
-        dlcx_dropout(x, None, out, self.dropout, self.seed, draw)
+        self._drop(x, None, out, draw)
         return out
 
     def forward(self, x, route, x8=None, draw=None, training=True):
@@ -273,7 +278,7 @@ class AdapterProjection:
                               self.stored["p_copy"], h, None if drops else dx, own, self.stored["dq"], self.stored["dp"],
                               self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
         if drops:
-            dlcx_dropout(own, dx, dx, self.dropout, self.seed, draw)
+            self._drop(own, dx, dx, draw)
         return dx
 
     def fold_workspace_bytes(self, group, mma):

@@ -45,3 +45,32 @@ def test_two_projections_have_masks_of_their_own():
         proj, route, x, _ = projection("f32", 16, 0.3, **kw)
         ys.append(proj.forward(x, route, draw=7)[0])
     assert not torch.equal(ys[0], ys[1]) and torch.equal(ys[2], ys[3])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_captured_step_draws_anew(dtype):
+    """A step with weights in 8 bits, whose number is on the device: replays have the masks of the numbers that it had,
+    and the bits of eager steps with these numbers."""
+    proj, route, x, dy = projection(dtype, 8, 0.3)
+    step = torch.zeros(1, device=DEV, dtype=torch.int64)
+
+    def both(draw):
+        y, h = proj.forward(x, route, draw=draw)
+        dx = proj.backward(x, h, dy, route, draw=draw)
+        return y, h, dx, proj.dq, proj.dp
+
+    both(step)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = both(step)
+    seen = []
+    for k in (0, 1, 2, 1 << 40):
+        step.fill_(k)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = both(k)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        seen.append(got[0])
+    assert not any(torch.equal(a, b) for a, b in zip(seen, seen[1:]))
