@@ -346,7 +346,7 @@ def train(m=512, n=512, workers=2, r=8, rows=256, inner=20, outer=8, bits=32, dt
           dropout=0.0, norm=False):
     """Workers train adapters of rank r towards a teacher that is a rank-r step away from the shared
     weights; every `inner` steps an outer step.  base_bits, dropout: AdapterProjection's; norm: rows are normalised
-    before they are projected.  Every phase goes nearly the whole way, so with the step of
+    before they are projected, with weights that are the workers' common ones and stay as they are, like theta_g.  Every phase goes nearly the whole way, so with the step of
     delay an outer rate above 1/4 already overshoots a little.  Returns the losses at the phases' starts."""
     from .stage import MatrixState
     from . import MMA_F32
@@ -372,14 +372,12 @@ def train(m=512, n=512, workers=2, r=8, rows=256, inner=20, outer=8, bits=32, dt
             x = normal(workers * rows, n).to(dtype)      # every worker's own batch
             x8, draw = None, t * inner + k
             if norm:
-                x, x8, saved = front.forward(x, eight=base_bits == 8)
+                x, x8, _ = front.forward(x, eight=base_bits == 8)
             want = x.float() @ teacher.t()
             y, h = proj.forward(x, route, x8, draw)
             off = y.float() - want
             loss = (off * off).sum(1).view(workers, rows).mean(1) / m
-            dx = proj.backward(x, h, (off * (2.0 / (rows * m))).to(dtype), route, draw)
-            if norm:
-                front.backward(saved, dx)
+            proj.backward(x, h, (off * (2.0 / (rows * m))).to(dtype), route, draw)
             for opt in optimizers:
                 opt.step()
             if k == 0:
