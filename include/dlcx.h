@@ -549,6 +549,11 @@ int dlcx_profile_enable(int on);
 int dlcx_profile_kernels(void);
 const char *dlcx_profile_name(int kernel_id);
 int dlcx_profile_read(int kernel_id, double *total_ms_host, int64_t *launches_host);
+/* What dlcx_fp8_product of these sizes runs as (strides up to 2^23), to see that a test or a measurement takes the way it
+ * is meant to: *form is 0 for few rows (*tile: wavefronts that share a sum), 1 for a ring of stages, 2 for tiles in pairs,
+ * 3 for tiles of 256 x 256 (*tile: rows of a tile); *splits: launches' shares of a sum.  Host only. */
+int dlcx_fp8_product_plan(int64_t rows, int64_t m, int64_t n, int dtype, int32_t *form, int32_t *tile,
+                          int32_t *splits);
 
 const char *dlcx_strerror(int code);
 /* Text of the last HIP error seen by this thread's calls (empty if none). */

@@ -135,6 +135,7 @@ SYMBOLS = {
     "dlcx_fp8_quantize": (_int, [_i64, _i64, _vp, _i64, _int, _int, _vp, _vp, _vp]),
     "dlcx_fp8_decode": (_int, [_vp, _vp, _i64, _int, _vp]),
     "dlcx_fp8_product_workspace_bytes": (C.c_size_t, [_i64, _i64, _i64]),
+    "dlcx_fp8_product_plan": (_int, [_i64, _i64, _i64, _int, _vp, _vp, _vp]),
     "dlcx_fp8_product": (_int, [_vp, _vp, _vp, _i64, _vp, _i64, _int, _vp, _vp]),
     "dlcx_rms_norm": (_int, [_i64, _i64, _int, _vp, _i64, _vp, _i64, _vp, C.c_float, _vp, _i64, _vp, _i64,
                              _vp, _vp, _vp]),
@@ -684,6 +685,13 @@ def dlcx_fp8_decode(a, out, stream=None):
 @functools.lru_cache(maxsize=4096)  # (it looks at every smaller number of rows: up to 40 us, and every product asks)
 def dlcx_fp8_product_workspace_bytes(rows, m, n):
     return lib().dlcx_fp8_product_workspace_bytes(rows, m, n)
+
+
+def dlcx_fp8_product_plan(rows, m, n, dtype):
+    """(form, tile, splits) of a product of these sizes with results of F32 or BF16."""
+    out = [C.c_int32() for _ in range(3)]
+    _check(lib().dlcx_fp8_product_plan(rows, m, n, dtype, *(C.addressof(k) for k in out)), "dlcx_fp8_product_plan")
+    return tuple(k.value for k in out)
 
 
 def dlcx_fp8_product(x, w, y_in, y_out, workspace, stream=None):

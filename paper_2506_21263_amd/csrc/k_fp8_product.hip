@@ -858,6 +858,15 @@ size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n) {
     return a256x(most) + 256;
 }
 
+int dlcx_fp8_product_plan(int64_t rows, int64_t m, int64_t n, int dtype, int32_t *form, int32_t *tile, int32_t *splits) {
+    if (bad_product(rows, m, n) || (dtype != DLCX_F32 && dtype != DLCX_BF16) || !form || !tile || !splits) return DLCX_EINVAL;
+    const ProductPlan plan = product_plan(rows, m, n, dtype, 0);
+    *form = plan.form;
+    *tile = plan.form == kWide ? kWideTile : plan.form == kFew ? plan.kw : 32 * plan.kw;
+    *splits = plan.splits;
+    return DLCX_OK;
+}
+
 int dlcx_fp8_product(const dlcx_fp8 *x, const dlcx_fp8 *w, const void *y_in, int64_t ldy_in, void *y_out, int64_t ldy_out,
                      int dtype, void *workspace, void *stream) {
     if (check_fp8(x) != DLCX_OK || check_fp8(w) != DLCX_OK || x->cols != w->cols) return DLCX_EINVAL;
