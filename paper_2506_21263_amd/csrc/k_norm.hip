@@ -41,10 +41,17 @@ __device__ __forceinline__ float sum_lanes(float x, float *s_part) {
     return x;
 }
 
-template <typename T>
+// Codes from n on are zeros (in v they are NaN where rstd is not finite).
+template <bool ENDS>
 __device__ __forceinline__ void put_eight(const NormArgs &a, int64_t row, int col, const float (&v)[8], int lane) {
     const uint32_t s = scale_byte(max16(finite_max8(v)));
-    const uint2 c = codes8(v, scale_inverse(s));
+    uint2 c = codes8(v, scale_inverse(s));
+    const int there = a.n - col;
+    if (ENDS ? there < 8 : there <= 0) {
+        const uint64_t keep = ENDS && there > 0 ? (1ull << (8 * there)) - 1 : 0;
+        c.x &= (uint32_t)keep;
+        c.y &= (uint32_t)(keep >> 32);
+    }
     if (col < (a.n + 127) / 128 * 128) {
         *reinterpret_cast<uint2 *>(a.codes + row * a.ld8 + col) = c;
         if ((lane & 15) == 0) a.scales[row * a.lds + col / 128] = (uint8_t)s;
@@ -114,7 +121,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = v[c][i] * rstd * w[c][i];
             if (a.y) store8<T, ENDS>((elem *)a.y + row * a.ldy + col, a.n - col, v[c]);
-            if (a.codes) put_eight<T>(a, row, col, v[c], lane);
+            if (a.codes) put_eight<ENDS>(a, row, col, v[c], lane);
         }
         if (next >= a.rows) break;
         row = next;
@@ -158,7 +165,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * w[i];
             if (a.y) store8<T>((elem *)a.y + row * a.ldy + col, there, v);
-            if (a.codes) put_eight<T>(a, row, (int)col, v, lane);
+            if (a.codes) put_eight<true>(a, row, (int)col, v, lane);
         }
         __syncthreads();
     }
