@@ -636,7 +636,7 @@ def _bytes(t, kind, rows, pitch, what):
     step, inner = t.stride()
     if (inner != 1 and t.shape[1] > 1) or (step < t.shape[1] and rows > 1):
         raise ValueError("%s: the bytes of a row have to be consecutive, and rows apart" % what)
-    return t.data_ptr(), (step if rows > 1 else max(pitch, t.shape[1]))
+    return t.data_ptr(), (step if rows > 1 else pitch)  # (one row: its stride says nothing, and may be no multiple)
 
 
 def fp8(codes, scales, cols):
