@@ -443,9 +443,9 @@ int dlcx_fp8_decode(const dlcx_fp8 *a, void *out, int64_t ldo, int out_dtype, vo
 
 /* y_out = y_in + x w^T: x is rows x n, w m x n, both in 8 bits; y is rows x m, DLCX_F32 or DLCX_BF16.  y_in may be y_out,
  * or NULL for zeros.  DLCX_F32: fp32 sums of exact products.  DLCX_BF16: the matrix cores' 8-bit products, which lose
- * what is below 2^-13 of the largest of eight before they are added in fp32 (1.5e-5 of a result of normal inputs), y rounded
- * once.  A projection's output from (x, theta_g), its
- * inputs' gradient from (dy, the transpose of theta_g), its weights' from (transpose of dy, transpose of x) added to
+ * what is below 2^-13 of the largest of eight before they are added in fp32 (1.5e-5 of a result of normal inputs; up to
+ * 2^-10 of the sum of magnitudes where large terms cancel), and products below 2^-149; y is rounded once, so that about 2 %
+ * of results of normal inputs are one bf16 step from those of fp32 sums.  A projection's output from (x, theta_g), its inputs' gradient from (dy, the transpose of theta_g), its weights' from (transpose of dy, transpose of x) added to
  * fp32 gradients.  The order of a sum hangs on rows, m and n.  The workspace serves up to `rows` rows.  One call has fewer
  * than 2^22 squares of 128 x 128 outputs, begun ones counted (2^36 outputs); DLCX_EUNSUPPORTED from there on. */
 size_t dlcx_fp8_product_workspace_bytes(int64_t rows, int64_t m, int64_t n);
@@ -454,8 +454,9 @@ int dlcx_fp8_product(const dlcx_fp8 *x, const dlcx_fp8 *w, const void *y_in, int
 
 /* For every row: s = x + residual, rounded to the type and written to sum_out (both or neither; without them s = x);
  * rstd = 1 / sqrt(mean(s^2) + eps); y = s rstd weight, to y_out (rounded once), to y8_out in 8 bits (from fp32, not from
- * y_out), or to both.  weight: n elements of the same type.  rstd_out: `rows` floats for the gradient, or NULL.  sum_out
- * may be x or residual.  Squares and their sum are fp32: rows whose sum of squares passes 2^128 give zeros. n 1 .. 2^24. */
+ * y_out), or to both; eps 0 .. 1e30.  weight: n elements of the same type.  rstd_out: `rows` floats for the gradient, or
+ * NULL.  sum_out may be x or residual.  Squares and their sum are fp32: rows whose sum of squares passes 2^128 give zeros.
+ * n 1 .. 2^24. */
 int dlcx_rms_norm(int64_t rows, int64_t n, int dtype, const void *x, int64_t ldx, const void *residual,
                   int64_t ldr, const void *weight, float eps, void *sum_out, int64_t ldsum, void *y_out,
                   int64_t ldy, const dlcx_fp8 *y8_out, float *rstd_out, void *stream);

@@ -2,7 +2,8 @@
 //
 // A value is code * 2^(s - 127), code in e4m3 (largest 448 = 1.75 * 2^8), s one byte for 128 consecutive elements
 // of a row.  s is the smallest that lets the largest finite magnitude fit, so x * 2^(127 - s) is exact and a code
-// is rounded once (to nearest, ties to even); a value loses bits only below 2^-15 of its block's largest.
+// is rounded once (to nearest, ties to even); a value loses bits only below the smallest normal code, 2^-6: that is
+// 2^-14.8 to 2^-13.8 of its block's largest, whose code is above 224.
 #pragma once
 #include "common.h"
 

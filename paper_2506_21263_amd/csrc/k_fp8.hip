@@ -3,7 +3,8 @@
 // Both are streams, bound by HBM.  The quantiser takes tiles of 128 x 128: a lane holds 8 x 8 elements, sixteen
 // lanes a row's 128 columns, so a row's largest is found among a row of lanes and a column's among the sixteen
 // such rows of the workgroup; both layouts come from one reading of x.
-// 16384 x 8192 of bf16 to both layouts: 129 us (4.2 TB/s; 537 MB, half of them written in two places), decoded 71 (5.7 TB/s).
+// 16384 x 8192 of bf16 to both layouts: 129 us (4.2 TB/s; 537 MB, half of them written in two places), along the rows alone 86
+// (4.7 TB/s), decoded 71 (5.7 TB/s); 28672 x 8192 of fp32 in squares, both ways, 281 (5.0 TB/s).
 #include "eight.h"
 
 namespace dlcx {

@@ -48,8 +48,8 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale = 1.f) {
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 // Where all scales of a quad are from 2^-63 to 2^64, they are applied as the codes are widened (bf16 has the exponents of
-// fp32, so that is exact, too) and blocks add up in one accumulator; products below 2^-126, whose sum no fp32 result holds
-// in full, are all that may be lost.  `outside` collects the quad's dwords: bit 7 of a byte from 64 to 191 differs from bit 6.
+// fp32, so that is exact, too) and blocks add up in one accumulator.  The smallest product is then 2^-144, and the matrix
+// cores keep what is below fp32's normal range, down to its last bit of 2^-149.  `outside` collects the quad's dwords: bit 7 of a byte from 64 to 191 differs from bit 6.
 __device__ __forceinline__ uint32_t outside(int scales) { return ~((uint32_t)scales ^ (uint32_t)scales << 1) & 0x80808080u; }
 // true for the whole wavefront if none of the first `count` blocks' scales is outside
 __device__ __forceinline__ bool all_inside(uint32_t collected, int count) {
@@ -132,8 +132,9 @@ __device__ __forceinline__ void multiply_scaled(const uint8_t *pw, const uint8_t
     }
 }
 // The same of widened codes, scaled as they are widened.  TIGHT: half of them at a time (two wavefronts to a SIMD have no
-// registers for more).  Widening takes as many cycles as three eighths of the products (64 rows) or a quarter (128 rows), and they
-// hardly overlap: 8192 x 8192 x 4096 takes 577 us (0.95 PFLOP/s) in tiles of 128 rows, 659 in tiles of 64.
+// registers for more).  Two conversions (128 rows; three: 64) of four cycles come to a matrix instruction of sixteen, 3.3 vector
+// instructions with all others, and the two hardly overlap: 8192 x 8192 x 4096 takes 577 us (0.95 PFLOP/s) in tiles of 128 rows,
+// 46 % of a SIMD's cycles matrix instructions and 38 % others; 659 us in tiles of 64.
 template <int S, int FN, bool TIGHT = false>
 __device__ __forceinline__ void multiply_widened(const uint8_t *pw, const uint8_t *px, int p0, int p1, const int (&scale_w)[4],
                                                  const int (&scale_x)[FN], f32x4 (&acc)[4][FN]) {
@@ -295,10 +296,10 @@ __global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs a) {
 // of 128 bytes, straight to LDS, two of them; a row's 16-byte pieces lie at piece ^ (row / 2 & 7), so that the sixteen
 // lanes that read at once hit all banks.  One barrier a stage, in its middle: from there on its operands are in
 // registers, so its place is fetched anew while the second half is multiplied, and the next stage is there to be read.
-// Scales go through LDS, too (four stages' to a dword): read by every lane that needs them they were 40 % of all
-// requests to the cache.  Results leave through LDS as whole lines.  Edge tiles are moved inside the matrix and write
+// Scales go through LDS, too (four stages' to a dword), so that not every lane that needs one asks the cache for it.  Results leave through LDS as whole lines.  Edge tiles are moved inside the matrix and write
 // only what is theirs, so no address is checked.
-// 16384 x 8192 x 8192: 0.85 ms, 2.6 PFLOP/s (0.64 without the fetches, 1.44 with 128 x 128 tiles); 8192^3 0.41 ms.
+// 16384 x 8192 x 8192: 0.87 ms, 2.5 PFLOP/s (1.44 ms with 128 x 128 tiles): matrix cores are at work 62 % of the cycles, 13 %
+// of a wavefront's are waits, and the clock is at 1.8 GHz; 8192^3 0.41 - 0.44 ms.  Added to y_in, which comes 8 bytes a lane: 0.93.
 constexpr int kWideTile = 256, kWideStage = 512 * 128, kWideLds = 2 * kWideStage + 2 * 2048;
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
@@ -535,7 +536,7 @@ __device__ __forceinline__ f32x4 block_product(const i32x8 &w, const i32x8 &x, c
 
 // Up to 16 rows of x (a lane whose row is not there has the last one's, and writes nothing).  Where m alone does not
 // fill the GPU, KW wavefronts of a workgroup take every KW'th quad and their sums are added through LDS, in order.
-// 1 row of 28672 x 8192: 48 us (5.0 TB/s); 16 rows: 65.
+// 1 row of 28672 x 8192: 45 - 48 us (5.0 TB/s); 16 rows: 64 - 66; fp32 results 47 - 50 and 65.
 template <typename T, int KW>
 __global__ __launch_bounds__(256, 2) void product_few_kernel(ProductArgs a) {
     constexpr int WR = 4 / KW;
@@ -603,9 +604,10 @@ __global__ __launch_bounds__(256, 2) void product_few_kernel(ProductArgs a) {
 // compute units.  Few rows are bound by the reading of w, so what counts is how much of it is on its way: a ring of as many
 // stages as LDS holds (128 bytes of each row, straight to LDS; pieces at piece ^ (row & 7)), all but one of them in flight,
 // 64 KB of w to a compute unit beside 96 rows.  (Twice as much, in registers and with a barrier only every four blocks,
-// measured the same: a compute unit takes in 24 - 28 bytes a ns from HBM, and x's are among them.)  96 rows of 28672 x 8192:
-// 70 us, 3.4 TB/s of w.  Scales come four stages to a dword, two dwords ahead, 256 rows (w's, then x's) to a load of the
-// workgroup.
+// measured the same.)  28672 x 8192, by 224 of the 256 compute units: 17 rows 59 us (4.0 TB/s of w), and 3 to 5 us for every 32
+// rows more, which come again for each 128 columns: 64 rows 64, 96 rows 70 (3.4 TB/s of w; 63 % of the cycles waits, 15 % matrix
+// instructions), 128 rows 71.  Where rows of w are 8320 bytes apart, not 8192, 96 rows take 66.  fp32 results, 128 rows: 98.
+// Scales come four stages to a dword, two dwords ahead, 256 rows (w's, then x's) to a load of the workgroup.
 template <typename T, int FN>
 struct SomeShape {
     static constexpr int kRows = 32 * FN, kStage = (128 + kRows) * 128, kRing = 152 * 1024 / kStage;

@@ -273,7 +273,9 @@ class AdapterProjection:
         drops = self._drops(draw, training)
         dx = dy @ self.base if self.base is not None else self._product(dy, self.base8_t)
         route.order.enter(None, [route.table])
-        own = torch.empty_like(dx) if drops else dx      # what comes through the adapters, or the whole
+        # what comes through the adapters, or the whole (with dropout it is rounded to the rows' type before it is masked and
+        # added: half a step of the adapters' part, where the sum's own rounding is half a step of the whole)
+        own = torch.empty_like(dx) if drops else dx
         dlcx_adapter_backward(self.d, self._dropped(x, draw, drops), dy, route.ids, self.stored["q_copy"],
                               self.stored["p_copy"], h, None if drops else dx, own, self.stored["dq"], self.stored["dp"],
                               self.workspace, scale=self.scale, ranks=self.ranks, route=route.table)
